@@ -1,4 +1,4 @@
-"""ctypes binding of libvla.so (include/vla.h, include/vla_ops.h): argument marshalling only.
+"""ctypes binding of libvla.so (include/vla.h, include/vla_ops.h, include/vla_lm.h): argument marshalling only.
 
 Every step of the hot path runs in the CUDA library.  There is no fallback: if the library
 is missing or fails to load, importing this module's functions raises.
@@ -30,6 +30,10 @@ VLA_STATUS_NONFINITE = 0x2
 VLA_STATUS_TIMEOUT = 0x4
 VLA_STATUS_BAD_FORCED = 0x8
 VLA_STATUS_SATURATED = 0x10
+VLA_STATUS_PAGES = 0x20
+
+VLA_F32, VLA_F16, VLA_BF16 = 0, 1, 2
+VLA_ROPE_PLAIN, VLA_ROPE_LINEAR, VLA_ROPE_TURNS, VLA_ROPE_LOG_TURNS = 0, 1, 2, 3
 
 KCLASS = ("gemm_prefill", "gemm_decode", "attn_prefill", "attn_decode", "head", "other")
 
@@ -53,6 +57,13 @@ class VlaWeights(ctypes.Structure):
                 ("lm_head", ctypes.c_void_p)]
 
 
+class VlaPagedKv(ctypes.Structure):
+    """One layer of a paged cache (include/vla_lm.h): k, v pointers, dtype, sizes, strides in elements."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p)] + \
+               [(n, ctypes.c_int) for n in ("dtype", "n_pages", "page_size", "n_heads", "head_dim")] + \
+               [(n, ctypes.c_int64) for n in ("page_stride", "head_stride", "slot_stride")]
+
+
 class VlaError(RuntimeError):
     def __init__(self, code: int, msg: str):
         super().__init__(f"vla error {code}: {msg}")
@@ -71,6 +82,7 @@ def load(path: str = LIB_PATH):
         raise FileNotFoundError(f"{path} is missing; run `python -c 'import __graft_entry__ as g; g.build()'`")
     lib = ctypes.CDLL(path)
     vp, i32, f32, u32, i64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_uint32, ctypes.c_int64
+    f64 = ctypes.c_double
     sig = {
         "vla_create": (i32, [ctypes.POINTER(VlaConfig), ctypes.POINTER(VlaWeights), vp, ctypes.POINTER(vp)]),
         "vla_prefill": (i32, [vp, i32, vp, i32, vp, ctypes.POINTER(ctypes.c_int32), i32]),
@@ -109,6 +121,15 @@ def load(path: str = LIB_PATH):
         "vla_op_attn_chunk_res": (i32, [vp, vp, vp, i32, i32, i32, i32, vp, i32, i32, vp, vp, vp, vp]),
         "vla_op_attn_rows_res": (i32, [vp, vp, vp, i32, i32, i32, i32, vp, i32, i32, vp, vp, vp, vp]),
         "vla_op_read_status": (i32, [vp, ctypes.POINTER(u32)]),
+        "vla_page_plan": (i32, [vp, vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, i32, vp]),
+        "vla_rope_table": (i32, [vp, i32, i32, f64, i32, f64, f64, f64, f64, f64, vp]),
+        "vla_rope_append": (i32, [vp, i64, vp, i64, vp, i64, i32, i32, i32, ctypes.POINTER(VlaPagedKv), vp, vp, f32, vp, i32, i32,
+                                  i32, vp, vp, vp, i64, vp]),
+        "vla_paged_attn": (i32, [vp, i64, i32, i32, i32, ctypes.POINTER(VlaPagedKv), vp, i32, i32, vp, vp, f32, vp, i64, vp, vp,
+                                 ctypes.c_size_t, vp]),
+        "vla_paged_attn_workspace_bytes": (ctypes.c_size_t, [i32]),
+        "vla_token_logprobs": (i32, [vp, i64, i32, i32, i32, vp, f32, i32, vp, vp, vp, vp, vp, vp]),
+        "vla_token_logprobs_grad": (i32, [vp, i64, i32, i32, i32, vp, f32, vp, vp, vp, vp, vp, i64, vp]),
         "vla_test_inject_launch_error": (i32, [i64, i32]),
         "vla_test_set_wait_limit_ns": (i32, [ctypes.c_uint64]),
         "vla_test_set_max_cluster": (i32, [i32]),
@@ -342,6 +363,55 @@ def vla_op_read_status(stream=0):
     st = ctypes.c_uint32(0)
     rc = load().vla_op_read_status(stream or None, ctypes.byref(st))
     return rc, st.value
+
+
+def vla_page_plan(ctx_in_ptr, new_len_ptr, release_ptr, n_env, page_size, table_ptr, max_pages, pool_ptr, n_pages, n_free_in_ptr,
+                  ctx_out_ptr, n_free_out_ptr, row_start_ptr, row_env_ptr, row_pos_ptr, row_slot_ptr, max_rows, stream=0) -> int:
+    return load().vla_page_plan(ctx_in_ptr or None, new_len_ptr or None, release_ptr or None, n_env, page_size, table_ptr or None,
+                                max_pages, pool_ptr or None, n_pages, n_free_in_ptr or None, ctx_out_ptr or None,
+                                n_free_out_ptr or None, row_start_ptr or None, row_env_ptr or None, row_pos_ptr or None,
+                                row_slot_ptr or None, max_rows, stream or None)
+
+
+def vla_rope_table(table_ptr, n_pos, rope_dim, theta, kind=VLA_ROPE_PLAIN, factor=1.0, original_len=0.0, low=0.0, high=0.0,
+                   amplitude=1.0, stream=0) -> int:
+    return load().vla_rope_table(table_ptr or None, n_pos, rope_dim, theta, kind, factor, original_len, low, high, amplitude,
+                                 stream or None)
+
+
+def vla_rope_append(q_ptr, ldq, k_ptr, ldk, v_ptr, ldv, dtype, rows, n_q_heads, kv, q_gain_ptr, k_gain_ptr, eps, rope_ptr, n_pos,
+                    rope_dim, interleaved, row_pos_ptr, row_slot_ptr, q_out_ptr, ldqo, stream=0) -> int:
+    """kv: a VlaPagedKv."""
+    return load().vla_rope_append(q_ptr or None, ldq, k_ptr or None, ldk, v_ptr or None, ldv, dtype, rows, n_q_heads, kv,
+                                  q_gain_ptr or None, k_gain_ptr or None, eps, rope_ptr or None, n_pos, rope_dim,
+                                  1 if interleaved else 0, row_pos_ptr or None, row_slot_ptr or None, q_out_ptr or None, ldqo,
+                                  stream or None)
+
+
+def vla_paged_attn(q_ptr, ldq, dtype, rows, n_q_heads, kv, table_ptr, max_pages, n_env, row_env_ptr, row_pos_ptr, scale, out_ptr,
+                   ldo, lse_ptr, ws_ptr, ws_bytes, stream=0) -> int:
+    """kv: a VlaPagedKv; the workspace is zeroed once by the caller."""
+    return load().vla_paged_attn(q_ptr or None, ldq, dtype, rows, n_q_heads, kv, table_ptr or None, max_pages, n_env,
+                                 row_env_ptr or None, row_pos_ptr or None, scale, out_ptr or None, ldo, lse_ptr or None,
+                                 ws_ptr or None, ws_bytes, stream or None)
+
+
+def vla_paged_attn_workspace_bytes(head_dim: int) -> int:
+    return load().vla_paged_attn_workspace_bytes(head_dim)
+
+
+def vla_token_logprobs(logits_ptr, ld, dtype, rows, vocab, tokens_ptr, temperature, top_k, logprob_ptr, entropy_ptr, lse_ptr,
+                       top_ids_ptr=0, top_logprobs_ptr=0, stream=0) -> int:
+    return load().vla_token_logprobs(logits_ptr or None, ld, dtype, rows, vocab, tokens_ptr or None, temperature, top_k,
+                                     logprob_ptr or None, entropy_ptr or None, lse_ptr or None, top_ids_ptr or None,
+                                     top_logprobs_ptr or None, stream or None)
+
+
+def vla_token_logprobs_grad(logits_ptr, ld, dtype, rows, vocab, tokens_ptr, temperature, lse_ptr, entropy_ptr, g_logprob_ptr,
+                            g_entropy_ptr, d_logits_ptr, ldd, stream=0) -> int:
+    return load().vla_token_logprobs_grad(logits_ptr or None, ld, dtype, rows, vocab, tokens_ptr or None, temperature,
+                                          lse_ptr or None, entropy_ptr or None, g_logprob_ptr or None, g_entropy_ptr or None,
+                                          d_logits_ptr or None, ldd, stream or None)
 
 
 def vla_test_inject_launch_error(nth_launch: int, cuda_error: int) -> int:
