@@ -89,6 +89,17 @@ __device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t&
   }
 }
 
+__device__ __forceinline__ int load_acquire(const int* p) {
+  int v;
+  asm volatile("ld.acquire.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(p) : "memory");
+  return v;
+}
+__device__ __forceinline__ int add_acq_rel(int* p, int n) {
+  int v;
+  asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], %2;" : "=r"(v) : "l"(p), "r"(n) : "memory");
+  return v;
+}
+
 // Where a CTA is in the list of work.
 struct Cursor {
   int row, item, block;   // item: (key-value head, tile) within the row; block within the item
@@ -270,6 +281,19 @@ __global__ void __launch_bounds__(32 * kWarps, kCtasPerSm) paged_attn_kernel(con
       }
       if constexpr (PAIR) report_saturation(a.status, sat);
     }
+    // the next item's queries on their way into L1 (one line a lane): read at its start, 1 us from L2 or memory
+    if (warp == 0 && done + steps < end) {
+      constexpr int kLine = 128 / (PAIR ? 4 : 2), kLines = HD / kLine;
+      Cursor next = use;
+      next.block = use.blocks - 1;
+      advance(next);
+      const int kv = next.item / tiles, h0 = kv * group + (next.item % tiles) * kHeads, h = h0 + lane / kLines;
+      if (lane < kHeads * kLines && h < (kv + 1) * group) {
+        const int64_t at = next.row * a.ldq + static_cast<int64_t>(h) * HD + lane % kLines * kLine;
+        uint32_t unused;
+        asm volatile("ld.global.b32 %0, [%1];" : "=r"(unused) : "l"(static_cast<const char*>(a.q) + at * (PAIR ? 4 : 2)));
+      }
+    }
     float o[HD / 8][4];
 #pragma unroll
     for (int i = 0; i < HD / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
@@ -356,13 +380,21 @@ __global__ void __launch_bounds__(32 * kWarps, kCtasPerSm) paged_attn_kernel(con
       for (int i = 0; i < HD / 8; ++i)
         *reinterpret_cast<float2*>(dst + 8 * i) = make_float2(o[i][0] + o[i][2], o[i][1] + o[i][3]);
     }
-    __syncthreads();
-    const int64_t item_first = done - from, item_last = item_first + use.blocks - 1;
-    const int c0 = cta_of(item_first), c1 = cta_of(item_last), me = static_cast<int>(blockIdx.x);
-    const int parts = c1 - c0 + 1;
+    // the item's share of other CTAs: the CTAs c0 .. c1 take part
     int* tickets = static_cast<int*>(a.workspace);
     float* slots = reinterpret_cast<float*>(static_cast<uint8_t*>(a.workspace) + kTicketBytes);
-    auto slot_of = [&](int c) { return 2 * c + (c == c0 ? 1 : 0); };
+    const int me = static_cast<int>(blockIdx.x);
+    int c0 = me, c1 = me;
+    if (from > 0) c0 = cta_of(done - from);
+    if (from + steps < use.blocks) c1 = cta_of(done - from + use.blocks - 1);
+    const int parts = c1 - c0 + 1;
+    const bool two = parts > kJoin;  // levels of joins
+    auto slot_of = [&](int c) { return slots + static_cast<size_t>(2 * c + (c == c0 ? 1 : 0)) * slot_floats(HD); };
+    auto ticket_of = [&](int c) { return tickets + 2 * c + (c == c0 ? 1 : 0); };
+    // where all others have already left their parts, this CTA joins them without leaving its own
+    if (parts > 1 && !two && tid == 0) last_here = load_acquire(ticket_of(c0)) == parts - 1;
+    __syncthreads();
+    const bool ready = parts > 1 && !two && last_here;
     constexpr int kAhead = 32 * kWarps / HD;  // heads handled at a time
     const int d = tid % HD;
     auto store = [&](int h, float top, float sum, float val) {
@@ -370,6 +402,28 @@ __global__ void __launch_bounds__(32 * kWarps, kCtasPerSm) paged_attn_kernel(con
       store_from_float(a.out, use.row * a.ldo + static_cast<int64_t>(head0 + h) * HD + d, val * inv, a.dtype);
       if (a.lse && d == 0)
         a.lse[static_cast<int64_t>(use.row) * a.n_q_heads + head0 + h] = (top + log2f(sum) - kShift) * 0.693147181f;
+    };
+    // the parts of `count` CTAs lo, lo + step, ..; `mine` >= 0: that one's from the arguments
+    auto join = [&](int h, int lo, int step, int count, int mine, float& top, float& sum, float& val) {
+      const float m0 = top, l0 = sum, v0 = val;
+      for (int i = 0; i < count; ++i)
+        if (i != mine) top = fmaxf(top, __ldcg(slot_of(lo + i * step) + kHeads * HD + h));
+      sum = val = 0.f;
+      for (int i = 0; i < count; ++i) {
+        const float* slot = slot_of(lo + i * step);
+        const float mi = i == mine ? m0 : __ldcg(slot + kHeads * HD + h), li = i == mine ? l0 : __ldcg(slot + kHeads * HD + kHeads + h);
+        const float vi = i == mine ? v0 : __ldcg(slot + h * HD + d), f = join_weight(mi, top);
+        sum += f * li;
+        val += f * vi;
+      }
+    };
+    auto leave = [&](int c, int h, float top, float sum, float val) {
+      float* slot = slot_of(c);
+      slot[h * HD + d] = val;
+      if (d == 0) {
+        slot[kHeads * HD + h] = top;
+        slot[kHeads * HD + kHeads + h] = sum;
+      }
     };
     for (int h = tid / HD; h < heads; h += kAhead) {
       float top = -INFINITY, sum = 0.f, val = 0.f;
@@ -381,65 +435,37 @@ __global__ void __launch_bounds__(32 * kWarps, kCtasPerSm) paged_attn_kernel(con
         sum += f * join_l[w][h];
         val += f * join_o[(w * kHeads + h) * HD + d];
       }
-      if (parts == 1) {
+      if (ready) join(h, c0, 1, parts, me - c0, top, sum, val);
+      if (parts == 1 || ready)
         store(h, top, sum, val);
-      } else {
-        float* slot = slots + static_cast<size_t>(slot_of(me)) * slot_floats(HD);
-        slot[h * HD + d] = val;
-        if (d == 0) {
-          slot[kHeads * HD + h] = top;
-          slot[kHeads * HD + kHeads + h] = sum;
-        }
-      }
+      else
+        leave(me, h, top, sum, val);
     }
-    if (parts > 1) {
+    if (ready) {
+      if (tid == 0) *ticket_of(c0) = 0;
+    } else if (parts > 1) {
       // groups of kJoin CTAs first, each group's result in its first member's slot, then the groups
-      int lo = c0, step = 1, count = parts;
-      const bool two = parts > kJoin;
-      for (int level = 0; level < (two ? 2 : 1); ++level) {
-        int ticket;
-        if (two && level == 0) {
-          lo = c0 + (me - c0) / kJoin * kJoin;
-          count = min(kJoin, c1 + 1 - lo);
-          ticket = slot_of(lo);
-        } else {
-          lo = c0;
-          step = two ? kJoin : 1;
-          count = two ? (parts + kJoin - 1) / kJoin : parts;
-          ticket = 2 * kMaxCtas + slot_of(c0);
-        }
-        __threadfence();
+      for (int level = two ? 0 : 1; level < 2; ++level) {
+        const int lo = level == 0 ? c0 + (me - c0) / kJoin * kJoin : c0, step = level == 1 && two ? kJoin : 1;
+        const int count = level == 0 ? min(kJoin, c1 + 1 - lo) : (parts + step - 1) / step;
+        int* ticket = ticket_of(lo) + (level == 1 && two ? 2 * kMaxCtas : 0);
         __syncthreads();
         if (tid == 0) {
-          const int before = atomicAdd(&tickets[ticket], 1);
-          last_here = before == count - 1;
-          if (last_here) tickets[ticket] = 0;
-          __threadfence();
+          // the barrier and the release order all threads' parts before the ticket
+          last_here = add_acq_rel(ticket, 1) == count - 1;
+          if (last_here) *ticket = 0;
         }
         __syncthreads();
         if (!last_here) break;
-        const bool final = level == 1 || !two;
         for (int h = tid / HD; h < heads; h += kAhead) {
           float top = -INFINITY, sum = 0.f, val = 0.f;
-          for (int i = 0; i < count; ++i) top = fmaxf(top, __ldcg(slots + static_cast<size_t>(slot_of(lo + i * step)) * slot_floats(HD) + kHeads * HD + h));
-          for (int i = 0; i < count; ++i) {
-            const float* slot = slots + static_cast<size_t>(slot_of(lo + i * step)) * slot_floats(HD);
-            const float f = join_weight(__ldcg(slot + kHeads * HD + h), top);
-            sum += f * __ldcg(slot + kHeads * HD + kHeads + h);
-            val += f * __ldcg(slot + h * HD + d);
-          }
-          if (final) {
+          join(h, lo, step, count, -1, top, sum, val);
+          if (level == 1) {
             store(h, top, sum, val);
           } else {
-            __syncwarp();
-            float* slot = slots + static_cast<size_t>(slot_of(lo)) * slot_floats(HD);
-            slot[h * HD + d] = val;
-            // m and l are read by every thread of this head above
+            // this head's m and l are read by all its threads above
             asm volatile("bar.sync %0, %1;" ::"r"(1 + tid / HD), "r"(HD) : "memory");
-            if (d == 0) {
-              slot[kHeads * HD + h] = top;
-              slot[kHeads * HD + kHeads + h] = sum;
-            }
+            leave(lo, h, top, sum, val);
           }
         }
       }
