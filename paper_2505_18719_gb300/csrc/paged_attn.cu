@@ -102,15 +102,17 @@ __device__ __forceinline__ int add_acq_rel(int* p, int n) {
 
 // Where a CTA is in the list of work.
 struct Cursor {
-  int row, item, block;   // item: (key-value head, tile) within the row; block within the item
-  int n, blocks, env;     // the row's positions, their blocks (at least 1), its environment
+  int row, kv, tile, block;  // an item is (row, key-value head, tile); block within the item
+  int n, blocks, env;        // the row's positions, their blocks (at least 1), its environment
 };
 
-template <int HD, bool BF16, bool PAIR, int STAGES>
+// ALIGNED: pages are multiples of 16 positions, so that a step's positions share a page.
+template <int HD, bool BF16, bool PAIR, bool ALIGNED, int STAGES>
 __global__ void __launch_bounds__(32 * kWarps, kCtasPerSm) paged_attn_kernel(const PagedAttnArgs a, const int page_shift, const int tiles) {
   using R = Ring<HD, STAGES>;
   constexpr float kShift = BF16 ? 0.f : 15.f;
-  extern __shared__ __align__(128) uint8_t sm[];
+  extern __shared__ __align__(128) uint8_t sm_raw[];
+  uint8_t* sm = sm_raw + (-smem_u32(sm_raw) & 255u);  // rows of 256 bytes at multiples of 256
   float* join_o = reinterpret_cast<float*>(sm + R::kBytes);  // [kWarps][kHeads][HD]
   __shared__ float join_m[kWarps][kHeads], join_l[kWarps][kHeads];
   __shared__ uint32_t seen[kWarps][STAGES];
@@ -135,8 +137,10 @@ __global__ void __launch_bounds__(32 * kWarps, kCtasPerSm) paged_attn_kernel(con
   auto advance = [&](Cursor& c) {
     if (++c.block < c.blocks) return;
     c.block = 0;
-    if (++c.item < items) return;
-    c.item = 0;
+    if (++c.tile < tiles) return;
+    c.tile = 0;
+    if (++c.kv < a.kv.n_heads) return;
+    c.kv = 0;
     if (++c.row < a.rows) row_of(c);
   };
 
@@ -194,19 +198,24 @@ __global__ void __launch_bounds__(32 * kWarps, kCtasPerSm) paged_attn_kernel(con
   row_of(use);
   {
     const int64_t in_row = first - start_sum;
-    use.item = static_cast<int>(in_row / use.blocks);
+    const int item = static_cast<int>(in_row / use.blocks);
     use.block = static_cast<int>(in_row % use.blocks);
+    use.kv = item / tiles;
+    use.tile = item % tiles;
   }
 
-  // ---- loading: the page of this lane's position (lanes 0-15) is known one step ahead
+  // ---- loading: the page of the step's positions (of lane i's position i, where they may differ) is known
+  // one step ahead
   Cursor load = use;
   int64_t to_load = end - first;
   int next_page = -1;
   const uint32_t ring = smem_u32(sm) + warp * STAGES * R::kStage;
+  constexpr int kChunks = HD / 8, kRows = 32 / kChunks;  // 16-byte pieces of a position, positions per instruction
+  const int chunk = lane % kChunks, my_row = lane / kChunks;
   auto look_up = [&]() {
     next_page = -1;
-    const int key = load.block * kBlock + warp * kStep + lane;
-    if (to_load > 0 && lane < kStep && key < load.n) {
+    const int key = load.block * kBlock + warp * kStep + (ALIGNED ? 0 : lane);
+    if (to_load > 0 && (ALIGNED || lane < kStep) && key < load.n) {
       const int col = page_shift >= 0 ? key >> page_shift : key / a.kv.page_size;
       next_page = a.table[static_cast<int64_t>(load.env) * a.max_pages + col];
       if (static_cast<unsigned>(next_page) >= static_cast<unsigned>(a.kv.n_pages)) {
@@ -216,26 +225,46 @@ __global__ void __launch_bounds__(32 * kWarps, kCtasPerSm) paged_attn_kernel(con
     }
   };
   auto issue = [&](int stage) {
-    const int key = load.block * kBlock + warp * kStep + lane;
+    const int key = load.block * kBlock + warp * kStep + (ALIGNED ? 0 : lane);
     const int slot = page_shift >= 0 ? key & ((1 << page_shift) - 1) : key % a.kv.page_size;
-    const int64_t off = next_page * a.kv.page_stride + slot * a.kv.slot_stride + (load.item / tiles) * a.kv.head_stride;
-    const uint32_t mask = __ballot_sync(0xffffffffu, next_page >= 0);
-    if (lane == 0) seen[warp][stage] = to_load > 0 ? mask : 0u;
-    if (mask) {
-      constexpr int kChunks = HD / 8, kRows = 32 / kChunks;  // 16-byte pieces of a position, positions per instruction
-      const int chunk = lane % kChunks;
-      const uint32_t dst0 = ring + stage * R::kStage;
+    int64_t off = next_page * a.kv.page_stride + slot * a.kv.slot_stride + load.kv * a.kv.head_stride;
+    const uint32_t dst0 = ring + stage * R::kStage + my_row * R::kRow;
+    uint32_t mask;
+    if constexpr (ALIGNED) {
+      const int some = next_page >= 0 ? min(kStep, load.n - key) : 0;
+      mask = (1u << some) - 1u;
+      if (some > 0) {
+        off += chunk * 8 + my_row * a.kv.slot_stride;
+        const uint16_t* k = static_cast<const uint16_t*>(a.kv.k) + off;
+        const uint16_t* v = static_cast<const uint16_t*>(a.kv.v) + off;
+        const int64_t pitch = kRows * a.kv.slot_stride;
 #pragma unroll
-      for (int i = 0; i < kStep / kRows; ++i) {
-        const int r = i * kRows + lane / kChunks;
-        const int64_t o = __shfl_sync(0xffffffffu, off, r);
-        const bool ok = (mask >> r) & 1u;
-        const uint32_t dst = dst0 + r * R::kRow + ((chunk ^ (r & 7)) << 4);
-        const int64_t from = ok ? o + chunk * 8 : 0;
-        cp16(dst, static_cast<const uint16_t*>(a.kv.k) + from, ok ? 16u : 0u);
-        cp16(dst + R::kPlane, static_cast<const uint16_t*>(a.kv.v) + from, ok ? 16u : 0u);
+        for (int i = 0; i < kStep / kRows; ++i) {
+          // a position past the last is not read: zeros, from an address that is not used
+          const bool ok = i * kRows + my_row < some;
+          const uint32_t dst = dst0 + i * kRows * R::kRow + ((chunk ^ ((i * kRows + my_row) & 7)) << 4);
+          cp16(dst, ok ? k : static_cast<const uint16_t*>(a.kv.k), ok ? 16u : 0u);
+          cp16(dst + R::kPlane, ok ? v : static_cast<const uint16_t*>(a.kv.v), ok ? 16u : 0u);
+          k += pitch;
+          v += pitch;
+        }
+      }
+    } else {
+      mask = __ballot_sync(0xffffffffu, next_page >= 0);
+      if (mask) {
+#pragma unroll
+        for (int i = 0; i < kStep / kRows; ++i) {
+          const int r = i * kRows + my_row;
+          const int64_t o = __shfl_sync(0xffffffffu, off, r);
+          const bool ok = (mask >> r) & 1u;
+          const uint32_t dst = dst0 + i * kRows * R::kRow + ((chunk ^ (r & 7)) << 4);
+          const int64_t from = ok ? o + chunk * 8 : 0;
+          cp16(dst, static_cast<const uint16_t*>(a.kv.k) + from, ok ? 16u : 0u);
+          cp16(dst + R::kPlane, static_cast<const uint16_t*>(a.kv.v) + from, ok ? 16u : 0u);
+        }
       }
     }
+    if (lane == 0) seen[warp][stage] = mask;
     asm volatile("cp.async.commit_group;" ::: "memory");
     if (to_load > 0) {
       --to_load;
@@ -255,23 +284,46 @@ __global__ void __launch_bounds__(32 * kWarps, kCtasPerSm) paged_attn_kernel(con
   while (done < end) {
     const int from = use.block;
     const int steps = static_cast<int>(min(static_cast<int64_t>(use.blocks - from), end - done));
-    const int kv_head = use.item / tiles, head0 = kv_head * group + (use.item % tiles) * kHeads;
-    const int heads = min(kHeads, (kv_head + 1) * group - head0);
+    const int head0 = use.kv * group + use.tile * kHeads;
+    const int heads = min(kHeads, group - use.tile * kHeads);
     uint32_t q[HD / 16][PAIR ? 4 : 2];
     {
       const int64_t q_at = use.row * a.ldq + static_cast<int64_t>(head0 + g) * HD + 2 * t;
-      uint32_t sat = 0;
+      if constexpr (PAIR) {
+        float far = 0.f;
 #pragma unroll
-      for (int k = 0; k < HD / 16; ++k) {
-        if constexpr (PAIR) {
+        for (int k = 0; k < HD / 16; ++k) {
           float2 x = make_float2(0.f, 0.f), y = x;
           if (g < heads) {
             x = *reinterpret_cast<const float2*>(static_cast<const float*>(a.q) + q_at + 16 * k);
             y = *reinterpret_cast<const float2*>(static_cast<const float*>(a.q) + q_at + 16 * k + 8);
           }
-          split_pack2_f16(x.x, x.y, q[k][0], q[k][1], sat);
-          split_pack2_f16(y.x, y.y, q[k][2], q[k][3], sat);
-        } else {
+          far = fmaxf(far, fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(y.x), fabsf(y.y))));
+          split2<false>(x.x, x.y, q[k][0], q[k][1]);
+          split2<false>(y.x, y.y, q[k][2], q[k][3]);
+        }
+        if (far > 65504.f) {  // as the other activations of the path: the largest fp16 value, and a status bit
+          uint32_t sat = 0;
+#pragma unroll 1
+          for (int k = 0; k < HD / 16; ++k) {
+            const float* x = static_cast<const float*>(a.q) + q_at + 16 * k;
+            uint32_t w[4];
+            split_pack2_f16(x[0], x[1], w[0], w[1], sat);
+            split_pack2_f16(x[8], x[9], w[2], w[3], sat);
+#pragma unroll
+            for (int i = 0; i < HD / 16; ++i)
+              if (i == k) {
+                q[i][0] = w[0];
+                q[i][1] = w[1];
+                q[i][2] = w[2];
+                q[i][3] = w[3];
+              }
+          }
+          report_saturation(a.status, sat);
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < HD / 16; ++k) {
           q[k][0] = q[k][1] = 0u;
           if (g < heads) {
             q[k][0] = *reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(a.q) + q_at + 16 * k);
@@ -279,7 +331,6 @@ __global__ void __launch_bounds__(32 * kWarps, kCtasPerSm) paged_attn_kernel(con
           }
         }
       }
-      if constexpr (PAIR) report_saturation(a.status, sat);
     }
     // the next item's queries on their way into L1 (one line a lane): read at its start, 1 us from L2 or memory
     if (warp == 0 && done + steps < end) {
@@ -287,9 +338,9 @@ __global__ void __launch_bounds__(32 * kWarps, kCtasPerSm) paged_attn_kernel(con
       Cursor next = use;
       next.block = use.blocks - 1;
       advance(next);
-      const int kv = next.item / tiles, h0 = kv * group + (next.item % tiles) * kHeads, h = h0 + lane / kLines;
-      if (lane < kHeads * kLines && h < (kv + 1) * group) {
-        const int64_t at = next.row * a.ldq + static_cast<int64_t>(h) * HD + lane % kLines * kLine;
+      const int h = next.tile * kHeads + lane / kLines;
+      if (lane < kHeads * kLines && h < group) {
+        const int64_t at = next.row * a.ldq + static_cast<int64_t>(next.kv * group + h) * HD + lane % kLines * kLine;
         uint32_t unused;
         asm volatile("ld.global.b32 %0, [%1];" : "=r"(unused) : "l"(static_cast<const char*>(a.q) + at * (PAIR ? 4 : 2)));
       }
@@ -309,12 +360,13 @@ __global__ void __launch_bounds__(32 * kWarps, kCtasPerSm) paged_attn_kernel(con
       if (!mask) continue;
       float s[2][4] = {};
       {
+        // piece 2k + b of row r lies at (2k + b) ^ (r & 7): the k-th step flips bits of one address
         const int r = (lane & 7) + ((lane >> 4) << 3);
-        const uint32_t row = keys + r * R::kRow;
+        const uint32_t row = (keys + r * R::kRow) | ((((lane >> 3) & 1) ^ (r & 7)) << 4);
 #pragma unroll
         for (int k = 0; k < HD / 16; ++k) {
           uint32_t b[4];
-          ldsm(b, row + (((2 * k + ((lane >> 3) & 1)) ^ (r & 7)) << 4));
+          ldsm(b, row ^ (k << 5));
           if constexpr (PAIR) {
             mma<BF16>(s[0], q[k][0], q[k][1], q[k][2], q[k][3], b[0], b[1]);
             mma<BF16>(s[1], q[k][0], q[k][1], q[k][2], q[k][3], b[2], b[3]);
@@ -356,11 +408,11 @@ __global__ void __launch_bounds__(32 * kWarps, kCtasPerSm) paged_attn_kernel(con
       split2<BF16>(p[2], p[3], p2, p3);
       {
         const int r = (lane & 7) + (((lane >> 3) & 1) << 3);
-        const uint32_t row = values + r * R::kRow;
+        const uint32_t row = (values + r * R::kRow) | (((lane >> 4) ^ (r & 7)) << 4);
 #pragma unroll
         for (int j = 0; j < HD / 16; ++j) {
           uint32_t b[4];
-          ldsm_t(b, row + (((2 * j + (lane >> 4)) ^ (r & 7)) << 4));
+          ldsm_t(b, row ^ (j << 5));
           mma<BF16>(o[2 * j], p0, p1, p2, p3, b[0], b[1]);
           mma<BF16>(o[2 * j + 1], p0, p1, p2, p3, b[2], b[3]);
         }
@@ -491,22 +543,21 @@ int paged_attn_launch(const PagedAttnArgs& a, cudaStream_t s) {
   const int64_t most = static_cast<int64_t>(a.rows) * a.kv.n_heads * tiles * ((static_cast<int64_t>(a.max_pages) * ps + kBlock - 1) / kBlock);
   const int grid = static_cast<int>(std::min<int64_t>(std::min(kCtasPerSm * sms, kMaxCtas), most));
   auto go = [&](auto kern, int ring_bytes, std::atomic<uint64_t>& done) -> int {
-    const int smem = ring_bytes + kWarps * kHeads * a.kv.head_dim * static_cast<int>(sizeof(float));
+    const int smem = 256 + ring_bytes + kWarps * kHeads * a.kv.head_dim * static_cast<int>(sizeof(float));
     VLA_CUDA_TRY(set_smem_limit(kern, smem, done));
     VLA_CUDA_TRY(launch_pdl(kern, dim3(grid), dim3(32 * kWarps), smem, s, a, shift, tiles));
     note_launch();
     VLA_CUDA_TRY(cudaGetLastError());
     return VLA_OK;
   };
-  static std::atomic<uint64_t> done[6] = {};
-  if (a.kv.head_dim == 128) {
-    if (a.kv.dtype == VLA_BF16) return go(paged_attn_kernel<128, true, false, 3>, Ring<128, 3>::kBytes, done[0]);
-    return a.dtype == VLA_F32 ? go(paged_attn_kernel<128, false, true, 3>, Ring<128, 3>::kBytes, done[1])
-                              : go(paged_attn_kernel<128, false, false, 3>, Ring<128, 3>::kBytes, done[2]);
-  }
-  if (a.kv.dtype == VLA_BF16) return go(paged_attn_kernel<64, true, false, 4>, Ring<64, 4>::kBytes, done[3]);
-  return a.dtype == VLA_F32 ? go(paged_attn_kernel<64, false, true, 4>, Ring<64, 4>::kBytes, done[4])
-                            : go(paged_attn_kernel<64, false, false, 4>, Ring<64, 4>::kBytes, done[5]);
+  static std::atomic<uint64_t> done[12] = {};
+  const bool pair = a.dtype == VLA_F32, bf = a.kv.dtype == VLA_BF16, aligned = ps % kStep == 0;
+#define VLA_PAGED(HD, BF, PAIR, ST, I)                                                                \
+  (aligned ? go(paged_attn_kernel<HD, BF, PAIR, true, ST>, Ring<HD, ST>::kBytes, done[2 * (I)])       \
+           : go(paged_attn_kernel<HD, BF, PAIR, false, ST>, Ring<HD, ST>::kBytes, done[2 * (I) + 1]))
+  if (a.kv.head_dim == 128) return bf ? VLA_PAGED(128, true, false, 3, 0) : pair ? VLA_PAGED(128, false, true, 3, 1) : VLA_PAGED(128, false, false, 3, 2);
+  return bf ? VLA_PAGED(64, true, false, 4, 3) : pair ? VLA_PAGED(64, false, true, 4, 4) : VLA_PAGED(64, false, false, 4, 5);
+#undef VLA_PAGED
 }
 
 }  // namespace vla
