@@ -1,7 +1,10 @@
 // The paged cache's bookkeeping and its writes: the page plan of a step (pages taken from a pool,
 // rows mapped to slots), the rotary table, and the step that normalises, rotates and files queries,
 // keys and values.
+#include <algorithm>
+
 #include "lm.h"
+#include "ptx.cuh"
 
 namespace vla {
 
@@ -11,9 +14,11 @@ namespace {
 // With ctx_e the positions cached (0 for an environment that starts over), have_e = ceil(ctx_e / ps) and
 // want_e = ceil((ctx_e + new_e) / ps), environment e takes want_e - have_e pages; exclusive sums over the
 // environments give its first row, its first page off the pool's end and, for releases, the place of its old
-// pages.  One CTA: the sums by a block scan in shared memory, then one thread per page and per row, which
-// finds its environment by bisection.
-constexpr int kPlanThreads = 1024;
+// pages.  Bound by latency for a decode step; a prefill writes 12 bytes a row.  One cluster: every CTA makes the sums
+// for itself (a block scan into shared memory), then the CTAs share the pages and the rows, four rows a thread,
+// which finds the first one's environment by bisection.  The cluster's barriers stand between reading
+// the state and writing it, and between pages given back and pages taken.
+constexpr int kPlanThreads = 512;
 
 __device__ __forceinline__ int64_t warp_inclusive(int64_t v) {
 #pragma unroll
@@ -37,26 +42,26 @@ __device__ __forceinline__ int env_of(const int* start, int n, int i) {
   return lo;
 }
 
-__device__ __forceinline__ int pages_of(int64_t positions, int page_size) {
-  return static_cast<int>((positions + page_size - 1) / page_size);
-}
-
-__global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PagePlanArgs a) {
+// `page_shift` >= 0: pages of 1 << page_shift positions.
+__global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PagePlanArgs a, const int parts, const int page_shift) {
   extern __shared__ int plan_sm[];
-  int* row_first = plan_sm;                 // [n_env]
-  int* page_first = row_first + a.n_env;    // [n_env]
-  int* old_first = page_first + a.n_env;    // [n_env] released pages before this environment's
-  int* ctx0 = old_first + a.n_env;          // [n_env] positions that stay
-  __shared__ int64_t sums[3][33];
+  int* row_first = plan_sm;                   // [n_env + 1]
+  int* page_first = row_first + a.n_env + 1;  // [n_env]
+  int* ctx0 = page_first + a.n_env;           // [n_env] positions that stay
+  int* old_first = ctx0 + a.n_env;            // [n_env] released pages before this environment's
+  __shared__ int64_t sums[3][kPlanThreads / 32];
   __shared__ int64_t carry[3];
   __shared__ int bad;
   pdl_launch_dependents();
   pdl_wait();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int part = static_cast<int>(blockIdx.x), all = parts * kPlanThreads, me = part * kPlanThreads + tid;
   if (tid < 3) carry[tid] = 0;
   if (tid == 0) bad = 0;
   const int n_free = *a.n_free_in;
   const int64_t room = static_cast<int64_t>(a.max_pages) * a.page_size;
+  auto page_of = [&](int position) { return page_shift >= 0 ? position >> page_shift : position / a.page_size; };
+  auto pages_of = [&](int64_t n) { return n > 0 ? page_of(static_cast<int>(n - 1)) + 1 : 0; };
   __syncthreads();
   for (int base = 0; base < a.n_env; base += kPlanThreads) {
     const int e = base + tid;
@@ -65,36 +70,41 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PagePlanA
       const int64_t ctx = a.ctx_in[e], add = a.new_len[e];
       const bool out = a.release && a.release[e] != 0;
       const int64_t kept = out ? 0 : ctx;
-      if (ctx < 0 || add < 0 || ctx > room || kept + add > room) {
+      if (ctx < 0 || add < 0 || ctx > room || kept + add > room || kept + add > 0x7fffffff) {
         bad = 1;
         ctx0[e] = 0;
       } else {
         v[0] = add;
-        v[1] = pages_of(kept + add, a.page_size) - pages_of(kept, a.page_size);
-        v[2] = out ? pages_of(ctx, a.page_size) : 0;
+        v[1] = pages_of(kept + add) - pages_of(kept);
+        v[2] = out ? pages_of(ctx) : 0;
         ctx0[e] = static_cast<int>(kept);
       }
     }
+    int64_t inc[3];
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
-      const int64_t inc = warp_inclusive(v[i]);
-      if (lane == 31) sums[i][warp] = inc;
-      v[i] = inc - v[i];
+      inc[i] = warp_inclusive(v[i]);
+      if (lane == 31) sums[i][warp] = inc[i];
     }
     __syncthreads();
-    if (warp < 3) {
-      const int64_t s = sums[warp][lane], inc = warp_inclusive(s);
-      sums[warp][lane] = carry[warp] + inc - s;
-      if (lane == 31) sums[warp][32] = carry[warp] + inc;
+    int64_t before[3], total[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      before[i] = total[i] = carry[i];
+#pragma unroll
+      for (int w = 0; w < kPlanThreads / 32; ++w) {
+        if (w < warp) before[i] += sums[i][w];
+        total[i] += sums[i][w];
+      }
     }
-    __syncthreads();
     if (e < a.n_env) {
       // totals beyond 32 bits do not fit the rows or the pool and are refused below
-      row_first[e] = static_cast<int>(v[0] + sums[0][warp]);
-      page_first[e] = static_cast<int>(v[1] + sums[1][warp]);
-      old_first[e] = static_cast<int>(v[2] + sums[2][warp]);
+      row_first[e] = static_cast<int>(before[0] + inc[0] - v[0]);
+      page_first[e] = static_cast<int>(before[1] + inc[1] - v[1]);
+      old_first[e] = static_cast<int>(before[2] + inc[2] - v[2]);
     }
-    if (tid < 3) carry[tid] = sums[tid][32];
+    __syncthreads();
+    if (tid < 3) carry[tid] = tid == 0 ? total[0] : tid == 1 ? total[1] : total[2];
     __syncthreads();
   }
   const int64_t rows64 = carry[0], taken64 = carry[1], old64 = carry[2];
@@ -102,38 +112,66 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PagePlanA
   const int rows = fits ? static_cast<int>(rows64) : 0, taken = fits ? static_cast<int>(taken64) : 0;
   const int old = fits ? static_cast<int>(old64) : 0;
   const int top = n_free + old;
-  if (!fits && tid == 0) raise_status(a.status, VLA_STATUS_PAGES);
-  for (int i = tid; i < old; i += kPlanThreads) {
+  if (!fits && me == 0) raise_status(a.status, VLA_STATUS_PAGES);
+  if (tid == 0) row_first[a.n_env] = static_cast<int>(rows64);
+  for (int i = me; i < old; i += all) {
     const int e = env_of(old_first, a.n_env, i);
     a.pool[n_free + i] = a.table[static_cast<int64_t>(e) * a.max_pages + (i - old_first[e])];
   }
-  __syncthreads();
-  for (int i = tid; i < taken; i += kPlanThreads) {
+  if (parts > 1)
+    cluster_sync();
+  else
+    __syncthreads();
+  for (int i = me; i < taken; i += all) {
     const int e = env_of(page_first, a.n_env, i);
-    const int col = pages_of(ctx0[e], a.page_size) + i - page_first[e];
-    a.table[static_cast<int64_t>(e) * a.max_pages + col] = a.pool[top - 1 - i];
+    const int col = pages_of(ctx0[e]) + i - page_first[e];
+    a.table[static_cast<int64_t>(e) * a.max_pages + col] = __ldcg(a.pool + top - 1 - i);
   }
-  for (int r = tid; r < a.max_rows; r += kPlanThreads) {
-    int e = -1, pos = -1, slot = -1;
-    if (r < rows) {
-      e = env_of(row_first, a.n_env, r);
-      pos = ctx0[e] + r - row_first[e];
-      const int have = pages_of(ctx0[e], a.page_size), col = pos / a.page_size;
-      const int page = col < have ? a.table[static_cast<int64_t>(e) * a.max_pages + col] : a.pool[top - 1 - (page_first[e] + col - have)];
-      if (static_cast<unsigned>(page) < static_cast<unsigned>(a.n_pages))
-        slot = page * a.page_size + pos % a.page_size;
-      else
-        raise_status(a.status, VLA_STATUS_PAGES);
+  const bool wide = !((reinterpret_cast<uintptr_t>(a.row_env) | reinterpret_cast<uintptr_t>(a.row_pos) | reinterpret_cast<uintptr_t>(a.row_slot)) & 15u);
+  for (int r0 = me * 4; r0 < a.max_rows; r0 += all * 4) {
+    int env[4], pos[4], slot[4];
+    int e = r0 < rows ? env_of(row_first, a.n_env, r0) : 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      env[i] = pos[i] = slot[i] = -1;
+      if (r0 + i < rows) {
+        while (r0 + i >= row_first[e + 1]) ++e;
+        env[i] = e;
+        pos[i] = ctx0[e] + r0 + i - row_first[e];
+        const int have = pages_of(ctx0[e]), col = page_of(pos[i]);
+        // a page of this call comes from the pool, where its table entry comes from too
+        slot[i] = col < have ? a.table[static_cast<int64_t>(e) * a.max_pages + col] : __ldcg(a.pool + top - 1 - (page_first[e] + col - have));
+      }
     }
-    a.row_env[r] = e;
-    a.row_pos[r] = pos;
-    a.row_slot[r] = slot;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (r0 + i >= rows) continue;
+      if (static_cast<unsigned>(slot[i]) < static_cast<unsigned>(a.n_pages)) {
+        slot[i] = slot[i] * a.page_size + pos[i] - page_of(pos[i]) * a.page_size;
+      } else {
+        slot[i] = -1;
+        raise_status(a.status, VLA_STATUS_PAGES);
+      }
+    }
+    if (wide && r0 + 4 <= a.max_rows) {
+      *reinterpret_cast<int4*>(a.row_env + r0) = make_int4(env[0], env[1], env[2], env[3]);
+      *reinterpret_cast<int4*>(a.row_pos + r0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
+      *reinterpret_cast<int4*>(a.row_slot + r0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (r0 + i >= a.max_rows) break;
+        a.row_env[r0 + i] = env[i];
+        a.row_pos[r0 + i] = pos[i];
+        a.row_slot[r0 + i] = slot[i];
+      }
+    }
   }
-  for (int e = tid; e < a.n_env; e += kPlanThreads) {
+  for (int e = me; e < a.n_env; e += all) {
     a.row_start[e] = fits ? row_first[e] : 0;
-    a.ctx_out[e] = fits ? ctx0[e] + (e + 1 < a.n_env ? row_first[e + 1] : rows) - row_first[e] : a.ctx_in[e];
+    a.ctx_out[e] = fits ? ctx0[e] + row_first[e + 1] - row_first[e] : a.ctx_in[e];
   }
-  if (tid == 0) {
+  if (me == 0) {
     a.row_start[a.n_env] = rows;
     *a.n_free_out = fits ? top - taken : n_free;
   }
@@ -162,7 +200,13 @@ __global__ void __launch_bounds__(256) rope_table_kernel(const RopeTableArgs a) 
 }
 
 // ------------------------------------------------------------------------------------ rope append
-// One warp per (row, head), the head's channels in shared memory between the norm and the rotation.
+// x <- x / sqrt(mean x^2 + eps) gain, then per pair (a, b) of channels (a cos - b sin, b cos + a sin).  Each element is
+// read and written once; bound by HBM for a prefill, by latency for a decode step.  hd / 8 lanes hold a head, 8
+// channels each in 16-byte accesses (32 for fp32); the partner of a channel in the other half is a shuffle
+// away.  A warp walks over heads of one row, whose cosines and sines stay in registers; a row of few is cut
+// over several warps so that a decode step fills the GPU.
+enum RopeLayout : int { kNoRope = 0, kHalves = 1, kPairs = 2 };
+
 __device__ __forceinline__ float clamp_f16(float x, uint32_t& sat) {
   if (fabsf(x) > 65504.f && fabsf(x) != INFINITY) {
     x = copysignf(65504.f, x);
@@ -171,58 +215,160 @@ __device__ __forceinline__ float clamp_f16(float x, uint32_t& sat) {
   return x;
 }
 
-__global__ void __launch_bounds__(256) rope_append_kernel(const RopeAppendArgs a) {
-  __shared__ float head_sm[8][128];
-  pdl_launch_dependents();
-  pdl_wait();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int heads = a.n_q_heads + 2 * a.kv.n_heads, hd = a.kv.head_dim;
-  const int64_t item = static_cast<int64_t>(blockIdx.x) * 8 + warp;
-  if (item >= static_cast<int64_t>(a.rows) * heads) return;
-  const int row = static_cast<int>(item / heads);
-  int head = static_cast<int>(item % heads);
-  const bool is_q = head < a.n_q_heads, is_v = head >= a.n_q_heads + a.kv.n_heads;
-  if (!is_q) head -= is_v ? a.n_q_heads + a.kv.n_heads : a.n_q_heads;
-  int pos = a.row_pos[row];
-  const int slot = a.row_slot[row];
-  bool bad = pos < -1 || (a.rope && pos >= a.n_pos);
-  const bool empty = pos == -1 || bad;
-  if (!is_q && !empty && slot != -1 && static_cast<unsigned>(slot) >= static_cast<unsigned>(a.kv.n_pages * a.kv.page_size)) bad = true;
-  if (bad && lane == 0) raise_status(a.status, VLA_STATUS_PAGES);
-  if (!is_q && (empty || bad || slot < 0)) return;
-  const void* src = is_q ? a.q : is_v ? a.v : a.k;
-  const int64_t at = row * (is_q ? a.ldq : is_v ? a.ldv : a.ldk) + static_cast<int64_t>(head) * hd;
-  float* x = head_sm[warp];
-  float ss = 0.f;
-  for (int c = lane; c < hd; c += 32) {
-    x[c] = load_as_float(src, at + c, a.dtype);
-    ss += x[c] * x[c];
+template <int DT>
+struct Eight {  // 8 channels of type DT as they lie in memory
+  uint4 v[DT == VLA_F32 ? 2 : 1];
+  __device__ __forceinline__ void load(const void* p, int64_t i) {
+    const uint4* q = reinterpret_cast<const uint4*>(static_cast<const char*>(p) + i * (DT == VLA_F32 ? 4 : 2));
+    v[0] = q[0];
+    if constexpr (DT == VLA_F32) v[1] = q[1];
   }
-  const bf16* gain = is_q ? a.q_gain : is_v ? nullptr : a.k_gain;
-  if (gain) {
-    const float r = rsqrtf(warp_sum(ss) / static_cast<float>(hd) + a.eps);
-    for (int c = lane; c < hd; c += 32) x[c] = x[c] * r * bf2f(gain[c]);
-  }
-  __syncwarp();
-  const int half = a.rope && !is_v ? a.rope_dim / 2 : 0;
-  uint32_t sat = 0;
-  for (int c = lane; c < hd; c += 32) {
-    float y = x[c];
-    if (c < 2 * half) {
-      const int pair = a.interleaved ? c >> 1 : c < half ? c : c - half;
-      const int other = a.interleaved ? c ^ 1 : c < half ? c + half : c - half;
-      const bool second = a.interleaved ? c & 1 : c >= half;
-      if (!empty) {
-        const float2 t = a.rope[static_cast<int64_t>(pos) * half + pair];
-        y = second ? x[c] * t.x + x[other] * t.y : x[c] * t.x - x[other] * t.y;
+  __device__ __forceinline__ void unpack(float (&x)[8]) const {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(v);
+#pragma unroll
+    for (int i = 0; i < (DT == VLA_F32 ? 8 : 4); ++i) {
+      if constexpr (DT == VLA_F32) {
+        x[i] = __uint_as_float(w[i]);
+      } else {
+        const float2 f = DT == VLA_F16 ? unpack_f16x2(w[i]) : unpack_bf16x2(w[i]);
+        x[2 * i] = f.x;
+        x[2 * i + 1] = f.y;
       }
     }
-    if (is_q) {
-      store_from_float(a.q_out, row * a.ldqo + static_cast<int64_t>(head) * hd + c, empty ? 0.f : y, a.dtype);
-    } else {
-      if (a.kv.dtype == VLA_F16) y = clamp_f16(y, sat);
-      const int64_t to = (slot / a.kv.page_size) * a.kv.page_stride + head * a.kv.head_stride + (slot % a.kv.page_size) * a.kv.slot_stride + c;
-      store_from_float(is_v ? a.kv.v : a.kv.k, to, y, a.kv.dtype);
+  }
+};
+__device__ __forceinline__ uint4 pack8(const float (&x)[8], bool f16_type) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = f16_type ? pack_f16x2(x[2 * i], x[2 * i + 1]) : pack_bf16x2(x[2 * i], x[2 * i + 1]);
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+constexpr int kAppendThreads = 128;
+
+// `slices` warps share a row's heads.
+template <int DT, int LAYOUT, bool NORM>
+__global__ void __launch_bounds__(kAppendThreads) rope_append_kernel(const RopeAppendArgs a, const int slices) {
+  constexpr int kUnroll = 4;
+  pdl_launch_dependents();
+  pdl_wait();
+  const int lane = threadIdx.x & 31, hd = a.kv.head_dim, span = hd / 8;  // lanes of a head
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kAppendThreads / 32) + (threadIdx.x >> 5);
+  if (unit >= static_cast<int64_t>(a.rows) * slices) return;
+  const int row = static_cast<int>(unit / slices), slice = static_cast<int>(unit % slices);
+  const int per = 32 / span, c0 = lane % span * 8;  // heads of an access; this lane's first channel
+  const int heads = a.n_q_heads + 2 * a.kv.n_heads, steps = (heads + per - 1) / per;
+  const int from = static_cast<int>(static_cast<int64_t>(steps) * slice / slices) * per;
+  const int to = min(heads, static_cast<int>(static_cast<int64_t>(steps) * (slice + 1) / slices) * per);
+  const int pos = a.row_pos[row], slot = a.row_slot[row];
+  const bool lost = pos < -1 || (LAYOUT != kNoRope && pos >= a.n_pos), empty = pos == -1 || lost;
+  const bool stray = slot < -1 || slot >= a.kv.n_pages * a.kv.page_size;
+  if ((lost || (stray && !empty)) && lane == 0 && slice == 0) raise_status(a.status, VLA_STATUS_PAGES);
+  const bool file = !empty && !stray && slot != -1;
+  const int64_t cell = file ? (slot / a.kv.page_size) * a.kv.page_stride + (slot % a.kv.page_size) * a.kv.slot_stride + c0 : 0;
+
+  const int half = a.rope_dim / 2;
+  const bool turns = LAYOUT != kNoRope && !empty && c0 < a.rope_dim;
+  const bool second = LAYOUT == kHalves && c0 >= half;
+  float cs[LAYOUT == kHalves ? 8 : 4], sn[LAYOUT == kHalves ? 8 : 4];
+  if constexpr (LAYOUT != kNoRope) {
+    constexpr int kPairs8 = LAYOUT == kHalves ? 8 : 4;
+    const float4* t = reinterpret_cast<const float4*>(a.rope + static_cast<int64_t>(pos) * half + (LAYOUT == kHalves ? (second ? c0 - half : c0) : c0 / 2));
+#pragma unroll
+    for (int i = 0; i < kPairs8 / 2; ++i) {
+      float4 x = make_float4(1.f, 0.f, 1.f, 0.f);
+      if (turns) x = t[i];
+      cs[2 * i] = x.x;
+      sn[2 * i] = second ? -x.y : x.y;  // b cos + a sin: the partner's sign turns
+      cs[2 * i + 1] = x.z;
+      sn[2 * i + 1] = second ? -x.w : x.w;
+    }
+  }
+  uint4 gq = make_uint4(0u, 0u, 0u, 0u), gk = gq;
+  if constexpr (NORM) {
+    if (a.q_gain) gq = *reinterpret_cast<const uint4*>(a.q_gain + c0);
+    if (a.k_gain) gk = *reinterpret_cast<const uint4*>(a.k_gain + c0);
+  }
+  const int partner = second ? lane - half / 8 : lane + half / 8;
+  uint32_t sat = 0;
+  for (int base = from; base < to; base += kUnroll * per) {
+    Eight<DT> raw[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const int h = base + u * per + lane / span;
+      if (h < to && !empty) {
+        if (h < a.n_q_heads)
+          raw[u].load(a.q, row * a.ldq + static_cast<int64_t>(h) * hd + c0);
+        else if (h < a.n_q_heads + a.kv.n_heads)
+          raw[u].load(a.k, row * a.ldk + static_cast<int64_t>(h - a.n_q_heads) * hd + c0);
+        else
+          raw[u].load(a.v, row * a.ldv + static_cast<int64_t>(h - a.n_q_heads - a.kv.n_heads) * hd + c0);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      if (base + u * per >= to) break;
+      const int h = base + u * per + lane / span;
+      const bool is_q = h < a.n_q_heads, is_v = h >= a.n_q_heads + a.kv.n_heads, live = h < to;
+      float x[8];
+      raw[u].unpack(x);
+      if constexpr (NORM) {
+        float ss = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
+        for (int o = span / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+        const bool normed = is_q ? a.q_gain != nullptr : !is_v && a.k_gain != nullptr;
+        if (normed) {
+          const float r = rsqrtf(ss / static_cast<float>(hd) + a.eps);
+          const uint4 gain = is_q ? gq : gk;
+          const uint32_t w[4] = {gain.x, gain.y, gain.z, gain.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float2 f = unpack_bf16x2(w[i]);
+            x[2 * i] *= r * f.x;
+            x[2 * i + 1] *= r * f.y;
+          }
+        }
+      }
+      if constexpr (LAYOUT == kHalves) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float y = __shfl_sync(0xffffffffu, x[i], partner & 31);
+          if (turns && !is_v) x[i] = x[i] * cs[i] - y * sn[i];
+        }
+      } else if constexpr (LAYOUT == kPairs) {
+        if (turns && !is_v) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float p = x[2 * i], q = x[2 * i + 1];
+            x[2 * i] = p * cs[i] - q * sn[i];
+            x[2 * i + 1] = q * cs[i] + p * sn[i];
+          }
+        }
+      }
+      if (!live) continue;
+      if (is_q) {
+        if (empty) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = 0.f;
+        }
+        char* p = static_cast<char*>(a.q_out) + (row * a.ldqo + static_cast<int64_t>(h) * hd + c0) * (DT == VLA_F32 ? 4 : 2);
+        if constexpr (DT == VLA_F32) {
+          reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+          reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+        } else {
+          *reinterpret_cast<uint4*>(p) = pack8(x, DT == VLA_F16);
+        }
+      } else if (file) {
+        const bool f16_type = a.kv.dtype == VLA_F16;
+        if (DT != VLA_F16 && f16_type) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = clamp_f16(x[i], sat);
+        }
+        const int kv_head = h - a.n_q_heads - (is_v ? a.kv.n_heads : 0);
+        uint16_t* p = static_cast<uint16_t*>(is_v ? a.kv.v : a.kv.k) + cell + kv_head * a.kv.head_stride;
+        *reinterpret_cast<uint4*>(p) = pack8(x, f16_type);
+      }
     }
   }
   report_saturation(a.status, sat);
@@ -231,9 +377,18 @@ __global__ void __launch_bounds__(256) rope_append_kernel(const RopeAppendArgs a
 }  // namespace
 
 int page_plan_launch(const PagePlanArgs& a, cudaStream_t s) {
-  static std::atomic<uint64_t> smem_done{0};
-  VLA_CUDA_TRY(set_smem_limit(page_plan_kernel, 4 * kMaxPlanEnvs * static_cast<int>(sizeof(int)), smem_done));
-  VLA_CUDA_TRY(launch_pdl(page_plan_kernel, dim3(1), dim3(kPlanThreads), 4 * sizeof(int) * a.n_env, s, a));
+  static std::atomic<uint64_t> smem_done{0}, cluster_done{0};
+  static std::atomic<int> cluster_size[64] = {};
+  constexpr int kMost = (4 * kMaxPlanEnvs + 1) * static_cast<int>(sizeof(int));
+  VLA_CUDA_TRY(set_smem_limit(page_plan_kernel, kMost, smem_done));
+  VLA_CUDA_TRY(allow_wide_clusters(page_plan_kernel, cluster_done));
+  // a thread has four rows and takes them twice before another CTA joins
+  int parts = 1, most = 1;
+  while (parts < 16 && a.max_rows > parts * kPlanThreads * 8) parts *= 2;
+  VLA_CUDA_TRY(max_cluster_size(page_plan_kernel, dim3(kPlanThreads), kMost, 16, cluster_size, &most));
+  parts = std::min(parts, most);
+  const int ps = a.page_size, shift = (ps & (ps - 1)) ? -1 : __builtin_ctz(ps);
+  VLA_CUDA_TRY(launch_pdl_cluster(page_plan_kernel, dim3(parts), dim3(kPlanThreads), (4 * a.n_env + 1) * sizeof(int), s, parts, a, parts, shift));
   note_launch();
   VLA_CUDA_TRY(cudaGetLastError());
   return VLA_OK;
@@ -248,13 +403,32 @@ int rope_table_launch(const RopeTableArgs& a, cudaStream_t s) {
   return VLA_OK;
 }
 
-int rope_append_launch(const RopeAppendArgs& a, cudaStream_t s) {
-  const int64_t items = static_cast<int64_t>(a.rows) * (a.n_q_heads + 2 * a.kv.n_heads);
-  if ((items + 7) / 8 > 0x7fffffff) return record_error(VLA_ERR_UNSUPPORTED, "vla_rope_append: too many rows");
-  VLA_CUDA_TRY(launch_pdl(rope_append_kernel, dim3(static_cast<unsigned>((items + 7) / 8)), dim3(256), 0, s, a));
+namespace {
+template <int DT>
+int append_of(const RopeAppendArgs& a, cudaStream_t s) {
+  const int per = 256 / a.kv.head_dim, steps = (a.n_q_heads + 2 * a.kv.n_heads + per - 1) / per;
+  int dev = 0, sms = 0;
+  VLA_CUDA_TRY(cudaGetDevice(&dev));
+  VLA_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+  // a warp per row once they give every SM 32 warps; fewer rows are cut, down to one access a warp
+  const int64_t want = (32LL * sms + a.rows - 1) / a.rows;
+  const int slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(want, steps)));
+  const int64_t units = static_cast<int64_t>(a.rows) * slices, grid = (units + kAppendThreads / 32 - 1) / (kAppendThreads / 32);
+  if (grid > 0x7fffffff) return record_error(VLA_ERR_UNSUPPORTED, "vla_rope_append: too many rows");
+  const int layout = !a.rope ? kNoRope : a.interleaved ? kPairs : kHalves;
+  const bool norm = a.q_gain || a.k_gain;
+  auto kern = layout == kNoRope  ? (norm ? rope_append_kernel<DT, kNoRope, true> : rope_append_kernel<DT, kNoRope, false>)
+              : layout == kPairs ? (norm ? rope_append_kernel<DT, kPairs, true> : rope_append_kernel<DT, kPairs, false>)
+                                 : (norm ? rope_append_kernel<DT, kHalves, true> : rope_append_kernel<DT, kHalves, false>);
+  VLA_CUDA_TRY(launch_pdl(kern, dim3(static_cast<unsigned>(grid)), dim3(kAppendThreads), 0, s, a, slices));
   note_launch();
   VLA_CUDA_TRY(cudaGetLastError());
   return VLA_OK;
+}
+}  // namespace
+
+int rope_append_launch(const RopeAppendArgs& a, cudaStream_t s) {
+  return a.dtype == VLA_F32 ? append_of<VLA_F32>(a, s) : a.dtype == VLA_F16 ? append_of<VLA_F16>(a, s) : append_of<VLA_BF16>(a, s);
 }
 
 }  // namespace vla

@@ -288,40 +288,37 @@ __global__ void __launch_bounds__(32 * kWarps, kCtasPerSm) paged_attn_kernel(con
     const int heads = min(kHeads, group - use.tile * kHeads);
     uint32_t q[HD / 16][PAIR ? 4 : 2];
     {
-      const int64_t q_at = use.row * a.ldq + static_cast<int64_t>(head0 + g) * HD + 2 * t;
       if constexpr (PAIR) {
-        float far = 0.f;
+        // four channels a lane, split and laid out in this warp's part of join_o as each lane's operands (high
+        // and low words of two pairs of channels): 8 idle rows of lanes would repeat the split otherwise
+        uint32_t* mine = reinterpret_cast<uint32_t*>(join_o + warp * kHeads * HD);
+        constexpr int kLanes = HD / 4;
+        const int c = lane % kLanes * 4;
+        uint32_t sat = 0;
+        for (int h = lane / kLanes; h < heads; h += 32 / kLanes) {
+          const float4 x = *reinterpret_cast<const float4*>(static_cast<const float*>(a.q) + use.row * a.ldq + static_cast<int64_t>(head0 + h) * HD + c);
+          uint2 u, v;
+          split_pack2_f16(x.x, x.y, u.x, u.y, sat);
+          split_pack2_f16(x.z, x.w, v.x, v.y, sat);
+          // channels 16k + 8 half + 2t: lane t, words 2 half of the k-th step
+          uint32_t* dst = mine + h * HD + c / 16 * 16 + c % 8 * 2 + (c & 8) / 4;
+          *reinterpret_cast<uint2*>(dst) = u;
+          *reinterpret_cast<uint2*>(dst + 4) = v;
+        }
+        report_saturation(a.status, sat);
+        __syncwarp();
 #pragma unroll
         for (int k = 0; k < HD / 16; ++k) {
-          float2 x = make_float2(0.f, 0.f), y = x;
-          if (g < heads) {
-            x = *reinterpret_cast<const float2*>(static_cast<const float*>(a.q) + q_at + 16 * k);
-            y = *reinterpret_cast<const float2*>(static_cast<const float*>(a.q) + q_at + 16 * k + 8);
-          }
-          far = fmaxf(far, fmaxf(fmaxf(fabsf(x.x), fabsf(x.y)), fmaxf(fabsf(y.x), fabsf(y.y))));
-          split2<false>(x.x, x.y, q[k][0], q[k][1]);
-          split2<false>(y.x, y.y, q[k][2], q[k][3]);
+          uint4 x = make_uint4(0u, 0u, 0u, 0u);
+          if (g < heads) x = *reinterpret_cast<const uint4*>(mine + g * HD + k * 16 + t * 4);
+          q[k][0] = x.x;
+          q[k][1] = x.y;
+          q[k][2] = x.z;
+          q[k][3] = x.w;
         }
-        if (far > 65504.f) {  // as the other activations of the path: the largest fp16 value, and a status bit
-          uint32_t sat = 0;
-#pragma unroll 1
-          for (int k = 0; k < HD / 16; ++k) {
-            const float* x = static_cast<const float*>(a.q) + q_at + 16 * k;
-            uint32_t w[4];
-            split_pack2_f16(x[0], x[1], w[0], w[1], sat);
-            split_pack2_f16(x[8], x[9], w[2], w[3], sat);
-#pragma unroll
-            for (int i = 0; i < HD / 16; ++i)
-              if (i == k) {
-                q[i][0] = w[0];
-                q[i][1] = w[1];
-                q[i][2] = w[2];
-                q[i][3] = w[3];
-              }
-          }
-          report_saturation(a.status, sat);
-        }
+        __syncwarp();
       } else {
+        const int64_t q_at = use.row * a.ldq + static_cast<int64_t>(head0 + g) * HD + 2 * t;
 #pragma unroll
         for (int k = 0; k < HD / 16; ++k) {
           q[k][0] = q[k][1] = 0u;

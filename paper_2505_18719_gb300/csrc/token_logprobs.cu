@@ -1,20 +1,87 @@
 // Log-probs of given tokens with entropy and the best alternatives, and their gradient.
+//
+// Forward, one row of logits z: with c = log2(e) / T and M = max z, s = sum 2^((z - M) c) and w = sum (z - M) c 2^((z - M) c)
+// give log p_j = (z_j - M) / T - ln s, lse = M / T + ln s and the entropy ln 2 (log2 s - w / s), from one pass with a running
+// maximum per thread (a sum relative to m goes over to m' by s' = f s, w' = f (w + (m - m') c s), f = 2^((m - m') c)).
+// Bound by reading the logits, for 16-bit types closely followed by issuing about 7 instructions an element.
+//
+// The best alternatives come from the same pass: each thread's maximum is known, and the k-th largest maximum over
+// disjoint groups of threads is a bound that at least k logits reach.  Only threads whose maximum reaches it
+// read their logits again (from L2: a few dozen), and what they find above the bound is ranked by counting.
+#include <algorithm>
+
 #include "lm.h"
+#include "ptx.cuh"
 
 namespace vla {
 
 namespace {
 
-constexpr int kLpThreads = 512;
+constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 
-// Whole numbers in the order of the floats (negative zero as zero), so that (value, lower id first) is one
-// 64-bit comparison.
+__device__ __forceinline__ float exp2_fast(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {  // NaN if either is
+  float y;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(y) : "f"(a), "f"(b));
+  return y;
+}
+
+// 16 bytes of logits.
+template <int DT>
+struct Vec {
+  static constexpr int kN = DT == VLA_F32 ? 4 : 8;
+  static constexpr int kBytes = 16 / kN;
+  static constexpr uint32_t kLowest = DT == VLA_F32 ? 0xFF800000u : DT == VLA_F16 ? 0xFC00FC00u : 0xFF80FF80u;  // -infinity
+  static __device__ __forceinline__ void unpack(const uint4& v, float (&z)[kN]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (DT == VLA_F32) {
+        z[i] = __uint_as_float(w[i]);
+      } else {
+        const float2 f = DT == VLA_F16 ? unpack_f16x2(w[i]) : make_float2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+        z[2 * i] = f.x;
+        z[2 * i + 1] = f.y;
+      }
+    }
+  }
+  static __device__ __forceinline__ uint32_t word_max(uint32_t a, uint32_t b) {
+    if constexpr (DT == VLA_F32) {
+      return __float_as_uint(max_nan(__uint_as_float(a), __uint_as_float(b)));
+    } else if constexpr (DT == VLA_F16) {
+      const __half2 y = __hmax2_nan(*reinterpret_cast<const __half2*>(&a), *reinterpret_cast<const __half2*>(&b));
+      return *reinterpret_cast<const uint32_t*>(&y);
+    } else {
+      const __nv_bfloat162 y = __hmax2_nan(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+      return *reinterpret_cast<const uint32_t*>(&y);
+    }
+  }
+  static __device__ __forceinline__ float word_float_max(uint32_t a) {
+    if constexpr (DT == VLA_F32) return __uint_as_float(a);
+    const float2 f = DT == VLA_F16 ? unpack_f16x2(a) : make_float2(__uint_as_float(a << 16), __uint_as_float(a & 0xFFFF0000u));
+    return max_nan(f.x, f.y);
+  }
+  static __device__ __forceinline__ float load(const void* p, int64_t i) { return load_as_float(p, i, DT); }
+};
+
+// Elements before the first 16-byte boundary of a row at `p`, at most n.
+template <int DT>
+__device__ __forceinline__ int head_of(const void* p, int n) {
+  return min(n, static_cast<int>((-reinterpret_cast<uintptr_t>(p) & 15u) / Vec<DT>::kBytes));
+}
+
+// Whole numbers in the order of the floats (negative zero as zero); with the id they make one 64-bit key, larger
+// for a larger value and, among equals, for a lower id.
 __device__ __forceinline__ int ordered(float x) {
   const int b = __float_as_int(x + 0.f);
   return b ^ ((b >> 31) & 0x7fffffff);
 }
-__device__ __forceinline__ int64_t top_key(float x, int id) {
-  return (static_cast<int64_t>(ordered(x)) << 32) | static_cast<uint32_t>(0x7fffffff - id);
+__device__ __forceinline__ int64_t make_key(int order, int id) {
+  return (static_cast<int64_t>(order) << 32) | static_cast<uint32_t>(0x7fffffff - id);
 }
 __device__ __forceinline__ float key_value(int64_t key) {
   const int b = static_cast<int>(key >> 32);
@@ -22,118 +89,387 @@ __device__ __forceinline__ float key_value(int64_t key) {
 }
 __device__ __forceinline__ int key_id(int64_t key) { return 0x7fffffff - static_cast<int>(key & 0x7fffffff); }
 
-// One CTA per row.  With m the largest z / T: s = sum e^(z/T - m), w = sum (z/T - m) e^(z/T - m), lse = m + log s,
-// entropy = log s - w / s; then the best ids one by one, each the largest key below the one before.
-__global__ void __launch_bounds__(kLpThreads) token_logprobs_kernel(const LogprobArgs a) {
-  __shared__ float red[3][kLpThreads / 32];
-  __shared__ int64_t red_key[kLpThreads / 32];
+// Running sums of a set of logits: maximum m (raw), s and w relative to it.
+struct Sums {
+  float m = -INFINITY, s = 0.f, w = 0.f;
+  __device__ __forceinline__ void rise(float to, float c) {
+    const float d = m == -INFINITY ? 0.f : fmaxf((m - to) * c, -200.f), f = exp2_fast(d);
+    w = f * (w + d * s);
+    s *= f;
+    m = to;
+  }
+  __device__ __forceinline__ void add(float d) {  // d = (z - m) c; below 2^-200 a weight is 0, and 0 * -infinity no number
+    d = fmaxf(d, -200.f);
+    const float e = exp2_fast(d);
+    s += e;
+    w = fmaf(d, e, w);
+  }
+};
+
+// One cluster of `parts` CTAs per row, each a slice of the ids.
+template <int DT, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == 32 ? 32 : 4) token_logprobs_kernel(const LogprobArgs a, const int parts) {
+  using V = Vec<DT>;
+  constexpr int kWarps = THREADS / 32, kUnroll = 4;
+  constexpr int kGroups = THREADS == 32 ? 32 : kWarps * 16;  // threads, or lanes of a warp that are equal modulo 16
+  constexpr int kList = THREADS == 32 ? 128 : 512;
+  __shared__ float red[3][kWarps];
+  __shared__ int group_max[kGroups];
+  __shared__ int64_t above[kList];
+  __shared__ int level_ids[kList];
+  __shared__ int n_above, n_level, bound;
+  __shared__ int64_t best[kMaxTopK];               // this slice's best keys, in order
+  __shared__ float3 slice;                         // its sums
+  __shared__ float3 all_slices[8];
+  __shared__ int64_t all_best[8 * kMaxTopK];
+  __shared__ int64_t round_key[kWarps];
   pdl_launch_dependents();
   pdl_wait();
-  const int row = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int64_t at = row * a.ld;
-  const float inv_t = 1.f / a.temperature;
-  float m = -INFINITY;
-  bool odd = false;
-  for (int j = tid; j < a.vocab; j += kLpThreads) {
-    const float z = load_as_float(a.logits, at + j, a.dtype);
-    odd |= !(z < INFINITY);
-    m = fmaxf(m, z * inv_t);
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int row = blockIdx.x / parts, part = blockIdx.x % parts;
+  const int first = static_cast<int>(static_cast<int64_t>(a.vocab) * part / parts);
+  const int n = static_cast<int>(static_cast<int64_t>(a.vocab) * (part + 1) / parts) - first;
+  const char* base = static_cast<const char*>(a.logits) + (row * a.ld + first) * V::kBytes;
+  const int head = head_of<DT>(base, n), vecs = (n - head) / V::kN, tail = n - head - vecs * V::kN;
+  const uint4* body = reinterpret_cast<const uint4*>(base + head * V::kBytes);
+  const float inv_t = 1.f / a.temperature, c = kLog2e * inv_t;
+
+  // the token's logit is read beside the pass
+  int token = -1;
+  float chosen = 0.f;
+  if (part == 0 && tid == 0 && a.tokens) {
+    token = a.tokens[row];
+    if (static_cast<unsigned>(token) < static_cast<unsigned>(a.vocab)) {
+      chosen = V::load(a.logits, row * a.ld + token);
+    } else {
+      if (token != -1) raise_status(a.status, VLA_STATUS_BAD_TOKEN);
+      token = -1;
+    }
   }
-  m = warp_max(m);
-  if (lane == 0) red[0][warp] = m;
-  odd = __syncthreads_or(odd);
-  for (int i = 0; i < kLpThreads / 32; ++i) m = fmaxf(m, red[0][i]);
+
+  Sums x;
+  auto chunk = [&](const uint4 (&v)[kUnroll]) {
+    uint32_t top = v[0].x;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      top = V::word_max(top, V::word_max(V::word_max(v[u].x, v[u].y), V::word_max(v[u].z, v[u].w)));
+    }
+    const float m = max_nan(x.m, V::word_float_max(top));
+    x.rise(m, c);
+    // the difference first: fma(z, c, -m c) is off by the rounding of m c, which for logits far from zero is
+    // more than a weight's whole exponent.  Nothing but -infinity so far: any reference gives zeros.
+    const float ref = m == -INFINITY ? 0.f : m;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      float z[V::kN];
+      V::unpack(v[u], z);
+#pragma unroll
+      for (int i = 0; i < V::kN; ++i) x.add((z[i] - ref) * c);
+    }
+  };
+  for (int i = tid; i < vecs; i += THREADS * kUnroll) {
+    uint4 v[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      v[u] = make_uint4(V::kLowest, V::kLowest, V::kLowest, V::kLowest);
+      if (i + u * THREADS < vecs) v[u] = body[i + u * THREADS];
+    }
+    chunk(v);
+  }
+  // up to 7 elements before and after the vectors: one a thread
+  const int edge = tid < head ? tid : tid < head + tail ? n - tail + tid - head : -1;
+  if (edge >= 0) {
+    const float z = V::load(base, edge), m = max_nan(x.m, z);
+    x.rise(m, c);
+    if (m != -INFINITY) x.add((z - m) * c);
+  }
+  const int mine = ordered(x.m);
+
+  // the CTA's maximum, then its sums
+  float top = x.m;
+  if (THREADS == 32) group_max[lane] = mine;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if (THREADS > 32 && o == 16 && lane < 16) group_max[warp * 16 + lane] = ordered(top);
+  }
+  if (lane == 0) red[0][warp] = top;
+  if (tid == 0) n_above = n_level = 0;
   __syncthreads();
-  float s = 0.f, w = 0.f;
-  for (int j = tid; j < a.vocab; j += kLpThreads) {
-    const float d = load_as_float(a.logits, at + j, a.dtype) * inv_t - m;
-    const float e = m == -INFINITY ? 0.f : expf(d);
-    s += e;
-    if (e > 0.f) w += d * e;
-  }
-  s = warp_sum(s);
-  w = warp_sum(w);
+  top = red[0][0];
+#pragma unroll
+  for (int i = 1; i < kWarps; ++i) top = max_nan(top, red[0][i]);
+  if (x.m != -INFINITY) x.rise(top, c);
+  x.s = warp_sum(x.s);
+  x.w = warp_sum(x.w);
   if (lane == 0) {
-    red[1][warp] = s;
-    red[2][warp] = w;
+    red[1][warp] = x.s;
+    red[2][warp] = x.w;
   }
-  __syncthreads();
-  s = w = 0.f;
-  for (int i = 0; i < kLpThreads / 32; ++i) {
-    s += red[1][i];
-    w += red[2][i];
-  }
-  float log_s = logf(s), lse = m + log_s, entropy = s > 0.f ? log_s - w / s : 0.f;
-  if (odd) lse = entropy = NAN;
-  if (tid == 0) {
-    if (odd) raise_status(a.status, VLA_STATUS_NONFINITE);
-    if (a.lse) a.lse[row] = lse;
-    if (a.entropy) a.entropy[row] = entropy;
-    if (a.tokens) {
-      const int t = a.tokens[row];
-      const bool ok = static_cast<unsigned>(t) < static_cast<unsigned>(a.vocab);
-      if (!ok && t != -1) raise_status(a.status, VLA_STATUS_BAD_TOKEN);
-      if (a.logprob) {
-        const float z = ok ? load_as_float(a.logits, at + t, a.dtype) * inv_t : 0.f;
-        a.logprob[row] = !ok ? 0.f : odd ? NAN : z == -INFINITY ? z : z - lse;
+  const bool odd = !(top < INFINITY);  // a NaN or +infinity in the slice
+
+  // ---- the slice's best keys
+  if (a.top_k > 0) {
+    const int k = min(a.top_k, n);
+    // the k-th largest of the groups' maxima, or nothing below all
+    if (tid == 0) bound = INT32_MIN;
+    __syncthreads();
+    if (kGroups >= k) {
+      for (int i = tid; i < kGroups; i += THREADS) {
+        const int v = group_max[i];
+        int rank = 0;
+#pragma unroll 8
+        for (int j = 0; j < kGroups; ++j) rank += group_max[j] > v || (group_max[j] == v && j < i);
+        if (rank == k - 1) bound = v;
       }
     }
-  }
-  int64_t last = INT64_MAX;
-  for (int i = 0; i < a.top_k; ++i) {
-    int64_t best = INT64_MIN;
-    for (int j = tid; j < a.vocab; j += kLpThreads) {
-      const int64_t key = top_key(load_as_float(a.logits, at + j, a.dtype), j);
-      if (key < last && key > best) best = key;
-    }
+    __syncthreads();
+    const int at_least = bound;
+    bool fits = !odd;
+    if (!odd) {
+      if (mine >= at_least) {
+        auto take = [&](float z, int id) {
+          const int o = ordered(z);
+          if (o > at_least) {
+            const int at = atomicAdd(&n_above, 1);
+            if (at < kList) above[at] = make_key(o, id);
+          } else if (o == at_least) {
+            const int at = atomicAdd(&n_level, 1);
+            if (at < kList) level_ids[at] = id;
+          }
+        };
+        for (int i = tid; i < vecs; i += THREADS) {
+          float z[V::kN];
+          V::unpack(body[i], z);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) best = max(best, __shfl_xor_sync(0xffffffffu, best, o));
-    __syncthreads();
-    if (lane == 0) red_key[warp] = best;
-    __syncthreads();
-    for (int k = 0; k < kLpThreads / 32; ++k) best = max(best, red_key[k]);
-    last = best;
-    if (tid == 0) {
-      const float z = key_value(best) * inv_t;
-      a.top_ids[static_cast<int64_t>(row) * a.top_k + i] = key_id(best);
-      a.top_logprobs[static_cast<int64_t>(row) * a.top_k + i] = odd ? NAN : z == -INFINITY ? z : z - lse;
+          for (int j = 0; j < V::kN; ++j) take(z[j], first + head + i * V::kN + j);
+        }
+        if (edge >= 0) take(V::load(base, edge), first + edge);
+      }
+      __syncthreads();
+      const bool ties = n_above < k;  // equals of the bound are among the best
+      fits = n_above <= kList && (!ties || n_level <= kList);
+      if (fits) {
+        const int more = ties ? n_level : 0, total = n_above + more;
+        for (int i = tid; i < total; i += THREADS) {
+          const int64_t key = i < n_above ? above[i] : make_key(at_least, level_ids[i - n_above]);
+          int rank = 0;
+          for (int j = 0; j < n_above; ++j) rank += above[j] > key;
+          if (i >= n_above)  // equals follow in the order of their ids
+            for (int j = 0; j < more; ++j) rank += level_ids[j] < level_ids[i - n_above];
+          if (rank < k) best[rank] = key;
+        }
+      }
     }
+    if (!fits) {  // more equal logits than the list holds: the largest key below the one before, k times over
+      int64_t last = INT64_MAX;
+      for (int r = 0; r < k; ++r) {
+        int64_t key = INT64_MIN;
+        for (int j = tid; j < n; j += THREADS) {
+          const int64_t q = make_key(ordered(V::load(base, j)), first + j);
+          if (q < last && q > key) key = q;
+        }
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) key = max(key, __shfl_xor_sync(0xffffffffu, key, o));
+        __syncthreads();
+        if (lane == 0) round_key[warp] = key;
+        __syncthreads();
+        for (int i = 0; i < kWarps; ++i) key = max(key, round_key[i]);
+        last = key;
+        if (tid == 0) best[r] = key;
+      }
+    }
+    for (int i = k + tid; i < a.top_k; i += THREADS) best[i] = INT64_MIN;
+  }
+  __syncthreads();
+
+  // ---- the slices' results meet in the first CTA
+  if (tid == 0) {
+    float s = 0.f, w = 0.f;
+    for (int i = 0; i < kWarps; ++i) {
+      s += red[1][i];
+      w += red[2][i];
+    }
+    slice = make_float3(top, s, w);
+  }
+  Sums total;
+  if (parts > 1) {
+    cluster_sync();
+    if (part == 0) {
+      for (int i = tid; i < parts * a.top_k; i += THREADS) {
+        const uint32_t at = mapa_shared(smem_u32(&best[i % a.top_k]), i / a.top_k);
+        asm volatile("ld.shared::cluster.s64 %0, [%1];" : "=l"(all_best[i]) : "r"(at) : "memory");
+      }
+      if (tid < parts) {
+        const uint32_t at = mapa_shared(smem_u32(&slice), tid);
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(all_slices[tid].x) : "r"(at) : "memory");
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(all_slices[tid].y) : "r"(at + 4) : "memory");
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(all_slices[tid].z) : "r"(at + 8) : "memory");
+      }
+    }
+    cluster_sync();  // the other CTAs' results stay until the first has them
+    if (part != 0) return;
+    float m = -INFINITY;
+    for (int i = 0; i < parts; ++i) m = max_nan(m, all_slices[i].x);
+    total.m = m;
+    for (int i = 0; i < parts; ++i) {
+      Sums y;
+      y.m = all_slices[i].x;
+      y.s = all_slices[i].y;
+      y.w = all_slices[i].z;
+      if (y.m != -INFINITY) y.rise(m, c);
+      total.s += y.s;
+      total.w += y.w;
+    }
+    // disjoint sorted lists: a key's place is the number of larger ones
+    for (int i = tid; i < parts * a.top_k; i += THREADS) {
+      const int64_t key = all_best[i];
+      int rank = 0;
+      for (int j = 0; j < parts * a.top_k; ++j) rank += all_best[j] > key;
+      if (key != INT64_MIN && rank < a.top_k) best[rank] = key;
+    }
+    __syncthreads();
+  } else {
+    __syncthreads();
+    total.m = slice.x;
+    total.s = slice.y;
+    total.w = slice.z;
+  }
+
+  const bool bad = !(total.m < INFINITY), none = total.m == -INFINITY;
+  const float ln_s = logf(total.s);
+  if (tid == 0) {
+    if (bad) raise_status(a.status, VLA_STATUS_NONFINITE);
+    const float lse = bad ? NAN : none ? -INFINITY : fmaf(total.m, inv_t, ln_s);
+    if (a.lse) a.lse[row] = lse;
+    if (a.entropy) a.entropy[row] = bad ? NAN : none ? 0.f : ln_s - total.w / total.s * kLn2;
+    if (a.logprob) a.logprob[row] = token < 0 ? 0.f : bad ? NAN : none ? -INFINITY : (chosen - total.m) * inv_t - ln_s;
+  }
+  for (int i = tid; i < a.top_k; i += THREADS) {
+    const int64_t key = best[i], at = static_cast<int64_t>(row) * a.top_k + i;
+    a.top_ids[at] = key_id(key);
+    a.top_logprobs[at] = bad ? NAN : none ? -INFINITY : (key_value(key) - total.m) * inv_t - ln_s;
   }
 }
 
-// One CTA per row, one element per thread and round.
-__global__ void __launch_bounds__(kLpThreads) token_logprobs_grad_kernel(const LogprobGradArgs a) {
+// The gradient, element by element: with d = z / T - lse, -e^d (g + h (d + entropy)) / T, and g / T more at the token.
+// One CTA per row and slice.  Where logits and gradient lie alike towards 16 bytes, both move in 16-byte
+// pieces; else one element a lane and access, which is coalesced all the same.
+template <int DT>
+__global__ void __launch_bounds__(256) token_logprobs_grad_kernel(const LogprobGradArgs a, const int parts) {
+  using V = Vec<DT>;
+  constexpr int kUnroll = 4;
   pdl_launch_dependents();
   pdl_wait();
-  const int row = blockIdx.x, t = a.tokens[row];
-  const bool ok = static_cast<unsigned>(t) < static_cast<unsigned>(a.vocab);
-  if (!ok && t != -1 && threadIdx.x == 0) raise_status(a.status, VLA_STATUS_BAD_TOKEN);
-  const float inv_t = 1.f / a.temperature, lse = a.lse[row];
-  const float g = ok ? a.g_logprob[row] * inv_t : 0.f, h = ok && a.g_entropy ? a.g_entropy[row] * inv_t : 0.f;
-  const float entropy = a.entropy ? a.entropy[row] : 0.f;
-  for (int j = threadIdx.x; j < a.vocab; j += kLpThreads) {
-    float d = 0.f;
-    if (ok) {
-      const float z = load_as_float(a.logits, row * a.ld + j, a.dtype) * inv_t;
-      const float lp = z - lse, p = z == -INFINITY ? 0.f : expf(lp);
-      if (z != -INFINITY) d = -p * (g + h * (lp + entropy));
-      if (j == t) d += g;
+  const int tid = threadIdx.x, row = blockIdx.x / parts, part = blockIdx.x % parts;
+  // slices begin at multiples of 64 elements, so that none cuts a 16-byte piece of an aligned row
+  const int units = (a.vocab + 63) / 64;
+  const int first = static_cast<int>(static_cast<int64_t>(units) * part / parts) * 64;
+  const int n = min(a.vocab, static_cast<int>(static_cast<int64_t>(units) * (part + 1) / parts) * 64) - first;
+  int token = a.tokens[row];
+  const bool kept = static_cast<unsigned>(token) < static_cast<unsigned>(a.vocab);
+  if (!kept && token != -1 && part == 0 && tid == 0) raise_status(a.status, VLA_STATUS_BAD_TOKEN);
+  const float lse = a.lse[row], inv_t = 1.f / a.temperature;
+  float g = kept ? a.g_logprob[row] * inv_t : 0.f;
+  const float h = kept && a.g_entropy ? a.g_entropy[row] * inv_t : 0.f;
+  if (kept && lse != lse) g = lse;  // a row whose numbers are none
+  const float gh = h != 0.f ? fmaf(h, a.entropy[row], g) : g;
+  token = kept ? token - first : -1;
+  const char* src = static_cast<const char*>(a.logits) + (row * a.ld + first) * V::kBytes;
+  char* dst = static_cast<char*>(a.d_logits) + (row * a.ldd + first) * V::kBytes;
+  auto slope = [&](float z) {
+    // below e^-1000 a weight is 0, and 0 * -infinity no number
+    const float d = fmaxf(fmaf(z, inv_t, -lse), -1000.f);
+    return -exp2_fast(d * kLog2e) * fmaf(h, d, gh);
+  };
+  const bool alike = ((reinterpret_cast<uintptr_t>(src) ^ reinterpret_cast<uintptr_t>(dst)) & 15u) == 0;
+  const int head = alike ? head_of<DT>(src, n) : n, vecs = (n - head) / V::kN;
+  const uint4* from = reinterpret_cast<const uint4*>(src + head * V::kBytes);
+  uint4* to = reinterpret_cast<uint4*>(dst + head * V::kBytes);
+  for (int i = tid; i < vecs; i += 256 * kUnroll) {
+    uint4 v[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u)
+      if (kept && i + u * 256 < vecs) v[u] = from[i + u * 256];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      if (i + u * 256 >= vecs) break;
+      uint4 y = make_uint4(0u, 0u, 0u, 0u);
+      if (kept) {
+        float z[V::kN];
+        V::unpack(v[u], z);
+#pragma unroll
+        for (int j = 0; j < V::kN; ++j) z[j] = slope(z[j]);
+        const int at = token - (head + (i + u * 256) * V::kN);
+        if (static_cast<unsigned>(at) < static_cast<unsigned>(V::kN)) {
+#pragma unroll
+          for (int j = 0; j < V::kN; ++j)
+            if (j == at) z[j] += g;
+        }
+        uint32_t* w = reinterpret_cast<uint32_t*>(&y);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          w[j] = DT == VLA_F32 ? __float_as_uint(z[j]) : DT == VLA_F16 ? pack_f16x2(z[2 * j % V::kN], z[(2 * j + 1) % V::kN]) : pack_bf16x2(z[2 * j % V::kN], z[(2 * j + 1) % V::kN]);
+      }
+      to[i + u * 256] = y;
     }
-    store_from_float(a.d_logits, row * a.ldd + j, d, a.dtype);
   }
+  const int done = head + vecs * V::kN;
+  auto single = [&](int j, float z) {
+    float d = kept ? slope(z) : 0.f;
+    if (j == token) d += g;
+    store_from_float(dst, j, d, DT);
+  };
+  for (int j0 = tid; j0 < head; j0 += 256 * 8) {
+    float z[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) z[u] = kept && j0 + u * 256 < head ? V::load(src, j0 + u * 256) : 0.f;
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (j0 + u * 256 < head) single(j0 + u * 256, z[u]);
+  }
+  if (done + tid < n) single(done + tid, kept ? V::load(src, done + tid) : 0.f);
 }
 
-}  // namespace
-
-int token_logprobs_launch(const LogprobArgs& a, cudaStream_t s) {
-  VLA_CUDA_TRY(launch_pdl(token_logprobs_kernel, dim3(a.rows), dim3(kLpThreads), 0, s, a));
+template <int DT>
+int logprobs_of(const LogprobArgs& a, cudaStream_t s, int sms) {
+  // up to 1024 ids a warp has a row to itself, and no barrier costs anything
+  const bool small = a.vocab <= 1024;
+  int parts = 1;
+  if (!small)
+    while (parts < 8 && static_cast<int64_t>(a.rows) * parts * 2 <= 2 * sms && a.vocab / (parts * 2) >= 2048) parts *= 2;
+  if (static_cast<int64_t>(a.rows) * parts > 0x7fffffff) return record_error(VLA_ERR_UNSUPPORTED, "vla_token_logprobs: too many rows");
+  if (small) VLA_CUDA_TRY(launch_pdl(token_logprobs_kernel<DT, 32>, dim3(a.rows), dim3(32), 0, s, a, 1));
+  else VLA_CUDA_TRY(launch_pdl_cluster(token_logprobs_kernel<DT, 256>, dim3(a.rows * parts), dim3(256), 0, s, parts, a, parts));
   note_launch();
   VLA_CUDA_TRY(cudaGetLastError());
   return VLA_OK;
 }
 
+int num_sms(int* sms) {
+  int dev = 0;
+  VLA_CUDA_TRY(cudaGetDevice(&dev));
+  VLA_CUDA_TRY(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
+  return VLA_OK;
+}
+
+}  // namespace
+
+int token_logprobs_launch(const LogprobArgs& a, cudaStream_t s) {
+  int sms = 0;
+  if (const int rc = num_sms(&sms)) return rc;
+  return a.dtype == VLA_F32 ? logprobs_of<VLA_F32>(a, s, sms) : a.dtype == VLA_F16 ? logprobs_of<VLA_F16>(a, s, sms) : logprobs_of<VLA_BF16>(a, s, sms);
+}
+
 int token_logprobs_grad_launch(const LogprobGradArgs& a, cudaStream_t s) {
-  VLA_CUDA_TRY(launch_pdl(token_logprobs_grad_kernel, dim3(a.rows), dim3(kLpThreads), 0, s, a));
+  int sms = 0;
+  if (const int rc = num_sms(&sms)) return rc;
+  // slices of at least 2048 elements while the rows alone do not fill the SMs four times
+  int parts = 1;
+  while (parts < 64 && static_cast<int64_t>(a.rows) * parts < 4 * sms && a.vocab / (parts * 2) >= 2048) parts *= 2;
+  if (static_cast<int64_t>(a.rows) * parts > 0x7fffffff) return record_error(VLA_ERR_UNSUPPORTED, "vla_token_logprobs_grad: too many rows");
+  auto kern = a.dtype == VLA_F32 ? token_logprobs_grad_kernel<VLA_F32> : a.dtype == VLA_F16 ? token_logprobs_grad_kernel<VLA_F16> : token_logprobs_grad_kernel<VLA_BF16>;
+  VLA_CUDA_TRY(launch_pdl(kern, dim3(a.rows * parts), dim3(256), 0, s, a, parts));
   note_launch();
   VLA_CUDA_TRY(cudaGetLastError());
   return VLA_OK;
