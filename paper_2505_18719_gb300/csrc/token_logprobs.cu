@@ -6,8 +6,8 @@
 // Bound by reading the logits, for 16-bit types closely followed by issuing about 7 instructions an element.
 //
 // The best alternatives come from the same pass: each thread's maximum is known, and the k-th largest maximum over
-// disjoint groups of threads is a bound that at least k logits reach.  Only threads whose maximum reaches it
-// read their logits again (from L2: a few dozen), and what they find above the bound is ranked by counting.
+// disjoint groups of threads is a bound that at least k logits reach.  Only threads whose maximum reaches it read
+// their logits again (from L2), and what lies above the bound is ranked by counting.
 #include <algorithm>
 
 #include "lm.h"
@@ -16,6 +16,8 @@
 namespace vla {
 
 namespace {
+
+constexpr int kWarpVocab = 1024, kSmallVocab = 6144;  // ids up to which a row has 32, 64 threads
 
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 
@@ -83,10 +85,8 @@ __device__ __forceinline__ int ordered(float x) {
 __device__ __forceinline__ int64_t make_key(int order, int id) {
   return (static_cast<int64_t>(order) << 32) | static_cast<uint32_t>(0x7fffffff - id);
 }
-__device__ __forceinline__ float key_value(int64_t key) {
-  const int b = static_cast<int>(key >> 32);
-  return __int_as_float(b ^ ((b >> 31) & 0x7fffffff));
-}
+__device__ __forceinline__ float float_of(int order) { return __int_as_float(order ^ ((order >> 31) & 0x7fffffff)); }
+__device__ __forceinline__ float key_value(int64_t key) { return float_of(static_cast<int>(key >> 32)); }
 __device__ __forceinline__ int key_id(int64_t key) { return 0x7fffffff - static_cast<int>(key & 0x7fffffff); }
 
 // Running sums of a set of logits: maximum m (raw), s and w relative to it.
@@ -108,20 +108,20 @@ struct Sums {
 
 // One cluster of `parts` CTAs per row, each a slice of the ids.
 template <int DT, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == 32 ? 32 : 4) token_logprobs_kernel(const LogprobArgs a, const int parts) {
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel(const LogprobArgs a, const int parts) {
   using V = Vec<DT>;
   constexpr int kWarps = THREADS / 32, kUnroll = 4;
-  constexpr int kGroups = THREADS == 32 ? 32 : kWarps * 16;  // threads, or lanes of a warp that are equal modulo 16
+  constexpr int kGroups = THREADS == 32 ? 32 : 64, kGroupLanes = kGroups / kWarps;  // lanes of a warp that are equal modulo kGroupLanes
   constexpr int kList = THREADS == 32 ? 128 : 512;
+  constexpr int kMostParts = 8;
+  __shared__ __align__(16) int group_max[kGroups];
   __shared__ float red[3][kWarps];
-  __shared__ int group_max[kGroups];
   __shared__ int64_t above[kList];
   __shared__ int level_ids[kList];
   __shared__ int n_above, n_level, bound;
   __shared__ int64_t best[kMaxTopK];               // this slice's best keys, in order
-  __shared__ float3 slice;                         // its sums
-  __shared__ float3 all_slices[8];
-  __shared__ int64_t all_best[8 * kMaxTopK];
+  __shared__ int64_t all_best[THREADS == 256 ? kMostParts * kMaxTopK : 1];
+  __shared__ float3 all_slices[kMostParts], slice;  // (m, s, w) of the slices
   __shared__ int64_t round_key[kWarps];
   pdl_launch_dependents();
   pdl_wait();
@@ -133,6 +133,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 32 ? 32 : 4) token_logprob
   const int head = head_of<DT>(base, n), vecs = (n - head) / V::kN, tail = n - head - vecs * V::kN;
   const uint4* body = reinterpret_cast<const uint4*>(base + head * V::kBytes);
   const float inv_t = 1.f / a.temperature, c = kLog2e * inv_t;
+  const int k = min(a.top_k, n);  // of this slice
 
   // the token's logit is read beside the pass
   int token = -1;
@@ -146,14 +147,17 @@ __global__ void __launch_bounds__(THREADS, THREADS == 32 ? 32 : 4) token_logprob
       token = -1;
     }
   }
+  if (tid == 0) {
+    n_above = n_level = 0;
+    bound = INT32_MIN;
+  }
 
   Sums x;
   auto chunk = [&](const uint4 (&v)[kUnroll]) {
     uint32_t top = v[0].x;
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
+    for (int u = 0; u < kUnroll; ++u)
       top = V::word_max(top, V::word_max(V::word_max(v[u].x, v[u].y), V::word_max(v[u].z, v[u].w)));
-    }
     const float m = max_nan(x.m, V::word_float_max(top));
     x.rise(m, c);
     // the difference first: fma(z, c, -m c) is off by the rounding of m c, which for logits far from zero is
@@ -185,16 +189,15 @@ __global__ void __launch_bounds__(THREADS, THREADS == 32 ? 32 : 4) token_logprob
   }
   const int mine = ordered(x.m);
 
-  // the CTA's maximum, then its sums
+  // the CTA's maximum and its groups'
   float top = x.m;
-  if (THREADS == 32) group_max[lane] = mine;
+  if (kGroupLanes == 32) group_max[warp * 32 + lane] = mine;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
     top = max_nan(top, __shfl_xor_sync(0xffffffffu, top, o));
-    if (THREADS > 32 && o == 16 && lane < 16) group_max[warp * 16 + lane] = ordered(top);
+    if (o == kGroupLanes && lane < kGroupLanes) group_max[warp * kGroupLanes + lane] = ordered(top);
   }
   if (lane == 0) red[0][warp] = top;
-  if (tid == 0) n_above = n_level = 0;
   __syncthreads();
   top = red[0][0];
 #pragma unroll
@@ -207,51 +210,80 @@ __global__ void __launch_bounds__(THREADS, THREADS == 32 ? 32 : 4) token_logprob
     red[2][warp] = x.w;
   }
   const bool odd = !(top < INFINITY);  // a NaN or +infinity in the slice
+  if (k > 0 && tid < kGroups) {
+    // the largest maximum that k groups reach
+    const int v = group_max[tid];
+    int reach = 0;
+#pragma unroll
+    for (int j = 0; j < kGroups; j += 4) {
+      const int4 w = *reinterpret_cast<const int4*>(group_max + j);
+      reach += (w.x >= v) + (w.y >= v) + (w.z >= v) + (w.w >= v);
+    }
+    if (reach >= k) atomicMax(&bound, v);
+  }
+  __syncthreads();
+  Sums total;
+  total.m = top;
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) {
+    total.s += red[1][i];
+    total.w += red[2][i];
+  }
 
   // ---- the slice's best keys
-  if (a.top_k > 0) {
-    const int k = min(a.top_k, n);
-    // the k-th largest of the groups' maxima, or nothing below all
-    if (tid == 0) bound = INT32_MIN;
-    __syncthreads();
-    if (kGroups >= k) {
-      for (int i = tid; i < kGroups; i += THREADS) {
-        const int v = group_max[i];
-        int rank = 0;
-#pragma unroll 8
-        for (int j = 0; j < kGroups; ++j) rank += group_max[j] > v || (group_max[j] == v && j < i);
-        if (rank == k - 1) bound = v;
-      }
-    }
-    __syncthreads();
+  if (k > 0) {
     const int at_least = bound;
+    const float limit = float_of(at_least);
+    const bool lowest = limit == -INFINITY;  // then all that is not above it is equal to it
     bool fits = !odd;
     if (!odd) {
-      if (mine >= at_least) {
-        auto take = [&](float z, int id) {
-          const int o = ordered(z);
-          if (o > at_least) {
-            const int at = atomicAdd(&n_above, 1);
-            if (at < kList) above[at] = make_key(o, id);
-          } else if (o == at_least) {
-            const int at = atomicAdd(&n_level, 1);
-            if (at < kList) level_ids[at] = id;
-          }
-        };
-        for (int i = tid; i < vecs; i += THREADS) {
-          float z[V::kN];
-          V::unpack(body[i], z);
+      auto take = [&](int j) {
+        const int o = ordered(V::load(base, j));
+        int* const count = o > at_least ? &n_above : &n_level;
+        const int at = atomicAdd(count, 1);
+        if (at >= kList) return;
+        if (o > at_least)
+          above[at] = make_key(o, first + j);
+        else
+          level_ids[at] = first + j;
+      };
+      if (lowest ? mine > at_least : mine >= at_least) {
+        for (int i = tid; i < vecs; i += THREADS * kUnroll) {
+          uint4 v[kUnroll];
 #pragma unroll
-          for (int j = 0; j < V::kN; ++j) take(z[j], first + head + i * V::kN + j);
+          for (int u = 0; u < kUnroll; ++u) v[u] = body[min(i + u * THREADS, vecs - 1)];
+#pragma unroll
+          for (int u = 0; u < kUnroll; ++u) {
+            if (i + u * THREADS >= vecs) break;
+            const float most = V::word_float_max(V::word_max(V::word_max(v[u].x, v[u].y), V::word_max(v[u].z, v[u].w)));
+            if (lowest ? !(most > limit) : !(most >= limit)) continue;
+            float z[V::kN];
+            V::unpack(v[u], z);
+            uint32_t found = 0;
+#pragma unroll
+            for (int j = 0; j < V::kN; ++j) found |= (lowest ? z[j] > limit : z[j] >= limit) ? 1u << j : 0u;
+            for (; found; found &= found - 1) take(head + (i + u * THREADS) * V::kN + __ffs(found) - 1);
+          }
         }
-        if (edge >= 0) take(V::load(base, edge), first + edge);
+        if (edge >= 0) {
+          const float z = V::load(base, edge);
+          if (lowest ? z > limit : z >= limit) take(edge);
+        }
       }
       __syncthreads();
       const bool ties = n_above < k;  // equals of the bound are among the best
+      if (lowest && ties) {  // the first k + n_above ids hold k of them
+        for (int j = tid; j < min(n, k + n_above); j += THREADS)
+          if (V::load(base, j) == limit) {
+            const int at = atomicAdd(&n_level, 1);
+            if (at < kList) level_ids[at] = first + j;
+          }
+        __syncthreads();
+      }
       fits = n_above <= kList && (!ties || n_level <= kList);
       if (fits) {
-        const int more = ties ? n_level : 0, total = n_above + more;
-        for (int i = tid; i < total; i += THREADS) {
+        const int more = ties ? n_level : 0, count = n_above + more;
+        for (int i = tid; i < count; i += THREADS) {
           const int64_t key = i < n_above ? above[i] : make_key(at_least, level_ids[i - n_above]);
           int rank = 0;
           for (int j = 0; j < n_above; ++j) rank += above[j] > key;
@@ -280,20 +312,12 @@ __global__ void __launch_bounds__(THREADS, THREADS == 32 ? 32 : 4) token_logprob
       }
     }
     for (int i = k + tid; i < a.top_k; i += THREADS) best[i] = INT64_MIN;
+    __syncthreads();
   }
-  __syncthreads();
 
   // ---- the slices' results meet in the first CTA
-  if (tid == 0) {
-    float s = 0.f, w = 0.f;
-    for (int i = 0; i < kWarps; ++i) {
-      s += red[1][i];
-      w += red[2][i];
-    }
-    slice = make_float3(top, s, w);
-  }
-  Sums total;
-  if (parts > 1) {
+  if (THREADS == 256 && parts > 1) {
+    if (tid == 0) slice = make_float3(total.m, total.s, total.w);
     cluster_sync();
     if (part == 0) {
       for (int i = tid; i < parts * a.top_k; i += THREADS) {
@@ -312,6 +336,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 32 ? 32 : 4) token_logprob
     float m = -INFINITY;
     for (int i = 0; i < parts; ++i) m = max_nan(m, all_slices[i].x);
     total.m = m;
+    total.s = total.w = 0.f;
     for (int i = 0; i < parts; ++i) {
       Sums y;
       y.m = all_slices[i].x;
@@ -329,13 +354,9 @@ __global__ void __launch_bounds__(THREADS, THREADS == 32 ? 32 : 4) token_logprob
       if (key != INT64_MIN && rank < a.top_k) best[rank] = key;
     }
     __syncthreads();
-  } else {
-    __syncthreads();
-    total.m = slice.x;
-    total.s = slice.y;
-    total.w = slice.z;
   }
 
+  if (tid >= max(1, a.top_k)) return;
   const bool bad = !(total.m < INFINITY), none = total.m == -INFINITY;
   const float ln_s = logf(total.s);
   if (tid == 0) {
@@ -345,8 +366,8 @@ __global__ void __launch_bounds__(THREADS, THREADS == 32 ? 32 : 4) token_logprob
     if (a.entropy) a.entropy[row] = bad ? NAN : none ? 0.f : ln_s - total.w / total.s * kLn2;
     if (a.logprob) a.logprob[row] = token < 0 ? 0.f : bad ? NAN : none ? -INFINITY : (chosen - total.m) * inv_t - ln_s;
   }
-  for (int i = tid; i < a.top_k; i += THREADS) {
-    const int64_t key = best[i], at = static_cast<int64_t>(row) * a.top_k + i;
+  if (tid < a.top_k) {
+    const int64_t key = best[tid], at = static_cast<int64_t>(row) * a.top_k + tid;
     a.top_ids[at] = key_id(key);
     a.top_logprobs[at] = bad ? NAN : none ? -INFINITY : (key_value(key) - total.m) * inv_t - ln_s;
   }
@@ -433,14 +454,14 @@ __global__ void __launch_bounds__(256) token_logprobs_grad_kernel(const LogprobG
 
 template <int DT>
 int logprobs_of(const LogprobArgs& a, cudaStream_t s, int sms) {
-  // up to 1024 ids a warp has a row to itself, and no barrier costs anything
-  const bool small = a.vocab <= 1024;
+  // a row has few threads where it is short: their number is what its barriers cost
+  const int threads = a.vocab <= kWarpVocab ? 32 : a.vocab <= kSmallVocab ? 64 : 256;
   int parts = 1;
-  if (!small)
-    while (parts < 8 && static_cast<int64_t>(a.rows) * parts * 2 <= 2 * sms && a.vocab / (parts * 2) >= 2048) parts *= 2;
+  if (threads == 256)
+    while (parts < 8 && static_cast<int64_t>(a.rows) * parts < 2 * sms && a.vocab / (parts * 2) >= 2048) parts *= 2;
   if (static_cast<int64_t>(a.rows) * parts > 0x7fffffff) return record_error(VLA_ERR_UNSUPPORTED, "vla_token_logprobs: too many rows");
-  if (small) VLA_CUDA_TRY(launch_pdl(token_logprobs_kernel<DT, 32>, dim3(a.rows), dim3(32), 0, s, a, 1));
-  else VLA_CUDA_TRY(launch_pdl_cluster(token_logprobs_kernel<DT, 256>, dim3(a.rows * parts), dim3(256), 0, s, parts, a, parts));
+  auto kern = threads == 32 ? token_logprobs_kernel<DT, 32> : threads == 64 ? token_logprobs_kernel<DT, 64> : token_logprobs_kernel<DT, 256>;
+  VLA_CUDA_TRY(launch_pdl_cluster(kern, dim3(a.rows * parts), dim3(threads), 0, s, parts, a, parts));
   note_launch();
   VLA_CUDA_TRY(cudaGetLastError());
   return VLA_OK;
