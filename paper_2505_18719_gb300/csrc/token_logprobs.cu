@@ -1,13 +1,17 @@
 // Log-probs of given tokens with entropy and the best alternatives, and their gradient.
 //
-// Forward, one row of logits z: with c = log2(e) / T and M = max z, s = sum 2^((z - M) c) and w = sum (z - M) c 2^((z - M) c)
-// give log p_j = (z_j - M) / T - ln s, lse = M / T + ln s and the entropy ln 2 (log2 s - w / s), from one pass with a running
-// maximum per thread (a sum relative to m goes over to m' by s' = f s, w' = f (w + (m - m') c s), f = 2^((m - m') c)).
-// Bound by reading the logits, for 16-bit types closely followed by issuing about 7 instructions an element.
+// Forward, one row of logits z, in powers of two: with c = log2(e) / T, any reference r near the largest z c,
+// s = sum 2^(z c - r) and w = sum (z c - r) 2^(z c - r), log p_j = ln 2 (z_j c - r - log2 s), lse = ln 2 (r + log2 s) and the entropy is
+// ln 2 (log2 s - w / s).  One pass with a running reference per thread (a sum relative to r goes over to r' by s' = f s,
+// w' = f (w + (r - r') s), f = 2^(r - r')).  The reference is the rounded product of the maximum and c and every z c - r
+// one fma, exact up to its own size: logits far from zero lose nothing while |r| is below 2^24.  (Rows beyond, such as one of
+// nothing but a type's lowest values, are read again with the difference to the maximum taken first.)  Bound by reading the logits, for 16-bit types
+// as much by issuing 5 instructions an element (two elements share an fma, an addition and an fma).
 //
 // The best alternatives come from the same pass: each thread's maximum is known, and the k-th largest maximum over
 // disjoint groups of threads is a bound that at least k logits reach.  Only threads whose maximum reaches it read
-// their logits again (from L2), and what lies above the bound is ranked by counting.
+// logits again (from L2), and only those rounds of the pass whose maximum, kept in shared memory, reaches it too; what
+// lies above the bound is ranked by counting.
 #include <algorithm>
 
 #include "lm.h"
@@ -16,8 +20,6 @@
 namespace vla {
 
 namespace {
-
-constexpr int kWarpVocab = 1024, kSmallVocab = 6144;  // ids up to which a row has 32, 64 threads
 
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 
@@ -89,20 +91,60 @@ __device__ __forceinline__ float float_of(int order) { return __int_as_float(ord
 __device__ __forceinline__ float key_value(int64_t key) { return float_of(static_cast<int>(key >> 32)); }
 __device__ __forceinline__ int key_id(int64_t key) { return 0x7fffffff - static_cast<int>(key & 0x7fffffff); }
 
-// Running sums of a set of logits: maximum m (raw), s and w relative to it.
+// Two fp32 values in a register pair, and what the SM does to both at once.
+__device__ __forceinline__ uint64_t pair_of(float a, float b) {
+  uint64_t y;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(a), "f"(b));
+  return y;
+}
+__device__ __forceinline__ float2 halves_of(uint64_t x) {
+  float2 y;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(y.x), "=f"(y.y) : "l"(x));
+  return y;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t y;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
+  return y;
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+  uint64_t y;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(a), "l"(b), "l"(c));
+  return y;
+}
+
+// Whether the rounding of r = m c may be more than a fraction of a power of two.
+__device__ __forceinline__ bool is_far(float m, float c) { return m != -INFINITY && !(fabsf(m * c) < 16777216.f); }
+// The reference that goes with a maximum of some of a row's logits: none for one so low that its logits weigh nothing
+// beside any row that is not far.
+__device__ __forceinline__ float reference_of(float m, float c) { return m * c > -16777216.f ? m * c : -INFINITY; }
+
+// Below 2^-200 a weight is 0, and 0 * -infinity no number.
+constexpr float kFloor = -200.f;
+
+// Running sums of a set of logits relative to 2^r; r = -infinity: nothing but zeros so far.
 struct Sums {
-  float m = -INFINITY, s = 0.f, w = 0.f;
-  __device__ __forceinline__ void rise(float to, float c) {
-    const float d = m == -INFINITY ? 0.f : fmaxf((m - to) * c, -200.f), f = exp2_fast(d);
-    w = f * (w + d * s);
+  float r = -INFINITY, s = 0.f, w = 0.f;
+  __device__ __forceinline__ void rise(float to) {
+    const float d = r == -INFINITY ? 0.f : fmaxf(r - to, kFloor), f = exp2_fast(d);
+    w = f * fmaf(d, s, w);
     s *= f;
-    m = to;
+    r = to;
   }
-  __device__ __forceinline__ void add(float d) {  // d = (z - m) c; below 2^-200 a weight is 0, and 0 * -infinity no number
-    d = fmaxf(d, -200.f);
+  __device__ __forceinline__ void add(float d) {
+    d = fmaxf(d, kFloor);
     const float e = exp2_fast(d);
     s += e;
     w = fmaf(d, e, w);
+  }
+  // two at a time into pairs of sums
+  static __device__ __forceinline__ void add_pair(uint64_t d, uint64_t& s, uint64_t& w) {
+    float2 x = halves_of(d);
+    x.x = fmaxf(x.x, kFloor);
+    x.y = fmaxf(x.y, kFloor);
+    const uint64_t e = pair_of(exp2_fast(x.x), exp2_fast(x.y));
+    s = add2(s, e);
+    w = fma2(pair_of(x.x, x.y), e, w);
   }
 };
 
@@ -114,6 +156,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
   constexpr int kGroups = THREADS == 32 ? 32 : 64, kGroupLanes = kGroups / kWarps;  // lanes of a warp that are equal modulo kGroupLanes
   constexpr int kList = THREADS == 32 ? 128 : 512;
   constexpr int kMostParts = 8;
+  constexpr int kRounds = 16;                      // rounds of the pass are kept modulo 16
+  __shared__ float round_max[kRounds][THREADS];
   __shared__ __align__(16) int group_max[kGroups];
   __shared__ float red[3][kWarps];
   __shared__ int64_t above[kList];
@@ -153,44 +197,51 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
   }
 
   Sums x;
-  auto chunk = [&](const uint4 (&v)[kUnroll]) {
-    uint32_t top = v[0].x;
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u)
-      top = V::word_max(top, V::word_max(V::word_max(v[u].x, v[u].y), V::word_max(v[u].z, v[u].w)));
-    const float m = max_nan(x.m, V::word_float_max(top));
-    x.rise(m, c);
-    // the difference first: fma(z, c, -m c) is off by the rounding of m c, which for logits far from zero is
-    // more than a weight's whole exponent.  Nothing but -infinity so far: any reference gives zeros.
-    const float ref = m == -INFINITY ? 0.f : m;
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      float z[V::kN];
-      V::unpack(v[u], z);
-#pragma unroll
-      for (int i = 0; i < V::kN; ++i) x.add((z[i] - ref) * c);
-    }
-  };
-  for (int i = tid; i < vecs; i += THREADS * kUnroll) {
+  float most = -INFINITY;  // this thread's maximum
+  const uint64_t c2 = pair_of(c, c);
+  for (int i = tid, round = 0; i < vecs; i += THREADS * kUnroll, ++round) {
     uint4 v[kUnroll];
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) {
       v[u] = make_uint4(V::kLowest, V::kLowest, V::kLowest, V::kLowest);
       if (i + u * THREADS < vecs) v[u] = body[i + u * THREADS];
     }
-    chunk(v);
+    uint32_t up = v[0].x;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) up = V::word_max(up, V::word_max(V::word_max(v[u].x, v[u].y), V::word_max(v[u].z, v[u].w)));
+    const float peak = V::word_float_max(up);
+    if (k > 0) {
+      float& kept = round_max[round % kRounds][tid];
+      kept = round < kRounds ? peak : fmaxf(kept, peak);
+    }
+    most = max_nan(most, peak);
+    x.rise(reference_of(most, c));
+    const float ref = x.r == -INFINITY ? 0.f : x.r;
+    const uint64_t r2 = pair_of(-ref, -ref);
+    uint64_t s2 = 0, w2 = 0;  // zeros
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      float z[V::kN];
+      V::unpack(v[u], z);
+#pragma unroll
+      for (int j = 0; j < V::kN; j += 2) Sums::add_pair(fma2(pair_of(z[j], z[j + 1]), c2, r2), s2, w2);
+    }
+    const float2 s = halves_of(s2), w = halves_of(w2);
+    x.s += s.x + s.y;
+    x.w += w.x + w.y;
   }
   // up to 7 elements before and after the vectors: one a thread
   const int edge = tid < head ? tid : tid < head + tail ? n - tail + tid - head : -1;
   if (edge >= 0) {
-    const float z = V::load(base, edge), m = max_nan(x.m, z);
-    x.rise(m, c);
-    if (m != -INFINITY) x.add((z - m) * c);
+    const float z = V::load(base, edge);
+    most = max_nan(most, z);
+    x.rise(reference_of(most, c));
+    if (x.r != -INFINITY) x.add(fmaf(z, c, -x.r));
   }
-  const int mine = ordered(x.m);
+  const int mine = ordered(most);
 
   // the CTA's maximum and its groups'
-  float top = x.m;
+  float top = most;
   if (kGroupLanes == 32) group_max[warp * 32 + lane] = mine;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) {
@@ -202,14 +253,21 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
   top = red[0][0];
 #pragma unroll
   for (int i = 1; i < kWarps; ++i) top = max_nan(top, red[0][i]);
-  if (x.m != -INFINITY) x.rise(top, c);
+  const bool odd = !(top < INFINITY);  // a NaN or +infinity in the slice
+  const bool far = !odd && is_far(top, c);
+  if (far) {
+    x = Sums();
+    x.r = 0.f;
+    for (int j = tid; j < n; j += THREADS) x.add((V::load(base, j) - top) * c);
+  } else if (x.r != -INFINITY) {
+    x.rise(top * c);
+  }
   x.s = warp_sum(x.s);
   x.w = warp_sum(x.w);
   if (lane == 0) {
     red[1][warp] = x.s;
     red[2][warp] = x.w;
   }
-  const bool odd = !(top < INFINITY);  // a NaN or +infinity in the slice
   if (k > 0 && tid < kGroups) {
     // the largest maximum that k groups reach
     const int v = group_max[tid];
@@ -222,8 +280,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
     if (reach >= k) atomicMax(&bound, v);
   }
   __syncthreads();
-  Sums total;
-  total.m = top;
+  Sums total;  // relative to the maximum `top`
+  total.r = far ? 0.f : top * c;
 #pragma unroll
   for (int i = 0; i < kWarps; ++i) {
     total.s += red[1][i];
@@ -248,15 +306,17 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
           level_ids[at] = first + j;
       };
       if (lowest ? mine > at_least : mine >= at_least) {
-        for (int i = tid; i < vecs; i += THREADS * kUnroll) {
+        for (int i = tid, round = 0; i < vecs; i += THREADS * kUnroll, ++round) {
+          const float there = round_max[round % kRounds][tid];
+          if (lowest ? !(there > limit) : !(there >= limit)) continue;
           uint4 v[kUnroll];
 #pragma unroll
           for (int u = 0; u < kUnroll; ++u) v[u] = body[min(i + u * THREADS, vecs - 1)];
 #pragma unroll
           for (int u = 0; u < kUnroll; ++u) {
             if (i + u * THREADS >= vecs) break;
-            const float most = V::word_float_max(V::word_max(V::word_max(v[u].x, v[u].y), V::word_max(v[u].z, v[u].w)));
-            if (lowest ? !(most > limit) : !(most >= limit)) continue;
+            const float peak = V::word_float_max(V::word_max(V::word_max(v[u].x, v[u].y), V::word_max(v[u].z, v[u].w)));
+            if (lowest ? !(peak > limit) : !(peak >= limit)) continue;
             float z[V::kN];
             V::unpack(v[u], z);
             uint32_t found = 0;
@@ -317,7 +377,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
 
   // ---- the slices' results meet in the first CTA
   if (THREADS == 256 && parts > 1) {
-    if (tid == 0) slice = make_float3(total.m, total.s, total.w);
+    if (tid == 0) slice = make_float3(top, total.s, total.w);
     cluster_sync();
     if (part == 0) {
       for (int i = tid; i < parts * a.top_k; i += THREADS) {
@@ -333,18 +393,15 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
     }
     cluster_sync();  // the other CTAs' results stay until the first has them
     if (part != 0) return;
-    float m = -INFINITY;
-    for (int i = 0; i < parts; ++i) m = max_nan(m, all_slices[i].x);
-    total.m = m;
+    top = -INFINITY;
+    for (int i = 0; i < parts; ++i) top = max_nan(top, all_slices[i].x);
     total.s = total.w = 0.f;
     for (int i = 0; i < parts; ++i) {
-      Sums y;
-      y.m = all_slices[i].x;
-      y.s = all_slices[i].y;
-      y.w = all_slices[i].z;
-      if (y.m != -INFINITY) y.rise(m, c);
-      total.s += y.s;
-      total.w += y.w;
+      const float m = all_slices[i].x, wide = is_far(m, c) || is_far(top, c) ? (m - top) * c : m * c - top * c;
+      if (m == -INFINITY) continue;
+      const float d = fmaxf(wide, kFloor), f = exp2_fast(d);
+      total.s = fmaf(f, all_slices[i].y, total.s);
+      total.w = fmaf(f, fmaf(d, all_slices[i].y, all_slices[i].z), total.w);
     }
     // disjoint sorted lists: a key's place is the number of larger ones
     for (int i = tid; i < parts * a.top_k; i += THREADS) {
@@ -357,19 +414,21 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
   }
 
   if (tid >= max(1, a.top_k)) return;
-  const bool bad = !(total.m < INFINITY), none = total.m == -INFINITY;
-  const float ln_s = logf(total.s);
+  const bool bad = !(top < INFINITY), none = top == -INFINITY, apart = !bad && is_far(top, c);
+  // the difference to the maximum in natural units (a log-prob may be as low as a type's lowest value), and what the
+  // rounded reference is off the maximum
+  const float log2_s = log2f(total.s), r = top * c, rest = (apart ? 0.f : fmaf(top, c, -r)) - log2_s;
+  auto logprob = [&](float z) { return bad ? NAN : none ? -INFINITY : fmaf(rest, kLn2, (z - top) * inv_t); };
   if (tid == 0) {
     if (bad) raise_status(a.status, VLA_STATUS_NONFINITE);
-    const float lse = bad ? NAN : none ? -INFINITY : fmaf(total.m, inv_t, ln_s);
-    if (a.lse) a.lse[row] = lse;
-    if (a.entropy) a.entropy[row] = bad ? NAN : none ? 0.f : ln_s - total.w / total.s * kLn2;
-    if (a.logprob) a.logprob[row] = token < 0 ? 0.f : bad ? NAN : none ? -INFINITY : (chosen - total.m) * inv_t - ln_s;
+    if (a.lse) a.lse[row] = bad ? NAN : none ? -INFINITY : apart ? fmaf(top, inv_t, log2_s * kLn2) : (r + log2_s) * kLn2;
+    if (a.entropy) a.entropy[row] = bad ? NAN : none ? 0.f : (log2_s - total.w / total.s) * kLn2;
+    if (a.logprob) a.logprob[row] = token < 0 ? 0.f : logprob(chosen);
   }
   if (tid < a.top_k) {
     const int64_t key = best[tid], at = static_cast<int64_t>(row) * a.top_k + tid;
     a.top_ids[at] = key_id(key);
-    a.top_logprobs[at] = bad ? NAN : none ? -INFINITY : (key_value(key) - total.m) * inv_t - ln_s;
+    a.top_logprobs[at] = logprob(key_value(key));
   }
 }
 
@@ -454,13 +513,24 @@ __global__ void __launch_bounds__(256) token_logprobs_grad_kernel(const LogprobG
 
 template <int DT>
 int logprobs_of(const LogprobArgs& a, cudaStream_t s, int sms) {
-  // a row has few threads where it is short: their number is what its barriers cost
-  const int threads = a.vocab <= kWarpVocab ? 32 : a.vocab <= kSmallVocab ? 64 : 256;
+  // Threads a row: the SMs hold 1024 each, so rows go in waves of 1024 sms / threads, and a wave takes about as long as
+  // 44 ids a thread for the row's own steps and one for each id that a thread has (3584 rows x 32064 bf16: 72, 64, 54, 62 us
+  // with 32, 64, 128, 256 threads; 4000 x 1200: 9.2, 12, 17 with 32, 64, 128; 500 x 32064: 36, 22, 18, 11).
+  int threads = 32;
+  int64_t least = INT64_MAX;
+  for (int t = 32; t <= 256; t *= 2) {
+    const int64_t waves = (static_cast<int64_t>(a.rows) * t - 1) / (1024LL * sms) + 1, cost = waves * (44 + a.vocab / t);
+    if (cost < least) {
+      least = cost;
+      threads = t;
+    }
+  }
+  // few long rows are cut over a cluster
   int parts = 1;
   if (threads == 256)
     while (parts < 8 && static_cast<int64_t>(a.rows) * parts < 2 * sms && a.vocab / (parts * 2) >= 2048) parts *= 2;
   if (static_cast<int64_t>(a.rows) * parts > 0x7fffffff) return record_error(VLA_ERR_UNSUPPORTED, "vla_token_logprobs: too many rows");
-  auto kern = threads == 32 ? token_logprobs_kernel<DT, 32> : threads == 64 ? token_logprobs_kernel<DT, 64> : token_logprobs_kernel<DT, 256>;
+  auto kern = threads == 32 ? token_logprobs_kernel<DT, 32> : threads == 64 ? token_logprobs_kernel<DT, 64> : threads == 128 ? token_logprobs_kernel<DT, 128> : token_logprobs_kernel<DT, 256>;
   VLA_CUDA_TRY(launch_pdl_cluster(kern, dim3(a.rows * parts), dim3(threads), 0, s, parts, a, parts));
   note_launch();
   VLA_CUDA_TRY(cudaGetLastError());
