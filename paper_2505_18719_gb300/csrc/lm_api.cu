@@ -7,6 +7,8 @@
 namespace vla {
 namespace {
 
+constexpr int kMostHeads = 65535;  // channels of a row fit 32 bits
+
 bool misaligned(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p) & (bytes - 1); }
 bool is_dtype(int d) { return d == VLA_F32 || d == VLA_F16 || d == VLA_BF16; }
 int elem_bytes(int d) { return d == VLA_F32 ? 4 : 2; }
@@ -73,6 +75,7 @@ int vla_rope_append(const void* q, int64_t ldq, const void* k, int64_t ldk, cons
                               "vla_rope_append: cache of fp16 or bf16 with heads of 64 or 128"))
     return rc;
   if (!is_dtype(dtype)) return record_error(VLA_ERR_UNSUPPORTED, "vla_rope_append: unknown dtype");
+  if (n_q_heads > kMostHeads || kv->n_heads > kMostHeads) return record_error(VLA_ERR_UNSUPPORTED, "vla_rope_append: more than 65535 heads");
   if (rows < 0 || n_q_heads < 1) return record_error(VLA_ERR_ARG, "vla_rope_append: rows < 0 or no query heads");
   if (rows == 0) return VLA_OK;
   const int64_t hd = kv->head_dim;
@@ -103,6 +106,7 @@ int vla_paged_attn(const void* q, int64_t ldq, int dtype, int rows, int n_q_head
     return rc;
   if (dtype != kv->dtype && !(dtype == VLA_F32 && kv->dtype == VLA_F16))
     return record_error(VLA_ERR_UNSUPPORTED, "vla_paged_attn: queries of the cache's type, or f32 over an fp16 cache");
+  if (n_q_heads > kMostHeads) return record_error(VLA_ERR_UNSUPPORTED, "vla_paged_attn: more than 65535 heads");
   if (rows < 0 || n_q_heads < 1 || n_q_heads % kv->n_heads)
     return record_error(VLA_ERR_ARG, "vla_paged_attn: rows < 0, or query heads no multiple of the cache's");
   if (rows == 0) return VLA_OK;

@@ -201,10 +201,11 @@ __global__ void __launch_bounds__(256) rope_table_kernel(const RopeTableArgs a) 
 
 // ------------------------------------------------------------------------------------ rope append
 // x <- x / sqrt(mean x^2 + eps) gain, then per pair (a, b) of channels (a cos - b sin, b cos + a sin).  Each element is
-// read and written once; bound by HBM for a prefill, by latency for a decode step.  hd / 8 lanes hold a head, 8
-// channels each in 16-byte accesses (32 for fp32); the partner of a channel in the other half is a shuffle
-// away.  A warp walks over heads of one row, whose cosines and sines stay in registers; a row of few is cut
-// over several warps so that a decode step fills the GPU.
+// read and written once; bound by HBM for a prefill, closely followed by issuing instructions, by latency for a decode
+// step.  hd / 8 lanes hold a head, 8 channels each in 16-byte accesses (32 for fp32), so that an access of a warp is
+// 256 channels that follow each other in the row; the partner of a channel in the other half is a shuffle away.  A
+// warp walks over the queries, keys and values of one row, whose cosines and sines stay in registers; a row of few
+// is cut over several warps so that a decode step fills the GPU.
 enum RopeLayout : int { kNoRope = 0, kHalves = 1, kPairs = 2 };
 
 __device__ __forceinline__ float clamp_f16(float x, uint32_t& sat) {
@@ -249,95 +250,79 @@ constexpr int kAppendThreads = 128;
 // `slices` warps share a row's heads.
 template <int DT, int LAYOUT, bool NORM>
 __global__ void __launch_bounds__(kAppendThreads) rope_append_kernel(const RopeAppendArgs a, const int slices) {
-  constexpr int kUnroll = 4;
+  constexpr int kUnroll = 4, kSize = DT == VLA_F32 ? 4 : 2, kSpan = 256;  // channels of an access
   pdl_launch_dependents();
   pdl_wait();
   const int lane = threadIdx.x & 31, hd = a.kv.head_dim, span = hd / 8;  // lanes of a head
   const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kAppendThreads / 32) + (threadIdx.x >> 5);
   if (unit >= static_cast<int64_t>(a.rows) * slices) return;
   const int row = static_cast<int>(unit / slices), slice = static_cast<int>(unit % slices);
-  const int per = 32 / span, c0 = lane % span * 8;  // heads of an access; this lane's first channel
-  const int heads = a.n_q_heads + 2 * a.kv.n_heads, steps = (heads + per - 1) / per;
-  const int from = static_cast<int>(static_cast<int64_t>(steps) * slice / slices) * per;
-  const int to = min(heads, static_cast<int>(static_cast<int64_t>(steps) * (slice + 1) / slices) * per);
+  const int c0 = lane % span * 8;  // this lane's first channel of a head
+  // accesses: queries, keys, values; this warp's
+  const int q_steps = (a.n_q_heads * hd + kSpan - 1) / kSpan, kv_steps = (a.kv.n_heads * hd + kSpan - 1) / kSpan, steps = q_steps + 2 * kv_steps;
+  const int from = steps * slice / slices, to = steps * (slice + 1) / slices;
   const int pos = a.row_pos[row], slot = a.row_slot[row];
   const bool lost = pos < -1 || (LAYOUT != kNoRope && pos >= a.n_pos), empty = pos == -1 || lost;
   const bool stray = slot < -1 || slot >= a.kv.n_pages * a.kv.page_size;
   if ((lost || (stray && !empty)) && lane == 0 && slice == 0) raise_status(a.status, VLA_STATUS_PAGES);
   const bool file = !empty && !stray && slot != -1;
-  const int64_t cell = file ? (slot / a.kv.page_size) * a.kv.page_stride + (slot % a.kv.page_size) * a.kv.slot_stride + c0 : 0;
 
   const int half = a.rope_dim / 2;
   const bool turns = LAYOUT != kNoRope && !empty && c0 < a.rope_dim;
   const bool second = LAYOUT == kHalves && c0 >= half;
-  float cs[LAYOUT == kHalves ? 8 : 4], sn[LAYOUT == kHalves ? 8 : 4];
-  if constexpr (LAYOUT != kNoRope) {
-    constexpr int kPairs8 = LAYOUT == kHalves ? 8 : 4;
+  constexpr int kPairs8 = LAYOUT == kHalves ? 8 : 4;  // rotations of a lane's 8 channels; none: (1, 0)
+  float cs[kPairs8], sn[kPairs8];
+  if (LAYOUT != kNoRope && from < q_steps + kv_steps) {
     const float4* t = reinterpret_cast<const float4*>(a.rope + static_cast<int64_t>(pos) * half + (LAYOUT == kHalves ? (second ? c0 - half : c0) : c0 / 2));
 #pragma unroll
     for (int i = 0; i < kPairs8 / 2; ++i) {
       float4 x = make_float4(1.f, 0.f, 1.f, 0.f);
       if (turns) x = t[i];
       cs[2 * i] = x.x;
-      sn[2 * i] = second ? -x.y : x.y;  // b cos + a sin: the partner's sign turns
+      sn[2 * i] = LAYOUT == kHalves && !second ? -x.y : x.y;  // a cos - b sin, b cos + a sin: the partner's sign turns
       cs[2 * i + 1] = x.z;
-      sn[2 * i + 1] = second ? -x.w : x.w;
+      sn[2 * i + 1] = LAYOUT == kHalves && !second ? -x.w : x.w;
     }
   }
-  uint4 gq = make_uint4(0u, 0u, 0u, 0u), gk = gq;
-  if constexpr (NORM) {
-    if (a.q_gain) gq = *reinterpret_cast<const uint4*>(a.q_gain + c0);
-    if (a.k_gain) gk = *reinterpret_cast<const uint4*>(a.k_gain + c0);
-  }
-  const int partner = second ? lane - half / 8 : lane + half / 8;
+  const int partner = (second ? lane - half / 8 : lane + half / 8) & 31;
   uint32_t sat = 0;
-  for (int base = from; base < to; base += kUnroll * per) {
-    Eight<DT> raw[kUnroll];
-#pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      const int h = base + u * per + lane / span;
-      if (h < to && !empty) {
-        if (h < a.n_q_heads)
-          raw[u].load(a.q, row * a.ldq + static_cast<int64_t>(h) * hd + c0);
-        else if (h < a.n_q_heads + a.kv.n_heads)
-          raw[u].load(a.k, row * a.ldk + static_cast<int64_t>(h - a.n_q_heads) * hd + c0);
-        else
-          raw[u].load(a.v, row * a.ldv + static_cast<int64_t>(h - a.n_q_heads - a.kv.n_heads) * hd + c0);
-      }
+
+  // `n` channels of src, in accesses [j0, j1); put(access, values) stores 8 channels of this lane
+  auto walk = [&](const void* src, int n, int j0, int j1, const bf16* gain, bool turned, auto put) {
+    float g[8];
+    if (NORM && gain) {
+      const uint4 w = *reinterpret_cast<const uint4*>(gain + c0);
+      Eight<VLA_BF16>{{w}}.unpack(g);
     }
+    for (int j = j0; j < j1; j += kUnroll) {
+      Eight<DT> raw[kUnroll];
 #pragma unroll
-    for (int u = 0; u < kUnroll; ++u) {
-      if (base + u * per >= to) break;
-      const int h = base + u * per + lane / span;
-      const bool is_q = h < a.n_q_heads, is_v = h >= a.n_q_heads + a.kv.n_heads, live = h < to;
-      float x[8];
-      raw[u].unpack(x);
-      if constexpr (NORM) {
-        float ss = 0.f;
+      for (int u = 0; u < kUnroll; ++u)
+        if (j + u < j1 && (j + u) * kSpan + lane * 8 < n) raw[u].load(src, (j + u) * kSpan + lane * 8);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
-        for (int o = span / 2; o > 0; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-        const bool normed = is_q ? a.q_gain != nullptr : !is_v && a.k_gain != nullptr;
-        if (normed) {
-          const float r = rsqrtf(ss / static_cast<float>(hd) + a.eps);
-          const uint4 gain = is_q ? gq : gk;
-          const uint32_t w[4] = {gain.x, gain.y, gain.z, gain.w};
+      for (int u = 0; u < kUnroll; ++u) {
+        if (j + u >= j1) break;
+        float x[8];
+        raw[u].unpack(x);
+        if (NORM && gain) {
+          float ss = 0.f;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float2 f = unpack_bf16x2(w[i]);
-            x[2 * i] *= r * f.x;
-            x[2 * i + 1] *= r * f.y;
+          for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
+          ss += __shfl_xor_sync(0xffffffffu, ss, 4);
+          ss += __shfl_xor_sync(0xffffffffu, ss, 2);
+          ss += __shfl_xor_sync(0xffffffffu, ss, 1);
+          if (span == 16) ss += __shfl_xor_sync(0xffffffffu, ss, 8);
+          const float r = rsqrtf(ss * (1.f / 64.f) * (span == 16 ? 0.5f : 1.f) + a.eps);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] *= r * g[i];
+        }
+        if (LAYOUT == kHalves && turned) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float y = __shfl_sync(0xffffffffu, x[i], partner);
+            if (turns) x[i] = x[i] * cs[i] + y * sn[i];
           }
-        }
-      }
-      if constexpr (LAYOUT == kHalves) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float y = __shfl_sync(0xffffffffu, x[i], partner & 31);
-          if (turns && !is_v) x[i] = x[i] * cs[i] - y * sn[i];
-        }
-      } else if constexpr (LAYOUT == kPairs) {
-        if (turns && !is_v) {
+        } else if (LAYOUT == kPairs && turned) {
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const float p = x[2 * i], q = x[2 * i + 1];
@@ -345,31 +330,47 @@ __global__ void __launch_bounds__(kAppendThreads) rope_append_kernel(const RopeA
             x[2 * i + 1] = q * cs[i] + p * sn[i];
           }
         }
-      }
-      if (!live) continue;
-      if (is_q) {
-        if (empty) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = 0.f;
-        }
-        char* p = static_cast<char*>(a.q_out) + (row * a.ldqo + static_cast<int64_t>(h) * hd + c0) * (DT == VLA_F32 ? 4 : 2);
-        if constexpr (DT == VLA_F32) {
-          reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-          reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
-        } else {
-          *reinterpret_cast<uint4*>(p) = pack8(x, DT == VLA_F16);
-        }
-      } else if (file) {
-        const bool f16_type = a.kv.dtype == VLA_F16;
-        if (DT != VLA_F16 && f16_type) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = clamp_f16(x[i], sat);
-        }
-        const int kv_head = h - a.n_q_heads - (is_v ? a.kv.n_heads : 0);
-        uint16_t* p = static_cast<uint16_t*>(is_v ? a.kv.v : a.kv.k) + cell + kv_head * a.kv.head_stride;
-        *reinterpret_cast<uint4*>(p) = pack8(x, f16_type);
+        if ((j + u) * kSpan + lane * 8 < n) put(j + u, x);
       }
     }
+  };
+
+  if (from < q_steps) {
+    char* const out = static_cast<char*>(a.q_out) + (row * a.ldqo + lane * 8) * kSize;
+    auto put = [&](int j, const float(&x)[8]) {
+      char* p = out + j * (kSpan * kSize);
+      if constexpr (DT == VLA_F32) {
+        reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+        reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+      } else {
+        *reinterpret_cast<uint4*>(p) = pack8(x, DT == VLA_F16);
+      }
+    };
+    if (empty) {
+      const float none[8] = {};
+      for (int j = from; j < min(to, q_steps); ++j)
+        if (j * kSpan + lane * 8 < a.n_q_heads * hd) put(j, none);
+    } else {
+      walk(static_cast<const char*>(a.q) + row * a.ldq * kSize, a.n_q_heads * hd, from, min(to, q_steps), a.q_gain, true, put);
+    }
+  }
+  if (!file || to <= q_steps) return;
+  const bool f16_type = a.kv.dtype == VLA_F16;
+  const int64_t cell = (slot / a.kv.page_size) * a.kv.page_stride + (slot % a.kv.page_size) * a.kv.slot_stride + lane / span * a.kv.head_stride + c0;
+  const int64_t hop = (32 / span) * a.kv.head_stride;  // from access to access
+#pragma unroll 1
+  for (int v = from < q_steps + kv_steps ? 0 : 1; v < 2; ++v) {  // keys, then values
+    const int before = q_steps + v * kv_steps, j0 = max(from - before, 0), j1 = min(to - before, kv_steps);
+    if (j0 >= j1) continue;
+    uint16_t* const out = static_cast<uint16_t*>(v ? a.kv.v : a.kv.k) + cell;
+    walk(static_cast<const char*>(v ? a.v : a.k) + row * (v ? a.ldv : a.ldk) * kSize, a.kv.n_heads * hd, j0, j1, v ? nullptr : a.k_gain, v == 0,
+         [&](int j, float(&x)[8]) {
+           if (f16_type) {
+#pragma unroll
+             for (int i = 0; i < 8; ++i) x[i] = clamp_f16(x[i], sat);
+           }
+           *reinterpret_cast<uint4*>(out + j * hop) = pack8(x, f16_type);
+         });
   }
   report_saturation(a.status, sat);
 }
@@ -406,7 +407,7 @@ int rope_table_launch(const RopeTableArgs& a, cudaStream_t s) {
 namespace {
 template <int DT>
 int append_of(const RopeAppendArgs& a, cudaStream_t s) {
-  const int per = 256 / a.kv.head_dim, steps = (a.n_q_heads + 2 * a.kv.n_heads + per - 1) / per;
+  const int hd = a.kv.head_dim, steps = (a.n_q_heads * hd + 255) / 256 + 2 * ((a.kv.n_heads * hd + 255) / 256);
   int dev = 0, sms = 0;
   VLA_CUDA_TRY(cudaGetDevice(&dev));
   VLA_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
