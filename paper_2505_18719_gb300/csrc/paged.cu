@@ -201,10 +201,12 @@ __global__ void __launch_bounds__(256) rope_table_kernel(const RopeTableArgs a) 
 
 // ------------------------------------------------------------------------------------ rope append
 // x <- x / sqrt(mean x^2 + eps) gain, then per pair (a, b) of channels (a cos - b sin, b cos + a sin).  Each element is
-// read and written once; bound by HBM for a prefill, closely followed by issuing instructions, by latency for a decode
-// step.  hd / 8 lanes hold a head, 8 channels each in 16-byte accesses (32 for fp32), so that an access of a warp is
-// 256 channels that follow each other in the row; the partner of a channel in the other half is a shuffle away.  A
-// warp walks over the queries, keys and values of one row, whose cosines and sines stay in registers; a row of few
+// read and written once; bound by HBM for a prefill, for 16-bit types as much by issuing instructions, by latency for a
+// decode step.  hd / 8 lanes hold a head, 8 channels each, so that an access of a warp is 256 channels that follow each
+// other in the row.  Where pairs lie half a rotation apart, the partner of a 16-bit channel is a shuffle away; in fp32 a
+// lane has 4 channels of each half instead (fp32 rows of 32 / 32 heads: 226 us for 18432 against 232; 16-bit ones in pieces
+// of 8 bytes: 131 against 95).  A warp walks over the queries, keys and values of one row, some accesses ahead (the
+// first ones before the row's position is known), and the row's cosines and sines stay in registers; a row of few
 // is cut over several warps so that a decode step fills the GPU.
 enum RopeLayout : int { kNoRope = 0, kHalves = 1, kPairs = 2 };
 
@@ -217,12 +219,31 @@ __device__ __forceinline__ float clamp_f16(float x, uint32_t& sat) {
 }
 
 template <int DT>
-struct Eight {  // 8 channels of type DT as they lie in memory
+struct Eight {  // 8 channels of type DT, in two pieces of 4 that follow each other in memory or (SPLIT) do not
   uint4 v[DT == VLA_F32 ? 2 : 1];
-  __device__ __forceinline__ void load(const void* p, int64_t i) {
-    const uint4* q = reinterpret_cast<const uint4*>(static_cast<const char*>(p) + i * (DT == VLA_F32 ? 4 : 2));
-    v[0] = q[0];
-    if constexpr (DT == VLA_F32) v[1] = q[1];
+  template <bool SPLIT>
+  __device__ __forceinline__ void load(const char* p, int gap) {  // the second piece `gap` bytes after the first
+    if constexpr (DT == VLA_F32) {
+      v[0] = *reinterpret_cast<const uint4*>(p);
+      v[1] = *reinterpret_cast<const uint4*>(p + gap);
+    } else if constexpr (SPLIT) {
+      const uint2 a = *reinterpret_cast<const uint2*>(p), b = *reinterpret_cast<const uint2*>(p + gap);
+      v[0] = make_uint4(a.x, a.y, b.x, b.y);
+    } else {
+      v[0] = *reinterpret_cast<const uint4*>(p);
+    }
+  }
+  template <bool SPLIT>
+  __device__ __forceinline__ void store(char* p, int gap) const {
+    if constexpr (DT == VLA_F32) {
+      *reinterpret_cast<uint4*>(p) = v[0];
+      *reinterpret_cast<uint4*>(p + gap) = v[1];
+    } else if constexpr (SPLIT) {
+      *reinterpret_cast<uint2*>(p) = make_uint2(v[0].x, v[0].y);
+      *reinterpret_cast<uint2*>(p + gap) = make_uint2(v[0].z, v[0].w);
+    } else {
+      *reinterpret_cast<uint4*>(p) = v[0];
+    }
   }
   __device__ __forceinline__ void unpack(float (&x)[8]) const {
     const uint32_t* w = reinterpret_cast<const uint32_t*>(v);
@@ -247,64 +268,96 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8], bool f16_type) {
 
 constexpr int kAppendThreads = 128;
 
-// `slices` warps share a row's heads.
+// `slices` warps share a row's heads.  Accesses ahead and warps an SM as measured on 18432 rows: bf16 of 32 / 8 heads with norms
+// 80 us with 4 ahead and 28 warps, 86 with 20 warps, 92 with 3 ahead and 32 (pairs in halves 89 with 24 warps, 95 with 28); f32 of
+// 32 / 32 heads 232 us with 2 ahead and 28 warps, 283 with 4 and the fewer warps that leaves.
 template <int DT, int LAYOUT, bool NORM>
-__global__ void __launch_bounds__(kAppendThreads) rope_append_kernel(const RopeAppendArgs a, const int slices) {
-  constexpr int kUnroll = 4, kSize = DT == VLA_F32 ? 4 : 2, kSpan = 256;  // channels of an access
+__global__ void __launch_bounds__(kAppendThreads, LAYOUT == kHalves && NORM ? 6 : 7) rope_append_kernel(const RopeAppendArgs a, const int slices) {
+  constexpr int kAhead = DT == VLA_F32 ? 2 : 4, kSize = DT == VLA_F32 ? 4 : 2, kSpan = 256;  // channels of an access
+  constexpr bool kSplit = LAYOUT == kHalves && DT == VLA_F32, kShuffle = LAYOUT == kHalves && !kSplit;
   pdl_launch_dependents();
   pdl_wait();
   const int lane = threadIdx.x & 31, hd = a.kv.head_dim, span = hd / 8;  // lanes of a head
   const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kAppendThreads / 32) + (threadIdx.x >> 5);
   if (unit >= static_cast<int64_t>(a.rows) * slices) return;
-  const int row = static_cast<int>(unit / slices), slice = static_cast<int>(unit % slices);
-  const int c0 = lane % span * 8;  // this lane's first channel of a head
+  const int row = static_cast<int>(unit / slices), slice = static_cast<int>(unit - static_cast<int64_t>(row) * slices);
+  const int half = a.rope_dim / 2, part = lane % span;
+  const bool in_turn = LAYOUT != kNoRope && part * 8 < a.rope_dim;
+  // this lane's channels of a head: 4 from c0, 4 more `gap` on
+  const int c0 = kSplit && in_turn ? part * 4 : part * 8, gap = kSplit && in_turn ? half : 4, mine = lane / span * hd + c0;
   // accesses: queries, keys, values; this warp's
-  const int q_steps = (a.n_q_heads * hd + kSpan - 1) / kSpan, kv_steps = (a.kv.n_heads * hd + kSpan - 1) / kSpan, steps = q_steps + 2 * kv_steps;
-  const int from = steps * slice / slices, to = steps * (slice + 1) / slices;
+  const int q_channels = a.n_q_heads * hd, kv_channels = a.kv.n_heads * hd;
+  const int keys = (q_channels + kSpan - 1) / kSpan, kv_steps = (kv_channels + kSpan - 1) / kSpan, values = keys + kv_steps;
+  const int steps = values + kv_steps, from = steps * slice / slices, to = steps * (slice + 1) / slices;
+  // the rows' first elements, as if each began at access 0
+  const char* const q_row = static_cast<const char*>(a.q) + (row * a.ldq + mine) * kSize;
+  const char* const k_row = static_cast<const char*>(a.k) + (row * a.ldk + mine - keys * kSpan) * kSize;
+  const char* const v_row = static_cast<const char*>(a.v) + (row * a.ldv + mine - values * kSpan) * kSize;
+  // whether this lane's head of access j is there
+  auto there = [&](int j) {
+    const int first = j < keys ? 0 : j < values ? keys : values;
+    return (j - first) * kSpan + lane / span * hd < (j < keys ? q_channels : kv_channels);
+  };
+  Eight<DT> raw[kAhead];
+  auto fetch = [&](int j, Eight<DT>& r) {
+    if (j < to && there(j)) r.template load<kSplit>((j < keys ? q_row : j < values ? k_row : v_row) + j * (kSpan * kSize), gap * kSize);
+  };
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) fetch(from + u, raw[u]);
+
   const int pos = a.row_pos[row], slot = a.row_slot[row];
   const bool lost = pos < -1 || (LAYOUT != kNoRope && pos >= a.n_pos), empty = pos == -1 || lost;
   const bool stray = slot < -1 || slot >= a.kv.n_pages * a.kv.page_size;
   if ((lost || (stray && !empty)) && lane == 0 && slice == 0) raise_status(a.status, VLA_STATUS_PAGES);
   const bool file = !empty && !stray && slot != -1;
 
-  const int half = a.rope_dim / 2;
-  const bool turns = LAYOUT != kNoRope && !empty && c0 < a.rope_dim;
-  const bool second = LAYOUT == kHalves && c0 >= half;
-  constexpr int kPairs8 = LAYOUT == kHalves ? 8 : 4;  // rotations of a lane's 8 channels; none: (1, 0)
-  float cs[kPairs8], sn[kPairs8];
-  if (LAYOUT != kNoRope && from < q_steps + kv_steps) {
-    const float4* t = reinterpret_cast<const float4*>(a.rope + static_cast<int64_t>(pos) * half + (LAYOUT == kHalves ? (second ? c0 - half : c0) : c0 / 2));
+  // the rotations of this lane's pairs (one for each channel where the partner is elsewhere); none: (1, 0)
+  constexpr int kTurns = kShuffle ? 8 : 4;
+  const bool second = kShuffle && in_turn && c0 >= half;
+  const int partner = (second ? lane - half / 8 : lane + half / 8) & 31;
+  float cs[kTurns], sn[kTurns];
+  if (LAYOUT != kNoRope && from < values) {
+    const float4* t = reinterpret_cast<const float4*>(a.rope + static_cast<int64_t>(pos) * half + (kShuffle ? (second ? c0 - half : c0) : part * 4));
 #pragma unroll
-    for (int i = 0; i < kPairs8 / 2; ++i) {
+    for (int i = 0; i < kTurns / 2; ++i) {
       float4 x = make_float4(1.f, 0.f, 1.f, 0.f);
-      if (turns) x = t[i];
+      if (in_turn && !empty) x = t[i];
       cs[2 * i] = x.x;
-      sn[2 * i] = LAYOUT == kHalves && !second ? -x.y : x.y;  // a cos - b sin, b cos + a sin: the partner's sign turns
+      sn[2 * i] = kShuffle && !second ? -x.y : x.y;  // a cos - b sin, b cos + a sin: the partner's sign turns
       cs[2 * i + 1] = x.z;
-      sn[2 * i + 1] = LAYOUT == kHalves && !second ? -x.w : x.w;
+      sn[2 * i + 1] = kShuffle && !second ? -x.w : x.w;
     }
   }
-  const int partner = (second ? lane - half / 8 : lane + half / 8) & 31;
+  const bool f16_cache = a.kv.dtype == VLA_F16;
+  char* const out = static_cast<char*>(a.q_out) + (row * a.ldqo + mine) * kSize;
+  int64_t cell = 0, hop = 0;  // this lane's channels in the cache's slot, and from access to access
+  if (file) {
+    cell = (slot / a.kv.page_size) * a.kv.page_stride + (slot % a.kv.page_size) * a.kv.slot_stride + lane / span * a.kv.head_stride + c0;
+    hop = (32 / span) * a.kv.head_stride;
+  }
+  float gain[8];
+  bool normed = false;
   uint32_t sat = 0;
-
-  // `n` channels of src, in accesses [j0, j1); put(access, values) stores 8 channels of this lane
-  auto walk = [&](const void* src, int n, int j0, int j1, const bf16* gain, bool turned, auto put) {
-    float g[8];
-    if (NORM && gain) {
-      const uint4 w = *reinterpret_cast<const uint4*>(gain + c0);
-      Eight<VLA_BF16>{{w}}.unpack(g);
-    }
-    for (int j = j0; j < j1; j += kUnroll) {
-      Eight<DT> raw[kUnroll];
+  for (int base = from; base < to; base += kAhead) {
 #pragma unroll
-      for (int u = 0; u < kUnroll; ++u)
-        if (j + u < j1 && (j + u) * kSpan + lane * 8 < n) raw[u].load(src, (j + u) * kSpan + lane * 8);
-#pragma unroll
-      for (int u = 0; u < kUnroll; ++u) {
-        if (j + u >= j1) break;
-        float x[8];
-        raw[u].unpack(x);
-        if (NORM && gain) {
+    for (int u = 0; u < kAhead; ++u) {
+      const int j = base + u;
+      if (j >= to) break;
+      const bool is_q = j < keys, is_v = j >= values;
+      float x[8];
+      raw[u].unpack(x);
+      fetch(j + kAhead, raw[u]);
+      if constexpr (NORM) {
+        if (j == from || j == keys || j == values) {
+          const bf16* g = is_q ? a.q_gain : is_v ? nullptr : a.k_gain;
+          normed = g != nullptr;
+          if (normed) {
+            Eight<VLA_BF16> e;
+            e.load<kSplit>(reinterpret_cast<const char*>(g + c0), gap * 2);
+            e.unpack(gain);
+          }
+        }
+        if (normed) {
           float ss = 0.f;
 #pragma unroll
           for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
@@ -312,65 +365,50 @@ __global__ void __launch_bounds__(kAppendThreads) rope_append_kernel(const RopeA
           ss += __shfl_xor_sync(0xffffffffu, ss, 2);
           ss += __shfl_xor_sync(0xffffffffu, ss, 1);
           if (span == 16) ss += __shfl_xor_sync(0xffffffffu, ss, 8);
-          const float r = rsqrtf(ss * (1.f / 64.f) * (span == 16 ? 0.5f : 1.f) + a.eps);
+          const float r = rsqrtf(ss * (span == 16 ? 1.f / 128.f : 1.f / 64.f) + a.eps);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] *= r * g[i];
+          for (int i = 0; i < 8; ++i) x[i] *= r * gain[i];
         }
-        if (LAYOUT == kHalves && turned) {
+      }
+      if (kShuffle && !is_v) {
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float y = __shfl_sync(0xffffffffu, x[i], partner);
-            if (turns) x[i] = x[i] * cs[i] + y * sn[i];
-          }
-        } else if (LAYOUT == kPairs && turned) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float p = x[2 * i], q = x[2 * i + 1];
-            x[2 * i] = p * cs[i] - q * sn[i];
-            x[2 * i + 1] = q * cs[i] + p * sn[i];
-          }
+        for (int i = 0; i < 8; ++i) {
+          const float y = __shfl_sync(0xffffffffu, x[i], partner);
+          if (in_turn) x[i] = x[i] * cs[i % kTurns] + y * sn[i % kTurns];
         }
-        if ((j + u) * kSpan + lane * 8 < n) put(j + u, x);
+      } else if (LAYOUT != kNoRope && !is_v) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float &p = x[kSplit ? i : 2 * i], &q = x[kSplit ? i + 4 : 2 * i + 1];
+          const float turned = p * cs[i] - q * sn[i];
+          q = q * cs[i] + p * sn[i];
+          p = turned;
+        }
+      }
+      if (!there(j)) continue;
+      if (is_q) {
+        if (empty) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = 0.f;
+        }
+        Eight<DT> y;
+        if constexpr (DT == VLA_F32) {
+          y.v[0] = make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+          y.v[1] = make_uint4(__float_as_uint(x[4]), __float_as_uint(x[5]), __float_as_uint(x[6]), __float_as_uint(x[7]));
+        } else {
+          y.v[0] = pack8(x, DT == VLA_F16);
+        }
+        y.template store<kSplit>(out + j * (kSpan * kSize), gap * kSize);
+      } else if (file) {
+        if (f16_cache) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = clamp_f16(x[i], sat);
+        }
+        Eight<VLA_F16> y;  // (16 bits of either type)
+        y.v[0] = pack8(x, f16_cache);
+        y.store<kSplit>(reinterpret_cast<char*>(static_cast<uint16_t*>(is_v ? a.kv.v : a.kv.k) + cell + (j - (is_v ? values : keys)) * hop), gap * 2);
       }
     }
-  };
-
-  if (from < q_steps) {
-    char* const out = static_cast<char*>(a.q_out) + (row * a.ldqo + lane * 8) * kSize;
-    auto put = [&](int j, const float(&x)[8]) {
-      char* p = out + j * (kSpan * kSize);
-      if constexpr (DT == VLA_F32) {
-        reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
-        reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
-      } else {
-        *reinterpret_cast<uint4*>(p) = pack8(x, DT == VLA_F16);
-      }
-    };
-    if (empty) {
-      const float none[8] = {};
-      for (int j = from; j < min(to, q_steps); ++j)
-        if (j * kSpan + lane * 8 < a.n_q_heads * hd) put(j, none);
-    } else {
-      walk(static_cast<const char*>(a.q) + row * a.ldq * kSize, a.n_q_heads * hd, from, min(to, q_steps), a.q_gain, true, put);
-    }
-  }
-  if (!file || to <= q_steps) return;
-  const bool f16_type = a.kv.dtype == VLA_F16;
-  const int64_t cell = (slot / a.kv.page_size) * a.kv.page_stride + (slot % a.kv.page_size) * a.kv.slot_stride + lane / span * a.kv.head_stride + c0;
-  const int64_t hop = (32 / span) * a.kv.head_stride;  // from access to access
-#pragma unroll 1
-  for (int v = from < q_steps + kv_steps ? 0 : 1; v < 2; ++v) {  // keys, then values
-    const int before = q_steps + v * kv_steps, j0 = max(from - before, 0), j1 = min(to - before, kv_steps);
-    if (j0 >= j1) continue;
-    uint16_t* const out = static_cast<uint16_t*>(v ? a.kv.v : a.kv.k) + cell;
-    walk(static_cast<const char*>(v ? a.v : a.k) + row * (v ? a.ldv : a.ldk) * kSize, a.kv.n_heads * hd, j0, j1, v ? nullptr : a.k_gain, v == 0,
-         [&](int j, float(&x)[8]) {
-           if (f16_type) {
-#pragma unroll
-             for (int i = 0; i < 8; ++i) x[i] = clamp_f16(x[i], sat);
-           }
-           *reinterpret_cast<uint4*>(out + j * hop) = pack8(x, f16_type);
-         });
   }
   report_saturation(a.status, sat);
 }

@@ -91,28 +91,6 @@ __device__ __forceinline__ float float_of(int order) { return __int_as_float(ord
 __device__ __forceinline__ float key_value(int64_t key) { return float_of(static_cast<int>(key >> 32)); }
 __device__ __forceinline__ int key_id(int64_t key) { return 0x7fffffff - static_cast<int>(key & 0x7fffffff); }
 
-// Two fp32 values in a register pair, and what the SM does to both at once.
-__device__ __forceinline__ uint64_t pair_of(float a, float b) {
-  uint64_t y;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(a), "f"(b));
-  return y;
-}
-__device__ __forceinline__ float2 halves_of(uint64_t x) {
-  float2 y;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(y.x), "=f"(y.y) : "l"(x));
-  return y;
-}
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t y;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(y) : "l"(a), "l"(b));
-  return y;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
-  uint64_t y;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(y) : "l"(a), "l"(b), "l"(c));
-  return y;
-}
-
 // Whether the rounding of r = m c may be more than a fraction of a power of two.
 __device__ __forceinline__ bool is_far(float m, float c) { return m != -INFINITY && !(fabsf(m * c) < 16777216.f); }
 // The reference that goes with a maximum of some of a row's logits: none for one so low that its logits weigh nothing
