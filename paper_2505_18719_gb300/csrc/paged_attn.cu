@@ -380,7 +380,9 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
   const float to_log2 = a.scale * 1.44269504f;
   const int tile_heads = min(group, kHeads), buffers = tile_heads <= 2 ? 4 : tile_heads <= 4 ? 2 : 1;
   uint32_t q[HD / 16][PAIR ? 4 : 2];
-  float o[HD / 8][4], m = -INFINITY, l = 0.f;
+  // outputs: c0, c1 of the query head, c2, c3 of the weights' low parts; PAIR: both, added after each step
+  constexpr int kOut = PAIR ? 2 : 4;
+  float o[HD / 8][kOut], m = -INFINITY, l = 0.f;
   Segment seg{};
   int head0 = 0, heads = 0, turn = -1, left = 0, stage = 0;
   float *crew_o = nullptr, *my_o = nullptr;
@@ -440,7 +442,9 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
         }
       }
 #pragma unroll
-      for (int i = 0; i < HD / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+      for (int i = 0; i < HD / 8; ++i)
+#pragma unroll
+        for (int e = 0; e < kOut; ++e) o[i][e] = 0.f;
       m = -INFINITY;
       l = 0.f;
     }
@@ -453,7 +457,10 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
     stage = stage + 1 == kStages ? 0 : stage + 1;
     if (mask) {
       constexpr int kTiles = kStep / 8;  // of 8 positions
-      float s[kTiles][4] = {};
+      // The tensor cores truncate what they add to an accumulator; fp32 outputs keep more of their bits with two
+      // chains for the scores and a fresh accumulator a step for the outputs, added in fp32.
+      constexpr int kChains = PAIR ? 2 : 1;
+      float s[kChains][kTiles][4] = {};
       {
         // piece 2k + b of row r lies at (2k + b) ^ (r & 7): the k-th step flips bits of one address
         const int r = (lane & 7) + ((lane >> 4) << 3);
@@ -465,11 +472,11 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
             uint32_t b[4];
             ldsm(b, (at ^ (k << 5)) + i * 8 * R::kRow);
             if constexpr (PAIR) {
-              mma<BF16>(s[i], q[k][0], q[k][1], q[k][2], q[k][3], b[0], b[1]);
-              mma<BF16>(s[i + 1], q[k][0], q[k][1], q[k][2], q[k][3], b[2], b[3]);
+              mma<BF16>(s[k & 1][i], q[k][0], q[k][1], q[k][2], q[k][3], b[0], b[1]);
+              mma<BF16>(s[k & 1][i + 1], q[k][0], q[k][1], q[k][2], q[k][3], b[2], b[3]);
             } else {
-              mma<BF16>(s[i], q[k][0], 0u, q[k][1], 0u, b[0], b[1]);
-              mma<BF16>(s[i + 1], q[k][0], 0u, q[k][1], 0u, b[2], b[3]);
+              mma<BF16>(s[0][i], q[k][0], 0u, q[k][1], 0u, b[0], b[1]);
+              mma<BF16>(s[0][i + 1], q[k][0], 0u, q[k][1], 0u, b[2], b[3]);
             }
           }
         }
@@ -478,7 +485,8 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
       const uint32_t mine = mask >> (2 * t);
 #pragma unroll
       for (int i = 0; i < 2 * kTiles; ++i) {
-        const float x = PAIR ? s[i >> 1][i & 1] + s[i >> 1][2 + (i & 1)] : s[i >> 1][i & 1];
+        float x = s[0][i >> 1][i & 1];
+        if constexpr (PAIR) x = (x + s[1][i >> 1][i & 1]) + (s[0][i >> 1][2 + (i & 1)] + s[1][i >> 1][2 + (i & 1)]);
         p[i] = (mine >> ((i >> 1) * 8 + (i & 1))) & 1u ? x * to_log2 : -INFINITY;
         top = fmaxf(top, p[i]);
       }
@@ -488,12 +496,9 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
         const float keep = join_weight(m, top);
         l *= keep;
 #pragma unroll
-        for (int i = 0; i < HD / 8; ++i) {
-          o[i][0] *= keep;
-          o[i][1] *= keep;
-          o[i][2] *= keep;
-          o[i][3] *= keep;
-        }
+        for (int i = 0; i < HD / 8; ++i)
+#pragma unroll
+          for (int e = 0; e < kOut; ++e) o[i][e] *= keep;
         m = top;
       }
       const float base = (m == -INFINITY ? 0.f : m) - kShift;
@@ -505,17 +510,27 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
       {
         const int r = (lane & 7) + (((lane >> 3) & 1) << 3);
         const uint32_t at = (values + r * R::kRow) | (((lane >> 4) ^ (r & 7)) << 4);
+        uint32_t w[2 * kTiles];  // the weights as operands: high and low words
 #pragma unroll
-        for (int i = 0; i < kTiles; i += 2) {
-          uint32_t p0, p1, p2, p3;
-          split2<BF16>(p[2 * i], p[2 * i + 1], p0, p1);
-          split2<BF16>(p[2 * i + 2], p[2 * i + 3], p2, p3);
+        for (int i = 0; i < kTiles; ++i) split2<BF16>(p[2 * i], p[2 * i + 1], w[2 * i], w[2 * i + 1]);
 #pragma unroll
-          for (int j = 0; j < HD / 16; ++j) {
+        for (int j = 0; j < HD / 16; ++j) {
+          float c[2][4] = {};
+#pragma unroll
+          for (int i = 0; i < kTiles; i += 2) {
             uint32_t b[4];
             ldsm_t(b, (at ^ (j << 5)) + i * 8 * R::kRow);
-            mma<BF16>(o[2 * j], p0, p1, p2, p3, b[0], b[1]);
-            mma<BF16>(o[2 * j + 1], p0, p1, p2, p3, b[2], b[3]);
+            if constexpr (PAIR) {
+              mma<BF16>(c[0], w[2 * i], w[2 * i + 1], w[2 * i + 2], w[2 * i + 3], b[0], b[1]);
+              mma<BF16>(c[1], w[2 * i], w[2 * i + 1], w[2 * i + 2], w[2 * i + 3], b[2], b[3]);
+            } else {
+              mma<BF16>(o[2 * j], w[2 * i], w[2 * i + 1], w[2 * i + 2], w[2 * i + 3], b[0], b[1]);
+              mma<BF16>(o[2 * j + 1], w[2 * i], w[2 * i + 1], w[2 * i + 2], w[2 * i + 3], b[2], b[3]);
+            }
+          }
+          if constexpr (PAIR) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[2 * j + (e >> 1)][e & 1] += c[e >> 1][e & 1] + c[e >> 1][2 + (e & 1)];
           }
         }
       }
@@ -530,7 +545,7 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
       float* dst = my_o + g * HD + 2 * t;
 #pragma unroll
       for (int i = 0; i < HD / 8; ++i)
-        *reinterpret_cast<float2*>(dst + 8 * i) = make_float2(o[i][0] + o[i][2], o[i][1] + o[i][3]);
+        *reinterpret_cast<float2*>(dst + 8 * i) = PAIR ? make_float2(o[i][0], o[i][1]) : make_float2(o[i][0] + o[i][kOut - 2], o[i][1] + o[i][kOut - 1]);
     }
     int h0 = 0, h_step = 1;  // this warp joins heads h0, h0 + h_step, ..
     if (crew == 1) {
