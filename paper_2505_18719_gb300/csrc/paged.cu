@@ -18,8 +18,6 @@ namespace {
 // for itself (a block scan into shared memory), then the CTAs share the pages and the rows, four rows a thread,
 // which finds the first one's environment by bisection.  The cluster's barriers stand between reading
 // the state and writing it, and between pages given back and pages taken.
-constexpr int kPlanThreads = 512;
-
 __device__ __forceinline__ int64_t warp_inclusive(int64_t v) {
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -43,6 +41,7 @@ __device__ __forceinline__ int env_of(const int* start, int n, int i) {
 }
 
 // `page_shift` >= 0: pages of 1 << page_shift positions.
+template <int kPlanThreads>
 __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PagePlanArgs a, const int parts, const int page_shift) {
   extern __shared__ int plan_sm[];
   int* row_first = plan_sm;                   // [n_env + 1]
@@ -415,22 +414,31 @@ __global__ void __launch_bounds__(kAppendThreads, LAYOUT == kHalves && NORM ? 6 
 
 }  // namespace
 
-int page_plan_launch(const PagePlanArgs& a, cudaStream_t s) {
+namespace {
+template <int THREADS>
+int plan_of(const PagePlanArgs& a, cudaStream_t s) {
   static std::atomic<uint64_t> smem_done{0}, cluster_done{0};
   static std::atomic<int> cluster_size[64] = {};
   constexpr int kMost = (4 * kMaxPlanEnvs + 1) * static_cast<int>(sizeof(int));
-  VLA_CUDA_TRY(set_smem_limit(page_plan_kernel, kMost, smem_done));
-  VLA_CUDA_TRY(allow_wide_clusters(page_plan_kernel, cluster_done));
+  VLA_CUDA_TRY(set_smem_limit(page_plan_kernel<THREADS>, kMost, smem_done));
+  VLA_CUDA_TRY(allow_wide_clusters(page_plan_kernel<THREADS>, cluster_done));
   // a thread has four rows and takes them twice before another CTA joins
   int parts = 1, most = 1;
-  while (parts < 16 && a.max_rows > parts * kPlanThreads * 8) parts *= 2;
-  VLA_CUDA_TRY(max_cluster_size(page_plan_kernel, dim3(kPlanThreads), kMost, 16, cluster_size, &most));
+  while (parts < 16 && a.max_rows > parts * THREADS * 8) parts *= 2;
+  VLA_CUDA_TRY(max_cluster_size(page_plan_kernel<THREADS>, dim3(THREADS), kMost, 16, cluster_size, &most));
   parts = std::min(parts, most);
   const int ps = a.page_size, shift = (ps & (ps - 1)) ? -1 : __builtin_ctz(ps);
-  VLA_CUDA_TRY(launch_pdl_cluster(page_plan_kernel, dim3(parts), dim3(kPlanThreads), (4 * a.n_env + 1) * sizeof(int), s, parts, a, parts, shift));
+  VLA_CUDA_TRY(launch_pdl_cluster(page_plan_kernel<THREADS>, dim3(parts), dim3(THREADS), (4 * a.n_env + 1) * sizeof(int), s, parts, a, parts, shift));
   note_launch();
   VLA_CUDA_TRY(cudaGetLastError());
   return VLA_OK;
+}
+}  // namespace
+
+int page_plan_launch(const PagePlanArgs& a, cudaStream_t s) {
+  // the sums' barriers are shorter with fewer warps: 16 environments of a row each take 3.8 us with 256 threads and 4.5 with 512,
+  // 186 of 106 rows 6.2 and 6.9, 256 of 296 rows 11.1 and 8.7, 438 of 5 rows 7.1 and 6.8
+  return a.n_env <= 256 && a.max_rows <= 32768 ? plan_of<256>(a, s) : plan_of<512>(a, s);
 }
 
 int rope_table_launch(const RopeTableArgs& a, cudaStream_t s) {

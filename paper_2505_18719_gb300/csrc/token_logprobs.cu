@@ -516,10 +516,16 @@ int logprobs_of(const LogprobArgs& a, cudaStream_t s, int sms) {
       threads = t;
     }
   }
-  // few long rows are cut over a cluster
+  // Few long rows are cut over a cluster, whose barriers cost 2 to 3 us: into slices of 8 KB while two of its CTAs an SM are not
+  // reached, of 36 KB up to four (with 8 alternatives 130 x 60000 f32 takes 11.8, 14.9, 17.0 us on 4, 2, 1 CTAs a row, 64 x 151000
+  // bf16 12.4, 14.2, 15.2 on 8, 4, 2, 200 x 32064 bf16 10.3, 8.2 on 2, 1).
   int parts = 1;
-  if (threads == 256)
-    while (parts < 8 && static_cast<int64_t>(a.rows) * parts < 2 * sms && a.vocab / (parts * 2) >= 2048) parts *= 2;
+  const int64_t bytes = static_cast<int64_t>(a.vocab) * Vec<DT>::kBytes;
+  while (threads == 256 && parts < 8) {
+    const int64_t ctas = static_cast<int64_t>(a.rows) * parts * 2, slice = bytes / (parts * 2);
+    if (!(ctas <= 2 * sms && slice >= 8192) && !(ctas <= 4 * sms && slice >= 36864)) break;
+    parts *= 2;
+  }
   if (static_cast<int64_t>(a.rows) * parts > 0x7fffffff) return record_error(VLA_ERR_UNSUPPORTED, "vla_token_logprobs: too many rows");
   auto kern = threads == 32 ? token_logprobs_kernel<DT, 32> : threads == 64 ? token_logprobs_kernel<DT, 64> : threads == 128 ? token_logprobs_kernel<DT, 128> : token_logprobs_kernel<DT, 256>;
   VLA_CUDA_TRY(launch_pdl_cluster(kern, dim3(a.rows * parts), dim3(threads), 0, s, parts, a, parts));
