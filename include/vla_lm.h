@@ -110,9 +110,9 @@ int vla_rope_append(const void* q, int64_t ldq, const void* k, int64_t ldk, cons
  *              every call leaves it fit for the next, of any size.  Not shared by calls that may overlap.
  * f32 queries beyond the fp16 range are read as +-65504 and raise VLA_STATUS_SATURATED.
  * A row of position -1 gives zeros (lse -infinity).  Positions past row_pos[r] may hold anything (NaN
- * included): they are not read.  Products and softmax weights keep at least 16 significant bits (22 over an
+ * included): they are not read; a NaN or infinity at one that is read may give NaN.  Products and softmax weights keep at least 16 significant bits (22 over an
  * fp16 cache), sums are 32-bit; the split of long contexts and the order of its sums depend on the lengths
- * alone, so equal calls give equal bits.  rows 0 or more. */
+ * alone, so equal calls give equal bits.  rows 0 or more, rows * n_q_heads at most 2^30. */
 int vla_paged_attn(const void* q, int64_t ldq, int dtype, int rows, int n_q_heads, const vla_paged_kv* kv, const int32_t* table,
                    int max_pages, int n_env, const int32_t* row_env, const int32_t* row_pos, float scale, void* out, int64_t ldo,
                    float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);
@@ -126,7 +126,8 @@ size_t vla_paged_attn_workspace_bytes(int head_dim);
  *   logprob, entropy, lse  f32 [rows]: the token's log-prob, -sum p log p, and log sum exp(z / T); any of
  *                 them may be NULL;
  *   top_ids, top_logprobs  int32 / f32 [rows][top_k]: the top_k largest logits, largest first, the lower id
- *                 first among equals (0 <= top_k <= 32, at most vocab; both may be NULL when it is 0).
+ *                 first among equals (0 <= top_k <= 32, at most vocab; both may be NULL when it is 0); vocab at most
+ *                 2^30.
  * Logits of -infinity (masked ids) have probability 0; a row of nothing else has lse -infinity, entropy 0
  * and log-probs of -infinity.  A NaN or +infinity makes the row's numbers NaN and raises
  * VLA_STATUS_NONFINITE.  rows 0 or more. */

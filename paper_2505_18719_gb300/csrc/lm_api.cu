@@ -8,6 +8,7 @@ namespace vla {
 namespace {
 
 constexpr int kMostHeads = 65535;  // channels of a row fit 32 bits
+constexpr int kMostIds = 1 << 30;  // a round past the last id fits 32 bits
 
 bool misaligned(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p) & (bytes - 1); }
 bool is_dtype(int d) { return d == VLA_F32 || d == VLA_F16 || d == VLA_BF16; }
@@ -110,6 +111,7 @@ int vla_paged_attn(const void* q, int64_t ldq, int dtype, int rows, int n_q_head
   if (rows < 0 || n_q_heads < 1 || n_q_heads % kv->n_heads)
     return record_error(VLA_ERR_ARG, "vla_paged_attn: rows < 0, or query heads no multiple of the cache's");
   if (rows == 0) return VLA_OK;
+  if (static_cast<int64_t>(rows) * n_q_heads > (1 << 30)) return record_error(VLA_ERR_UNSUPPORTED, "vla_paged_attn: more than 2^30 rows x query heads");
   const int64_t width = static_cast<int64_t>(n_q_heads) * kv->head_dim;
   if (bad_rows(q, ldq, width) || bad_rows(out, ldo, width))
     return record_error(VLA_ERR_ARG, "vla_paged_attn: q and out: 16-byte aligned, row strides multiples of 8 that hold a row");
@@ -129,6 +131,7 @@ int vla_token_logprobs(const void* logits, int64_t ld, int dtype, int rows, int 
   if (!is_dtype(dtype)) return record_error(VLA_ERR_UNSUPPORTED, "vla_token_logprobs: unknown dtype");
   if (rows < 0 || vocab < 1 || !(temperature >= 0.f) || !isfinite(temperature) || top_k < 0 || top_k > vocab)
     return record_error(VLA_ERR_ARG, "vla_token_logprobs: bad argument");
+  if (vocab > kMostIds) return record_error(VLA_ERR_UNSUPPORTED, "vla_token_logprobs: more than 2^30 ids");
   if (top_k > kMaxTopK) return record_error(VLA_ERR_UNSUPPORTED, "vla_token_logprobs: more than 32 alternatives");
   if (rows == 0) return VLA_OK;
   if (!logits || ld < vocab || misaligned(logits, elem_bytes(dtype)) || (top_k > 0 && (!top_ids || !top_logprobs)))
@@ -146,6 +149,7 @@ int vla_token_logprobs_grad(const void* logits, int64_t ld, int dtype, int rows,
   if (!is_dtype(dtype)) return record_error(VLA_ERR_UNSUPPORTED, "vla_token_logprobs_grad: unknown dtype");
   if (rows < 0 || vocab < 1 || !(temperature >= 0.f) || !isfinite(temperature))
     return record_error(VLA_ERR_ARG, "vla_token_logprobs_grad: bad argument");
+  if (vocab > kMostIds) return record_error(VLA_ERR_UNSUPPORTED, "vla_token_logprobs_grad: more than 2^30 ids");
   if (rows == 0) return VLA_OK;
   if (!logits || ld < vocab || !d_logits || ldd < vocab || misaligned(logits, elem_bytes(dtype)) ||
       misaligned(d_logits, elem_bytes(dtype)) || (d_logits == logits && ldd != ld))

@@ -127,7 +127,8 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PagePlanA
     a.table[static_cast<int64_t>(e) * a.max_pages + col] = __ldcg(a.pool + top - 1 - i);
   }
   const bool wide = !((reinterpret_cast<uintptr_t>(a.row_env) | reinterpret_cast<uintptr_t>(a.row_pos) | reinterpret_cast<uintptr_t>(a.row_slot)) & 15u);
-  for (int r0 = me * 4; r0 < a.max_rows; r0 += all * 4) {
+  for (unsigned next = me * 4u; next < static_cast<unsigned>(a.max_rows); next += all * 4u) {
+    const int r0 = static_cast<int>(next);
     int env[4], pos[4], slot[4];
     int e = r0 < rows ? env_of(row_first, a.n_env, r0) : 0;
 #pragma unroll
@@ -152,14 +153,14 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PagePlanA
         raise_status(a.status, VLA_STATUS_PAGES);
       }
     }
-    if (wide && r0 + 4 <= a.max_rows) {
+    if (wide && r0 <= a.max_rows - 4) {
       *reinterpret_cast<int4*>(a.row_env + r0) = make_int4(env[0], env[1], env[2], env[3]);
       *reinterpret_cast<int4*>(a.row_pos + r0) = make_int4(pos[0], pos[1], pos[2], pos[3]);
       *reinterpret_cast<int4*>(a.row_slot + r0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
     } else {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        if (r0 + i >= a.max_rows) break;
+        if (i >= a.max_rows - r0) break;
         a.row_env[r0 + i] = env[i];
         a.row_pos[r0 + i] = pos[i];
         a.row_slot[r0 + i] = slot[i];

@@ -44,6 +44,7 @@ constexpr int kJoin = 32;        // partial results that one warp joins at a tim
 constexpr int kMinBlocks = 4;    // a share of cut items is no smaller while items are longer
 constexpr int kCutBlocks = 8;    // blocks that the join of a cut item costs
 constexpr int kItem = 1;         // what an item costs beside its blocks, in blocks: its queries and its join
+constexpr int kLastPosition = 0x7fffff00;  // a whole block past it still fits 32 bits
 constexpr int kAlone = 16;       // steps of the longest item that single warps take
 
 // Workspace: tickets of the first level [kSlots][8], of the second as many, then the partial results: per slot
@@ -193,7 +194,7 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
     const int pos = a.row_pos[row];
     env = a.row_env[row];
     const int col = page_shift >= 0 ? pos >> page_shift : pos / a.kv.page_size;
-    const bool ok = pos >= 0 && col < a.max_pages && static_cast<unsigned>(env) < static_cast<unsigned>(a.n_env);
+    const bool ok = pos >= 0 && pos <= kLastPosition && col < a.max_pages && static_cast<unsigned>(env) < static_cast<unsigned>(a.n_env);
     if (!ok && pos != -1) raise_status(a.status, VLA_STATUS_PAGES);
     return ok ? pos + 1 : 0;
   };
@@ -666,7 +667,6 @@ int paged_attn_launch(const PagedAttnArgs& a, cudaStream_t s) {
   const int group = a.n_q_heads / a.kv.n_heads, tiles = (group + kHeads - 1) / kHeads;
   const int ps = a.kv.page_size, shift = (ps & (ps - 1)) ? -1 : __builtin_ctz(ps);
   const bool pair = a.dtype == VLA_F32, bf = a.kv.dtype == VLA_BF16, aligned = ps % 8 == 0;
-  if (static_cast<int64_t>(a.rows) * a.kv.n_heads * tiles > 0x7fffffff) return record_error(VLA_ERR_UNSUPPORTED, "vla_paged_attn: too many rows");
   auto go = [&](auto ring, auto kern, std::atomic<uint64_t>& done) -> int {
     using R = decltype(ring);
     // no more CTAs than have a step to take at the longest rows that the table holds

@@ -495,6 +495,18 @@ def test_paged_attn_status():
     assert bool(torch.isfinite(out[4].float()).all())
 
 
+def test_paged_attn_positions_at_the_end_of_32_bits():
+    ps = 1 << 20
+    k, v = (torch.zeros(1, 1, ps, 64, dtype=torch.float16, device="cuda") for _ in range(2))
+    q = torch.ones(3, 1, 64, dtype=torch.float16, device="cuda")
+    table = torch.zeros(1, 2048, dtype=torch.int32, device="cuda")
+    env, pos = torch.zeros(3, dtype=torch.int32, device="cuda"), torch.tensor([2**31 - 1, 5, -1], dtype=torch.int32, device="cuda")
+    v[0, 0, :6] = 1.0
+    out, lse = attend_call(q, k, v, table, env, pos, "f16", "f16", 0.1, workspace(64))
+    assert status() == V.VLA_STATUS_PAGES
+    assert bool((out[::2] == 0).all()) and bool((lse[::2] == -math.inf).all()) and bool((out[1] == 1).all())
+
+
 def test_paged_attn_offsets_beyond_32_bits():
     # one buffer of 2^31 + elements; its last pages lie past the 32-bit element offsets
     hd, ps, n_pages = 64, 16, 1040

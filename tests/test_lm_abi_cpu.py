@@ -167,3 +167,10 @@ def test_token_logprobs_grad_refusals(change):
 def test_token_logprobs_grad_unsupported_and_no_rows():
     refused(grad(dtype=-1), V.VLA_ERR_UNSUPPORTED, "vla_token_logprobs_grad")
     assert grad(rows=0) == V.VLA_OK
+
+
+def test_counts_whose_arithmetic_would_pass_32_bits():
+    many = (1 << 30) + 1
+    refused(attend(cache(n_heads=1), n_q_heads=1, ldq=128, ldo=128, rows=many), V.VLA_ERR_UNSUPPORTED, "2^30")
+    refused(logprobs(vocab=many, ld=many), V.VLA_ERR_UNSUPPORTED, "2^30")
+    refused(grad(vocab=many, ld=many, ldd=many), V.VLA_ERR_UNSUPPORTED, "2^30")
