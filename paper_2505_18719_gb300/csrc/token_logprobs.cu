@@ -143,12 +143,13 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
   __shared__ int64_t above[kList];
   __shared__ int level_ids[kList];
   __shared__ int n_above, n_level, bound;
-  __shared__ int64_t best[kMaxTopK];               // this slice's best keys, in order
-  __shared__ int64_t all_best[THREADS == 256 ? kMostParts * kMaxTopK : 1];
-  __shared__ float3 all_slices[kMostParts], slice;  // (m, s, w) of the slices
+  __shared__ __align__(16) int64_t all_best[THREADS == 256 ? kMostParts * kMaxTopK : 2];  // the slices' best keys, each in order
+  __shared__ float all_slices[kMostParts][3];      // (m, s, w) of the slices
   __shared__ int64_t round_key[kWarps];
   pdl_launch_dependents();
   pdl_wait();
+  const bool cut = THREADS == 256 && parts > 1;
+  if (cut) cluster_arrive();  // the first CTA has begun once all have passed the wait
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int row = blockIdx.x / parts, part = blockIdx.x % parts;
   const int first = static_cast<int>(static_cast<int64_t>(a.vocab) * part / parts);
@@ -171,10 +172,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
       token = -1;
     }
   }
-  if (tid == 0) {
-    n_above = n_level = 0;
-    bound = INT32_MIN;
-  }
+  if (tid == 0) n_above = n_level = 0;
 
   Sums x;
   float most = -INFINITY;  // this thread's maximum
@@ -248,16 +246,22 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
     red[1][warp] = x.s;
     red[2][warp] = x.w;
   }
-  if (k > 0 && tid < kGroups) {
-    // the largest maximum that k groups reach
-    const int v = group_max[tid];
-    int reach = 0;
-#pragma unroll
-    for (int j = 0; j < kGroups; j += 4) {
-      const int4 w = *reinterpret_cast<const int4*>(group_max + j);
-      reach += (w.x >= v) + (w.y >= v) + (w.z >= v) + (w.w >= v);
+  if (k > 0 && warp == kWarps - 1) {
+    // the largest maximum that k groups reach: the largest ones go in turn, two a lane
+    int hi = group_max[lane], lo = INT32_MIN, reach = 0, v;
+    if (kGroups == 64) {
+      const int other = group_max[lane + 32];
+      lo = min(hi, other);
+      hi = max(hi, other);
     }
-    if (reach >= k) atomicMax(&bound, v);
+    do {
+      v = __reduce_max_sync(0xffffffffu, hi);
+      const bool goes = hi == v;
+      reach += __popc(__ballot_sync(0xffffffffu, goes));
+      hi = goes ? lo : hi;
+      lo = goes ? INT32_MIN : lo;
+    } while (reach < k);
+    if (lane == 0) bound = v;
   }
   __syncthreads();
   Sums total;  // relative to the maximum `top`
@@ -268,7 +272,34 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
     total.w += red[2][i];
   }
 
+  // The row's numbers, of all slices once they have met; the difference to the maximum in natural units (a log-prob may be
+  // as low as a type's lowest value), and what the rounded reference is off the maximum.
+  float log2_s, r, rest;
+  bool bad, none, apart;
+  auto settle = [&]() {
+    bad = !(top < INFINITY);
+    none = top == -INFINITY;
+    apart = !bad && is_far(top, c);
+    log2_s = log2f(total.s);
+    r = top * c;
+    rest = (apart ? 0.f : fmaf(top, c, -r)) - log2_s;
+  };
+  auto logprob = [&](float z) { return bad ? NAN : none ? -INFINITY : fmaf(rest, kLn2, (z - top) * inv_t); };
+  auto put = [&](int rank, int64_t key) {
+    const int64_t at = static_cast<int64_t>(row) * a.top_k + rank;
+    a.top_ids[at] = key_id(key);
+    a.top_logprobs[at] = logprob(key_value(key));
+  };
+  settle();
+  if (cut) cluster_wait();
+
   // ---- the slice's best keys
+  auto place = [&](int rank, int64_t key) {
+    if (cut)
+      asm volatile("st.shared::cluster.s64 [%0], %1;" ::"r"(mapa_shared(smem_u32(&all_best[part * a.top_k + rank]), 0)), "l"(key) : "memory");
+    else
+      put(rank, key);
+  };
   if (k > 0) {
     const int at_least = bound;
     const float limit = float_of(at_least);
@@ -286,9 +317,14 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
           level_ids[at] = first + j;
       };
       if (lowest ? mine > at_least : mine >= at_least) {
+        uint32_t rounds = 0;
+#pragma unroll 4
+        for (int i = 0; i < min(kRounds, (vecs - tid + THREADS * kUnroll - 1) / (THREADS * kUnroll)); ++i) {
+          const float there = round_max[i][tid];
+          rounds |= (lowest ? there > limit : there >= limit) ? 1u << i : 0u;
+        }
         for (int i = tid, round = 0; i < vecs; i += THREADS * kUnroll, ++round) {
-          const float there = round_max[round % kRounds][tid];
-          if (lowest ? !(there > limit) : !(there >= limit)) continue;
+          if (!(rounds >> round % kRounds & 1u)) continue;
           uint4 v[kUnroll];
 #pragma unroll
           for (int u = 0; u < kUnroll; ++u) v[u] = body[min(i + u * THREADS, vecs - 1)];
@@ -329,13 +365,13 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
           for (int j = 0; j < n_above; ++j) rank += above[j] > key;
           if (i >= n_above)  // equals follow in the order of their ids
             for (int j = 0; j < more; ++j) rank += level_ids[j] < level_ids[i - n_above];
-          if (rank < k) best[rank] = key;
+          if (rank < k) place(rank, key);
         }
       }
     }
     if (!fits) {  // more equal logits than the list holds: the largest key below the one before, k times over
       int64_t last = INT64_MAX;
-      for (int r = 0; r < k; ++r) {
+      for (int i = 0; i < k; ++i) {
         int64_t key = INT64_MIN;
         for (int j = tid; j < n; j += THREADS) {
           const int64_t q = make_key(ordered(V::load(base, j)), first + j);
@@ -346,69 +382,50 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
         __syncthreads();
         if (lane == 0) round_key[warp] = key;
         __syncthreads();
-        for (int i = 0; i < kWarps; ++i) key = max(key, round_key[i]);
+        for (int w = 0; w < kWarps; ++w) key = max(key, round_key[w]);
         last = key;
-        if (tid == 0) best[r] = key;
+        if (tid == 0) place(i, key);
       }
     }
-    for (int i = k + tid; i < a.top_k; i += THREADS) best[i] = INT64_MIN;
-    __syncthreads();
   }
 
   // ---- the slices' results meet in the first CTA
-  if (THREADS == 256 && parts > 1) {
-    if (tid == 0) slice = make_float3(top, total.s, total.w);
-    cluster_sync();
-    if (part == 0) {
-      for (int i = tid; i < parts * a.top_k; i += THREADS) {
-        const uint32_t at = mapa_shared(smem_u32(&best[i % a.top_k]), i / a.top_k);
-        asm volatile("ld.shared::cluster.s64 %0, [%1];" : "=l"(all_best[i]) : "r"(at) : "memory");
-      }
-      if (tid < parts) {
-        const uint32_t at = mapa_shared(smem_u32(&slice), tid);
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(all_slices[tid].x) : "r"(at) : "memory");
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(all_slices[tid].y) : "r"(at + 4) : "memory");
-        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(all_slices[tid].z) : "r"(at + 8) : "memory");
-      }
+  if (cut) {
+    if (tid < 3) {
+      const float mine = tid == 0 ? top : tid == 1 ? total.s : total.w;
+      asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(mapa_shared(smem_u32(&all_slices[part][tid]), 0)), "f"(mine) : "memory");
     }
-    cluster_sync();  // the other CTAs' results stay until the first has them
+    cluster_sync();
     if (part != 0) return;
     top = -INFINITY;
-    for (int i = 0; i < parts; ++i) top = max_nan(top, all_slices[i].x);
+    for (int i = 0; i < parts; ++i) top = max_nan(top, all_slices[i][0]);
     total.s = total.w = 0.f;
     for (int i = 0; i < parts; ++i) {
-      const float m = all_slices[i].x, wide = is_far(m, c) || is_far(top, c) ? (m - top) * c : m * c - top * c;
+      const float m = all_slices[i][0], wide = is_far(m, c) || is_far(top, c) ? (m - top) * c : m * c - top * c;
       if (m == -INFINITY) continue;
       const float d = fmaxf(wide, kFloor), f = exp2_fast(d);
-      total.s = fmaf(f, all_slices[i].y, total.s);
-      total.w = fmaf(f, fmaf(d, all_slices[i].y, all_slices[i].z), total.w);
+      total.s = fmaf(f, all_slices[i][1], total.s);
+      total.w = fmaf(f, fmaf(d, all_slices[i][1], all_slices[i][2]), total.w);
     }
-    // disjoint sorted lists: a key's place is the number of larger ones
-    for (int i = tid; i < parts * a.top_k; i += THREADS) {
-      const int64_t key = all_best[i];
+    settle();
+    // disjoint sets of keys: a key's place is the number of larger ones
+    if (tid < parts * a.top_k) {
+      const int64_t key = all_best[tid];
       int rank = 0;
-      for (int j = 0; j < parts * a.top_k; ++j) rank += all_best[j] > key;
-      if (key != INT64_MIN && rank < a.top_k) best[rank] = key;
+#pragma unroll 4
+      for (int j = 0; j < parts * a.top_k; j += 2) {
+        const longlong2 two = *reinterpret_cast<const longlong2*>(all_best + j);
+        rank += (two.x > key) + (two.y > key);
+      }
+      if (rank < a.top_k) put(rank, key);
     }
-    __syncthreads();
   }
 
-  if (tid >= max(1, a.top_k)) return;
-  const bool bad = !(top < INFINITY), none = top == -INFINITY, apart = !bad && is_far(top, c);
-  // the difference to the maximum in natural units (a log-prob may be as low as a type's lowest value), and what the
-  // rounded reference is off the maximum
-  const float log2_s = log2f(total.s), r = top * c, rest = (apart ? 0.f : fmaf(top, c, -r)) - log2_s;
-  auto logprob = [&](float z) { return bad ? NAN : none ? -INFINITY : fmaf(rest, kLn2, (z - top) * inv_t); };
   if (tid == 0) {
     if (bad) raise_status(a.status, VLA_STATUS_NONFINITE);
     if (a.lse) a.lse[row] = bad ? NAN : none ? -INFINITY : apart ? fmaf(top, inv_t, log2_s * kLn2) : (r + log2_s) * kLn2;
     if (a.entropy) a.entropy[row] = bad ? NAN : none ? 0.f : (log2_s - total.w / total.s) * kLn2;
     if (a.logprob) a.logprob[row] = token < 0 ? 0.f : logprob(chosen);
-  }
-  if (tid < a.top_k) {
-    const int64_t key = best[tid], at = static_cast<int64_t>(row) * a.top_k + tid;
-    a.top_ids[at] = key_id(key);
-    a.top_logprobs[at] = logprob(key_value(key));
   }
 }
 
