@@ -45,7 +45,10 @@ constexpr int kMinBlocks = 4;    // a share of cut items is no smaller while ite
 constexpr int kCutBlocks = 8;    // blocks that the join of a cut item costs
 constexpr int kItem = 1;         // what an item costs beside its blocks, in blocks: its queries and its join
 constexpr int kLastPosition = 0x7fffff00;  // a whole block past it still fits 32 bits
-constexpr int kAlone = 16;       // steps of the longest item that single warps take
+// Single warps take items of up to kAlone steps where that is less than all warps of a CTA take, an item counted as its steps
+// and kEnds more (bf16 heads of 128, device time of single warps and of whole CTAs: 1152 items of 2 / 60 / 250 positions 5.0, 10.2,
+// 27.0 us and 9.7, 12.6, 27.8; 360 items 4.7, 7.8, 18.5 and 6.5, 7.0, 15.0; 1536 items of 250 38 and 36, 3000 items 63 and 62)
+constexpr int kAlone = 16, kEnds = 2;
 
 // Workspace: tickets of the first level [kSlots][8], of the second as many, then the partial results: per slot
 // o [8][hd], (m, l) [8].  Two slots a CTA: the item that it found begun, and the one that it leaves.
@@ -238,12 +241,12 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
     // at least the mean, without a 64-bit division
     share = static_cast<int64_t>(static_cast<float>(total - 1) * 1.000001f / static_cast<float>(ctas)) + 1;
     to_load = INT64_MAX;
-    if (all_items >= kWarps * ctas && most <= kAlone) {
-      const int per = (all_items - 1) / (ctas * kWarps) + 1;
+    const int per = (all_items - 1) / ctas + 1, per_warp = (per + kWarps - 1) / kWarps, longest_item = (most + kWarps - 1) / kWarps;
+    if (most <= kAlone && static_cast<int64_t>(per_warp) * (most + kEnds) < static_cast<int64_t>(per) * (longest_item + kEnds)) {
       crew = 1;
-      item = min(all_items, (me * kWarps + warp) * per);
-      end_item = min(all_items, item + per);
-    } else if (const int per = (all_items - 1) / ctas + 1; static_cast<int64_t>(per) * ((most + kWarps - 1) / kWarps + kItem) <= share + kCutBlocks || share > (1 << 30)) {
+      item = min(all_items, (me * kWarps + warp) * per_warp);
+      end_item = min(all_items, item + per_warp);
+    } else if (static_cast<int64_t>(per) * (longest_item + kItem) <= share + kCutBlocks || share > (1 << 30)) {
       item = min(all_items, me * per);
       end_item = min(all_items, item + per);
     } else {
