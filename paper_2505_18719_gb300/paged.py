@@ -9,6 +9,7 @@ from __future__ import annotations
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import vla as V
 
@@ -28,11 +29,24 @@ def _ok(rc: int) -> None:
         raise V.VlaError(rc, V.vla_last_error())
 
 
+def _on_gpu(*tensors: Optional[torch.Tensor]) -> None:
+    for t in tensors:
+        if t is not None and t.device.index != torch.cuda.current_device():
+            raise ValueError(f"a tensor of the current GPU expected, got one on {t.device}")
+
+
+def _code(t: torch.Tensor) -> int:
+    if t.dtype not in _CODE:
+        raise ValueError(f"float32, float16 or bfloat16 expected, got {t.dtype}")
+    return _CODE[t.dtype]
+
+
 def _rows_of(t: torch.Tensor, heads: int, hd: int) -> int:
-    """Row stride of [rows, heads, hd] or [rows, heads * hd] whose rows are dense."""
-    if t.shape[-1] != (hd if t.dim() == 3 else heads * hd) or t.stride(-1) != 1 or (t.dim() == 3 and (t.shape[1], t.stride(1)) != (heads, hd)):
+    """Row stride of [rows, heads, hd] or [rows, heads * hd] whose rows are dense (a lone row's or head's does not count)."""
+    if (t.dim() not in (2, 3) or t.shape[-1] != (hd if t.dim() == 3 else heads * hd) or t.stride(-1) != 1 or
+            (t.dim() == 3 and (t.shape[1] != heads or (heads > 1 and t.stride(1) != hd)))):
         raise ValueError(f"rows of {heads} heads of {hd} expected, got {tuple(t.shape)} with strides {t.stride()}")
-    return t.stride(0)
+    return t.stride(0) if t.shape[0] > 1 else heads * hd
 
 
 class Rows(NamedTuple):
@@ -74,6 +88,7 @@ class PagedCache:
         for t in (new_len, release):
             if t is not None and (t.dtype, t.shape, t.is_contiguous()) != (torch.int32, (self.n_env,), True):
                 raise ValueError("new_len and release: int32 [n_env], contiguous")
+        _on_gpu(self.data, new_len, release)
         e = lambda n: torch.empty(n, dtype=torch.int32, device=self.ctx.device)  # noqa: E731
         rows = Rows(e(max_rows), e(max_rows), e(max_rows), e(self.n_env + 1))
         _ok(V.vla_page_plan(self.ctx.data_ptr(), new_len.data_ptr(), _ptr(release), self.n_env, self.page_size, self.table.data_ptr(),
@@ -94,9 +109,12 @@ class PagedCache:
                 raise ValueError("gains: bf16 [head_dim]")
         if not q.shape[0] == k.shape[0] == v.shape[0] == rows.pos.shape[0]:
             raise ValueError("q, k, v and the plan have the same rows")
+        if rope is not None and (rope.dtype, rope.dim(), rope.shape[-1], rope.is_contiguous()) != (torch.float32, 3, 2, True):
+            raise ValueError("rope: float32 [positions, rope_dim / 2, 2]")
+        _on_gpu(self.data, q, k, v, rows.pos, rope, q_gain, k_gain)
         out = torch.empty(q.shape[0], heads, hd, dtype=q.dtype, device=q.device)
         _ok(V.vla_rope_append(q.data_ptr(), _rows_of(q, heads, hd), k.data_ptr(), _rows_of(k, self.n_heads, hd), v.data_ptr(),
-                              _rows_of(v, self.n_heads, hd), _CODE[q.dtype], q.shape[0], heads, self.layers[layer], _ptr(q_gain),
+                              _rows_of(v, self.n_heads, hd), _code(q), q.shape[0], heads, self.layers[layer], _ptr(q_gain),
                               _ptr(k_gain), eps, _ptr(rope), rope.shape[0] if rope is not None else 0,
                               2 * rope.shape[1] if rope is not None else 0, interleaved, rows.pos.data_ptr(), rows.slot.data_ptr(),
                               out.data_ptr(), heads * hd, _stream()))
@@ -108,9 +126,10 @@ class PagedCache:
         heads = q.shape[1] if q.dim() == 3 else q.shape[1] // hd
         if q.shape[0] != rows.pos.shape[0]:
             raise ValueError("q and the plan have the same rows")
+        _on_gpu(self.data, q, rows.pos)
         out = torch.empty(q.shape[0], heads, hd, dtype=q.dtype, device=q.device)
         lse = torch.empty(q.shape[0], heads, dtype=torch.float32, device=q.device) if want_lse else None
-        _ok(V.vla_paged_attn(q.data_ptr(), _rows_of(q, heads, hd), _CODE[q.dtype], q.shape[0], heads, self.layers[layer],
+        _ok(V.vla_paged_attn(q.data_ptr(), _rows_of(q, heads, hd), _code(q), q.shape[0], heads, self.layers[layer],
                              self.table.data_ptr(), self.max_pages, self.n_env, rows.env.data_ptr(), rows.pos.data_ptr(),
                              hd ** -0.5 if scale is None else scale, out.data_ptr(), heads * hd, _ptr(lse), self.workspace.data_ptr(),
                              self.workspace.numel(), _stream()))
@@ -131,6 +150,7 @@ class PagedCache:
 def rope_table(n_pos: int, rope_dim: int, theta: float = 1e4, device="cuda", **scaling) -> torch.Tensor:
     """(cos, sin) f32 [n_pos, rope_dim / 2, 2]; `scaling` as in ``vla_rope_table`` (kind, factor, original_len, low, high, amplitude)."""
     t = torch.empty(n_pos, rope_dim // 2, 2, dtype=torch.float32, device=device)
+    _on_gpu(t)
     _ok(V.vla_rope_table(t.data_ptr(), n_pos, rope_dim, theta, stream=_stream(), **scaling))
     return t
 
@@ -140,11 +160,12 @@ class _TokenLogprobs(torch.autograd.Function):
     def forward(ctx, logits, tokens, temperature, top_k):
         if logits.dim() != 2 or logits.stride(1) != 1 or (tokens.dtype, tokens.shape, tokens.is_contiguous()) != (torch.int32, logits.shape[:1], True):
             raise ValueError("logits [rows, vocab] with dense rows, tokens int32 [rows]")
+        _on_gpu(logits, tokens)
         n, vocab = logits.shape
         f = lambda *s: torch.empty(*s, dtype=torch.float32, device=logits.device)  # noqa: E731
         logprob, entropy, lse, top = f(n), f(n), f(n), f(n, top_k)
         ids = torch.empty(n, top_k, dtype=torch.int32, device=logits.device)
-        _ok(V.vla_token_logprobs(logits.data_ptr(), logits.stride(0), _CODE[logits.dtype], n, vocab, tokens.data_ptr(), temperature, top_k,
+        _ok(V.vla_token_logprobs(logits.data_ptr(), logits.stride(0) if n > 1 else vocab, _code(logits), n, vocab, tokens.data_ptr(), temperature, top_k,
                                  logprob.data_ptr(), entropy.data_ptr(), lse.data_ptr(), ids.data_ptr() if top_k else 0,
                                  top.data_ptr() if top_k else 0, _stream()))
         ctx.save_for_backward(logits, tokens, lse, entropy)
@@ -153,13 +174,15 @@ class _TokenLogprobs(torch.autograd.Function):
         return logprob, entropy, lse, ids, top
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, g_logprob, g_entropy, *_):
         logits, tokens, lse, entropy = ctx.saved_tensors
+        n, vocab = logits.shape
+        g_logprob, g_entropy = g_logprob.contiguous(), g_entropy.contiguous()
         d = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-        _ok(V.vla_token_logprobs_grad(logits.data_ptr(), logits.stride(0), _CODE[logits.dtype], logits.shape[0], logits.shape[1],
-                                      tokens.data_ptr(), ctx.temperature, lse.data_ptr(), entropy.data_ptr(),
-                                      g_logprob.contiguous().data_ptr(), g_entropy.contiguous().data_ptr(), d.data_ptr(), d.stride(0),
-                                      _stream()))
+        _ok(V.vla_token_logprobs_grad(logits.data_ptr(), logits.stride(0) if n > 1 else vocab, _code(logits), n, vocab, tokens.data_ptr(),
+                                      ctx.temperature, lse.data_ptr(), entropy.data_ptr(), g_logprob.data_ptr(), g_entropy.data_ptr(),
+                                      d.data_ptr(), vocab, _stream()))
         return d, None, None, None
 
 

@@ -193,3 +193,82 @@ def test_logprob_gradients_of_rows_without_tokens_and_unused_outputs():
     h = -(lp.exp() * lp).sum(-1, keepdim=True)
     assert float((z.grad[0] + (lp.exp() * (lp + h))[0]).abs().max()) < 64 * 2.0 ** -24
     assert bool((z.grad[1:] == 0).all())
+
+
+def test_logprob_and_entropy_gradients_together():
+    # both gradients arrive as broadcast scalars; a lone row's stride is arbitrary; no second derivatives
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randn(7, 90, generator=g, device="cuda")
+    tokens = torch.arange(7, dtype=torch.int32, device="cuda") * 11
+    for rows in (slice(None), slice(2, 3)):
+        z = x[rows].clone().as_strided(x[rows].shape, (90 if rows == slice(None) else 1, 1)).requires_grad_()
+        out = P.token_logprobs(z, tokens[rows])
+        (2.0 * out.logprob.sum() - 0.25 * out.entropy.sum()).backward()
+        z64 = x[rows].to(F64).requires_grad_()
+        lp = torch.log_softmax(z64, -1)
+        (2.0 * lp.gather(1, tokens[rows].long()[:, None]).sum() + 0.25 * (lp.exp() * lp).sum()).backward()
+        assert float((z.grad - z64.grad).abs().max()) < 64 * 2.0 ** -24 * 2
+    z = x.clone().requires_grad_()
+    first, = torch.autograd.grad(P.token_logprobs(z, tokens).logprob.sum(), z, create_graph=True)
+    with pytest.raises(RuntimeError):
+        first.square().sum().backward()
+
+
+def test_wrappers_refuse_tensors_elsewhere_and_other_types():
+    cache = P.PagedCache(2, 4, 16, 1, 2, 64, 64)
+    new_len = torch.ones(2, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError):
+        cache.plan(new_len.cpu(), 2)
+    rows = cache.plan(new_len, 2)
+    q, k, v = torch.zeros(2, 3, 2, 64, device="cuda").unbind(1)
+    for bad in (q.cpu(), q.double()):
+        with pytest.raises(ValueError):
+            cache.append(0, bad, k.to(bad.dtype), v.to(bad.dtype), rows)
+        with pytest.raises(ValueError):
+            cache.attend(0, bad, rows)
+    for rope in (torch.zeros(64, 32, 2), torch.zeros(64, 64, device="cuda"), torch.zeros(64, 32, 2, device="cuda", dtype=F64)):
+        with pytest.raises(ValueError):
+            cache.append(0, q, k, v, rows, rope)
+    with pytest.raises(ValueError):
+        P.rope_table(8, 64, device="cpu")
+    tokens = torch.zeros(2, dtype=torch.int32, device="cuda")
+    for z, t in ((torch.zeros(2, 8), tokens.cpu()), (torch.zeros(2, 8, device="cuda"), tokens.cpu()), (torch.zeros(2, 8, device="cuda", dtype=F64), tokens)):
+        with pytest.raises(ValueError):
+            P.token_logprobs(z, t)
+    # one row, one head: their strides do not count
+    one = P.PagedCache(1, 1, 16, 1, 1, 64, 16)
+    x = torch.randn(64, device="cuda")
+    lone = x.as_strided((1, 1, 64), (3, 5, 1))
+    rows = one.plan(torch.ones(1, dtype=torch.int32, device="cuda"), 1)
+    out = one.attend(0, one.append(0, lone, lone, lone, rows), rows)
+    assert float((out.view(64) - x).abs().max()) <= 2.0 ** -11 * float(x.abs().max()) + 2.0 ** -20
+    one.check()
+
+
+def test_a_launch_that_fails_is_reported_and_leaves_the_next_call_sound():
+    out_of_resources = 701
+    cache = P.PagedCache(2, 4, 16, 1, 2, 64, 64)
+    new_len = torch.ones(2, dtype=torch.int32, device="cuda")
+    q, k, v = torch.randn(2, 3, 2, 64, device="cuda").unbind(1)
+    z = torch.randn(2, 40, device="cuda", requires_grad=True)
+    tokens = torch.zeros(2, dtype=torch.int32, device="cuda")
+
+    def failing(call):
+        assert V.vla_test_inject_launch_error(1, out_of_resources) == 0
+        try:
+            with pytest.raises(V.VlaError) as e:
+                call()
+            assert e.value.code == V.VLA_ERR_CUDA and "701" in str(e.value)
+        finally:
+            V.vla_test_inject_launch_error(0, 0)
+        return call()
+
+    failing(lambda: P.rope_table(16, 64))
+    rows = failing(lambda: cache.plan(new_len, 2))
+    turned = failing(lambda: cache.append(0, q, k, v, rows))
+    out = failing(lambda: cache.attend(0, turned, rows))
+    lp = failing(lambda: P.token_logprobs(z, tokens, top_k=3)).logprob
+    failing(lambda: torch.autograd.grad(lp.sum(), z, retain_graph=True))
+    assert cache.ctx.tolist() == [1, 1] and cache.free_pages() == 2
+    assert float((out - v).abs().max()) <= 2.0 ** -11 * float(v.abs().max()) + 2.0 ** -20  # one position: its values
+    cache.check()
