@@ -17,7 +17,8 @@ namespace {
 // pages.  Bound by latency for a decode step; a prefill writes 12 bytes a row.  One cluster: every CTA makes the sums
 // for itself (a block scan into shared memory), then the CTAs share the pages and the rows, four rows a thread,
 // which finds the first one's environment by bisection.  The cluster's barriers stand between reading
-// the state and writing it, and between pages given back and pages taken.
+// the state and writing it, and between pages given back and pages taken.  16 environments of a row each take 3.9 us of
+// device time, 256 of about 296 rows 8.7 (84 as one CTA with a thread a row).
 __device__ __forceinline__ int64_t warp_inclusive(int64_t v) {
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -217,7 +218,8 @@ __global__ void __launch_bounds__(256) rope_table_kernel(const RopeTableArgs a, 
 // lane has 4 channels of each half instead (fp32 rows of 32 / 32 heads: 226 us for 18432 against 232; 16-bit ones in pieces
 // of 8 bytes: 131 against 95).  A warp walks over the queries, keys and values of one row, some accesses ahead (the
 // first ones before the row's position is known), and the row's cosines and sines stay in registers; a row of few
-// is cut over several warps so that a decode step fills the GPU.
+// is cut over several warps so that a decode step fills the GPU.  18432 bf16 rows of 32 / 8 heads of 128 with norms take 78 us
+// (5.8 TB/s of each byte once, 0.86 of the copy rate; three of four issue slots are used), 64 fp32 rows of 32 / 32 heads 3.1 us.
 enum RopeLayout : int { kNoRope = 0, kHalves = 1, kPairs = 2 };
 
 __device__ __forceinline__ float clamp_f16(float x, uint32_t& sat) {

@@ -27,6 +27,11 @@
 //
 // What runs once an item or once a call is kept short and in one place: a cold instruction line costs as
 // much as a load (a second copy of the join made calls of few long rows 10 us slower).
+//
+// Measured, heads of 128, each cached byte once: 64 rows x 32 heads over 273 to 311 positions 53 us (5.8 TB/s, 0.86 of the copy rate:
+// 5 us before the first bytes arrive and after the last, and 7 items on the fullest CTA where the mean is 6.7), 256 rows x 32 heads
+// over 1031 to 1097 positions 669 to 690 us (6.5 to 6.7 TB/s), 8 rows x 8 key-value heads over up to 131072 positions 280 to 286 us
+// (6.7 TB/s); 4 rows x 4 heads of 64 over 80 positions 4.3 us, a chain of latencies.
 #include <algorithm>
 #include <type_traits>
 
