@@ -417,25 +417,23 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
         constexpr int kLanes = HD / 4;
         const int c = lane % kLanes * 4;
         uint32_t sat = 0;
-        constexpr int kApart = 32 / kLanes, kAtOnce = 4;  // heads whose loads wait together
-#pragma unroll 1
-        for (int h0 = lane / kLanes; h0 < heads; h0 += kApart * kAtOnce) {
-          float4 x[kAtOnce];
-          const float* from = static_cast<const float*>(a.q) + seg.row * a.ldq + static_cast<int64_t>(head0 + h0) * HD + c;
+        constexpr int kApart = 32 / kLanes, kMine = kHeads / kApart;  // this lane's heads, whose loads wait together
+        const int h0 = lane / kLanes;
+        const float* from = static_cast<const float*>(a.q) + seg.row * a.ldq + static_cast<int64_t>(head0 + h0) * HD + c;
+        float4 x[kMine];
 #pragma unroll
-          for (int i = 0; i < kAtOnce; ++i)
-            if (h0 + i * kApart < heads) x[i] = *reinterpret_cast<const float4*>(from + i * kApart * HD);
+        for (int i = 0; i < kMine; ++i)
+          if (h0 + i * kApart < heads) x[i] = *reinterpret_cast<const float4*>(from + i * kApart * HD);
 #pragma unroll
-          for (int i = 0; i < kAtOnce; ++i) {
-            if (h0 + i * kApart >= heads) break;
-            uint2 u, v;
-            split_pack2_f16(x[i].x, x[i].y, u.x, u.y, sat);
-            split_pack2_f16(x[i].z, x[i].w, v.x, v.y, sat);
-            // channels 16k + 8 half + 2t: lane t, words 2 half of the k-th step
-            uint32_t* dst = mine + (h0 + i * kApart) * HD + c / 16 * 16 + c % 8 * 2 + (c & 8) / 4;
-            *reinterpret_cast<uint2*>(dst) = u;
-            *reinterpret_cast<uint2*>(dst + 4) = v;
-          }
+        for (int i = 0; i < kMine; ++i) {
+          if (h0 + i * kApart >= heads) break;
+          uint2 u, v;
+          split_pack2_f16(x[i].x, x[i].y, u.x, u.y, sat);
+          split_pack2_f16(x[i].z, x[i].w, v.x, v.y, sat);
+          // channels 16k + 8 half + 2t: lane t, words 2 half of the k-th step
+          uint32_t* dst = mine + (h0 + i * kApart) * HD + c / 16 * 16 + c % 8 * 2 + (c & 8) / 4;
+          *reinterpret_cast<uint2*>(dst) = u;
+          *reinterpret_cast<uint2*>(dst + 4) = v;
         }
         report_saturation(a.status, sat);
         __syncwarp();
