@@ -325,22 +325,24 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
           const float there = round_max[i][tid];
           rounds |= (lowest ? there > limit : there >= limit) ? 1u << i : 0u;
         }
-        for (int i = tid, round = 0; i < vecs; i += THREADS * kUnroll, ++round) {
-          if (!(rounds >> round % kRounds & 1u)) continue;
-          uint4 v[kUnroll];
+        // each lane its own rounds, so that a warp's loads go together
+        for (; rounds; rounds &= rounds - 1) {
+          for (int i = tid + (__ffs(rounds) - 1) * (THREADS * kUnroll); i < vecs; i += kRounds * THREADS * kUnroll) {
+            uint4 v[kUnroll];
 #pragma unroll
-          for (int u = 0; u < kUnroll; ++u) v[u] = body[min(i + u * THREADS, vecs - 1)];
+            for (int u = 0; u < kUnroll; ++u) v[u] = body[min(i + u * THREADS, vecs - 1)];
 #pragma unroll
-          for (int u = 0; u < kUnroll; ++u) {
-            if (i + u * THREADS >= vecs) break;
-            const float peak = V::word_float_max(V::word_max(V::word_max(v[u].x, v[u].y), V::word_max(v[u].z, v[u].w)));
-            if (lowest ? !(peak > limit) : !(peak >= limit)) continue;
-            float z[V::kN];
-            V::unpack(v[u], z);
-            uint32_t found = 0;
+            for (int u = 0; u < kUnroll; ++u) {
+              if (i + u * THREADS >= vecs) break;
+              const float peak = V::word_float_max(V::word_max(V::word_max(v[u].x, v[u].y), V::word_max(v[u].z, v[u].w)));
+              if (lowest ? !(peak > limit) : !(peak >= limit)) continue;
+              float z[V::kN];
+              V::unpack(v[u], z);
+              uint32_t found = 0;
 #pragma unroll
-            for (int j = 0; j < V::kN; ++j) found |= (lowest ? z[j] > limit : z[j] >= limit) ? 1u << j : 0u;
-            for (; found; found &= found - 1) take(head + (i + u * THREADS) * V::kN + __ffs(found) - 1);
+              for (int j = 0; j < V::kN; ++j) found |= (lowest ? z[j] > limit : z[j] >= limit) ? 1u << j : 0u;
+              for (; found; found &= found - 1) take(head + (i + u * THREADS) * V::kN + __ffs(found) - 1);
+            }
           }
         }
         if (edge >= 0) {
