@@ -218,8 +218,8 @@ __global__ void __launch_bounds__(256) rope_table_kernel(const RopeTableArgs a, 
 // lane has 4 channels of each half instead (fp32 rows of 32 / 32 heads: 226 us for 18432 against 232; 16-bit ones in pieces
 // of 8 bytes: 131 against 95).  A warp walks over the queries, keys and values of one row, some accesses ahead (the
 // first ones before the row's position is known), and the row's cosines and sines stay in registers; a row of few
-// is cut over several warps so that a decode step fills the GPU.  18432 bf16 rows of 32 / 8 heads of 128 with norms take 78 us
-// (5.8 TB/s of each byte once, 0.86 of the copy rate; three of four issue slots are used), 64 fp32 rows of 32 / 32 heads 3.1 us.
+// is cut over several warps so that a decode step fills the GPU.  18432 bf16 rows of 32 / 8 heads of 128 with norms take 76 us
+// (6.0 TB/s of each byte once, 0.88 of the copy rate; three of four issue slots are used), 64 fp32 rows of 32 / 32 heads 2.8 us.
 enum RopeLayout : int { kNoRope = 0, kHalves = 1, kPairs = 2 };
 
 __device__ __forceinline__ float clamp_f16(float x, uint32_t& sat) {
@@ -280,27 +280,33 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8], bool f16_type) {
 
 constexpr int kAppendThreads = 128;
 
-// `slices` warps share a row's heads.  Accesses ahead and warps an SM as measured on 18432 rows: bf16 of 32 / 8 heads with norms
-// 80 us with 4 ahead and 28 warps, 86 with 20 warps, 92 with 3 ahead and 32 (pairs in halves 89 with 24 warps, 95 with 28); f32 of
-// 32 / 32 heads 232 us with 2 ahead and 28 warps, 283 with 4 and the fewer warps that leaves.
-template <int DT, int LAYOUT, bool NORM>
-__global__ void __launch_bounds__(kAppendThreads, LAYOUT == kHalves && NORM ? 6 : 7) rope_append_kernel(const RopeAppendArgs a, const int slices) {
+// `slices` warps share a row's heads (CUT: more than one).  Accesses ahead and warps an SM as measured on 18432 rows: bf16 of
+// 32 / 8 heads with norms 80 us with 4 ahead and 28 warps, 86 with 20 warps, 92 with 3 ahead and 32 (pairs in halves 89 with 24
+// warps, 95 with 28); f32 of 32 / 32 heads 232 us with 2 ahead and 28 warps, 283 with 4 and the fewer warps that leaves.  CUT and
+// HD known when compiled: 65536 rows of 64 / 8 heads 437 us, 482 without.
+template <int DT, int LAYOUT, bool NORM, bool CUT, int HD>
+__global__ void __launch_bounds__(kAppendThreads, LAYOUT == kHalves && NORM ? 6 : 7) rope_append_kernel(const RopeAppendArgs a, const int slices, const int page_shift) {
   constexpr int kAhead = DT == VLA_F32 ? 2 : 4, kSize = DT == VLA_F32 ? 4 : 2, kSpan = 256;  // channels of an access
   constexpr bool kSplit = LAYOUT == kHalves && DT == VLA_F32, kShuffle = LAYOUT == kHalves && !kSplit;
   pdl_launch_dependents();
   pdl_wait();
-  const int lane = threadIdx.x & 31, hd = a.kv.head_dim, span = hd / 8;  // lanes of a head
+  constexpr int hd = HD, span = HD / 8, span_shift = HD == 64 ? 3 : 4;  // lanes of a head
+  const int lane = threadIdx.x & 31;
   const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kAppendThreads / 32) + (threadIdx.x >> 5);
   if (unit >= static_cast<int64_t>(a.rows) * slices) return;
-  const int row = static_cast<int>(unit / slices), slice = static_cast<int>(unit - static_cast<int64_t>(row) * slices);
-  const int half = a.rope_dim / 2, part = lane % span;
+  int row = static_cast<int>(unit), slice = 0;
+  if constexpr (CUT) {  // (then rows * slices fits 32 bits)
+    slice = row % slices;
+    row /= slices;
+  }
+  const int half = a.rope_dim / 2, part = lane & (span - 1), head_of_span = lane >> span_shift;
   const bool in_turn = LAYOUT != kNoRope && part * 8 < a.rope_dim;
   // this lane's channels of a head: 4 from c0, 4 more `gap` on
-  const int c0 = kSplit && in_turn ? part * 4 : part * 8, gap = kSplit && in_turn ? half : 4, mine = lane / span * hd + c0;
+  const int c0 = kSplit && in_turn ? part * 4 : part * 8, gap = kSplit && in_turn ? half : 4, mine = head_of_span * hd + c0;
   // accesses: queries, keys, values; this warp's
   const int q_channels = a.n_q_heads * hd, kv_channels = a.kv.n_heads * hd;
   const int keys = (q_channels + kSpan - 1) / kSpan, kv_steps = (kv_channels + kSpan - 1) / kSpan, values = keys + kv_steps;
-  const int steps = values + kv_steps, from = steps * slice / slices, to = steps * (slice + 1) / slices;
+  const int steps = values + kv_steps, from = CUT ? steps * slice / slices : 0, to = CUT ? steps * (slice + 1) / slices : steps;
   // the rows' first elements, as if each began at access 0
   const char* const q_row = static_cast<const char*>(a.q) + (row * a.ldq + mine) * kSize;
   const char* const k_row = static_cast<const char*>(a.k) + (row * a.ldk + mine - keys * kSpan) * kSize;
@@ -308,7 +314,7 @@ __global__ void __launch_bounds__(kAppendThreads, LAYOUT == kHalves && NORM ? 6 
   // whether this lane's head of access j is there
   auto there = [&](int j) {
     const int first = j < keys ? 0 : j < values ? keys : values;
-    return (j - first) * kSpan + lane / span * hd < (j < keys ? q_channels : kv_channels);
+    return (j - first) * kSpan + head_of_span * hd < (j < keys ? q_channels : kv_channels);
   };
   Eight<DT> raw[kAhead];
   auto fetch = [&](int j, Eight<DT>& r) {
@@ -344,8 +350,9 @@ __global__ void __launch_bounds__(kAppendThreads, LAYOUT == kHalves && NORM ? 6 
   char* const out = static_cast<char*>(a.q_out) + (row * a.ldqo + mine) * kSize;
   int64_t cell = 0, hop = 0;  // this lane's channels in the cache's slot, and from access to access
   if (file) {
-    cell = (slot / a.kv.page_size) * a.kv.page_stride + (slot % a.kv.page_size) * a.kv.slot_stride + lane / span * a.kv.head_stride + c0;
-    hop = (32 / span) * a.kv.head_stride;
+    const int page = page_shift >= 0 ? slot >> page_shift : slot / a.kv.page_size;
+    cell = page * a.kv.page_stride + (slot - page * a.kv.page_size) * a.kv.slot_stride + head_of_span * a.kv.head_stride + c0;
+    hop = a.kv.head_stride << (5 - span_shift);
   }
   float gain[8];
   bool normed = false;
@@ -470,6 +477,13 @@ int rope_table_launch(const RopeTableArgs& a, cudaStream_t s) {
 }
 
 namespace {
+template <int DT, bool CUT, int HD>
+auto append_kernel(int layout, bool norm) {
+  return layout == kNoRope  ? (norm ? rope_append_kernel<DT, kNoRope, true, CUT, HD> : rope_append_kernel<DT, kNoRope, false, CUT, HD>)
+         : layout == kPairs ? (norm ? rope_append_kernel<DT, kPairs, true, CUT, HD> : rope_append_kernel<DT, kPairs, false, CUT, HD>)
+                            : (norm ? rope_append_kernel<DT, kHalves, true, CUT, HD> : rope_append_kernel<DT, kHalves, false, CUT, HD>);
+}
+
 template <int DT>
 int append_of(const RopeAppendArgs& a, cudaStream_t s) {
   const int hd = a.kv.head_dim, steps = (a.n_q_heads * hd + 255) / 256 + 2 * ((a.kv.n_heads * hd + 255) / 256);
@@ -483,10 +497,10 @@ int append_of(const RopeAppendArgs& a, cudaStream_t s) {
   if (grid > 0x7fffffff) return record_error(VLA_ERR_UNSUPPORTED, "vla_rope_append: too many rows");
   const int layout = !a.rope ? kNoRope : a.interleaved ? kPairs : kHalves;
   const bool norm = a.q_gain || a.k_gain;
-  auto kern = layout == kNoRope  ? (norm ? rope_append_kernel<DT, kNoRope, true> : rope_append_kernel<DT, kNoRope, false>)
-              : layout == kPairs ? (norm ? rope_append_kernel<DT, kPairs, true> : rope_append_kernel<DT, kPairs, false>)
-                                 : (norm ? rope_append_kernel<DT, kHalves, true> : rope_append_kernel<DT, kHalves, false>);
-  VLA_CUDA_TRY(launch_pdl(kern, dim3(static_cast<unsigned>(grid)), dim3(kAppendThreads), 0, s, a, slices));
+  auto kern = slices > 1 ? (hd == 64 ? append_kernel<DT, true, 64>(layout, norm) : append_kernel<DT, true, 128>(layout, norm))
+                         : (hd == 64 ? append_kernel<DT, false, 64>(layout, norm) : append_kernel<DT, false, 128>(layout, norm));
+  const int ps = a.kv.page_size, shift = (ps & (ps - 1)) ? -1 : __builtin_ctz(ps);
+  VLA_CUDA_TRY(launch_pdl(kern, dim3(static_cast<unsigned>(grid)), dim3(kAppendThreads), 0, s, a, slices, shift));
   note_launch();
   VLA_CUDA_TRY(cudaGetLastError());
   return VLA_OK;
