@@ -15,6 +15,7 @@
 // lies above the bound is ranked by counting.  That is a chain of some 3 us a row, which the rows on an SM do at about the same
 // time; 64 x 32064 fp32 take 8.4 us with 8 alternatives and 5.5 without.
 #include <algorithm>
+#include <type_traits>
 
 #include "lm.h"
 #include "ptx.cuh"
@@ -130,8 +131,9 @@ struct Sums {
   }
 };
 
-// One cluster of `parts` CTAs per row, each a slice of the ids.
-template <int DT, int THREADS>
+// CUT: one cluster of `parts` CTAs per row, each a slice of the ids; else one CTA per row.  TOP: with alternatives.  (Both known when
+// compiled: 2500 x 32064 fp32 without alternatives 50 us, 57 with one kernel for all; 3584 x 32064 bf16 with 4 of them 45.4 and 46.7.)
+template <int DT, int THREADS, bool TOP, bool CUT>
 __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel(const LogprobArgs a, const int parts) {
   using V = Vec<DT>;
   constexpr int kWarps = THREADS / 32, kUnroll = 4;
@@ -145,22 +147,21 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
   __shared__ int64_t above[kList];
   __shared__ int level_ids[kList];
   __shared__ int n_above, n_level, bound;
-  __shared__ __align__(16) int64_t all_best[THREADS == 256 ? kMostParts * kMaxTopK : 2];  // the slices' best keys, each in order
+  __shared__ __align__(16) int64_t all_best[CUT ? kMostParts * kMaxTopK : 2];  // the slices' best keys, each in order
   __shared__ float all_slices[kMostParts][3];      // (m, s, w) of the slices
   __shared__ int64_t round_key[kWarps];
   pdl_launch_dependents();
   pdl_wait();
-  const bool cut = THREADS == 256 && parts > 1;
-  if (cut) cluster_arrive();  // the first CTA has begun once all have passed the wait
+  if constexpr (CUT) cluster_arrive();  // the first CTA has begun once all have passed the wait
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int row = blockIdx.x / parts, part = blockIdx.x % parts;
-  const int first = static_cast<int>(static_cast<int64_t>(a.vocab) * part / parts);
-  const int n = static_cast<int>(static_cast<int64_t>(a.vocab) * (part + 1) / parts) - first;
+  const int row = CUT ? blockIdx.x / parts : blockIdx.x, part = CUT ? blockIdx.x % parts : 0;
+  const int first = CUT ? static_cast<int>(static_cast<int64_t>(a.vocab) * part / parts) : 0;
+  const int n = CUT ? static_cast<int>(static_cast<int64_t>(a.vocab) * (part + 1) / parts) - first : a.vocab;
   const char* base = static_cast<const char*>(a.logits) + (row * a.ld + first) * V::kBytes;
   const int head = head_of<DT>(base, n), vecs = (n - head) / V::kN, tail = n - head - vecs * V::kN;
   const uint4* body = reinterpret_cast<const uint4*>(base + head * V::kBytes);
   const float inv_t = 1.f / a.temperature, c = kLog2e * inv_t;
-  const int k = min(a.top_k, n);  // of this slice
+  const int k = TOP ? min(a.top_k, n) : 0;  // of this slice
 
   // the token's logit is read beside the pass
   int token = -1;
@@ -190,7 +191,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
 #pragma unroll
     for (int u = 0; u < kUnroll; ++u) up = V::word_max(up, V::word_max(V::word_max(v[u].x, v[u].y), V::word_max(v[u].z, v[u].w)));
     const float peak = V::word_float_max(up);
-    if (k > 0) {
+    if constexpr (TOP) {
       float& kept = round_max[round % kRounds][tid];
       kept = round < kRounds ? peak : fmaxf(kept, peak);
     }
@@ -248,7 +249,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
     red[1][warp] = x.s;
     red[2][warp] = x.w;
   }
-  if (k > 0 && warp == kWarps - 1) {
+  if (TOP && warp == kWarps - 1) {
     // the largest maximum that k groups reach: the largest ones go in turn, two a lane
     int hi = group_max[lane], lo = INT32_MIN, reach = 0, v;
     if (kGroups == 64) {
@@ -293,16 +294,16 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
     a.top_logprobs[at] = logprob(key_value(key));
   };
   settle();
-  if (cut) cluster_wait();
+  if constexpr (CUT) cluster_wait();
 
   // ---- the slice's best keys
   auto place = [&](int rank, int64_t key) {
-    if (cut)
+    if constexpr (CUT)
       asm volatile("st.shared::cluster.s64 [%0], %1;" ::"r"(mapa_shared(smem_u32(&all_best[part * a.top_k + rank]), 0)), "l"(key) : "memory");
     else
       put(rank, key);
   };
-  if (k > 0) {
+  if constexpr (TOP) {
     const int at_least = bound;
     const float limit = float_of(at_least);
     const bool lowest = limit == -INFINITY;  // then all that is not above it is equal to it
@@ -394,7 +395,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
   }
 
   // ---- the slices' results meet in the first CTA
-  if (cut) {
+  if constexpr (CUT) {
     if (tid < 3) {
       const float mine = tid == 0 ? top : tid == 1 ? total.s : total.w;
       asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(mapa_shared(smem_u32(&all_slices[part][tid]), 0)), "f"(mine) : "memory");
@@ -548,7 +549,15 @@ int logprobs_of(const LogprobArgs& a, cudaStream_t s, int sms) {
     parts *= 2;
   }
   if (static_cast<int64_t>(a.rows) * parts > 0x7fffffff) return record_error(VLA_ERR_UNSUPPORTED, "vla_token_logprobs: too many rows");
-  auto kern = threads == 32 ? token_logprobs_kernel<DT, 32> : threads == 64 ? token_logprobs_kernel<DT, 64> : threads == 128 ? token_logprobs_kernel<DT, 128> : token_logprobs_kernel<DT, 256>;
+  auto pick = [&](auto top) {
+    constexpr bool TOP = decltype(top)::value;
+    return parts > 1        ? token_logprobs_kernel<DT, 256, TOP, true>
+           : threads == 256 ? token_logprobs_kernel<DT, 256, TOP, false>
+           : threads == 128 ? token_logprobs_kernel<DT, 128, TOP, false>
+           : threads == 64  ? token_logprobs_kernel<DT, 64, TOP, false>
+                            : token_logprobs_kernel<DT, 32, TOP, false>;
+  };
+  auto kern = a.top_k > 0 ? pick(std::true_type()) : pick(std::false_type());
   VLA_CUDA_TRY(launch_pdl_cluster(kern, dim3(a.rows * parts), dim3(threads), 0, s, parts, a, parts));
   note_launch();
   VLA_CUDA_TRY(cudaGetLastError());
