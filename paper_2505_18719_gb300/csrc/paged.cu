@@ -17,8 +17,8 @@ namespace {
 // pages.  Bound by latency for a decode step; a prefill writes 12 bytes a row.  One cluster: every CTA makes the sums
 // for itself (a block scan into shared memory), then the CTAs share the pages and the rows, four rows a thread,
 // which finds the first one's environment by bisection.  The cluster's barriers stand between reading
-// the state and writing it, and between pages given back and pages taken.  16 environments of a row each take 3.9 us of
-// device time, 256 of about 296 rows 8.7 (84 as one CTA with a thread a row).
+// the state and writing it, and between pages given back and pages taken.  16 environments of a row each take 3.6 us of
+// device time, 256 of about 296 rows 8.3 (84 as one CTA with a thread a row).
 __device__ __forceinline__ int64_t warp_inclusive(int64_t v) {
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -41,8 +41,8 @@ __device__ __forceinline__ int env_of(const int* start, int n, int i) {
   return lo;
 }
 
-// `page_shift` >= 0: pages of 1 << page_shift positions.
-template <int kPlanThreads>
+// POW2: pages of 1 << page_shift positions (known when compiled 0.3 to 0.7 us a call).
+template <int kPlanThreads, bool POW2>
 __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PagePlanArgs a, const int parts, const int page_shift) {
   extern __shared__ int plan_sm[];
   int* row_first = plan_sm;                   // [n_env + 1]
@@ -60,7 +60,7 @@ __global__ void __launch_bounds__(kPlanThreads) page_plan_kernel(const PagePlanA
   if (tid == 0) bad = 0;
   const int n_free = *a.n_free_in;
   const int64_t room = static_cast<int64_t>(a.max_pages) * a.page_size;
-  auto page_of = [&](int position) { return page_shift >= 0 ? position >> page_shift : position / a.page_size; };
+  auto page_of = [&](int position) { return POW2 ? position >> page_shift : position / a.page_size; };
   auto pages_of = [&](int64_t n) { return n > 0 ? page_of(static_cast<int>(n - 1)) + 1 : 0; };
   __syncthreads();
   for (int base = 0; base < a.n_env; base += kPlanThreads) {
@@ -435,20 +435,20 @@ __global__ void __launch_bounds__(kAppendThreads, LAYOUT == kHalves && NORM ? 6 
 }  // namespace
 
 namespace {
-template <int THREADS>
+template <int THREADS, bool POW2>
 int plan_of(const PagePlanArgs& a, cudaStream_t s) {
   static std::atomic<uint64_t> smem_done{0}, cluster_done{0};
   static std::atomic<int> cluster_size[64] = {};
   constexpr int kMost = (4 * kMaxPlanEnvs + 1) * static_cast<int>(sizeof(int));
-  VLA_CUDA_TRY(set_smem_limit(page_plan_kernel<THREADS>, kMost, smem_done));
-  VLA_CUDA_TRY(allow_wide_clusters(page_plan_kernel<THREADS>, cluster_done));
+  VLA_CUDA_TRY(set_smem_limit(page_plan_kernel<THREADS, POW2>, kMost, smem_done));
+  VLA_CUDA_TRY(allow_wide_clusters(page_plan_kernel<THREADS, POW2>, cluster_done));
   // a thread has four rows and takes them twice before another CTA joins
   int parts = 1, most = 1;
   while (parts < 16 && a.max_rows > parts * THREADS * 8) parts *= 2;
-  VLA_CUDA_TRY(max_cluster_size(page_plan_kernel<THREADS>, dim3(THREADS), kMost, 16, cluster_size, &most));
+  VLA_CUDA_TRY(max_cluster_size(page_plan_kernel<THREADS, POW2>, dim3(THREADS), kMost, 16, cluster_size, &most));
   parts = std::min(parts, most);
-  const int ps = a.page_size, shift = (ps & (ps - 1)) ? -1 : __builtin_ctz(ps);
-  VLA_CUDA_TRY(launch_pdl_cluster(page_plan_kernel<THREADS>, dim3(parts), dim3(THREADS), (4 * a.n_env + 1) * sizeof(int), s, parts, a, parts, shift));
+  const int shift = __builtin_ctz(a.page_size);
+  VLA_CUDA_TRY(launch_pdl_cluster(page_plan_kernel<THREADS, POW2>, dim3(parts), dim3(THREADS), (4 * a.n_env + 1) * sizeof(int), s, parts, a, parts, shift));
   note_launch();
   VLA_CUDA_TRY(cudaGetLastError());
   return VLA_OK;
@@ -458,7 +458,9 @@ int plan_of(const PagePlanArgs& a, cudaStream_t s) {
 int page_plan_launch(const PagePlanArgs& a, cudaStream_t s) {
   // the sums' barriers are shorter with fewer warps: 16 environments of a row each take 3.8 us with 256 threads and 4.5 with 512,
   // 186 of 106 rows 6.2 and 6.9, 256 of 296 rows 11.1 and 8.7, 438 of 5 rows 7.1 and 6.8
-  return a.n_env <= 256 && a.max_rows <= 32768 ? plan_of<256>(a, s) : plan_of<512>(a, s);
+  const bool few = a.n_env <= 256 && a.max_rows <= 32768;
+  if (a.page_size & (a.page_size - 1)) return few ? plan_of<256, false>(a, s) : plan_of<512, false>(a, s);
+  return few ? plan_of<256, true>(a, s) : plan_of<512, true>(a, s);
 }
 
 int rope_table_launch(const RopeTableArgs& a, cudaStream_t s) {
