@@ -174,12 +174,15 @@ struct Segment {
   int from, blocks;          // the first of them; the item's blocks
 };
 
-// ALIGNED: pages are multiples of 8 positions, so that 8 rows of ldmatrix share a page.
-template <int HD, bool BF16, bool PAIR, bool ALIGNED>
+enum Pages : int { kAnyPage = 0, kEights = 1, kShifted = 2 };  // kEights: multiples of 8 positions; kShifted: and powers of two
+
+// Pages of multiples of 8 positions: 8 rows of ldmatrix share a page.
+template <int HD, bool BF16, bool PAIR, int PAGES>
 __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_kernel(const PagedAttnArgs a, const int page_shift, const int tiles) {
   using R = Ring<HD>;
   using Some = Channels<HD>;
   constexpr int kStep = R::kStep, kStages = R::kStages;
+  constexpr bool ALIGNED = PAGES != kAnyPage;
   constexpr float kShift = BF16 ? 0.f : 15.f;
   extern __shared__ __align__(128) uint8_t sm_raw[];
   uint8_t* sm = sm_raw + (-smem_u32(sm_raw) & 255u);  // rows of 256 bytes at multiples of 256
@@ -201,7 +204,7 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
   auto length_of = [&](int row, int& env) {
     const int pos = a.row_pos[row];
     env = a.row_env[row];
-    const int col = page_shift >= 0 ? pos >> page_shift : pos / a.kv.page_size;
+    const int col = PAGES == kShifted ? pos >> page_shift : pos / a.kv.page_size;
     const bool ok = pos >= 0 && pos <= kLastPosition && col < a.max_pages && static_cast<unsigned>(env) < static_cast<unsigned>(a.n_env);
     if (!ok && pos != -1) raise_status(a.status, VLA_STATUS_PAGES);
     return ok ? pos + 1 : 0;
@@ -318,7 +321,7 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
     next_page = -1;
     const int key = block * block_len + my_key;
     if (item < end_item && to_load > 0 && (ALIGNED || lane < kStep) && key < n) {
-      const int col = page_shift >= 0 ? key >> page_shift : key / a.kv.page_size;
+      const int col = PAGES == kShifted ? key >> page_shift : key / a.kv.page_size;
       next_page = a.table[static_cast<int64_t>(env) * a.max_pages + col];
       if (static_cast<unsigned>(next_page) >= static_cast<unsigned>(a.kv.n_pages)) {
         raise_status(a.status, VLA_STATUS_PAGES);
@@ -328,7 +331,7 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
   };
   auto issue = [&](int stage) {
     const int key = block * block_len + my_key;
-    const int slot = page_shift >= 0 ? key & ((1 << page_shift) - 1) : key % a.kv.page_size;
+    const int slot = PAGES == kShifted ? key & ((1 << page_shift) - 1) : key % a.kv.page_size;
     int64_t off = next_page * a.kv.page_stride + slot * a.kv.slot_stride + kv * a.kv.head_stride;
     const uint32_t dst0 = ring + stage * R::kStage + my_row * R::kRow;
     const uint16_t *const k0 = static_cast<const uint16_t*>(a.kv.k), *const v0 = static_cast<const uint16_t*>(a.kv.v);
@@ -680,8 +683,8 @@ int paged_attn_launch(const PagedAttnArgs& a, cudaStream_t s) {
   VLA_CUDA_TRY(cudaGetDevice(&dev));
   VLA_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
   const int group = a.n_q_heads / a.kv.n_heads, tiles = (group + kHeads - 1) / kHeads;
-  const int ps = a.kv.page_size, shift = (ps & (ps - 1)) ? -1 : __builtin_ctz(ps);
-  const bool pair = a.dtype == VLA_F32, bf = a.kv.dtype == VLA_BF16, aligned = ps % 8 == 0;
+  const int ps = a.kv.page_size, shift = __builtin_ctz(ps);
+  const bool pair = a.dtype == VLA_F32, bf = a.kv.dtype == VLA_BF16, eights = ps % 8 == 0, shifted = eights && !(ps & (ps - 1));
   auto go = [&](auto ring, auto kern, std::atomic<uint64_t>& done) -> int {
     using R = decltype(ring);
     // no more CTAs than have a step to take at the longest rows that the table holds
@@ -694,10 +697,11 @@ int paged_attn_launch(const PagedAttnArgs& a, cudaStream_t s) {
     VLA_CUDA_TRY(cudaGetLastError());
     return VLA_OK;
   };
-  static std::atomic<uint64_t> done[12] = {};
+  static std::atomic<uint64_t> done[18] = {};
 #define VLA_PAGED(HD, BF, PAIR, I)                                                        \
-  (aligned ? go(Ring<HD>(), paged_attn_kernel<HD, BF, PAIR, true>, done[2 * (I)])         \
-           : go(Ring<HD>(), paged_attn_kernel<HD, BF, PAIR, false>, done[2 * (I) + 1]))
+  (shifted  ? go(Ring<HD>(), paged_attn_kernel<HD, BF, PAIR, kShifted>, done[3 * (I)])    \
+   : eights ? go(Ring<HD>(), paged_attn_kernel<HD, BF, PAIR, kEights>, done[3 * (I) + 1]) \
+            : go(Ring<HD>(), paged_attn_kernel<HD, BF, PAIR, kAnyPage>, done[3 * (I) + 2]))
   if (a.kv.head_dim == 128) return bf ? VLA_PAGED(128, true, false, 0) : pair ? VLA_PAGED(128, false, true, 1) : VLA_PAGED(128, false, false, 2);
   return bf ? VLA_PAGED(64, true, false, 3) : pair ? VLA_PAGED(64, false, true, 4) : VLA_PAGED(64, false, false, 5);
 #undef VLA_PAGED
