@@ -438,8 +438,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
 // Bound by HBM.  One CTA per row and slice, in 16-byte pieces of the gradient; where the logits lie differently towards
 // 16 bytes, a piece of theirs is cut out of the two aligned ones that it lies in (the row's ends, whose neighbours are
 // not the row's, element by element).  3584 x 32064 bf16 take 68 to 72 us (6.4 to 6.8 TB/s, the copy rate); 4000 x 8000 bf16 with
-// logits 5 elements further apart than the gradient's 25.0 us, 24.8 where both are dense, 46 element by element.
-template <int DT, int THREADS>
+// logits 5 elements further apart than the gradient's 25.0 us, 46 element by element.  ALIKE: all rows of both lie alike (known when
+// compiled: 1500 x 20000 bf16 21.4 us, 24.1 with the check; 3000 x 10000 24.1 and 27.2).
+template <int DT, int THREADS, bool ALIKE>
 __global__ void __launch_bounds__(THREADS) token_logprobs_grad_kernel(const LogprobGradArgs a, const int parts) {
   using V = Vec<DT>;
   constexpr int kUnroll = 4;
@@ -467,7 +468,7 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_grad_kernel(const Logp
     return -exp2_fast(d * kLog2e) * fmaf(h, d, gh);
   };
   const int head = head_of<DT>(dst, n);
-  const int off = static_cast<int>(reinterpret_cast<uintptr_t>(src + head * V::kBytes) & 15u);
+  const int off = ALIKE ? 0 : static_cast<int>(reinterpret_cast<uintptr_t>(src + head * V::kBytes) & 15u);
   // pieces [v0, v1) whose logits, or both aligned pieces around them, are the row's
   const int inside = (n - head) * V::kBytes;
   const int v0 = off > head * V::kBytes ? 1 : 0, v1 = max(v0, off ? (inside + off - 16) / 16 : inside / 16);
@@ -588,10 +589,15 @@ int token_logprobs_grad_launch(const LogprobGradArgs& a, cudaStream_t s) {
   int parts = 1;
   while (parts < 64 && static_cast<int64_t>(a.rows) * parts < 4 * sms && a.vocab / (parts * 2) >= 2048) parts *= 2;
   if (static_cast<int64_t>(a.rows) * parts > 0x7fffffff) return record_error(VLA_ERR_UNSUPPORTED, "vla_token_logprobs_grad: too many rows");
-  auto pick = [&](auto small, auto large) { return threads == 64 ? small : large; };
-  auto kern = a.dtype == VLA_F32   ? pick(token_logprobs_grad_kernel<VLA_F32, 64>, token_logprobs_grad_kernel<VLA_F32, 256>)
-              : a.dtype == VLA_F16 ? pick(token_logprobs_grad_kernel<VLA_F16, 64>, token_logprobs_grad_kernel<VLA_F16, 256>)
-                                   : pick(token_logprobs_grad_kernel<VLA_BF16, 64>, token_logprobs_grad_kernel<VLA_BF16, 256>);
+  auto pick = [&](auto type) {
+    constexpr int DT = decltype(type)::value;
+    const bool alike = !(((reinterpret_cast<uintptr_t>(a.logits) ^ reinterpret_cast<uintptr_t>(a.d_logits)) | ((a.ld - a.ldd) * Vec<DT>::kBytes)) & 15);
+    return threads == 64 ? (alike ? token_logprobs_grad_kernel<DT, 64, true> : token_logprobs_grad_kernel<DT, 64, false>)
+                         : (alike ? token_logprobs_grad_kernel<DT, 256, true> : token_logprobs_grad_kernel<DT, 256, false>);
+  };
+  auto kern = a.dtype == VLA_F32   ? pick(std::integral_constant<int, VLA_F32>())
+              : a.dtype == VLA_F16 ? pick(std::integral_constant<int, VLA_F16>())
+                                   : pick(std::integral_constant<int, VLA_BF16>());
   VLA_CUDA_TRY(launch_pdl(kern, dim3(a.rows * parts), dim3(threads), 0, s, a, parts));
   note_launch();
   VLA_CUDA_TRY(cudaGetLastError());
