@@ -28,10 +28,10 @@
 // What runs once an item or once a call is kept short and in one place: a cold instruction line costs as
 // much as a load (a second copy of the join made calls of few long rows 10 us slower).
 //
-// Measured, heads of 128, each cached byte once: 64 rows x 32 heads over 273 to 311 positions 53 us (5.8 TB/s, 0.86 of the copy rate:
+// Measured, heads of 128, each cached byte once: 64 rows x 32 heads over 273 to 311 positions 52 us (5.9 TB/s, 0.88 of the copy rate:
 // 5 us before the first bytes arrive and after the last, and 7 items on the fullest CTA where the mean is 6.7), 256 rows x 32 heads
 // over 1031 to 1097 positions 669 to 690 us (6.5 to 6.7 TB/s), 8 rows x 8 key-value heads over up to 131072 positions 280 to 286 us
-// (6.7 TB/s); 4 rows x 4 heads of 64 over 80 positions 4.3 us, a chain of latencies.
+// (6.7 TB/s); 4 rows x 4 heads of 64 over 80 positions 3.8 us, a chain of latencies.
 #include <algorithm>
 #include <type_traits>
 
@@ -176,8 +176,9 @@ struct Segment {
 
 enum Pages : int { kAnyPage = 0, kEights = 1, kShifted = 2 };  // kEights: multiples of 8 positions; kShifted: and powers of two
 
-// Pages of multiples of 8 positions: 8 rows of ldmatrix share a page.
-template <int HD, bool BF16, bool PAIR, int PAGES>
+// Pages of multiples of 8 positions: 8 rows of ldmatrix share a page.  ONE: a query head for each key-value head (known when compiled: 64
+// rows x 32 heads 51.7 us, 52.3 without; 150 rows x 20 heads over 4 positions 9.3 and 10.2).
+template <int HD, bool BF16, bool PAIR, int PAGES, bool ONE>
 __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_kernel(const PagedAttnArgs a, const int page_shift, const int tiles) {
   using R = Ring<HD>;
   using Some = Channels<HD>;
@@ -198,7 +199,7 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
   pdl_launch_dependents();
   pdl_wait();
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const int items = a.kv.n_heads * tiles, group = a.n_q_heads / a.kv.n_heads, all_items = a.rows * items;
+  const int items = ONE ? a.kv.n_heads : a.kv.n_heads * tiles, group = ONE ? 1 : a.n_q_heads / a.kv.n_heads, all_items = a.rows * items;
 
   // positions of a row, 0 where it has none or what it says of itself is out of range
   auto length_of = [&](int row, int& env) {
@@ -291,7 +292,7 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
 
   // ---- loading side: the pages of a step's positions (of 8 at a time, or of each lane's) are known one step ahead
   int row = item / items, n, blocks, env;
-  int kv = (item - row * items) / tiles, tile = item - row * items - kv * tiles, segments = 0;
+  int kv = ONE ? item - row * items : (item - row * items) / tiles, tile = ONE ? 0 : item - row * items - kv * tiles, segments = 0;
   int next_page = -1;
   const uint32_t ring = smem_u32(sm) + warp * kStages * R::kStage;
   constexpr int kChunks = HD / 8, kRows = 32 / kChunks;   // 16-byte pieces of a position, positions per instruction
@@ -369,7 +370,7 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
         ++item;
         to_load -= kItem;
         fresh_item = true;
-        if (++tile == tiles) {
+        if (ONE || ++tile == tiles) {
           tile = 0;
           if (++kv == a.kv.n_heads) {
             kv = 0;
@@ -390,7 +391,7 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
   // ---- computing side
   const int g = lane >> 2, t = lane & 3;
   const float to_log2 = a.scale * 1.44269504f;
-  const int tile_heads = min(group, kHeads), buffers = tile_heads <= 2 ? 4 : tile_heads <= 4 ? 2 : 1;
+  const int tile_heads = ONE ? 1 : min(group, kHeads), buffers = ONE || tile_heads <= 2 ? 4 : tile_heads <= 4 ? 2 : 1;
   uint32_t q[HD / 16][PAIR ? 4 : 2];
   // outputs: c0, c1 of the query head, c2, c3 of the weights' low parts; PAIR: both, added after each step
   constexpr int kOut = PAIR ? 2 : 4;
@@ -411,8 +412,8 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
       crew_o = crew == 1 ? join_all + warp * (kHeads * HD) : join_all + buffer * (kJoinFloats / buffers);
       crew_ml = crew == 1 ? join_ml + warp * kHeads : join_ml + buffer * (kWarps * kHeads / buffers);
       my_o = crew_o + sub * tile_heads * HD;
-      head0 = seg.kv * group + seg.tile * kHeads;
-      heads = min(kHeads, group - seg.tile * kHeads);
+      head0 = ONE ? seg.kv : seg.kv * group + seg.tile * kHeads;
+      heads = ONE ? 1 : min(kHeads, group - seg.tile * kHeads);
       if constexpr (PAIR) {
         // four channels a lane, split and laid out in this warp's part as each lane's operands (high and low words of
         // two pairs of channels): idle lanes would repeat the split otherwise
@@ -420,7 +421,7 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
         constexpr int kLanes = HD / 4;
         const int c = lane % kLanes * 4;
         uint32_t sat = 0;
-        constexpr int kApart = 32 / kLanes, kMine = kHeads / kApart;  // this lane's heads, whose loads wait together
+        constexpr int kApart = 32 / kLanes, kMine = ONE ? 1 : kHeads / kApart;  // this lane's heads, whose loads wait together
         const int h0 = lane / kLanes;
         const float* from = static_cast<const float*>(a.q) + seg.row * a.ldq + static_cast<int64_t>(head0 + h0) * HD + c;
         float4 x[kMine];
@@ -585,11 +586,11 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
     // two heads at a time, so that they wait for memory together
 #pragma unroll 1
     for (; h0 < heads; h0 += 2 * h_step) {
-      const bool both = h0 + h_step < heads;
+      const bool both = !ONE && h0 + h_step < heads;
       float top[2], sum[2];
       Some val[2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < (ONE ? 1 : 2); ++i) {
         const int h = i == 0 || both ? h0 + i * h_step : h0;
         float2 x[kWarps];
 #pragma unroll
@@ -697,11 +698,12 @@ int paged_attn_launch(const PagedAttnArgs& a, cudaStream_t s) {
     VLA_CUDA_TRY(cudaGetLastError());
     return VLA_OK;
   };
-  static std::atomic<uint64_t> done[18] = {};
-#define VLA_PAGED(HD, BF, PAIR, I)                                                        \
-  (shifted  ? go(Ring<HD>(), paged_attn_kernel<HD, BF, PAIR, kShifted>, done[3 * (I)])    \
-   : eights ? go(Ring<HD>(), paged_attn_kernel<HD, BF, PAIR, kEights>, done[3 * (I) + 1]) \
-            : go(Ring<HD>(), paged_attn_kernel<HD, BF, PAIR, kAnyPage>, done[3 * (I) + 2]))
+  static std::atomic<uint64_t> done[24] = {};
+#define VLA_PAGED(HD, BF, PAIR, I)                                                                             \
+  (shifted && group == 1 ? go(Ring<HD>(), paged_attn_kernel<HD, BF, PAIR, kShifted, true>, done[4 * (I)])      \
+   : shifted             ? go(Ring<HD>(), paged_attn_kernel<HD, BF, PAIR, kShifted, false>, done[4 * (I) + 1]) \
+   : eights              ? go(Ring<HD>(), paged_attn_kernel<HD, BF, PAIR, kEights, false>, done[4 * (I) + 2])  \
+                         : go(Ring<HD>(), paged_attn_kernel<HD, BF, PAIR, kAnyPage, false>, done[4 * (I) + 3]))
   if (a.kv.head_dim == 128) return bf ? VLA_PAGED(128, true, false, 0) : pair ? VLA_PAGED(128, false, true, 1) : VLA_PAGED(128, false, false, 2);
   return bf ? VLA_PAGED(64, true, false, 3) : pair ? VLA_PAGED(64, false, true, 4) : VLA_PAGED(64, false, false, 5);
 #undef VLA_PAGED
