@@ -7,13 +7,13 @@
 // one fma, exact up to its own size: logits far from zero lose nothing while |r| is below 2^24.  (Rows beyond, such as one of
 // nothing but a type's lowest values, are read again with the difference to the maximum taken first.)  Bound by reading the
 // logits, for 16-bit types nearly as much by issuing 5 instructions an element (two elements share an fma, an addition and an
-// fma): 3584 x 32064 bf16 take 40 us (5.8 TB/s, 0.85 of the copy rate), 48 with 4 alternatives, fp32 72 us (6.4 TB/s).
+// fma): 3584 x 32064 bf16 take 38 us (6.0 TB/s, 0.88 of the copy rate), 45 with 4 alternatives.
 //
 // The best alternatives come from the same pass: each thread's maximum is known, and the k-th largest maximum over
 // disjoint groups of threads is a bound that at least k logits reach.  Only threads whose maximum reaches it read
 // logits again (from L2), and only those rounds of the pass whose maximum, kept in shared memory, reaches it too; what
 // lies above the bound is ranked by counting.  That is a chain of some 3 us a row, which the rows on an SM do at about the same
-// time; 64 x 32064 fp32 take 8.4 us with 8 alternatives and 5.5 without.
+// time; 64 x 32064 fp32 take 7.7 us with 8 alternatives and 4.7 without.
 #include <algorithm>
 #include <type_traits>
 
@@ -24,7 +24,8 @@ namespace vla {
 
 namespace {
 
-constexpr int kGradShort = 8192;  // ids up to which a row's gradient has 64 threads
+constexpr int kLongRow = 160 << 10;  // bytes from which a row of logits may be cut
+constexpr int kGradShort = 8192;     // ids up to which a row's gradient has 64 threads
 
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
 
@@ -437,7 +438,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
 // The gradient, element by element: with d = z / T - lse, -e^d (g + h (d + entropy)) / T, and g / T more at the token.
 // Bound by HBM.  One CTA per row and slice, in 16-byte pieces of the gradient; where the logits lie differently towards
 // 16 bytes, a piece of theirs is cut out of the two aligned ones that it lies in (the row's ends, whose neighbours are
-// not the row's, element by element).  3584 x 32064 bf16 take 68 to 72 us (6.4 to 6.8 TB/s, the copy rate); 4000 x 8000 bf16 with
+// not the row's, element by element).  3584 x 32064 bf16 take 68 us (6.7 TB/s, the copy rate); 4000 x 8000 bf16 with
 // logits 5 elements further apart than the gradient's 25.0 us, 46 element by element.  ALIKE: all rows of both lie alike (known when
 // compiled: 1500 x 20000 bf16 21.4 us, 24.1 with the check; 3000 x 10000 24.1 and 27.2).
 template <int DT, int THREADS, bool ALIKE>
@@ -528,8 +529,8 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_grad_kernel(const Logp
 template <int DT>
 int logprobs_of(const LogprobArgs& a, cudaStream_t s, int sms) {
   // Threads a row: the SMs hold 1024 each, so rows go in waves of 1024 sms / threads, and a wave takes about as long as
-  // 44 ids a thread for the row's own steps and one for each id that a thread has (3584 rows x 32064 bf16: 72, 64, 54, 62 us
-  // with 32, 64, 128, 256 threads; 4000 x 1200: 9.2, 12, 17 with 32, 64, 128; 500 x 32064: 36, 22, 18, 11).
+  // 44 ids a thread for the row's own steps and one for each id that a thread has (bf16 with 4 alternatives on 32, 64, 128,
+  // 256 threads: 3584 x 32064 49, 48, 45, 53 us; 4000 x 1200 8.5, 10, 15, 24; 500 x 32064 27, 17, 15, 10).
   int threads = 32;
   int64_t least = INT64_MAX;
   for (int t = 32; t <= 256; t *= 2) {
@@ -539,14 +540,14 @@ int logprobs_of(const LogprobArgs& a, cudaStream_t s, int sms) {
       threads = t;
     }
   }
-  // Few long rows are cut over a cluster, whose barriers cost 2 to 3 us: into slices of 8 KB while two of its CTAs an SM are not
-  // reached, of 36 KB up to four (with 8 alternatives 130 x 60000 f32 takes 11.8, 14.9, 17.0 us on 4, 2, 1 CTAs a row, 64 x 151000
-  // bf16 12.4, 14.2, 15.2 on 8, 4, 2, 200 x 32064 bf16 10.3, 8.2 on 2, 1).
+  // Few long rows are cut over a cluster, which costs 2 to 4 us: from kLongRow on, while two of its CTAs an SM are not reached, or
+  // four with slices of 36 KB (with 8 alternatives on 1, 2, 4, 8 CTAs a row: 64 x 32064 f32 6.6, 7.5, 7.8, 7.7 us, one row
+  // of it 6.0, 6.2, 5.7, 5.8; 130 x 50000 f32 12.1, 11.5, 10.0, 15.7, one row 7.6, 7.1, 6.5, 6.2; 64 x 151000 bf16 13.6, 12.9, 12.3, 11.2).
   int parts = 1;
   const int64_t bytes = static_cast<int64_t>(a.vocab) * Vec<DT>::kBytes;
-  while (threads == 256 && parts < 8) {
+  while (threads == 256 && bytes >= kLongRow && parts < 8) {
     const int64_t ctas = static_cast<int64_t>(a.rows) * parts * 2, slice = bytes / (parts * 2);
-    if (!(ctas <= 2 * sms && slice >= 8192) && !(ctas <= 4 * sms && slice >= 36864)) break;
+    if (ctas > 2 * sms && !(ctas <= 4 * sms && slice >= 36864)) break;
     parts *= 2;
   }
   if (static_cast<int64_t>(a.rows) * parts > 0x7fffffff) return record_error(VLA_ERR_UNSUPPORTED, "vla_token_logprobs: too many rows");
