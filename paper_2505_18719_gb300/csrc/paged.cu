@@ -218,8 +218,8 @@ __global__ void __launch_bounds__(256) rope_table_kernel(const RopeTableArgs a, 
 // lane has 4 channels of each half instead (fp32 rows of 32 / 32 heads: 226 us for 18432 against 232; 16-bit ones in pieces
 // of 8 bytes: 131 against 95).  A warp walks over the queries, keys and values of one row, some accesses ahead (the
 // first ones before the row's position is known), and the row's cosines and sines stay in registers; a row of few
-// is cut over several warps so that a decode step fills the GPU.  18432 bf16 rows of 32 / 8 heads of 128 with norms take 76 us
-// (6.0 TB/s of each byte once, 0.88 of the copy rate; three of four issue slots are used), 64 fp32 rows of 32 / 32 heads 2.8 us.
+// is cut over several warps so that a decode step fills the GPU.  18432 bf16 rows of 32 / 8 heads of 128 with norms take 73 us
+// (6.2 TB/s of each byte once, 0.91 of the copy rate; three of four issue slots are used), 64 fp32 rows of 32 / 32 heads 2.8 us.
 enum RopeLayout : int { kNoRope = 0, kHalves = 1, kPairs = 2 };
 
 __device__ __forceinline__ float clamp_f16(float x, uint32_t& sat) {
@@ -280,13 +280,21 @@ __device__ __forceinline__ uint4 pack8(const float (&x)[8], bool f16_type) {
 
 constexpr int kAppendThreads = 128;
 
-// `slices` warps share a row's heads (CUT: more than one).  Accesses ahead and warps an SM as measured on 18432 rows: bf16 of
-// 32 / 8 heads with norms 80 us with 4 ahead and 28 warps, 86 with 20 warps, 92 with 3 ahead and 32 (pairs in halves 89 with 24
-// warps, 95 with 28); f32 of 32 / 32 heads 232 us with 2 ahead and 28 warps, 283 with 4 and the fewer warps that leaves.  CUT and
-// HD known when compiled: 65536 rows of 64 / 8 heads 437 us, 482 without.
+// `slices` warps share a row's heads (CUT: more than one).  Accesses ahead and warps an SM as measured on 18432 bf16 rows of
+// 32 / 8 heads with norms, in pairs and in halves: 3 ahead and 32 warps 73 and 79 us, 4 and 28 76 and 80, 4 and 32 74 and 102 (too
+// few registers), 2 and 32 79 and 80, 3 and 36 92 and 105; 15600 rows of 32 / 32 heads in halves without norms 120 with 3 and 32, 116
+// with 4 and 28; f32 of 32 / 32 heads 225 with 2 ahead, 276 with 4.  CUT and HD known when
+// compiled: 65536 rows of 64 / 8 heads 437 us, 482 without.
+template <int DT, int LAYOUT, bool NORM>
+struct Ahead {
+  static constexpr bool kPlainHalves = LAYOUT == kHalves && !NORM;
+  static constexpr int kAccesses = DT == VLA_F32 ? 2 : kPlainHalves ? 4 : 3;
+  static constexpr int kCtas = DT == VLA_F32 ? (LAYOUT == kHalves && NORM ? 6 : 7) : kPlainHalves ? 7 : 8;
+};
+
 template <int DT, int LAYOUT, bool NORM, bool CUT, int HD>
-__global__ void __launch_bounds__(kAppendThreads, LAYOUT == kHalves && NORM ? 6 : 7) rope_append_kernel(const RopeAppendArgs a, const int slices, const int page_shift) {
-  constexpr int kAhead = DT == VLA_F32 ? 2 : 4, kSize = DT == VLA_F32 ? 4 : 2, kSpan = 256;  // channels of an access
+__global__ void __launch_bounds__(kAppendThreads, Ahead<DT, LAYOUT, NORM>::kCtas) rope_append_kernel(const RopeAppendArgs a, const int slices, const int page_shift) {
+  constexpr int kAhead = Ahead<DT, LAYOUT, NORM>::kAccesses, kSize = DT == VLA_F32 ? 4 : 2, kSpan = 256;  // channels of an access
   constexpr bool kSplit = LAYOUT == kHalves && DT == VLA_F32, kShuffle = LAYOUT == kHalves && !kSplit;
   pdl_launch_dependents();
   pdl_wait();
@@ -492,8 +500,9 @@ int append_of(const RopeAppendArgs& a, cudaStream_t s) {
   int dev = 0, sms = 0;
   VLA_CUDA_TRY(cudaGetDevice(&dev));
   VLA_CUDA_TRY(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-  // a warp per row once they give every SM 32 warps; fewer rows are cut, down to one access a warp
-  const int64_t want = (32LL * sms + a.rows - 1) / a.rows;
+  // fewer rows than give every SM 32 warps are cut into as many slices as stay below that, down to one access a warp (300 bf16 rows of
+  // 28 / 4 heads 4.2 us, 4.8 rounded up; 4500 18.3 and 22.1; 3000 fp16 rows of 32 / 8 heads 20.4 and 18.3)
+  const int64_t want = 32LL * sms / a.rows;
   const int slices = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(want, steps)));
   const int64_t units = static_cast<int64_t>(a.rows) * slices, grid = (units + kAppendThreads / 32 - 1) / (kAppendThreads / 32);
   if (grid > 0x7fffffff) return record_error(VLA_ERR_UNSUPPORTED, "vla_rope_append: too many rows");
