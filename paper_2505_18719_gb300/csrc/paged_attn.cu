@@ -30,8 +30,8 @@
 //
 // Measured, heads of 128, each cached byte once: 64 rows x 32 heads over 273 to 311 positions 52 us (5.9 TB/s, 0.88 of the copy rate:
 // 5 us before the first bytes arrive and after the last, and 7 items on the fullest CTA where the mean is 6.7), 256 rows x 32 heads
-// over 1031 to 1097 positions 669 to 690 us (6.5 to 6.7 TB/s), 8 rows x 8 key-value heads over up to 131072 positions 280 to 286 us
-// (6.7 TB/s); 4 rows x 4 heads of 64 over 80 positions 3.8 us, a chain of latencies.
+// over 1031 to 1097 positions 661 to 690 us (6.5 to 6.8 TB/s), 8 rows x 8 key-value heads over up to 131072 positions 279 to 286 us
+// (6.8 TB/s); 4 rows x 4 heads of 64 over 80 positions 3.8 us, a chain of latencies.
 #include <algorithm>
 #include <type_traits>
 
