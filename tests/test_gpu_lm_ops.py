@@ -650,6 +650,37 @@ def test_token_logprobs_nonfinite_and_bad_tokens():
     assert torch.equal(only["entropy"], clean["entropy"])
 
 
+# 32, 64 and 128 threads a row; rows cut over 2, 4 and 8 CTAs (16-bit rows of 41111 ids stay whole)
+@pytest.mark.parametrize("act", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,vocab,pad", [(4000, 300, 3), (2000, 700, 1), (2100, 1290, 0), (1000, 2999, 2), (200, 41111, 1), (130, 90001, 3),
+                                            (20, 90001, 5)])
+@pytest.mark.parametrize("T,top", [(1.0, 0), (1.5, 2), (0.7, 32)])
+def test_token_logprobs_threads_and_cuts(act, rows, vocab, pad, T, top):
+    test_token_logprobs(act, rows, vocab, pad, T, top)
+
+
+@pytest.mark.parametrize("act", ["f32", "bf16"])
+def test_token_logprobs_ties_and_masks_of_cut_rows(act):
+    test_token_logprobs_ties_and_masks(act, 100003)
+
+
+@pytest.mark.parametrize("act", ["f32", "f16"])
+def test_token_logprobs_nonfinite_in_a_slice(act):
+    g = gen(9)
+    x = normal(g, 6, 100001, dtype=TYPE[act])
+    x[1, 99999] = float("nan")
+    x[3, 40000] = float("inf")
+    x[5, 0] = float("nan")
+    tokens = ints([1, 99999, 2, 50000, 100000, 7])
+    clean = logprob_call(x[::2].contiguous(), tokens[::2].contiguous(), 1.0, 5, act)
+    assert status() == 0
+    got = logprob_call(x, tokens, 1.0, 5, act)
+    assert status() == V.VLA_STATUS_NONFINITE
+    for k in ("logprob", "entropy", "lse", "lps"):
+        assert torch.equal(got[k][::2], clean[k]) and bool(torch.isnan(got[k][1::2]).all()), k
+    assert torch.equal(got["ids"][::2], clean["ids"])
+
+
 # ------------------------------------------------------------------------------------------ gradient
 def grad_call(x, tokens, T, lse, entropy, g, h, act, out=None):
     n, vocab = x.shape
