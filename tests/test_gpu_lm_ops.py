@@ -430,6 +430,19 @@ def test_paged_attn_lengths(act, cache, lengths, H, Hk, hd):
 
 
 @pytest.mark.parametrize("act,cache", TYPES)
+@pytest.mark.parametrize("ps,H,Hk,hd", [(16, 12, 12, 128), (24, 12, 12, 128), (5, 12, 12, 128), (32, 10, 10, 64), (12, 10, 10, 64), (16, 28, 4, 128),
+                                        (40, 16, 4, 64), (8, 16, 1, 64)])
+def test_paged_attn_many_short_items(act, cache, ps, H, Hk, hd):
+    # single warps take whole items, one to three each, some of no position; then a few longer ones, which all warps share
+    lengths = [(7 * e) % 41 for e in range(110 * 12 // Hk)]
+    for n in (0, 900):
+        s = attend_state(ps + n, lengths + [n], H, Hk, hd, act, cache, ps, "head")
+        out, lse = attend_call(*s, act, cache, hd ** -0.5, workspace(hd))
+        attend_check(*s[:4], ps, s[4], s[5], act, cache, out, lse, hd ** -0.5)
+    assert status() == 0
+
+
+@pytest.mark.parametrize("act,cache", TYPES)
 def test_paged_attn_peaked_weights_over_a_flat_tail(act, cache):
     # one position holds half of the weight, 30000 others share the rest: each of their weights is 1e-5
     n, hd = 30001, 64
