@@ -290,6 +290,16 @@ def test_rope_append_rows_pages_and_orders(rows, ps, order):
     assert status() == 0
 
 
+@pytest.mark.parametrize("act,cache", [("f32", "f16"), ("f16", "f16"), ("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f16")])
+@pytest.mark.parametrize("H,Hk,hd,dim,interleaved", [(5, 2, 64, 64, False), (9, 1, 64, 32, True), (6, 2, 128, 128, False), (4, 4, 128, 64, True),
+                                                     (3, 1, 64, 0, False), (2, 2, 128, 0, False)])
+@pytest.mark.parametrize("norm", [False, True])
+def test_rope_append_whole_rows(act, cache, H, Hk, hd, dim, interleaved, norm):
+    # more rows than are cut over several warps
+    append_case(H * hd + dim, 5003, H, Hk, hd, act, cache, norm, dim, interleaved, 16, "slot", pad=8, holes=((3, "pos"), (4999, "slot"), (5002, "pos")))
+    assert status() == 0
+
+
 def test_rope_append_status_and_saturation():
     g = gen(1)
     k_cache, v_cache = make_cache(g, 2, 4, 1, 64, "f16", "head", fill=5.0)
