@@ -97,11 +97,17 @@ __device__ __forceinline__ float float_of(int order) { return __int_as_float(ord
 __device__ __forceinline__ float key_value(int64_t key) { return float_of(static_cast<int>(key >> 32)); }
 __device__ __forceinline__ int key_id(int64_t key) { return 0x7fffffff - static_cast<int>(key & 0x7fffffff); }
 
-// Whether the rounding of r = m c may be more than a fraction of a power of two.
-__device__ __forceinline__ bool is_far(float m, float c) { return m != -INFINITY && !(fabsf(m * c) < 16777216.f); }
+// m c rounded, as a reference has to be before anything is taken from it: a compiler that makes one fma of the product and the
+// subtraction has another reference there, off by up to half an ulp (3e-4 in each log-prob at logits of 1e4).
+__device__ __forceinline__ float rounded_product(float m, float c) { return __fmul_rn(m, c); }
+// Whether the rounding of m c may be more than a fraction of a power of two.
+__device__ __forceinline__ bool is_far(float m, float c) { return m != -INFINITY && !(fabsf(rounded_product(m, c)) < 16777216.f); }
 // The reference that goes with a maximum of some of a row's logits: none for one so low that its logits weigh nothing
 // beside any row that is not far.
-__device__ __forceinline__ float reference_of(float m, float c) { return m * c > -16777216.f ? m * c : -INFINITY; }
+__device__ __forceinline__ float reference_of(float m, float c) {
+  const float r = rounded_product(m, c);
+  return r > -16777216.f ? r : -INFINITY;
+}
 
 // Below 2^-200 a weight is 0, and 0 * -infinity no number.
 constexpr float kFloor = -200.f;
@@ -242,7 +248,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
     x.r = 0.f;
     for (int j = tid; j < n; j += THREADS) x.add((V::load(base, j) - top) * c);
   } else if (x.r != -INFINITY) {
-    x.rise(top * c);
+    x.rise(rounded_product(top, c));
   }
   x.s = warp_sum(x.s);
   x.w = warp_sum(x.w);
@@ -268,8 +274,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
     if (lane == 0) bound = v;
   }
   __syncthreads();
-  Sums total;  // relative to the maximum `top`
-  total.r = far ? 0.f : top * c;
+  Sums total;  // relative to the reference of the maximum `top`, or (far) to the maximum
 #pragma unroll
   for (int i = 0; i < kWarps; ++i) {
     total.s += red[1][i];
@@ -277,7 +282,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
   }
 
   // The row's numbers, of all slices once they have met; the difference to the maximum in natural units (a log-prob may be
-  // as low as a type's lowest value), and what the rounded reference is off the maximum.
+  // as low as a type's lowest value), and what the reference is off the maximum.
   float log2_s, r, rest;
   bool bad, none, apart;
   auto settle = [&]() {
@@ -285,7 +290,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
     none = top == -INFINITY;
     apart = !bad && is_far(top, c);
     log2_s = log2f(total.s);
-    r = top * c;
+    r = rounded_product(top, c);
     rest = (apart ? 0.f : fmaf(top, c, -r)) - log2_s;
   };
   auto logprob = [&](float z) { return bad ? NAN : none ? -INFINITY : fmaf(rest, kLn2, (z - top) * inv_t); };
@@ -407,7 +412,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
     for (int i = 0; i < parts; ++i) top = max_nan(top, all_slices[i][0]);
     total.s = total.w = 0.f;
     for (int i = 0; i < parts; ++i) {
-      const float m = all_slices[i][0], wide = is_far(m, c) || is_far(top, c) ? (m - top) * c : m * c - top * c;
+      const float m = all_slices[i][0];
+      const float wide = is_far(m, c) || is_far(top, c) ? (m - top) * c : rounded_product(m, c) - rounded_product(top, c);
       if (m == -INFINITY) continue;
       const float d = fmaxf(wide, kFloor), f = exp2_fast(d);
       total.s = fmaf(f, all_slices[i][1], total.s);
@@ -430,7 +436,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
   if (tid == 0) {
     if (bad) raise_status(a.status, VLA_STATUS_NONFINITE);
     if (a.lse) a.lse[row] = bad ? NAN : none ? -INFINITY : apart ? fmaf(top, inv_t, log2_s * kLn2) : (r + log2_s) * kLn2;
-    if (a.entropy) a.entropy[row] = bad ? NAN : none ? 0.f : (log2_s - total.w / total.s) * kLn2;
+    if (a.entropy) a.entropy[row] = bad ? NAN : none ? 0.f : fmaf(log2_s, total.s, -total.w) / total.s * kLn2;
     if (a.logprob) a.logprob[row] = token < 0 ? 0.f : logprob(chosen);
   }
 }

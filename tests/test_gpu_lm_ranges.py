@@ -1,0 +1,54 @@
+"""The token log-probs far from zero, against plain 64-bit forms.
+
+A log-prob depends on differences of logits alone, so its tolerance here goes by the row's spread, not by how far from
+zero the row lies: `E` = 2^-24 for every 32-bit rounding, 8 of them for a difference and its products, and those of a
+sum of `vocab` weights as in test_gpu_lm_ops.py."""
+import math
+
+import pytest
+import torch
+
+from tests.test_gpu_lm_ops import E, F64, TYPE, gen, logprob_call, logprob_reference, normal, status, within
+
+pytestmark = pytest.mark.gpu
+
+
+def spread_of(x, T):
+    """Largest less smallest finite logit of each row, over T."""
+    z = x.to(F64)
+    finite = torch.isfinite(z)
+    top = torch.where(finite, z, -math.inf).amax(-1)
+    low = torch.where(finite, z, math.inf).amin(-1)
+    return ((top - low) / T).clamp(min=0.0)
+
+
+def check_differences(x, tokens, T, top, got):
+    want = logprob_reference(x, tokens, T, top)
+    vocab = x.shape[1]
+    tol = 8 * E * spread_of(x, T) + (32 + 4 * vocab ** 0.5) * E + 8 * E * math.log(vocab + 1)
+    within(got["logprob"], want["logprob"], 2 * tol, "logprob")
+    within(got["entropy"], want["entropy"], tol * (2 + math.log(vocab)), "entropy")
+    # the log-sum itself has the size of the logits
+    size = torch.where(torch.isfinite(x), x.to(F64), 0.0).abs().amax(-1) / T
+    within(got["lse"], want["lse"], 8 * E * size + tol, "lse")
+    if top:
+        assert torch.equal(got["ids"].long(), want["ids"]), "ids"
+        within(got["lps"], want["lps"], 2 * tol[:, None], "top log-probs")
+
+
+# a row of one warp, of a CTA, of a CTA with all its rounds, and one cut over a cluster
+VOCABS = [(6, 40), (9, 4099), (5, 32064), (3, 100003)]
+
+
+@pytest.mark.parametrize("act", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows,vocab", VOCABS)
+@pytest.mark.parametrize("T", [1.0, 0.7, 1.5])
+def test_token_logprobs_keep_their_bits_far_from_zero(act, rows, vocab, T):
+    g = gen(vocab + 1)
+    for far in (0.0, 31.0, 1e3, 1e4, 1e5, 1e6, 9e6, 3e7, 1e9) if act == "f32" else (0.0, 31.0, 1e3, 1e4):
+        for sign in (-1.0, 1.0):
+            x = (normal(g, rows, vocab, std=2.5) + sign * far).to(TYPE[act])
+            tokens = torch.randint(0, vocab, (rows,), generator=g, device="cuda").to(torch.int32)
+            got = logprob_call(x, tokens, T, 0, act)
+            assert status() == 0
+            check_differences(x, tokens, T, 0, got)
