@@ -101,16 +101,23 @@ __device__ __forceinline__ int key_id(int64_t key) { return 0x7fffffff - static_
 // subtraction has another reference there, off by up to half an ulp (3e-4 in each log-prob at logits of 1e4).
 __device__ __forceinline__ float rounded_product(float m, float c) { return __fmul_rn(m, c); }
 // Whether the rounding of m c may be more than a fraction of a power of two.
-__device__ __forceinline__ bool is_far(float m, float c) { return m != -INFINITY && !(fabsf(rounded_product(m, c)) < 16777216.f); }
-// The reference that goes with a maximum of some of a row's logits: none for one so low that its logits weigh nothing
-// beside any row that is not far.
-__device__ __forceinline__ float reference_of(float m, float c) {
-  const float r = rounded_product(m, c);
-  return r > -16777216.f ? r : -INFINITY;
-}
-
+constexpr float kFar = 16777216.f;
+__device__ __forceinline__ bool is_far(float m, float c) { return m != -INFINITY && !(fabsf(rounded_product(m, c)) < kFar); }
 // Below 2^-200 a weight is 0, and 0 * -infinity no number.
 constexpr float kFloor = -200.f;
+// The reference that goes with a maximum of some of a row's logits: none for one so low that its logits weigh nothing
+// beside any row that is not far, that is, more than the floor below the lowest of those.
+__device__ __forceinline__ float reference_of(float m, float c) {
+  const float r = rounded_product(m, c);
+  return r > -kFar - 256.f ? r : -INFINITY;
+}
+static_assert(-kFloor < 256.f, "what has no reference weighs nothing");
+// The reference of a set of maximum m (m c itself where that is far, else rounded) less that of one of maximum top.
+__device__ __forceinline__ float reference_difference(float m, float top, float c) {
+  const float low = rounded_product(m, c), high = rounded_product(top, c);
+  if (is_far(m, c)) return is_far(top, c) ? (m - top) * c : fmaf(m, c, -high);
+  return is_far(top, c) ? -fmaf(top, c, -low) : low - high;
+}
 
 // Running sums of a set of logits relative to 2^r; r = -infinity: nothing but zeros so far.
 struct Sums {
@@ -413,9 +420,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
     total.s = total.w = 0.f;
     for (int i = 0; i < parts; ++i) {
       const float m = all_slices[i][0];
-      const float wide = is_far(m, c) || is_far(top, c) ? (m - top) * c : rounded_product(m, c) - rounded_product(top, c);
       if (m == -INFINITY) continue;
-      const float d = fmaxf(wide, kFloor), f = exp2_fast(d);
+      const float d = fmaxf(reference_difference(m, top, c), kFloor), f = exp2_fast(d);
       total.s = fmaf(f, all_slices[i][1], total.s);
       total.w = fmaf(f, fmaf(d, all_slices[i][1], all_slices[i][2]), total.w);
     }

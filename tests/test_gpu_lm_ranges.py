@@ -8,7 +8,7 @@ import math
 import pytest
 import torch
 
-from tests.test_gpu_lm_ops import E, F64, TYPE, gen, logprob_call, logprob_reference, normal, status, within
+from tests.test_gpu_lm_ops import E, F64, TYPE, gen, ints, logprob_call, logprob_reference, normal, status, within
 
 pytestmark = pytest.mark.gpu
 
@@ -52,3 +52,20 @@ def test_token_logprobs_keep_their_bits_far_from_zero(act, rows, vocab, T):
             got = logprob_call(x, tokens, T, 0, act)
             assert status() == 0
             check_differences(x, tokens, T, 0, got)
+
+
+@pytest.mark.parametrize("rows,vocab", VOCABS)
+@pytest.mark.parametrize("limit,T", [(11629079.5, 1.0), (11.6290795, 2.0 ** -20 * 1.048576), (2907269.75, 0.25)])
+def test_token_logprobs_around_the_largest_reference(rows, vocab, limit, T):
+    # rows whose logits lie on both sides of z log2(e) / T = -2^24, from which on differences are taken first
+    T = float(torch.tensor(T, dtype=torch.float32))
+    g = gen(vocab)
+    steps = torch.randint(-3, 4, (rows, vocab), generator=g, device="cuda").to(torch.float32)
+    for sign in (-1.0, 1.0):
+        x = sign * limit + steps * T
+        x[0] = -math.inf  # one weight of e^-1 beside the largest, from one thread (and slice) to another
+        x[0, 0], x[0, vocab - 1] = sign * limit + 0.5 * T, sign * limit - 0.5 * T
+        tokens = ints([vocab - 1] + list(range(1, rows)))
+        got = logprob_call(x, tokens, T, 2, "f32")
+        assert status() == 0
+        check_differences(x, tokens, T, 2, got)
