@@ -139,7 +139,9 @@ int vla_token_logprobs(const void* logits, int64_t ld, int dtype, int rows, int 
  *   d_logits[r][j] = (g_logprob ([j = token] - p_j) - g_entropy p_j (log p_j + entropy)) / T,
  * of type `dtype`, row stride ldd; may be the logits themselves (same stride).  lse and entropy f32 [rows]
  * are those of vla_token_logprobs at the same T; g_logprob f32 [rows]; g_entropy f32 [rows] or NULL (zeros; entropy
- * may then be NULL).  Rows whose token is -1 (or out of range, as above) get zeros.  rows 0 or more. */
+ * may then be NULL).  Where |lse| is 128 or more, and its rounding to 32 bits would show in p_j, the row's maximum and the sum
+ * relative to it are taken from the logits again.  Rows whose token is -1 (or out of range, as above) get zeros.
+ * rows 0 or more. */
 int vla_token_logprobs_grad(const void* logits, int64_t ld, int dtype, int rows, int vocab, const int32_t* tokens, float temperature,
                             const float* lse, const float* entropy, const float* g_logprob, const float* g_entropy,
                             void* d_logits, int64_t ldd, void* cuda_stream);

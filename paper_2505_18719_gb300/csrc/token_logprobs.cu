@@ -290,15 +290,14 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
 
   // The row's numbers, of all slices once they have met; the difference to the maximum in natural units (a log-prob may be
   // as low as a type's lowest value), and what the reference is off the maximum.
-  float log2_s, r, rest;
+  float log2_s, rest;
   bool bad, none, apart;
   auto settle = [&]() {
     bad = !(top < INFINITY);
     none = top == -INFINITY;
     apart = !bad && is_far(top, c);
     log2_s = log2f(total.s);
-    r = rounded_product(top, c);
-    rest = (apart ? 0.f : fmaf(top, c, -r)) - log2_s;
+    rest = (apart ? 0.f : fmaf(top, c, -rounded_product(top, c))) - log2_s;
   };
   auto logprob = [&](float z) { return bad ? NAN : none ? -INFINITY : fmaf(rest, kLn2, (z - top) * inv_t); };
   auto put = [&](int rank, int64_t key) {
@@ -441,20 +440,92 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) token_logprobs_kernel
 
   if (tid == 0) {
     if (bad) raise_status(a.status, VLA_STATUS_NONFINITE);
-    if (a.lse) a.lse[row] = bad ? NAN : none ? -INFINITY : apart ? fmaf(top, inv_t, log2_s * kLn2) : (r + log2_s) * kLn2;
+    // (the maximum in natural units, rounded once with the sum: the gradient's weights are as far off as this is)
+    if (a.lse) a.lse[row] = bad ? NAN : none ? -INFINITY : fmaf(top, inv_t, -rest * kLn2);
     if (a.entropy) a.entropy[row] = bad ? NAN : none ? 0.f : fmaf(log2_s, total.s, -total.w) / total.s * kLn2;
     if (a.logprob) a.logprob[row] = token < 0 ? 0.f : logprob(chosen);
   }
 }
 
+// A log-sum of this size and more is off by over 2^-18 in 32 bits (or is no number of theirs), and each weight e^(z / T - lse) by
+// as much.
+constexpr float kLargeLse = 128.f;
+
+// The largest of n logits and log sum exp((z - largest) / T), by all threads of a cluster of CTAs, each of which gets both.  No CTA
+// returns before all have read their share of the logits.
+template <int DT, int THREADS>
+__device__ __forceinline__ void log_sum_below_top(const char* row, int n, float c, int cluster, float& top, float& log_sum) {
+  using V = Vec<DT>;
+  constexpr int kWarps = THREADS / 32, kUnroll = 4;
+  __shared__ float2 shares[kWarps];  // (largest, sum relative to it) of each warp
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int64_t rank = cluster > 1 ? cluster_ctarank() : 0;
+  const int first = static_cast<int>(n * rank / cluster), mine = static_cast<int>(n * (rank + 1) / cluster) - first;
+  row += static_cast<int64_t>(first) * V::kBytes;
+  const int head = head_of<DT>(row, mine), vecs = (mine - head) / V::kN, tail = mine - head - vecs * V::kN;
+  const uint4* body = reinterpret_cast<const uint4*>(row + head * V::kBytes);
+  float m = -INFINITY, s = 0.f;
+  auto reach = [&](float to) {  // whether there is anything to add
+    if (to > m) {
+      s *= exp2_fast((m - to) * c);
+      m = to;
+    }
+    return m != -INFINITY;
+  };
+  for (int i = tid; i < vecs; i += THREADS * kUnroll) {
+    uint4 v[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      v[u] = make_uint4(V::kLowest, V::kLowest, V::kLowest, V::kLowest);
+      if (i + u * THREADS < vecs) v[u] = body[i + u * THREADS];
+    }
+    uint32_t up = v[0].x;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) up = V::word_max(up, V::word_max(V::word_max(v[u].x, v[u].y), V::word_max(v[u].z, v[u].w)));
+    if (!reach(V::word_float_max(up))) continue;
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      float z[V::kN];
+      V::unpack(v[u], z);
+#pragma unroll
+      for (int j = 0; j < V::kN; ++j) s += exp2_fast((z[j] - m) * c);
+    }
+  }
+  const int edge = tid < head ? tid : tid < head + tail ? mine - tail + tid - head : -1;
+  if (edge >= 0) {
+    const float z = V::load(row, edge);
+    if (reach(z)) s += exp2_fast((z - m) * c);
+  }
+  auto join = [&]() {  // over a warp
+    const float high = warp_max(m);
+    s = warp_sum(m == -INFINITY ? 0.f : s * exp2_fast((m - high) * c));
+    m = high;
+  };
+  join();
+  if (lane == 0) shares[warp] = make_float2(m, s);
+  cluster_sync();
+  m = -INFINITY;
+  s = 0.f;
+  for (int i = lane; i < cluster * kWarps; i += 32) {
+    float2 x;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(mapa_shared(smem_u32(&shares[i % kWarps]), i / kWarps)) : "memory");
+    if (reach(x.x)) s = fmaf(x.y, exp2_fast((x.x - m) * c), s);
+  }
+  join();
+  cluster_sync();  // (until then the others' shared memory is there)
+  top = m;
+  log_sum = log2f(s) * kLn2;
+}
+
 // The gradient, element by element: with d = z / T - lse, -e^d (g + h (d + entropy)) / T, and g / T more at the token.
-// Bound by HBM.  One CTA per row and slice, in 16-byte pieces of the gradient; where the logits lie differently towards
-// 16 bytes, a piece of theirs is cut out of the two aligned ones that it lies in (the row's ends, whose neighbours are
-// not the row's, element by element).  3584 x 32064 bf16 take 68 us (6.7 TB/s, the copy rate); 4000 x 8000 bf16 with
+// Rows far from zero (kLargeLse) are read once more first, for d as a difference to the maximum less a log-sum relative to it,
+// by clusters of their CTAs, in place by all of them.  Bound by HBM.  One CTA per row and slice, in 16-byte
+// pieces of the gradient; where the logits lie differently towards 16 bytes, a piece of theirs is cut out of the two aligned ones
+// that it lies in (the row's ends, whose neighbours are not the row's, element by element).  3584 x 32064 bf16 take 68 us (6.7 TB/s, the copy rate); 4000 x 8000 bf16 with
 // logits 5 elements further apart than the gradient's 25.0 us, 46 element by element.  ALIKE: all rows of both lie alike (known when
 // compiled: 1500 x 20000 bf16 21.4 us, 24.1 with the check; 3000 x 10000 24.1 and 27.2).
 template <int DT, int THREADS, bool ALIKE>
-__global__ void __launch_bounds__(THREADS) token_logprobs_grad_kernel(const LogprobGradArgs a, const int parts) {
+__global__ void __launch_bounds__(THREADS) token_logprobs_grad_kernel(const LogprobGradArgs a, const int parts, const int cluster) {
   using V = Vec<DT>;
   constexpr int kUnroll = 4;
   pdl_launch_dependents();
@@ -464,22 +535,8 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_grad_kernel(const Logp
   const int units = (a.vocab + 63) / 64;
   const int first = static_cast<int>(static_cast<int64_t>(units) * part / parts) * 64;
   const int n = min(a.vocab, static_cast<int>(static_cast<int64_t>(units) * (part + 1) / parts) * 64) - first;
-  int token = a.tokens[row];
-  const bool kept = static_cast<unsigned>(token) < static_cast<unsigned>(a.vocab);
-  if (!kept && token != -1 && part == 0 && tid == 0) raise_status(a.status, VLA_STATUS_BAD_TOKEN);
-  const float lse = a.lse[row], inv_t = 1.f / a.temperature;
-  float g = kept ? a.g_logprob[row] * inv_t : 0.f;
-  const float h = kept && a.g_entropy ? a.g_entropy[row] * inv_t : 0.f;
-  if (kept && lse != lse) g = lse;  // a row whose numbers are none
-  const float gh = h != 0.f ? fmaf(h, a.entropy[row], g) : g;
-  token = kept ? token - first : -1;
   const char* src = static_cast<const char*>(a.logits) + (row * a.ld + first) * V::kBytes;
   char* dst = static_cast<char*>(a.d_logits) + (row * a.ldd + first) * V::kBytes;
-  auto slope = [&](float z) {
-    // below e^-1000 a weight is 0, and 0 * -infinity no number
-    const float d = fmaxf(fmaf(z, inv_t, -lse), -1000.f);
-    return -exp2_fast(d * kLog2e) * fmaf(h, d, gh);
-  };
   const int head = head_of<DT>(dst, n);
   const int off = ALIKE ? 0 : static_cast<int>(reinterpret_cast<uintptr_t>(src + head * V::kBytes) & 15u);
   // pieces [v0, v1) whose logits, or both aligned pieces around them, are the row's
@@ -488,6 +545,40 @@ __global__ void __launch_bounds__(THREADS) token_logprobs_grad_kernel(const Logp
   const uint4* from = reinterpret_cast<const uint4*>(src + head * V::kBytes - off);
   uint4* to = reinterpret_cast<uint4*>(dst + head * V::kBytes);
   const int words = off >> 2, bits = (off & 3) * 8;
+  int token = a.tokens[row];
+  // x = z scale - base, d = x ratio - rest
+  const float inv_t = 1.f / a.temperature;
+  float scale = inv_t, base = a.lse[row], ratio = 1.f, rest = 0.f;
+  const bool kept = static_cast<unsigned>(token) < static_cast<unsigned>(a.vocab);
+  if (!kept && token != -1 && part == 0 && tid == 0) raise_status(a.status, VLA_STATUS_BAD_TOKEN);
+  float g = kept ? a.g_logprob[row] * inv_t : 0.f;
+  float h = kept && a.g_entropy ? a.g_entropy[row] * inv_t : 0.f;
+  if (kept && base != base) g = base;  // a row whose numbers are none
+  token = kept ? token - first : -1;
+  if (kept && fabsf(base) >= kLargeLse) {
+    float top, log_sum;
+    log_sum_below_top<DT, THREADS>(static_cast<const char*>(a.logits) + row * a.ld * V::kBytes, a.vocab, kLog2e * inv_t, cluster, top, log_sum);
+    if (fabsf(top) < INFINITY) {
+      // differences to the top, at the power of two next below 1 / T: no product is rounded.  Where that takes the top past 32 bits,
+      // what is not equal to the top weighs nothing, and does so at a scale that takes the top to 2^100.
+      const uint32_t exponent = (__float_as_uint(top) >> 23) & 255u;
+      scale = __uint_as_float(max(__float_as_uint(inv_t) & 0x7f800000u, 0x00800000u));
+      ratio = inv_t / scale;
+      if (!(fabsf(top * scale) < INFINITY)) {
+        scale = __uint_as_float((354u - exponent) << 23);
+        ratio = 1.f;
+      }
+      base = top * scale;
+      rest = log_sum;
+    }
+  }
+  const float gh = h != 0.f ? fmaf(h, a.entropy[row] - rest, g) : g, to_log2 = ratio * kLog2e, rest2 = rest * kLog2e;
+  h *= ratio;
+  auto slope = [&](float z) {
+    // below e^-1000 a weight is 0, and 0 * -infinity no number
+    const float x = fmaxf(fmaf(z, scale, -base), -1000.f);
+    return -exp2_fast(fmaf(x, to_log2, -rest2)) * fmaf(h, x, gh);
+  };
   for (int i = v0 + tid; i < v1; i += THREADS * kUnroll) {
     uint4 v[kUnroll], w[kUnroll];
 #pragma unroll
@@ -599,8 +690,12 @@ int token_logprobs_grad_launch(const LogprobGradArgs& a, cudaStream_t s) {
   // few rows: slices of at least 2048 elements while the rows alone do not fill the SMs four times; short rows: fewer threads
   // (f16, 64 against 256 threads: 7607 x 1438 13.1 and 26.2 us, 4785 x 5319 19.9 and 24.3, 4000 x 8000 23.6 and 23.8)
   const int threads = a.vocab <= kGradShort ? 64 : 256;
+  // a row's slices are clusters of up to 8, which read a row far from zero together, in place one such cluster (16 x 151936 bf16 4.7 us,
+  // 15.8 with all rows far, 40 where each slice's CTA reads the whole row; clusters cost 0.1 to 0.4 us; in place one row of 151936 3.6
+  // us, 2.2 as 64 slices)
+  const int most = a.d_logits == a.logits ? 8 : 64;
   int parts = 1;
-  while (parts < 64 && static_cast<int64_t>(a.rows) * parts < 4 * sms && a.vocab / (parts * 2) >= 2048) parts *= 2;
+  while (parts < most && static_cast<int64_t>(a.rows) * parts < 4 * sms && a.vocab / (parts * 2) >= 2048) parts *= 2;
   if (static_cast<int64_t>(a.rows) * parts > 0x7fffffff) return record_error(VLA_ERR_UNSUPPORTED, "vla_token_logprobs_grad: too many rows");
   auto pick = [&](auto type) {
     constexpr int DT = decltype(type)::value;
@@ -611,7 +706,8 @@ int token_logprobs_grad_launch(const LogprobGradArgs& a, cudaStream_t s) {
   auto kern = a.dtype == VLA_F32   ? pick(std::integral_constant<int, VLA_F32>())
               : a.dtype == VLA_F16 ? pick(std::integral_constant<int, VLA_F16>())
                                    : pick(std::integral_constant<int, VLA_BF16>());
-  VLA_CUDA_TRY(launch_pdl(kern, dim3(a.rows * parts), dim3(threads), 0, s, a, parts));
+  const int cluster = std::min(parts, 8);
+  VLA_CUDA_TRY(launch_pdl_cluster(kern, dim3(a.rows * parts), dim3(threads), 0, s, cluster, a, parts, cluster));
   note_launch();
   VLA_CUDA_TRY(cudaGetLastError());
   return VLA_OK;
