@@ -108,7 +108,7 @@ int vla_rope_append(const void* q, int64_t ldq, const void* k, int64_t ldk, cons
  *   lse        f32 [rows][n_q_heads] or NULL: log sum_p exp(scale q . K[p]);
  *   workspace  vla_paged_attn_workspace_bytes(hd) bytes, 16-byte aligned, zeroed once before its first use;
  *              every call leaves it fit for the next, of any size.  Not shared by calls that may overlap.
- * f32 queries beyond the fp16 range are read as +-65504 and raise VLA_STATUS_SATURATED.
+ * f32 queries may be of any size: a head counts relative to its largest channel.
  * A row of position -1 gives zeros (lse -infinity).  Positions past row_pos[r] may hold anything (NaN
  * included): they are not read; a NaN or infinity at one that is read may give NaN.  Products and softmax weights keep at least 16 significant bits (22 over an
  * fp16 cache), sums are 32-bit; the split of long contexts and the order of its sums depend on the lengths

@@ -18,7 +18,8 @@
 // ldmatrix reads without bank conflicts.  Scores and outputs run on mma.sync m16n8k16 with the 8 query heads as
 // rows 0-7; rows 8-15 hold the low parts, x - fp16(x) (or bf16), of fp32 queries and of the softmax weights, so that
 // they keep 22 (16) significant bits at no further instruction.  fp16 weights are 2^15 times the true ones: a weight
-// of 1e-5 beside one of 1 keeps its bits.
+// of 1e-5 beside one of 1 keeps its bits.  So do fp32 queries of any size: each head of them is taken times the power of two
+// that brings its largest channel to [2^14, 2^15), and its scores times the inverse.
 //
 // The warps of a CTA meet in shared memory at an item's end, each query head joined by one warp.  With one or two heads
 // a tile that is the warps in turn, over four buffers: the others only arrive at its barrier and go on.  (A warp has its
@@ -390,7 +391,7 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
 
   // ---- computing side
   const int g = lane >> 2, t = lane & 3;
-  const float to_log2 = a.scale * 1.44269504f;
+  float to_log2 = a.scale * 1.44269504f;  // of this lane's query head
   const int tile_heads = ONE ? 1 : min(group, kHeads), buffers = ONE || tile_heads <= 2 ? 4 : tile_heads <= 4 ? 2 : 1;
   uint32_t q[HD / 16][PAIR ? 4 : 2];
   // outputs: c0, c1 of the query head, c2, c3 of the weights' low parts; PAIR: both, added after each step
@@ -420,7 +421,6 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
         uint32_t* mine = reinterpret_cast<uint32_t*>(my_o);
         constexpr int kLanes = HD / 4;
         const int c = lane % kLanes * 4;
-        uint32_t sat = 0;
         constexpr int kApart = 32 / kLanes, kMine = ONE ? 1 : kHeads / kApart;  // this lane's heads, whose loads wait together
         const int h0 = lane / kLanes;
         const float* from = static_cast<const float*>(a.q) + seg.row * a.ldq + static_cast<int64_t>(head0 + h0) * HD + c;
@@ -430,17 +430,34 @@ __global__ void __launch_bounds__(32 * kWarps, Ring<HD>::kCtasPerSm) paged_attn_
           if (h0 + i * kApart < heads) x[i] = *reinterpret_cast<const float4*>(from + i * kApart * HD);
 #pragma unroll
         for (int i = 0; i < kMine; ++i) {
-          if (h0 + i * kApart >= heads) break;
+          if (i * kApart >= heads) break;
+          // exponents of the largest channel from 2^-112 on (below, the two powers of two would leave fp32)
+          uint32_t most = 0;
+          if (h0 + i * kApart < heads) {
+            const float near = fmaxf(fmaxf(fabsf(x[i].x), fabsf(x[i].y)), fmaxf(fabsf(x[i].z), fabsf(x[i].w)));
+            most = __float_as_uint(near);
+          }
+          const uint32_t first = __reduce_max_sync(0xffffffffu, h0 == 0 ? most : 0u);
+          if constexpr (kApart == 2) {
+            const uint32_t second = __reduce_max_sync(0xffffffffu, h0 == 0 ? 0u : most);
+            most = h0 == 0 ? first : second;
+          } else {
+            most = first;
+          }
+          if (h0 + i * kApart >= heads) continue;
+          const uint32_t exponent = min(max(most >> 23, 15u), 254u);
+          const float up = __uint_as_float((268u - exponent) << 23);
+          if (c == 0) crew_ml[sub * tile_heads + h0 + i * kApart].x = __uint_as_float((exponent - 14u) << 23);
           uint2 u, v;
-          split_pack2_f16(x[i].x, x[i].y, u.x, u.y, sat);
-          split_pack2_f16(x[i].z, x[i].w, v.x, v.y, sat);
+          split2<false>(x[i].x * up, x[i].y * up, u.x, u.y);
+          split2<false>(x[i].z * up, x[i].w * up, v.x, v.y);
           // channels 16k + 8 half + 2t: lane t, words 2 half of the k-th step
           uint32_t* dst = mine + (h0 + i * kApart) * HD + c / 16 * 16 + c % 8 * 2 + (c & 8) / 4;
           *reinterpret_cast<uint2*>(dst) = u;
           *reinterpret_cast<uint2*>(dst + 4) = v;
         }
-        report_saturation(a.status, sat);
         __syncwarp();
+        if (g < heads) to_log2 = crew_ml[sub * tile_heads + g].x * a.scale * 1.44269504f;
 #pragma unroll
         for (int k = 0; k < HD / 16; ++k) {
           uint4 x = make_uint4(0u, 0u, 0u, 0u);
