@@ -20,6 +20,10 @@ def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
+def _capturing() -> bool:
+    return torch.cuda.is_current_stream_capturing()
+
+
 def _ptr(t: Optional[torch.Tensor]) -> int:
     return t.data_ptr() if t is not None else 0
 
@@ -61,6 +65,9 @@ class PagedCache:
     """Keys and values of `layers` layers for `n_env` contexts that share `n_pages` pages of `page_size` positions.
 
     A step is ``rows = cache.plan(new_len, max_rows)`` and then, layer by layer, ``cache.append`` and ``cache.attend``.
+
+    ``attend`` may run on several streams at once: each stream has a workspace of its own from its first call on.  Calls
+    captured into CUDA graphs share ``workspace``, so the replays of one cache's graphs follow one another.
     """
 
     def __init__(self, n_env: int, n_pages: int, page_size: int, layers: int, n_heads: int, head_dim: int,
@@ -81,6 +88,16 @@ class PagedCache:
         if not nbytes:
             raise V.VlaError(V.VLA_ERR_UNSUPPORTED, f"heads of {head_dim}")
         self.workspace = torch.zeros(nbytes, dtype=torch.uint8, device=device)
+        self._stream_workspaces: dict[int, torch.Tensor] = {}
+
+    def _workspace(self) -> torch.Tensor:
+        """Partial results and tickets of calls that may overlap must not mix (zeroed in the order of the stream that uses it)."""
+        if _capturing():
+            return self.workspace
+        stream = _stream()
+        if stream not in self._stream_workspaces:
+            self._stream_workspaces[stream] = torch.zeros_like(self.workspace)
+        return self._stream_workspaces[stream]
 
     def plan(self, new_len: torch.Tensor, max_rows: int, release: Optional[torch.Tensor] = None) -> Rows:
         """Takes pages for `new_len` (int32 [n_env] on the GPU) more tokens of each context; `release` (same shape)
@@ -129,10 +146,11 @@ class PagedCache:
         _on_gpu(self.data, q, rows.pos)
         out = torch.empty(q.shape[0], heads, hd, dtype=q.dtype, device=q.device)
         lse = torch.empty(q.shape[0], heads, dtype=torch.float32, device=q.device) if want_lse else None
+        workspace = self._workspace()
         _ok(V.vla_paged_attn(q.data_ptr(), _rows_of(q, heads, hd), _code(q), q.shape[0], heads, self.layers[layer],
                              self.table.data_ptr(), self.max_pages, self.n_env, rows.env.data_ptr(), rows.pos.data_ptr(),
-                             hd ** -0.5 if scale is None else scale, out.data_ptr(), heads * hd, _ptr(lse), self.workspace.data_ptr(),
-                             self.workspace.numel(), _stream()))
+                             hd ** -0.5 if scale is None else scale, out.data_ptr(), heads * hd, _ptr(lse), workspace.data_ptr(),
+                             workspace.numel(), _stream()))
         return (out, lse) if want_lse else out
 
     def free_pages(self) -> int:
