@@ -122,7 +122,7 @@ size_t vla_paged_attn_workspace_bytes(int head_dim);
  * row stride ld elements), as log softmax(z / T) over `vocab` ids:
  *   tokens        int32 [rows] or NULL; -1 = no token in this row (log-prob 0); another id outside
  *                 [0, vocab) is read as -1 and raises VLA_STATUS_BAD_TOKEN;
- *   temperature   T > 0; 0 stands for 1, as in vla_decode_actions;
+ *   temperature   T > 0, and log2(e) / T a 32-bit number (T from 4.3e-39 on); 0 stands for 1, as in vla_decode_actions;
  *   logprob, entropy, lse  f32 [rows]: the token's log-prob, -sum p log p, and log sum exp(z / T); any of
  *                 them may be NULL;
  *   top_ids, top_logprobs  int32 / f32 [rows][top_k]: the top_k largest logits, largest first, the lower id

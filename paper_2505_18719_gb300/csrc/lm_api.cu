@@ -14,6 +14,9 @@ bool misaligned(const void* p, uintptr_t bytes) { return reinterpret_cast<uintpt
 bool is_dtype(int d) { return d == VLA_F32 || d == VLA_F16 || d == VLA_BF16; }
 int elem_bytes(int d) { return d == VLA_F32 ? 4 : 2; }
 
+// 0 stands for 1; the kernels take 1 / T times log2(e), which has to be a 32-bit number.
+bool bad_temperature(float t) { return !(t >= 0.f) || !isfinite(t) || (t > 0.f && !isfinite(1.44269504f * (1.f / t))); }
+
 // Rows of n elements at stride ld that 16-byte accesses can read: VLA_OK or an error code.
 bool bad_rows(const void* p, int64_t ld, int64_t n) { return !p || misaligned(p, 16) || ld < n || (ld & 7); }
 
@@ -129,7 +132,7 @@ int vla_token_logprobs(const void* logits, int64_t ld, int dtype, int rows, int 
                        int top_k, float* logprob, float* entropy, float* lse, int32_t* top_ids, float* top_logprobs,
                        void* cuda_stream) {
   if (!is_dtype(dtype)) return record_error(VLA_ERR_UNSUPPORTED, "vla_token_logprobs: unknown dtype");
-  if (rows < 0 || vocab < 1 || !(temperature >= 0.f) || !isfinite(temperature) || top_k < 0 || top_k > vocab)
+  if (rows < 0 || vocab < 1 || bad_temperature(temperature) || top_k < 0 || top_k > vocab)
     return record_error(VLA_ERR_ARG, "vla_token_logprobs: bad argument");
   if (vocab > kMostIds) return record_error(VLA_ERR_UNSUPPORTED, "vla_token_logprobs: more than 2^30 ids");
   if (top_k > kMaxTopK) return record_error(VLA_ERR_UNSUPPORTED, "vla_token_logprobs: more than 32 alternatives");
@@ -147,7 +150,7 @@ int vla_token_logprobs_grad(const void* logits, int64_t ld, int dtype, int rows,
                             const float* lse, const float* entropy, const float* g_logprob, const float* g_entropy,
                             void* d_logits, int64_t ldd, void* cuda_stream) {
   if (!is_dtype(dtype)) return record_error(VLA_ERR_UNSUPPORTED, "vla_token_logprobs_grad: unknown dtype");
-  if (rows < 0 || vocab < 1 || !(temperature >= 0.f) || !isfinite(temperature))
+  if (rows < 0 || vocab < 1 || bad_temperature(temperature))
     return record_error(VLA_ERR_ARG, "vla_token_logprobs_grad: bad argument");
   if (vocab > kMostIds) return record_error(VLA_ERR_UNSUPPORTED, "vla_token_logprobs_grad: more than 2^30 ids");
   if (rows == 0) return VLA_OK;
