@@ -20,8 +20,7 @@ def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
-def _capturing() -> bool:
-    return torch.cuda.is_current_stream_capturing()
+_capturing = torch.cuda.is_current_stream_capturing
 
 
 def _ptr(t: Optional[torch.Tensor]) -> int:
@@ -90,14 +89,14 @@ class PagedCache:
         self.workspace = torch.zeros(nbytes, dtype=torch.uint8, device=device)
         self._stream_workspaces: dict[int, torch.Tensor] = {}
 
-    def _workspace(self) -> torch.Tensor:
+    def _workspace(self, stream: int) -> torch.Tensor:
         """Partial results and tickets of calls that may overlap must not mix (zeroed in the order of the stream that uses it)."""
         if _capturing():
             return self.workspace
-        stream = _stream()
-        if stream not in self._stream_workspaces:
-            self._stream_workspaces[stream] = torch.zeros_like(self.workspace)
-        return self._stream_workspaces[stream]
+        workspace = self._stream_workspaces.get(stream)
+        if workspace is None:
+            workspace = self._stream_workspaces[stream] = torch.zeros_like(self.workspace)
+        return workspace
 
     def plan(self, new_len: torch.Tensor, max_rows: int, release: Optional[torch.Tensor] = None) -> Rows:
         """Takes pages for `new_len` (int32 [n_env] on the GPU) more tokens of each context; `release` (same shape)
@@ -146,11 +145,12 @@ class PagedCache:
         _on_gpu(self.data, q, rows.pos)
         out = torch.empty(q.shape[0], heads, hd, dtype=q.dtype, device=q.device)
         lse = torch.empty(q.shape[0], heads, dtype=torch.float32, device=q.device) if want_lse else None
-        workspace = self._workspace()
+        stream = _stream()
+        workspace = self._workspace(stream)
         _ok(V.vla_paged_attn(q.data_ptr(), _rows_of(q, heads, hd), _code(q), q.shape[0], heads, self.layers[layer],
                              self.table.data_ptr(), self.max_pages, self.n_env, rows.env.data_ptr(), rows.pos.data_ptr(),
                              hd ** -0.5 if scale is None else scale, out.data_ptr(), heads * hd, _ptr(lse), workspace.data_ptr(),
-                             workspace.numel(), _stream()))
+                             workspace.numel(), stream))
         return (out, lse) if want_lse else out
 
     def free_pages(self) -> int:
