@@ -110,9 +110,9 @@ int vla_rope_append(const void* q, int64_t ldq, const void* k, int64_t ldk, cons
  *              every call leaves it fit for the next, of any size.  Not shared by calls that may overlap.
  * f32 queries may be of any size: a head counts relative to its largest channel.
  * A row of position -1 gives zeros (lse -infinity).  Positions past row_pos[r] may hold anything (NaN
- * included): they are not read; a NaN or infinity at one that is read may give NaN.  Products and softmax weights keep at least 16 significant bits (22 over an
- * fp16 cache), sums are 32-bit; the split of long contexts and the order of its sums depend on the lengths
- * alone, so equal calls give equal bits.  rows 0 or more, rows * n_q_heads at most 2^30. */
+ * included): they are not read; a NaN or infinity at one that is read may give NaN.  Products and softmax weights
+ * keep at least 16 significant bits (22 over an fp16 cache), sums are 32-bit; the split of long contexts and the
+ * order of its sums depend on the lengths alone, so equal calls give equal bits.  rows 0 or more, rows * n_q_heads at most 2^30. */
 int vla_paged_attn(const void* q, int64_t ldq, int dtype, int rows, int n_q_heads, const vla_paged_kv* kv, const int32_t* table,
                    int max_pages, int n_env, const int32_t* row_env, const int32_t* row_pos, float scale, void* out, int64_t ldo,
                    float* lse, void* workspace, size_t workspace_bytes, void* cuda_stream);

@@ -283,7 +283,8 @@ constexpr int kAppendThreads = 128;
 // `slices` warps share a row's heads (CUT: more than one).  Accesses ahead and warps an SM as measured on 18432 bf16 rows of
 // 32 / 8 heads with norms, in pairs and in halves: 3 ahead and 32 warps 73 and 79 us, 4 and 28 76 and 80, 4 and 32 74 and 102 (too
 // few registers), 2 and 32 79 and 80, 3 and 36 92 and 105; 15600 rows of 32 / 32 heads in halves without norms 120 with 3 and 32, 116
-// with 4 and 28; f32 of 32 / 32 heads 225 with 2 ahead, 276 with 4.  CUT and HD known when
+// with 4 and 28; f32 of 32 / 32 heads 225 with 2 ahead, 276 with 4.  (Kernels with norms spill 2 to 28 bytes at these settings; the
+// times have that in them.)  CUT and HD known when
 // compiled: 65536 rows of 64 / 8 heads 437 us, 482 without.
 template <int DT, int LAYOUT, bool NORM>
 struct Ahead {

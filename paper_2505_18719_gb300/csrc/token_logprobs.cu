@@ -24,7 +24,7 @@ namespace vla {
 
 namespace {
 
-constexpr int kLongRow = 160 << 10;  // bytes from which a row of logits may be cut
+constexpr int kLongRow = 160 << 10;  // bytes from which a row of logits may be cut: rows of 128 KB lose by it, of 200 KB gain; between them not measured
 constexpr int kGradShort = 8192;     // ids up to which a row's gradient has 64 threads
 
 constexpr float kLog2e = 1.44269504f, kLn2 = 0.693147181f;
@@ -521,9 +521,10 @@ __device__ __forceinline__ void log_sum_below_top(const char* row, int n, float 
 // Rows far from zero (kLargeLse) are read once more first, for d as a difference to the maximum less a log-sum relative to it,
 // by clusters of their CTAs, in place by all of them.  Bound by HBM.  One CTA per row and slice, in 16-byte
 // pieces of the gradient; where the logits lie differently towards 16 bytes, a piece of theirs is cut out of the two aligned ones
-// that it lies in (the row's ends, whose neighbours are not the row's, element by element).  3584 x 32064 bf16 take 68 us (6.7 TB/s, the copy rate); 4000 x 8000 bf16 with
-// logits 5 elements further apart than the gradient's 25.0 us, 46 element by element.  ALIKE: all rows of both lie alike (known when
-// compiled: 1500 x 20000 bf16 21.4 us, 24.1 with the check; 3000 x 10000 24.1 and 27.2).
+// that it lies in (the row's ends, whose neighbours are not the row's, element by element).  3584 x 32064 bf16 take 68.6 us (6.7 TB/s,
+// the copy rate), 85 where all rows are far from zero; a row waits for its log-sum before its first loads, which is 0.5 us of it.
+// 4000 x 8000 bf16 with logits 5 elements further apart than the gradient's took 25.0 us, 46 element by element.  ALIKE: all rows of
+// both lie alike (known when compiled: 1500 x 20000 bf16 21.4 us, 24.1 with the check; 3000 x 10000 24.1 and 27.2).
 template <int DT, int THREADS, bool ALIKE>
 __global__ void __launch_bounds__(THREADS) token_logprobs_grad_kernel(const LogprobGradArgs a, const int parts, const int cluster) {
   using V = Vec<DT>;
