@@ -1,0 +1,198 @@
+// What one warp does for one row of packed causal attention, in 32 bits and without matrix instructions: the sums of
+// include/vla_learn.h as they stand, over the rows that take part and no others.
+#pragma once
+#include "learn.h"
+
+namespace vla {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct Span {
+  int begin, end;  // rows of a sequence
+};
+// Starts outside the rows and sequences that end before they begin are clamped (and reported by check_starts).
+__device__ __forceinline__ Span span_of(const int* seq_start, int s, int rows) {
+  const int b = min(max(seq_start[s], 0), rows);
+  return Span{b, min(max(seq_start[s + 1], b), rows)};
+}
+// The sequence of a row; {row, row} where it belongs to none.
+__device__ __forceinline__ Span span_of_row(const int* seq_start, int n_seq, int rows, int row) {
+  int lo = 0, hi = n_seq;  // the last start at or before the row
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (seq_start[mid] <= row)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  if (lo == n_seq) return Span{row, row};
+  const Span sp = span_of(seq_start, lo, rows);
+  return sp.begin <= row && row < sp.end ? sp : Span{row, row};
+}
+__device__ __forceinline__ void check_starts(const int* seq_start, int n_seq, int rows, int first, int step, uint32_t* status) {
+  bool bad = false;
+  for (int s = first; s < n_seq; s += step) bad |= seq_start[s] < 0 || seq_start[s + 1] < seq_start[s] || seq_start[s + 1] > rows;
+  if (bad) raise_status(status, VLA_STATUS_SEQUENCES);
+}
+
+// HD / 32 channels of a head, lane after lane.
+template <int HD>
+struct Lane {
+  static constexpr int N = HD / 32;
+  float x[N];
+};
+template <int HD, bool FP16>
+__device__ __forceinline__ Lane<HD> load_lane(const void* row) {
+  Lane<HD> y;
+  const uint32_t* p = static_cast<const uint32_t*>(row) + (threadIdx.x & 31) * (HD / 64);
+#pragma unroll
+  for (int i = 0; i < HD / 64; ++i) {
+    const uint32_t w = p[i];
+    const float2 f = FP16 ? unpack_f16x2(w) : unpack_bf16x2(w);
+    y.x[2 * i] = f.x;
+    y.x[2 * i + 1] = f.y;
+  }
+  return y;
+}
+template <int HD, bool FP16>
+__device__ __forceinline__ void store_lane(void* row, const Lane<HD>& v, float scale) {
+  uint32_t* p = static_cast<uint32_t*>(row) + (threadIdx.x & 31) * (HD / 64);
+#pragma unroll
+  for (int i = 0; i < HD / 64; ++i) {
+    const float a = v.x[2 * i] * scale, b = v.x[2 * i + 1] * scale;
+    p[i] = FP16 ? pack_f16x2(a, b) : pack_bf16x2(a, b);
+  }
+}
+template <int HD>
+__device__ __forceinline__ float lane_dot(const Lane<HD>& a, const Lane<HD>& b) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < Lane<HD>::N; ++i) s = fmaf(a.x[i], b.x[i], s);
+  return s;
+}
+template <int HD>
+__device__ __forceinline__ void lane_add(Lane<HD>& y, float p, const Lane<HD>& v) {
+#pragma unroll
+  for (int i = 0; i < Lane<HD>::N; ++i) y.x[i] = fmaf(p, v.x[i], y.x[i]);
+}
+__device__ __forceinline__ const void* elem(const void* p, int64_t i) { return static_cast<const uint16_t*>(p) + i; }
+__device__ __forceinline__ void* elem(void* p, int64_t i) { return static_cast<uint16_t*>(p) + i; }
+
+// out[row][h] and its lse.
+template <int HD, bool FP16>
+__device__ __noinline__ void attend_row(const PromptArgs& a, int row, int h, int first) {
+  constexpr int U = 4;
+  const int g = h / (a.n_q_heads / a.n_kv_heads);
+  const float c = a.scale * kLog2e;
+  const Lane<HD> q = load_lane<HD, FP16>(elem(a.q, row * a.ldq + h * HD));
+  Lane<HD> o = {};
+  float m = -INFINITY, l = 0.f;
+  for (int j0 = first; j0 <= row; j0 += U) {
+    Lane<HD> v[U];
+    float s[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = min(j0 + u, row);
+      s[u] = lane_dot<HD>(q, load_lane<HD, FP16>(elem(a.k, j * a.ldk + g * HD)));
+      v[u] = load_lane<HD, FP16>(elem(a.v, j * a.ldv + g * HD));
+    }
+    float top = m;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      s[u] = warp_sum(s[u]) * c;
+      if (j0 + u <= row) top = fmaxf(top, s[u]);
+    }
+    const float ref = top == -INFINITY ? 0.f : top, alpha = exp2f(m - ref);
+    m = top;
+    l *= alpha;
+#pragma unroll
+    for (int i = 0; i < Lane<HD>::N; ++i) o.x[i] *= alpha;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (j0 + u > row) continue;
+      const float p = exp2f(s[u] - ref);
+      l += p;
+      if (p != 0.f) lane_add<HD>(o, p, v[u]);
+    }
+  }
+  store_lane<HD, FP16>(elem(a.out, row * a.ldo + h * HD), o, l > 0.f || l != l ? 1.f / l : 0.f);
+  if (a.lse && (threadIdx.x & 31) == 0) a.lse[static_cast<int64_t>(row) * a.n_q_heads + h] = (m + log2f(l)) * kLn2;
+}
+
+// D = d_out . out of one row and head.
+template <int HD, bool FP16>
+__device__ __forceinline__ float row_delta(const PromptGradArgs& a, int row, int h) {
+  return warp_sum(lane_dot<HD>(load_lane<HD, FP16>(elem(a.d_out, row * a.lddo + h * HD)),
+                               load_lane<HD, FP16>(elem(a.f.out, row * a.f.ldo + h * HD))));
+}
+
+// d_q[row][h].
+template <int HD, bool FP16>
+__device__ __noinline__ void grad_query_row(const PromptGradArgs& a, int row, int h, int first, float delta) {
+  constexpr int U = 4;
+  const int g = h / (a.f.n_q_heads / a.f.n_kv_heads);
+  const float c = a.f.scale * kLog2e, lse = a.f.lse[static_cast<int64_t>(row) * a.f.n_q_heads + h] * kLog2e;
+  const Lane<HD> q = load_lane<HD, FP16>(elem(a.f.q, row * a.f.ldq + h * HD));
+  const Lane<HD> d = load_lane<HD, FP16>(elem(a.d_out, row * a.lddo + h * HD));
+  Lane<HD> y = {};
+  for (int j0 = first; j0 <= row; j0 += U) {
+    Lane<HD> k[U];
+    float s[U], t[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int j = min(j0 + u, row);
+      k[u] = load_lane<HD, FP16>(elem(a.f.k, j * a.f.ldk + g * HD));
+      s[u] = lane_dot<HD>(q, k[u]);
+      t[u] = lane_dot<HD>(d, load_lane<HD, FP16>(elem(a.f.v, j * a.f.ldv + g * HD)));
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      s[u] = warp_sum(s[u]);
+      t[u] = warp_sum(t[u]);
+      const float p = exp2f(fmaf(s[u], c, -lse));
+      if (j0 + u <= row && p != 0.f) lane_add<HD>(y, p * (t[u] - delta), k[u]);
+    }
+  }
+  store_lane<HD, FP16>(elem(a.d_q, row * a.lddq + h * HD), y, a.f.scale);
+}
+
+// d_k[row][g] and d_v[row][g]; delta [n_q_heads][rows].
+template <int HD, bool FP16>
+__device__ __noinline__ void grad_key_row(const PromptGradArgs& a, int row, int g, int end, const float* delta) {
+  constexpr int U = 4;
+  const int group = a.f.n_q_heads / a.f.n_kv_heads;
+  const float c = a.f.scale * kLog2e;
+  const Lane<HD> k = load_lane<HD, FP16>(elem(a.f.k, row * a.f.ldk + g * HD));
+  const Lane<HD> v = load_lane<HD, FP16>(elem(a.f.v, row * a.f.ldv + g * HD));
+  Lane<HD> dk = {}, dv = {};
+  for (int h = g * group; h < (g + 1) * group; ++h) {
+    for (int i0 = row; i0 < end; i0 += U) {
+      Lane<HD> q[U], d[U];
+      float s[U], t[U], lse[U], dl[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int i = min(i0 + u, end - 1);
+        q[u] = load_lane<HD, FP16>(elem(a.f.q, i * a.f.ldq + h * HD));
+        d[u] = load_lane<HD, FP16>(elem(a.d_out, i * a.lddo + h * HD));
+        lse[u] = a.f.lse[static_cast<int64_t>(i) * a.f.n_q_heads + h];
+        dl[u] = delta[static_cast<int64_t>(h) * a.f.rows + i];
+        s[u] = lane_dot<HD>(q[u], k);
+        t[u] = lane_dot<HD>(d[u], v);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        s[u] = warp_sum(s[u]);
+        t[u] = warp_sum(t[u]);
+        const float p = exp2f(fmaf(s[u], c, -lse[u] * kLog2e));
+        if (i0 + u < end && p != 0.f) {
+          lane_add<HD>(dv, p, d[u]);
+          lane_add<HD>(dk, p * (t[u] - dl[u]), q[u]);
+        }
+      }
+    }
+  }
+  store_lane<HD, FP16>(elem(a.d_k, row * a.lddk + g * HD), dk, a.f.scale);
+  store_lane<HD, FP16>(elem(a.d_v, row * a.lddv + g * HD), dv, 1.f);
+}
+
+}  // namespace vla

@@ -31,6 +31,7 @@ VLA_STATUS_TIMEOUT = 0x4
 VLA_STATUS_BAD_FORCED = 0x8
 VLA_STATUS_SATURATED = 0x10
 VLA_STATUS_PAGES = 0x20
+VLA_STATUS_SEQUENCES = 0x40
 
 VLA_F32, VLA_F16, VLA_BF16 = 0, 1, 2
 VLA_ROPE_PLAIN, VLA_ROPE_LINEAR, VLA_ROPE_TURNS, VLA_ROPE_LOG_TURNS = 0, 1, 2, 3
@@ -130,6 +131,14 @@ def load(path: str = LIB_PATH):
         "vla_paged_attn_workspace_bytes": (ctypes.c_size_t, [i32]),
         "vla_token_logprobs": (i32, [vp, i64, i32, i32, i32, vp, f32, i32, vp, vp, vp, vp, vp, vp]),
         "vla_token_logprobs_grad": (i32, [vp, i64, i32, i32, i32, vp, f32, vp, vp, vp, vp, vp, i64, vp]),
+        "vla_prompt_attn": (i32, [vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, i32, vp, i32, f32, vp, i64, vp, vp]),
+        "vla_prompt_attn_grad": (i32, [vp, i64, vp, i64, vp, i64, i32, i32, i32, i32, i32, vp, i32, f32, vp, i64, vp, vp, i64, vp, i64, vp,
+                                       i64, vp, i64, vp, ctypes.c_size_t, vp]),
+        "vla_prompt_attn_grad_workspace_bytes": (ctypes.c_size_t, [i32, i32, i32, i32]),
+        "vla_block_norm": (i32, [vp, i64, i32, vp, i64, i32, i32, i32, vp, vp, i64, f32, vp, f32, vp, i64, vp, i64, vp, vp]),
+        "vla_block_norm_grad": (i32, [vp, i64, i32, vp, i64, i32, i32, i32, vp, vp, i64, f32, vp, vp, vp, i64, vp, i64, vp, i64, vp, i64, vp,
+                                      i64, vp, vp, vp, ctypes.c_size_t, vp]),
+        "vla_block_norm_grad_workspace_bytes": (ctypes.c_size_t, [i32, i32]),
         "vla_test_inject_launch_error": (i32, [i64, i32]),
         "vla_test_set_wait_limit_ns": (i32, [ctypes.c_uint64]),
         "vla_test_set_max_cluster": (i32, [i32]),
@@ -412,6 +421,45 @@ def vla_token_logprobs_grad(logits_ptr, ld, dtype, rows, vocab, tokens_ptr, temp
     return load().vla_token_logprobs_grad(logits_ptr or None, ld, dtype, rows, vocab, tokens_ptr or None, temperature,
                                           lse_ptr or None, entropy_ptr or None, g_logprob_ptr or None, g_entropy_ptr or None,
                                           d_logits_ptr or None, ldd, stream or None)
+
+
+def vla_prompt_attn(q_ptr, ldq, k_ptr, ldk, v_ptr, ldv, dtype, rows, n_q_heads, n_kv_heads, head_dim, seq_start_ptr, n_seq, scale,
+                    out_ptr, ldo, lse_ptr=0, stream=0) -> int:
+    return load().vla_prompt_attn(q_ptr or None, ldq, k_ptr or None, ldk, v_ptr or None, ldv, dtype, rows, n_q_heads, n_kv_heads,
+                                  head_dim, seq_start_ptr or None, n_seq, scale, out_ptr or None, ldo, lse_ptr or None, stream or None)
+
+
+def vla_prompt_attn_grad(q_ptr, ldq, k_ptr, ldk, v_ptr, ldv, dtype, rows, n_q_heads, n_kv_heads, head_dim, seq_start_ptr, n_seq, scale,
+                         out_ptr, ldo, lse_ptr, d_out_ptr, lddo, d_q_ptr, lddq, d_k_ptr, lddk, d_v_ptr, lddv, ws_ptr, ws_bytes,
+                         stream=0) -> int:
+    return load().vla_prompt_attn_grad(q_ptr or None, ldq, k_ptr or None, ldk, v_ptr or None, ldv, dtype, rows, n_q_heads, n_kv_heads,
+                                       head_dim, seq_start_ptr or None, n_seq, scale, out_ptr or None, ldo, lse_ptr or None,
+                                       d_out_ptr or None, lddo, d_q_ptr or None, lddq, d_k_ptr or None, lddk, d_v_ptr or None, lddv,
+                                       ws_ptr or None, ws_bytes, stream or None)
+
+
+def vla_prompt_attn_grad_workspace_bytes(rows: int, n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    return load().vla_prompt_attn_grad_workspace_bytes(rows, n_q_heads, n_kv_heads, head_dim)
+
+
+def vla_block_norm(y_ptr, ldy, dtype, h_ptr, ldh, h_dtype, rows, dim, post_gain_ptr, gate_ptr, ldg, residual_scale, pre_gain_ptr, eps,
+                   h_out_ptr, ldho, x_ptr, ldx, rstd_ptr=0, stream=0) -> int:
+    return load().vla_block_norm(y_ptr or None, ldy, dtype, h_ptr or None, ldh, h_dtype, rows, dim, post_gain_ptr or None, gate_ptr or None,
+                                 ldg, residual_scale, pre_gain_ptr or None, eps, h_out_ptr or None, ldho, x_ptr or None, ldx,
+                                 rstd_ptr or None, stream or None)
+
+
+def vla_block_norm_grad(y_ptr, ldy, dtype, h_out_ptr, ldho, h_dtype, rows, dim, post_gain_ptr, gate_ptr, ldg, residual_scale, pre_gain_ptr,
+                        rstd_ptr, d_x_ptr, lddx, d_h_out_ptr, lddho, d_h_ptr, lddh, d_y_ptr, lddy, d_gate_ptr, lddg, d_post_gain_ptr,
+                        d_pre_gain_ptr, ws_ptr, ws_bytes, stream=0) -> int:
+    return load().vla_block_norm_grad(y_ptr or None, ldy, dtype, h_out_ptr or None, ldho, h_dtype, rows, dim, post_gain_ptr or None,
+                                      gate_ptr or None, ldg, residual_scale, pre_gain_ptr or None, rstd_ptr or None, d_x_ptr or None, lddx,
+                                      d_h_out_ptr or None, lddho, d_h_ptr or None, lddh, d_y_ptr or None, lddy, d_gate_ptr or None, lddg,
+                                      d_post_gain_ptr or None, d_pre_gain_ptr or None, ws_ptr or None, ws_bytes, stream or None)
+
+
+def vla_block_norm_grad_workspace_bytes(rows: int, dim: int) -> int:
+    return load().vla_block_norm_grad_workspace_bytes(rows, dim)
 
 
 def vla_test_inject_launch_error(nth_launch: int, cuda_error: int) -> int:
