@@ -6,6 +6,14 @@
 
 namespace vla {
 
+// SMs of the current device.
+inline int device_sms(int* sms) {
+  int dev = 0;
+  VLA_CUDA_TRY(cudaGetDevice(&dev));
+  VLA_CUDA_TRY(cudaDeviceGetAttribute(sms, cudaDevAttrMultiProcessorCount, dev));
+  return VLA_OK;
+}
+
 struct PromptArgs {
   const void* q;
   const void* k;

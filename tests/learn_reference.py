@@ -63,6 +63,8 @@ def prompt_grad(q, k, v, start, scale, out, lse, d_out, act):
     z = lambda n: torch.zeros(rows, n, hd, dtype=F64, device=dev)  # noqa: E731
     dq, tq, dk, tk, dv, tv = z(H), z(H), z(Hk), z(Hk), z(Hk), z(Hk)
     u = 1.01 * U[act]
+    finite = lambda t: torch.where(torch.isfinite(t), t, 0).to(F64)  # noqa: E731
+    most = finite(d_out).norm(dim=-1).max() * finite(v).norm(dim=-1).max()
     for a, b in zip(start[:-1], start[1:]):
         n = b - a
         if not n:
@@ -80,12 +82,12 @@ def prompt_grad(q, k, v, start, scale, out, lse, d_out, act):
             e_d = (G.abs() @ W.abs().T + (G * O).abs().sum(-1, keepdim=True)) * sum_error(hd)
             ds = p * (dp - delta)
             e_ds = (u + e_p) * ds.abs() + p * e_d
-            if act == "f16":  # dS counts relative to the largest it can be over a sequence (38 bits below), P to 1 (14 bits of scale)
-                most = G.norm(dim=-1).max() * W.norm(dim=-1).max()
+            if act == "f16":  # dS counts relative to the largest that it can be (38 bits below), P to 1 (14 bits of scale)
                 e_ds = e_ds + torch.where(seen, most * 2.0 ** -38, 0.0)
                 floor = torch.where(seen, 2.0 ** -38, 0.0).to(F64)
-            else:
-                floor = torch.zeros_like(p)
+            else:  # a weight below the smallest normal number, 2^-126, may count as 0: its terms are lost whole
+                floor = torch.where(seen, 2.0 ** -126, 0.0).to(F64)
+                e_ds = e_ds + floor * (dp.abs() + delta.abs())
             e_w = (u + e_p) * p + floor
             s_n = sum_error(n * group)
             dq[a:b, h] = scale * ds @ K
