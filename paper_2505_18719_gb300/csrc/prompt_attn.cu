@@ -13,7 +13,7 @@
 //
 // Roles (384 threads):
 //   warp 0      TMA: Q tiles when the item before is done with them, key and value blocks into a ring;
-//   warp 1      owns the tensor memory; one thread issues S = Q K^T and O += P V (P in tensor memory over the S it came from, V as the
+//   warp 1      owns the tensor memory; issues S = Q K^T and O += P V (P in tensor memory over the S it came from, V as the
 //               MN-major operand), tile by tile as its operands get ready;
 //   warp 2      a sequence's last values land with it: those behind the last row become zeros (their weights are zeros, but a NaN
 //               would spoil the product), then the block counts as loaded;
@@ -172,89 +172,95 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (used[x]) wait_drain(BAR(QFULL + x), (used[x] - 1) & 1, limit);
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      // ------------------------------------------------------------------ MMAs
-      struct Cursor {
-        int k = 0, j = 0, nb = 0, other = 0, len = 0;  // item, block, its blocks here and of the other tile; sequence
-        int block = 0, base = 0;                       // blocks of this tile so far; blocks of the CTA's items before this one
-        int q = 0;                                     // Q tiles of this tile so far
-        bool open = false, pv = false, done = false;
-      } cur[2];
-      uint64_t t_last = globaltimer();
-      uint32_t spins = 0;
-      const uint32_t is_full = tile_idesc(128, FP16, false), io = tile_idesc(HD, FP16, true);
-      bool ok = true;
-      auto step = [&](Cursor& c, const int x) -> bool {
-        if (c.done) return false;
-        if (!c.open) {
-          if (!mbar_test_wait(BAR(IFULL + (c.k & 7)), (c.k >> 3) & 1)) return false;
-          const Item it = items[c.k & 7];
-          mbar_arrive(BAR(IFREE + (c.k & 7)));
-          ++c.k;
-          if (it.len < 0) return c.done = true;
-          const Tiles t = tiles_of(it, p.group);
-          c.nb = t.nb[x];
-          c.other = t.nb[x ^ 1];
-          c.len = it.len;
-          c.j = 0;
-          c.open = c.nb > 0;
-          if (!c.open) c.base += c.other;
-          return true;
-        }
-        const int keys = min(kTile, c.len - c.j * kTile), f = 2 * (c.base + c.j) + (c.pv ? 1 : 0), s = f % NS;
-        const bool shared = c.j < c.other;
-        if (!c.pv) {
-          // (the scores go over the weights of the block before, which its product has to have read)
-          if (!mbar_test_wait(BAR(KVFULL + s), (f / NS) & 1) || (c.j == 0 && !mbar_test_wait(BAR(QFULL + x), c.q & 1)) ||
-              (c.block > 0 && !mbar_test_wait(BAR(PVDONE + x), (c.block - 1) & 1)))
-            return false;
-          tc_fence_after();
-          const uint64_t dq = tile_desc(s0 + x * Sm::kTileBytes), dk = tile_desc(stage(f));
-#pragma unroll
-          for (int k = 0; k < HD / 16; ++k) tc_mma(tmem + kColS + x * 128, dq + k_major_step(k), dk + k_major_step(k), is_full, k > 0);
-          tc_commit(BAR(SFULL + x));
-          if (c.j == c.nb - 1) {
-            tc_commit(BAR(QFREE + x));
-            ++c.q;
-          }
-        } else {
-          if (!mbar_test_wait(BAR(PFULL + x), c.block & 1) || !mbar_test_wait(BAR(KVFULL + s), (f / NS) & 1)) return false;
-          tc_fence_after();
-          const uint64_t dv = tile_desc(stage(f));
-          const int steps = (keys + 15) / 16;
-          for (int k = 0; k < steps; ++k)
-            tc_mma_ts(tmem + kColO + x * 128, tmem + kColS + x * 128 + k * 8, dv + mn_major_step(k), io, c.j > 0 || k > 0);
-          tc_commit(BAR(PVDONE + x));
-        }
-        tc_commit(BAR(KVFREE + s));
-        if (!shared) tc_commit(BAR(KVFREE + s));
-        if (c.pv) {
-          ++c.block;
-          if (++c.j == c.nb) {
-            c.open = false;
-            c.base += max(c.nb, c.other);
-          }
-        }
-        c.pv = !c.pv;
+    // ------------------------------------------------------------------ MMAs
+    struct Cursor {
+      int k = 0, j = 0, nb = 0, other = 0, len = 0;  // item, block, its blocks here and of the other tile; sequence
+      int block = 0, base = 0;                       // blocks of this tile so far; blocks of the CTA's items before this one
+      int q = 0;                                     // Q tiles of this tile so far
+      bool open = false, pv = false, done = false;
+    } cur[2];
+    uint64_t t_last = 0;
+    uint32_t spins = 0;
+    const uint32_t is = tile_idesc(128, FP16, false), io = tile_idesc(HD, FP16, true);
+    auto ready = [&](int bar, int phase) { return warp_ready(BAR(bar), static_cast<uint32_t>(phase) & 1u); };
+    bool ok = true;
+    auto step = [&](Cursor& c, const int x) -> bool {
+      if (c.done) return false;
+      if (!c.open) {
+        if (!ready(IFULL + (c.k & 7), c.k >> 3)) return false;
+        const Item* src = items + (c.k & 7);
+        const Item it{0, uniform(src->len), uniform(src->a), uniform(src->b)};
+        if (lane == 0) mbar_arrive(BAR(IFREE + (c.k & 7)));
+        ++c.k;
+        if (it.len < 0) return c.done = true;
+        const Tiles t = tiles_of(it, p.group);
+        c.nb = t.nb[x];
+        c.other = t.nb[x ^ 1];
+        c.len = it.len;
+        c.j = 0;
+        c.open = c.nb > 0;
+        if (!c.open) c.base += c.other;
         return true;
-      };
-      while (ok && !(cur[0].done && cur[1].done)) {
-        const bool did = step(cur[0], 0) | step(cur[1], 1);
-        if (did) {
-          t_last = globaltimer();
-        } else if (((++spins) & 63u) == 0) {
-          if (*abort_flag) {
-            ok = false;
-          } else if (globaltimer() - t_last > limit) {
-            *abort_flag = 1;
-            if (status) atomicOr(status, VLA_STATUS_TIMEOUT);
-            ok = false;
-          }
+      }
+      const int f = 2 * (c.base + c.j) + (c.pv ? 1 : 0), s = f % NS;
+      const bool shared = c.j < c.other, last = c.j == c.nb - 1;
+      const uint32_t tS = tmem + kColS + x * 128, operand = tile_desc(stage(f));
+      if (!c.pv) {
+        // (the scores go over the weights of the block before, which its product has to have read)
+        if (!ready(KVFULL + s, f / NS) || (c.j == 0 && !ready(QFULL + x, c.q)) || (c.block > 0 && !ready(PVDONE + x, c.block - 1))) return false;
+        tc_fence_after();
+        const uint32_t dq = tile_desc(s0 + x * Sm::kTileBytes);
+        if (elected()) {
+#pragma unroll
+          for (int k = 0; k < HD / 16; ++k) tile_mma(tS, dq + k_major_step(k), operand + k_major_step(k), is, k > 0);
+          tc_commit(BAR(SFULL + x));
+          if (last) tc_commit(BAR(QFREE + x));
+          tc_commit(BAR(KVFREE + s));
+          if (!shared) tc_commit(BAR(KVFREE + s));
+        }
+        if (last) ++c.q;
+      } else {
+        if (!ready(PFULL + x, c.block) || !ready(KVFULL + s, f / NS)) return false;
+        tc_fence_after();
+        const int steps = (min(kTile, c.len - c.j * kTile) + 15) / 16;
+        const uint32_t tO = tmem + kColO + x * 128, more = c.j > 0;
+        if (elected()) {
+#pragma unroll
+          for (int k = 0; k < kTile / 16; ++k)
+            if (k < steps) tile_mma_ts(tO, tS + k * 8, operand + mn_major_step(k), io, k > 0 ? 1u : more);
+          tc_commit(BAR(PVDONE + x));
+          tc_commit(BAR(KVFREE + s));
+          if (!shared) tc_commit(BAR(KVFREE + s));
+        }
+        ++c.block;
+        if (++c.j == c.nb) {
+          c.open = false;
+          c.base += max(c.nb, c.other);
         }
       }
-      tc_commit(BAR(DRAIN));
-      wait_drain(BAR(DRAIN), 0, limit);
+      __syncwarp();
+      c.pv = !c.pv;
+      return true;
+    };
+    while (ok && !(cur[0].done && cur[1].done)) {
+      const bool did = step(cur[0], 0) | step(cur[1], 1);
+      if (did) {
+        spins = 0;
+      } else if (((++spins) & 1023u) == 0) {  // (the clock is slow to read)
+        if (spins == 1024) t_last = globaltimer();
+        if (__any_sync(0xffffffffu, *abort_flag != 0)) {
+          ok = false;
+        } else if (__any_sync(0xffffffffu, globaltimer() - t_last > limit)) {
+          if (lane == 0) {
+            *abort_flag = 1;
+            if (status) atomicOr(status, VLA_STATUS_TIMEOUT);
+          }
+          ok = false;
+        }
+      }
     }
+    if (elected()) tc_commit(BAR(DRAIN));
+    wait_drain(BAR(DRAIN), 0, limit);
   } else if (warp == 2) {
     // ------------------------------------------------------------------ values behind the last row
     int base = 0;

@@ -307,6 +307,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint32_t* status = f.status;
   const uint64_t limit = p.wait_limit;
   auto wait1 = [&](int bar, int phase) { return wait_bounded(sh.bar(bar), static_cast<uint32_t>(phase) & 1u, sh.abort_flag, status, limit); };
+  auto waita = [&](int bar, int phase) { return warp_wait_all(sh.bar(bar), static_cast<uint32_t>(phase) & 1u, sh.abort_flag, status, limit); };
   auto waitw = [&](int bar, int phase) { return warp_waits(sh.bar(bar), static_cast<uint32_t>(phase) & 1u, sh.abort_flag, status, limit); };
   auto tiles = [](const Item& it) { return (it.len + kTile - 1) / kTile; };
   auto rows_of = [](const Item& it, int t) { return min(kTile, it.len - t * kTile); };
@@ -348,79 +349,100 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (n_v) wait_drain(sh.bar(BFULL), (n_v - 1) & 1, limit);
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      const uint32_t tS = tmem, tP = tmem + 128, tV = tmem + 256, tK = tmem + 384;
-      const uint64_t dk = tile_desc(sh.s0), dv = tile_desc(sh.s0 + Sm::kTileBytes);
-      const uint32_t io = tile_idesc(HD, FP16, true);
-      int w = 0, k = 0;
-      Item it;
-      bool ok = true;
-      for (; ok && next_item(sh, k, it, status, limit, false); ++k) {
-        const int nt = tiles(it), per_head = nt - it.a, units = per_head * p.group;
-        auto steps_of = [&](int u) { return (rows_of(it, nt - 1 - u % per_head) + 15) / 16; };
-        // S of block u; dP
-        auto scores = [&](int u) {
-          const int s = (w + u) % NS;
-          if (!wait1(RAFULL + s, (w + u) / NS)) return false;
-          tc_fence_after();
-          const uint64_t dq = tile_desc(slot_a(w + u));
-          const uint32_t id = tile_idesc(16 * steps_of(u), FP16, false);
+    const uint32_t tS = tmem, tP = tmem + 128, tV = tmem + 256, tK = tmem + 384;
+    const uint32_t dk = tile_desc(sh.s0), dv = tile_desc(sh.s0 + Sm::kTileBytes), io = tile_idesc(HD, FP16, true);
+    int w = 0, k = 0;
+    Item it;
+    bool ok = true;
+    for (; ok && next_item(sh, k, it, status, limit, true); ++k) {
+      it = Item{0, uniform(it.len), uniform(it.a), uniform(it.b)};
+      const int nt = tiles(it), per_head = nt - it.a, units = per_head * p.group;
+      int ahead = 0;  // the next scores' block within its head
+      auto steps_at = [&](int at) { return (rows_of(it, nt - 1 - at) + 15) / 16; };
+      // S of block u; dP
+      auto scores = [&](int u) {
+        const int s = (w + u) % NS;
+        if (!waita(RAFULL + s, (w + u) / NS)) return false;
+        tc_fence_after();
+        const uint32_t dq = tile_desc(slot_a(w + u)), id = tile_idesc(16 * steps_at(ahead), FP16, false);
+        if (elected()) {
 #pragma unroll
-          for (int i = 0; i < HD / 16; ++i) tc_mma(tS, dk + k_major_step(i), dq + k_major_step(i), id, i > 0);
+          for (int i = 0; i < HD / 16; ++i) tile_mma(tS, dk + k_major_step(i), dq + k_major_step(i), id, i > 0);
           tc_commit(sh.bar(SFULL));
           if (u == units - 1) tc_commit(sh.bar(AFREE));
-          return true;
-        };
-        auto products = [&](int u) {
-          const int s = (w + u) % NS;
-          if (!wait1(RBFULL + s, (w + u) / NS)) return false;
-          tc_fence_after();
-          const uint64_t dg = tile_desc(slot_b(w + u));
-          const uint32_t id = tile_idesc(16 * steps_of(u), FP16, false);
+        }
+        __syncwarp();
+        return true;
+      };
+      auto products = [&](int u) {
+        const int s = (w + u) % NS;
+        if (!waita(RBFULL + s, (w + u) / NS)) return false;
+        tc_fence_after();
+        const uint32_t dg = tile_desc(slot_b(w + u)), id = tile_idesc(16 * steps_at(ahead), FP16, false);
+        if (elected()) {
 #pragma unroll
-          for (int i = 0; i < HD / 16; ++i) tc_mma(tP, dv + k_major_step(i), dg + k_major_step(i), id, i > 0);
+          for (int i = 0; i < HD / 16; ++i) tile_mma(tP, dv + k_major_step(i), dg + k_major_step(i), id, i > 0);
           tc_commit(sh.bar(DPFULL));
           if (u == units - 1) tc_commit(sh.bar(BFREE));
-          return true;
-        };
-        if (!(ok = wait1(AFULL, k) && (w == 0 || wait1(RBFREE + (w - 1) % NS, (w - 1) / NS)) && scores(0) && wait1(BFULL, k) &&
-                   (w == 0 || wait1(RAFREE + (w - 1) % NS, (w - 1) / NS)) && products(0)))
-          break;
-        for (int u = 0; u < units && ok; ++u) {
-          const int s = (w + u) % NS, steps = steps_of(u);
-          if (!(ok = wait1(PFULL, w + u))) break;
-          tc_fence_after();
-          const uint64_t dg = tile_desc(slot_b(w + u)), dq = tile_desc(slot_a(w + u));
-          for (int i = 0; i < steps; ++i) tc_mma_ts(tV, tS + halves_step(i), dg + mn_major_step(i), io, u > 0 || i > 0);
+        }
+        __syncwarp();
+        return true;
+      };
+      if (!(ok = waita(AFULL, k) && (w == 0 || waita(RBFREE + (w - 1) % NS, (w - 1) / NS)) && scores(0) && waita(BFULL, k) &&
+                 (w == 0 || waita(RAFREE + (w - 1) % NS, (w - 1) / NS)) && products(0)))
+        break;
+      for (int u = 0; u < units && ok; ++u) {
+        const int s = (w + u) % NS, steps = steps_at(ahead);
+        ahead = ahead + 1 == per_head ? 0 : ahead + 1;
+        if (!(ok = waita(PFULL, w + u))) break;
+        tc_fence_after();
+        const uint32_t dg = tile_desc(slot_b(w + u)), dq = tile_desc(slot_a(w + u)), more = u > 0;
+        if (elected()) {
+#pragma unroll
+          for (int i = 0; i < kTile / 16; ++i)
+            if (i < steps) tile_mma_ts(tV, tS + halves_step(i), dg + mn_major_step(i), io, i > 0 ? 1u : more);
           tc_commit(sh.bar(RBFREE + s));
-          // the next scores go over P once d_v has read it, the next dP over dS once d_k has; the first two in the order in which they get ready
-          bool next_s = u + 1 < units, this_k = true;
-          const uint64_t since = globaltimer();
-          uint32_t spins = 0;
-          while (ok && (next_s || this_k)) {
-            if (this_k && (!next_s || mbar_test_wait(sh.bar(DSFULL), (w + u) & 1))) {
-              if (!(ok = wait1(DSFULL, w + u))) break;
-              tc_fence_after();
-              for (int i = 0; i < steps; ++i) tc_mma_ts(tK, tP + halves_step(i), dq + mn_major_step(i), io, u > 0 || i > 0);
+        }
+        __syncwarp();
+        // the next scores go over P once d_v has read it, the next dP over dS once d_k has; the first two in the order in which they get ready
+        bool next_s = u + 1 < units, this_k = true;
+        uint64_t since = 0;
+        uint32_t spins = 0;
+        while (ok && (next_s || this_k)) {
+          if (this_k && warp_ready(sh.bar(DSFULL), (w + u) & 1)) {
+            tc_fence_after();
+            if (elected()) {
+#pragma unroll
+              for (int i = 0; i < kTile / 16; ++i)
+                if (i < steps) tile_mma_ts(tK, tP + halves_step(i), dq + mn_major_step(i), io, i > 0 ? 1u : more);
               tc_commit(sh.bar(RAFREE + s));
-              this_k = false;
-            } else if (next_s && (!this_k || mbar_test_wait(sh.bar(RBFREE + s), ((w + u) / NS) & 1))) {
-              if (!(ok = wait1(RBFREE + s, (w + u) / NS) && scores(u + 1))) break;
-              next_s = false;
-            } else if ((++spins & 63u) == 0 && (*sh.abort_flag || globaltimer() - since > limit)) {
-              if (!*sh.abort_flag && status) atomicOr(status, VLA_STATUS_TIMEOUT);
-              *sh.abort_flag = 1;
+            }
+            __syncwarp();
+            this_k = false;
+          } else if (next_s && warp_ready(sh.bar(RBFREE + s), ((w + u) / NS) & 1)) {
+            if (!(ok = scores(u + 1))) break;
+            next_s = false;
+          } else if ((++spins & 1023u) == 0) {  // (the clock is slow to read)
+            if (spins == 1024) since = globaltimer();
+            if (__any_sync(0xffffffffu, *sh.abort_flag != 0)) {
+              ok = false;
+            } else if (__any_sync(0xffffffffu, globaltimer() - since > limit)) {
+              if (lane == 0) {
+                *sh.abort_flag = 1;
+                if (status) atomicOr(status, VLA_STATUS_TIMEOUT);
+              }
               ok = false;
             }
           }
-          if (ok && u + 1 < units) ok = wait1(RAFREE + s, (w + u) / NS) && products(u + 1);
         }
-        tc_commit(sh.bar(DONE));
-        w += units;
+        if (ok && u + 1 < units) ok = waita(RAFREE + s, (w + u) / NS) && products(u + 1);
       }
-      tc_commit(sh.bar(DRAIN));
-      wait_drain(sh.bar(DRAIN), 0, limit);
+      if (elected()) tc_commit(sh.bar(DONE));
+      __syncwarp();
+      w += units;
     }
+    if (elected()) tc_commit(sh.bar(DRAIN));
+    wait_drain(sh.bar(DRAIN), 0, limit);
   } else if (warp == 2) {
     int w = 0, k = 0, phase = 0;  // phase: of each slot, its tiles so far that came here first, modulo 2
     Item it;
@@ -587,6 +609,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint32_t* status = f.status;
   const uint64_t limit = p.wait_limit;
   auto wait1 = [&](int bar, int phase) { return wait_bounded(sh.bar(bar), static_cast<uint32_t>(phase) & 1u, sh.abort_flag, status, limit); };
+  auto waita = [&](int bar, int phase) { return warp_wait_all(sh.bar(bar), static_cast<uint32_t>(phase) & 1u, sh.abort_flag, status, limit); };
   auto waitw = [&](int bar, int phase) { return warp_waits(sh.bar(bar), static_cast<uint32_t>(phase) & 1u, sh.abort_flag, status, limit); };
   auto slot_a = [&](int w) { return sh.s0 + Sm::kRingA + (w % NS) * Sm::kTileBytes; };  // K
   auto slot_b = [&](int w) { return sh.s0 + Sm::kRingB + (w % NS) * Sm::kTileBytes; };  // V
@@ -622,64 +645,70 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (n_g) wait_drain(sh.bar(BFULL), (n_g - 1) & 1, limit);
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      const uint32_t tS = tmem, tQ = tmem + 384;
-      const uint64_t dq = tile_desc(sh.s0), dg = tile_desc(sh.s0 + Sm::kTileBytes);
-      const uint32_t io = tile_idesc(HD, FP16, true);
-      int w = 0, k = 0;
-      Item it;
-      bool ok = true;
-      for (; ok && next_item(sh, k, it, status, limit, false); ++k) {
-        auto steps_of = [&](int j) { return (min(kTile, it.len - j * kTile) + 15) / 16; };
-        auto scores = [&](int j) {
-          const int s = (w + j) % NS;
-          if (!wait1(RAFULL + s, (w + j) / NS)) return false;
-          tc_fence_after();
-          const uint64_t dk = tile_desc(slot_a(w + j));
-          const uint32_t id = tile_idesc(16 * steps_of(j), FP16, false);
+    const uint32_t tS = tmem, tQ = tmem + 384;
+    const uint32_t dq = tile_desc(sh.s0), dg = tile_desc(sh.s0 + Sm::kTileBytes), io = tile_idesc(HD, FP16, true);
+    int w = 0, k = 0;
+    Item it;
+    bool ok = true;
+    for (; ok && next_item(sh, k, it, status, limit, true); ++k) {
+      it = Item{0, uniform(it.len), uniform(it.a), uniform(it.b)};
+      auto steps_of = [&](int j) { return (min(kTile, it.len - j * kTile) + 15) / 16; };
+      auto scores = [&](int j) {
+        const int s = (w + j) % NS;
+        if (!waita(RAFULL + s, (w + j) / NS)) return false;
+        tc_fence_after();
+        const uint32_t dk = tile_desc(slot_a(w + j)), id = tile_idesc(16 * steps_of(j), FP16, false);
+        if (elected()) {
 #pragma unroll
-          for (int i = 0; i < HD / 16; ++i) tc_mma(tS, dq + k_major_step(i), dk + k_major_step(i), id, i > 0);
+          for (int i = 0; i < HD / 16; ++i) tile_mma(tS, dq + k_major_step(i), dk + k_major_step(i), id, i > 0);
           tc_commit(sh.bar(SFULL));
           if (j == it.a) tc_commit(sh.bar(AFREE));
-          return true;
-        };
-        auto products = [&](int j) {
-          const int s = (w + j) % NS;
-          if (!wait1(RBFULL + s, (w + j) / NS)) return false;
-          tc_fence_after();
-          const uint64_t dv = tile_desc(slot_b(w + j));
-          const uint32_t id = tile_idesc(16 * steps_of(j), FP16, false);
+        }
+        __syncwarp();
+        return true;
+      };
+      auto products = [&](int j) {
+        const int s = (w + j) % NS;
+        if (!waita(RBFULL + s, (w + j) / NS)) return false;
+        tc_fence_after();
+        const uint32_t dv = tile_desc(slot_b(w + j)), id = tile_idesc(16 * steps_of(j), FP16, false), tP = tmem + 128 + ((w + j) & 1) * 128;
+        if (elected()) {
 #pragma unroll
-          for (int i = 0; i < HD / 16; ++i)
-            tc_mma(tmem + 128 + ((w + j) & 1) * 128, dg + k_major_step(i), dv + k_major_step(i), id, i > 0);
+          for (int i = 0; i < HD / 16; ++i) tile_mma(tP, dg + k_major_step(i), dv + k_major_step(i), id, i > 0);
           tc_commit(sh.bar(DPFULL + ((w + j) & 1)));
           tc_commit(sh.bar(RBFREE + s));
           if (j == it.a) tc_commit(sh.bar(BFREE));
-          return true;
-        };
-        // (an item's first dP: the item before has ended, or the threads would not have read its last scores)
-        if (!(ok = wait1(AFULL, k) && (w == 0 || wait1(SREAD, w - 1)) && scores(0) && wait1(BFULL, k) &&
-                   (w < 2 || wait1(RAFREE + (w - 2) % NS, (w - 2) / NS)) && products(0)))
+        }
+        __syncwarp();
+        return true;
+      };
+      // (an item's first dP: the item before has ended, or the threads would not have read its last scores)
+      if (!(ok = waita(AFULL, k) && (w == 0 || waita(SREAD, w - 1)) && scores(0) && waita(BFULL, k) &&
+                 (w < 2 || waita(RAFREE + (w - 2) % NS, (w - 2) / NS)) && products(0)))
+        break;
+      for (int j = 0; j <= it.a && ok; ++j) {
+        // the next scores once the threads have read these, the next dP over the dS of the block before once d_q has read it
+        if (j < it.a && !(ok = waita(SREAD, w + j) && scores(j + 1) && (w + j == 0 || waita(RAFREE + (w + j - 1) % NS, (w + j - 1) / NS)) &&
+                               products(j + 1)))
           break;
-        for (int j = 0; j <= it.a && ok; ++j) {
-          // the next scores once the threads have read these, the next dP over the dS of the block before once d_q has read it
-          if (j < it.a && !(ok = wait1(SREAD, w + j) && scores(j + 1) && (w + j == 0 || wait1(RAFREE + (w + j - 1) % NS, (w + j - 1) / NS)) &&
-                                 products(j + 1)))
-            break;
-          if (!(ok = wait1(DSFULL, w + j))) break;
-          tc_fence_after();
-          const uint64_t dk = tile_desc(slot_a(w + j));
-          const uint32_t tD = tmem + 128 + ((w + j) & 1) * 128;
-          const int steps = steps_of(j);
-          for (int i = 0; i < steps; ++i) tc_mma_ts(tQ, tD + halves_step(i), dk + mn_major_step(i), io, j > 0 || i > 0);
+        if (!(ok = waita(DSFULL, w + j))) break;
+        tc_fence_after();
+        const uint32_t dk = tile_desc(slot_a(w + j)), tD = tmem + 128 + ((w + j) & 1) * 128, more = j > 0;
+        const int steps = steps_of(j);
+        if (elected()) {
+#pragma unroll
+          for (int i = 0; i < kTile / 16; ++i)
+            if (i < steps) tile_mma_ts(tQ, tD + halves_step(i), dk + mn_major_step(i), io, i > 0 ? 1u : more);
           tc_commit(sh.bar(RAFREE + (w + j) % NS));
         }
-        tc_commit(sh.bar(DONE));
-        w += it.a + 1;
+        __syncwarp();
       }
-      tc_commit(sh.bar(DRAIN));
-      wait_drain(sh.bar(DRAIN), 0, limit);
+      if (elected()) tc_commit(sh.bar(DONE));
+      __syncwarp();
+      w += it.a + 1;
     }
+    if (elected()) tc_commit(sh.bar(DRAIN));
+    wait_drain(sh.bar(DRAIN), 0, limit);
   } else if (warp == 2) {
     int w = 0, k = 0, phase = 0;
     Item it;

@@ -12,27 +12,66 @@ namespace vla {
 constexpr int kTile = 128;
 constexpr uint32_t kBlockBytes = kTile * 128;  // a column block of a tile
 
-__device__ __forceinline__ uint64_t tile_desc(uint32_t saddr) {
-  return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | static_cast<uint64_t>(kBlockBytes >> 4) << 16 |
-         static_cast<uint64_t>(1024 >> 4) << 32 | static_cast<uint64_t>(1) << 46 | static_cast<uint64_t>(2) << 61;
-}
+// Low word of a tile's descriptor (the address, column blocks kBlockBytes apart); the high word is the same for all: groups of 8 rows
+// 1024 bytes apart, version 1, 128-byte swizzle.
+constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t tile_desc(uint32_t saddr) { return ((saddr & 0x3FFFFu) >> 4) | ((kBlockBytes >> 4) << 16); }
 // Offsets (in descriptor units of 16 bytes) of the k-th 16 elements along the sum: channels of a K-major operand, rows of an MN-major one.
-__device__ __forceinline__ constexpr uint64_t k_major_step(int k) { return (static_cast<uint64_t>(k >> 2) * kBlockBytes + (k & 3) * 32) >> 4; }
-__device__ __forceinline__ constexpr uint64_t mn_major_step(int k) { return static_cast<uint64_t>(k) * (2048 >> 4); }
+__device__ __forceinline__ constexpr uint32_t k_major_step(int k) { return (static_cast<uint32_t>(k >> 2) * kBlockBytes + (k & 3) * 32) >> 4; }
+__device__ __forceinline__ constexpr uint32_t mn_major_step(int k) { return static_cast<uint32_t>(k) * (2048 >> 4); }
 
 // kind::f16, f32 sums, M = 128, N; A K-major (or in tensor memory), B K-major or MN-major.
 __device__ __forceinline__ uint32_t tile_idesc(int N, bool fp16, bool b_mn_major) {
   return (1u << 4) | (fp16 ? 0u : (1u << 7) | (1u << 10)) | (b_mn_major ? 1u << 16 : 0u) | (static_cast<uint32_t>(N >> 3) << 17) |
          (static_cast<uint32_t>(kTile >> 4) << 24);
 }
-// D (tensor memory) (+)= A (tensor memory) B (shared memory)
-__device__ __forceinline__ void tc_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+// D (tensor memory) (+)= A B, both in shared memory, or A in tensor memory.
+__device__ __forceinline__ void tile_mma(uint32_t d_tmem, uint32_t a_desc, uint32_t b_desc, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\t"
+      "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\t"
       "setp.ne.b32 p, %4, 0;\n\t"
-      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d_tmem),
-      "r"(a_tmem), "l"(bdesc), "r"(idesc), "r"(accumulate)
+      "mov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_desc), "r"(b_desc), "r"(idesc), "r"(accumulate), "n"(kDescHigh)
       : "memory");
+}
+__device__ __forceinline__ void tile_mma_ts(uint32_t d_tmem, uint32_t a_tmem, uint32_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t.reg .b64 b;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "mov.b64 b, {%2, %5};\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}" ::"r"(d_tmem),
+      "r"(a_tmem), "r"(b_desc), "r"(idesc), "r"(accumulate), "n"(kDescHigh)
+      : "memory");
+}
+
+// The warp that issues MMAs runs as a whole, with its state in uniform registers (what the MMA takes its operands from; from one thread's
+// registers each operand costs a move and its latency, 70 cycles an MMA), and one thread of it, always the same, issues.
+__device__ __forceinline__ bool elected() {
+  uint32_t p;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+  return p != 0;
+}
+__device__ __forceinline__ int uniform(int v) { return __reduce_max_sync(0xffffffffu, v); }
+__device__ __forceinline__ bool warp_ready(uint32_t bar, uint32_t parity) { return __any_sync(0xffffffffu, mbar_test_wait(bar, parity)); }
+// Bounded wait of a whole warp.
+__device__ __forceinline__ bool warp_wait_all(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* status, uint64_t limit) {
+  if (warp_ready(bar, parity)) return true;
+  uint64_t t0 = 0;
+  for (uint32_t n = 1;; ++n) {
+    if (__any_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
+    if (n & 63u) continue;
+    if (n == 64) t0 = globaltimer();
+    const bool late = n > 64 && globaltimer() - t0 > limit;
+    if (__any_sync(0xffffffffu, late)) {
+      if ((threadIdx.x & 31) == 0) {
+        *abort_flag = 1;
+        if (status) atomicOr(status, VLA_STATUS_TIMEOUT);
+      }
+      return false;
+    }
+    if (__any_sync(0xffffffffu, *abort_flag != 0)) return false;
+  }
 }
 
 // All of an SM's tensor memory, by one warp; `slot` (shared memory) gets its address.
