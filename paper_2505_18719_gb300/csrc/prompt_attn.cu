@@ -14,7 +14,7 @@
 // Roles (384 threads):
 //   warp 0      TMA: Q tiles when the item before is done with them, key and value blocks into a ring;
 //   warp 1      owns the tensor memory; issues S = Q K^T and O += P V (P in tensor memory over the S it came from, V as the
-//               MN-major operand), tile by tile as its operands get ready;
+//               MN-major operand), a tile's next scores behind its product, so that one tile's softmax runs beside the other's products;
 //   warp 2      a sequence's last values land with it: those behind the last row become zeros (their weights are zeros, but a NaN
 //               would spoil the product), then the block counts as loaded;
 //   warp 3      finds the items: a scan over the sequences' lengths, 32 sequences a step, into a ring of descriptors;
@@ -47,7 +47,7 @@ struct Smem {
 
 // Barriers.
 enum : int { QFULL = 0, QFREE = 2, SFULL = 4, PFULL = 6, PVDONE = 8, DRAIN = 10, IFULL = 11, IFREE = 19, KVFULL = 27, KVFREE = 35, TAIL = 43, kBarCount = 51 };
-constexpr int kItemReaders = 1 + 2 + 1 + 8;  // producer, MMA (each tile), warp 2, softmax warps
+constexpr int kItemReaders = 1 + 1 + 1 + 8;  // producer, MMA, warp 2, softmax warps
 
 struct Params {
   PromptArgs a;
@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
   auto stage = [&](int f) { return s0 + Sm::kRing + (f % NS) * Sm::kTileBytes; };
-  auto wait1 = [&](int bar, uint32_t parity) { return wait_bounded(BAR(bar), parity & 1u, abort_flag, status, limit); };
+  auto wait1 = [&](int bar, uint32_t parity) { return quick_wait(BAR(bar), parity & 1u, abort_flag, status, limit); };
 
   if (warp == 0) {
     if (lane == 0) {
@@ -173,91 +173,72 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMAs
-    struct Cursor {
-      int k = 0, j = 0, nb = 0, other = 0, len = 0;  // item, block, its blocks here and of the other tile; sequence
-      int block = 0, base = 0;                       // blocks of this tile so far; blocks of the CTA's items before this one
-      int q = 0;                                     // Q tiles of this tile so far
-      bool open = false, pv = false, done = false;
-    } cur[2];
-    uint64_t t_last = 0;
-    uint32_t spins = 0;
     const uint32_t is = tile_idesc(128, FP16, false), io = tile_idesc(HD, FP16, true);
-    auto ready = [&](int bar, int phase) { return warp_ready(BAR(bar), static_cast<uint32_t>(phase) & 1u); };
-    bool ok = true;
-    auto step = [&](Cursor& c, const int x) -> bool {
-      if (c.done) return false;
-      if (!c.open) {
-        if (!ready(IFULL + (c.k & 7), c.k >> 3)) return false;
-        const Item* src = items + (c.k & 7);
-        const Item it{0, uniform(src->len), uniform(src->a), uniform(src->b)};
-        if (lane == 0) mbar_arrive(BAR(IFREE + (c.k & 7)));
-        ++c.k;
-        if (it.len < 0) return c.done = true;
-        const Tiles t = tiles_of(it, p.group);
-        c.nb = t.nb[x];
-        c.other = t.nb[x ^ 1];
-        c.len = it.len;
-        c.j = 0;
-        c.open = c.nb > 0;
-        if (!c.open) c.base += c.other;
-        return true;
-      }
-      const int f = 2 * (c.base + c.j) + (c.pv ? 1 : 0), s = f % NS;
-      const bool shared = c.j < c.other, last = c.j == c.nb - 1;
-      const uint32_t tS = tmem + kColS + x * 128, operand = tile_desc(stage(f));
-      if (!c.pv) {
-        // (the scores go over the weights of the block before, which its product has to have read)
-        if (!ready(KVFULL + s, f / NS) || (c.j == 0 && !ready(QFULL + x, c.q)) || (c.block > 0 && !ready(PVDONE + x, c.block - 1))) return false;
-        tc_fence_after();
-        const uint32_t dq = tile_desc(s0 + x * Sm::kTileBytes);
-        if (elected()) {
+    auto waits = [&](int bar, int phase) { return warp_waits(BAR(bar), static_cast<uint32_t>(phase) & 1u, abort_flag, status, limit); };
+    int base = 0, q[2] = {0, 0}, block[2] = {0, 0};  // blocks of the items before; Q tiles and blocks of each tile so far
+    auto free_kv = [&](int s, bool shared) {
+      tc_commit(BAR(KVFREE + s));
+      if (!shared) tc_commit(BAR(KVFREE + s));
+    };
+    // S of block j of tile x, over the weights of the block before (which its product has read)
+    auto scores = [&](const Tiles& t, int base, const int x, int j) {
+      const int f = 2 * (base + j), s = f % NS;
+      const bool first = j == 0, last = j == t.nb[x] - 1;
+      if (!waits(KVFULL + s, f / NS) || (first && !waits(QFULL + x, q[x])) || (block[x] > 0 && !waits(PVDONE + x, block[x] - 1))) return false;
+      tc_fence_after();
+      const uint32_t dq = tile_desc(s0 + x * Sm::kTileBytes), dk = tile_desc(stage(f)), tS = tmem + kColS + x * 128;
+      if (elected()) {
 #pragma unroll
-          for (int k = 0; k < HD / 16; ++k) tile_mma(tS, dq + k_major_step(k), operand + k_major_step(k), is, k > 0);
-          tc_commit(BAR(SFULL + x));
-          if (last) tc_commit(BAR(QFREE + x));
-          tc_commit(BAR(KVFREE + s));
-          if (!shared) tc_commit(BAR(KVFREE + s));
-        }
-        if (last) ++c.q;
-      } else {
-        if (!ready(PFULL + x, c.block) || !ready(KVFULL + s, f / NS)) return false;
-        tc_fence_after();
-        const int steps = (min(kTile, c.len - c.j * kTile) + 15) / 16;
-        const uint32_t tO = tmem + kColO + x * 128, more = c.j > 0;
-        if (elected()) {
-#pragma unroll
-          for (int k = 0; k < kTile / 16; ++k)
-            if (k < steps) tile_mma_ts(tO, tS + k * 8, operand + mn_major_step(k), io, k > 0 ? 1u : more);
-          tc_commit(BAR(PVDONE + x));
-          tc_commit(BAR(KVFREE + s));
-          if (!shared) tc_commit(BAR(KVFREE + s));
-        }
-        ++c.block;
-        if (++c.j == c.nb) {
-          c.open = false;
-          c.base += max(c.nb, c.other);
-        }
+        for (int k = 0; k < HD / 16; ++k) tile_mma(tS, dq + k_major_step(k), dk + k_major_step(k), is, k > 0);
+        tc_commit(BAR(SFULL + x));
+        if (last) tc_commit(BAR(QFREE + x));
+        free_kv(s, j < t.nb[x ^ 1]);
       }
       __syncwarp();
-      c.pv = !c.pv;
+      q[x] += last;
       return true;
     };
-    while (ok && !(cur[0].done && cur[1].done)) {
-      const bool did = step(cur[0], 0) | step(cur[1], 1);
-      if (did) {
-        spins = 0;
-      } else if (((++spins) & 1023u) == 0) {  // (the clock is slow to read)
-        if (spins == 1024) t_last = globaltimer();
-        if (__any_sync(0xffffffffu, *abort_flag != 0)) {
-          ok = false;
-        } else if (__any_sync(0xffffffffu, globaltimer() - t_last > limit)) {
-          if (lane == 0) {
-            *abort_flag = 1;
-            if (status) atomicOr(status, VLA_STATUS_TIMEOUT);
-          }
-          ok = false;
+    auto product = [&](const Tiles& t, int len, const int x, int j) {
+      const int f = 2 * (base + j) + 1, s = f % NS, steps = (min(kTile, len - j * kTile) + 15) / 16;
+      if (!waits(KVFULL + s, f / NS) || !waits(PFULL + x, block[x])) return false;
+      tc_fence_after();
+      const uint32_t dv = tile_desc(stage(f)), tP = tmem + kColS + x * 128, tO = tmem + kColO + x * 128, more = j > 0;
+      if (elected()) {
+#pragma unroll
+        for (int k = 0; k < kTile / 16; ++k)
+          if (k < steps) tile_mma_ts(tO, tP + k * 8, dv + mn_major_step(k), io, k > 0 ? 1u : more);
+        tc_commit(BAR(PVDONE + x));
+        free_kv(s, j < t.nb[x ^ 1]);
+      }
+      __syncwarp();
+      ++block[x];
+      return true;
+    };
+    // An item's blocks: each tile's product, then its next scores; at the end the next item's first scores.
+    Item it;
+    auto take = [&](int k, Item& it, Tiles& t) {
+      if (!waits(IFULL + (k & 7), k >> 3)) return false;
+      const Item* src = items + (k & 7);
+      it = Item{0, uniform(src->len), uniform(src->a), uniform(src->b)};
+      if (lane == 0) mbar_arrive(BAR(IFREE + (k & 7)));
+      if (it.len >= 0) t = tiles_of(it, p.group);
+      return true;
+    };
+    Tiles t{};
+    bool ok = take(0, it, t);
+    if (ok && it.len >= 0) ok = scores(t, 0, 0, 0) && (!t.nb[1] || scores(t, 0, 1, 0));
+    for (int k = 1; ok && it.len >= 0; ++k) {
+      const int nb = max(t.nb[0], t.nb[1]);
+      for (int j = 0; j < nb && ok; ++j) {
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if (j < t.nb[x]) ok = ok && product(t, it.len, x, j);
+          if (j + 1 < t.nb[x]) ok = ok && scores(t, base, x, j + 1);
         }
       }
+      base += nb;
+      ok = ok && take(k, it, t);
+      if (ok && it.len >= 0) ok = scores(t, base, 0, 0) && (!t.nb[1] || scores(t, base, 1, 0));
     }
     if (elected()) tc_commit(BAR(DRAIN));
     wait_drain(BAR(DRAIN), 0, limit);

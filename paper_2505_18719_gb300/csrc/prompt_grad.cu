@@ -228,7 +228,7 @@ __device__ __forceinline__ void end_of_kernel(uint32_t tmem) {
 // Next descriptor, for one thread or a whole warp of which lane 0 answers; false at a timeout.
 __device__ __forceinline__ bool next_item(const Shared& sh, int k, Item& it, uint32_t* status, uint64_t limit, bool whole_warp) {
   if (whole_warp ? !warp_waits(sh.bar(IFULL + (k & 7)), (k >> 3) & 1, sh.abort_flag, status, limit)
-                 : !wait_bounded(sh.bar(IFULL + (k & 7)), (k >> 3) & 1, sh.abort_flag, status, limit))
+                 : !quick_wait(sh.bar(IFULL + (k & 7)), (k >> 3) & 1, sh.abort_flag, status, limit))
     return false;
   it = sh.items[k & 7];
   if (whole_warp) __syncwarp();
@@ -306,8 +306,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint32_t* status = f.status;
   const uint64_t limit = p.wait_limit;
-  auto wait1 = [&](int bar, int phase) { return wait_bounded(sh.bar(bar), static_cast<uint32_t>(phase) & 1u, sh.abort_flag, status, limit); };
-  auto waita = [&](int bar, int phase) { return warp_wait_all(sh.bar(bar), static_cast<uint32_t>(phase) & 1u, sh.abort_flag, status, limit); };
+  auto wait1 = [&](int bar, int phase) { return quick_wait(sh.bar(bar), static_cast<uint32_t>(phase) & 1u, sh.abort_flag, status, limit); };
   auto waitw = [&](int bar, int phase) { return warp_waits(sh.bar(bar), static_cast<uint32_t>(phase) & 1u, sh.abort_flag, status, limit); };
   auto tiles = [](const Item& it) { return (it.len + kTile - 1) / kTile; };
   auto rows_of = [](const Item& it, int t) { return min(kTile, it.len - t * kTile); };
@@ -362,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       // S of block u; dP
       auto scores = [&](int u) {
         const int s = (w + u) % NS;
-        if (!waita(RAFULL + s, (w + u) / NS)) return false;
+        if (!waitw(RAFULL + s, (w + u) / NS)) return false;
         tc_fence_after();
         const uint32_t dq = tile_desc(slot_a(w + u)), id = tile_idesc(16 * steps_at(ahead), FP16, false);
         if (elected()) {
@@ -376,7 +375,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       };
       auto products = [&](int u) {
         const int s = (w + u) % NS;
-        if (!waita(RBFULL + s, (w + u) / NS)) return false;
+        if (!waitw(RBFULL + s, (w + u) / NS)) return false;
         tc_fence_after();
         const uint32_t dg = tile_desc(slot_b(w + u)), id = tile_idesc(16 * steps_at(ahead), FP16, false);
         if (elected()) {
@@ -388,13 +387,13 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         return true;
       };
-      if (!(ok = waita(AFULL, k) && (w == 0 || waita(RBFREE + (w - 1) % NS, (w - 1) / NS)) && scores(0) && waita(BFULL, k) &&
-                 (w == 0 || waita(RAFREE + (w - 1) % NS, (w - 1) / NS)) && products(0)))
+      if (!(ok = waitw(AFULL, k) && (w == 0 || waitw(RBFREE + (w - 1) % NS, (w - 1) / NS)) && scores(0) && waitw(BFULL, k) &&
+                 (w == 0 || waitw(RAFREE + (w - 1) % NS, (w - 1) / NS)) && products(0)))
         break;
       for (int u = 0; u < units && ok; ++u) {
         const int s = (w + u) % NS, steps = steps_at(ahead);
         ahead = ahead + 1 == per_head ? 0 : ahead + 1;
-        if (!(ok = waita(PFULL, w + u))) break;
+        if (!(ok = waitw(PFULL, w + u))) break;
         tc_fence_after();
         const uint32_t dg = tile_desc(slot_b(w + u)), dq = tile_desc(slot_a(w + u)), more = u > 0;
         if (elected()) {
@@ -435,7 +434,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
         }
-        if (ok && u + 1 < units) ok = waita(RAFREE + s, (w + u) / NS) && products(u + 1);
+        if (ok && u + 1 < units) ok = waitw(RAFREE + s, (w + u) / NS) && products(u + 1);
       }
       if (elected()) tc_commit(sh.bar(DONE));
       __syncwarp();
@@ -608,8 +607,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint32_t* status = f.status;
   const uint64_t limit = p.wait_limit;
-  auto wait1 = [&](int bar, int phase) { return wait_bounded(sh.bar(bar), static_cast<uint32_t>(phase) & 1u, sh.abort_flag, status, limit); };
-  auto waita = [&](int bar, int phase) { return warp_wait_all(sh.bar(bar), static_cast<uint32_t>(phase) & 1u, sh.abort_flag, status, limit); };
+  auto wait1 = [&](int bar, int phase) { return quick_wait(sh.bar(bar), static_cast<uint32_t>(phase) & 1u, sh.abort_flag, status, limit); };
   auto waitw = [&](int bar, int phase) { return warp_waits(sh.bar(bar), static_cast<uint32_t>(phase) & 1u, sh.abort_flag, status, limit); };
   auto slot_a = [&](int w) { return sh.s0 + Sm::kRingA + (w % NS) * Sm::kTileBytes; };  // K
   auto slot_b = [&](int w) { return sh.s0 + Sm::kRingB + (w % NS) * Sm::kTileBytes; };  // V
@@ -655,7 +653,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       auto steps_of = [&](int j) { return (min(kTile, it.len - j * kTile) + 15) / 16; };
       auto scores = [&](int j) {
         const int s = (w + j) % NS;
-        if (!waita(RAFULL + s, (w + j) / NS)) return false;
+        if (!waitw(RAFULL + s, (w + j) / NS)) return false;
         tc_fence_after();
         const uint32_t dk = tile_desc(slot_a(w + j)), id = tile_idesc(16 * steps_of(j), FP16, false);
         if (elected()) {
@@ -669,7 +667,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       };
       auto products = [&](int j) {
         const int s = (w + j) % NS;
-        if (!waita(RBFULL + s, (w + j) / NS)) return false;
+        if (!waitw(RBFULL + s, (w + j) / NS)) return false;
         tc_fence_after();
         const uint32_t dv = tile_desc(slot_b(w + j)), id = tile_idesc(16 * steps_of(j), FP16, false), tP = tmem + 128 + ((w + j) & 1) * 128;
         if (elected()) {
@@ -683,15 +681,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         return true;
       };
       // (an item's first dP: the item before has ended, or the threads would not have read its last scores)
-      if (!(ok = waita(AFULL, k) && (w == 0 || waita(SREAD, w - 1)) && scores(0) && waita(BFULL, k) &&
-                 (w < 2 || waita(RAFREE + (w - 2) % NS, (w - 2) / NS)) && products(0)))
+      if (!(ok = waitw(AFULL, k) && (w == 0 || waitw(SREAD, w - 1)) && scores(0) && waitw(BFULL, k) &&
+                 (w < 2 || waitw(RAFREE + (w - 2) % NS, (w - 2) / NS)) && products(0)))
         break;
       for (int j = 0; j <= it.a && ok; ++j) {
         // the next scores once the threads have read these, the next dP over the dS of the block before once d_q has read it
-        if (j < it.a && !(ok = waita(SREAD, w + j) && scores(j + 1) && (w + j == 0 || waita(RAFREE + (w + j - 1) % NS, (w + j - 1) / NS)) &&
+        if (j < it.a && !(ok = waitw(SREAD, w + j) && scores(j + 1) && (w + j == 0 || waitw(RAFREE + (w + j - 1) % NS, (w + j - 1) / NS)) &&
                                products(j + 1)))
           break;
-        if (!(ok = waita(DSFULL, w + j))) break;
+        if (!(ok = waitw(DSFULL, w + j))) break;
         tc_fence_after();
         const uint32_t dk = tile_desc(slot_a(w + j)), tD = tmem + 128 + ((w + j) & 1) * 128, more = j > 0;
         const int steps = steps_of(j);

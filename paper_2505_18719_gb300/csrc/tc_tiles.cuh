@@ -54,26 +54,6 @@ __device__ __forceinline__ bool elected() {
 }
 __device__ __forceinline__ int uniform(int v) { return __reduce_max_sync(0xffffffffu, v); }
 __device__ __forceinline__ bool warp_ready(uint32_t bar, uint32_t parity) { return __any_sync(0xffffffffu, mbar_test_wait(bar, parity)); }
-// Bounded wait of a whole warp.
-__device__ __forceinline__ bool warp_wait_all(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* status, uint64_t limit) {
-  if (warp_ready(bar, parity)) return true;
-  uint64_t t0 = 0;
-  for (uint32_t n = 1;; ++n) {
-    if (__any_sync(0xffffffffu, mbar_try_wait(bar, parity))) return true;
-    if (n & 63u) continue;
-    if (n == 64) t0 = globaltimer();
-    const bool late = n > 64 && globaltimer() - t0 > limit;
-    if (__any_sync(0xffffffffu, late)) {
-      if ((threadIdx.x & 31) == 0) {
-        *abort_flag = 1;
-        if (status) atomicOr(status, VLA_STATUS_TIMEOUT);
-      }
-      return false;
-    }
-    if (__any_sync(0xffffffffu, *abort_flag != 0)) return false;
-  }
-}
-
 // All of an SM's tensor memory, by one warp; `slot` (shared memory) gets its address.
 constexpr uint32_t kTmemAll = 512;
 __device__ __forceinline__ void tmem_take(uint32_t slot) {
@@ -122,13 +102,35 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return FP16 ? pack_f16x2(a, b) : pack_bf16x2(a, b);
 }
 
-// Bounded wait by lane 0, the verdict shared by the warp.
+// wait_bounded for waits that are as a rule short: the clock, which takes longer to read than the wait would last, comes in after 1024 tries.
+__device__ __forceinline__ bool quick_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* status, uint64_t limit) {
+  uint64_t t0 = 0;
+  for (uint32_t n = 1; !mbar_try_wait(bar, parity); ++n) {
+    if (n & 1023u) continue;
+    if (*abort_flag) return false;
+    if (n == 1024) t0 = globaltimer();
+    if (globaltimer() - t0 > limit) {
+      *abort_flag = 1;
+      if (status) atomicOr(status, VLA_STATUS_TIMEOUT);
+      return false;
+    }
+  }
+  return true;
+}
+// By a whole warp: all lanes ask at once.  (Asked by one lane with the others waiting for it, the answer comes 600 cycles later.)
 __device__ __forceinline__ bool warp_waits(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* status, uint64_t limit) {
-  int ok = 1;
-  if ((threadIdx.x & 31) == 0) ok = wait_bounded(bar, parity, abort_flag, status, limit) ? 1 : 0;
-  ok = __shfl_sync(0xffffffffu, ok, 0);
-  __syncwarp();  // what lane 0 waited for is every lane's to read
-  return ok != 0;
+  uint64_t t0 = 0;
+  for (uint32_t n = 1; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity)); ++n) {
+    if (n & 1023u) continue;
+    if (n == 1024) t0 = globaltimer();
+    const bool late = globaltimer() - t0 > limit, given_up = *abort_flag != 0;
+    if (__any_sync(0xffffffffu, late) && (threadIdx.x & 31) == 0) {
+      *abort_flag = 1;
+      if (status) atomicOr(status, VLA_STATUS_TIMEOUT);
+    }
+    if (__any_sync(0xffffffffu, late || given_up)) return false;
+  }
+  return true;
 }
 
 // Rows `from` .. `to` - 1 of a tile in shared memory become zeros (one warp).
