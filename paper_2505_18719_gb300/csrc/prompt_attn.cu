@@ -1,29 +1,34 @@
 // Causal attention of packed sequences on the tcgen05 tensor cores (include/vla_learn.h).
 //
-// With c = scale log2(e), for a query i over blocks of 128 keys: s = q K^T, m = max s, weights 2^(c (s - m)), l their sum,
+// With c = scale log2(e), for a query i over blocks of keys: s = q K^T, m = max s, weights 2^(c (s - m)), l their sum,
 // O = 2^(c (m' - m)) O + P V; out = O / l, lse = ln 2 (c m + log2 l).  The reference m moves only when a maximum passes it by more than
 // 2^8, so O is scaled again in few blocks.  Weights go to the values' type; fp16 ones are 2^7 times as large, so that one of
 // 2^-21 of the row's largest still keeps all its bits (at most 2^15 with the reference 2^8 behind).
 //
 // A tile is 128 rows of one sequence and query head.  The tiles of a sequence and key-value head are numbered row tile after row tile, query
 // head after query head, and an item is two neighbours: two query heads over the same rows where heads are shared, else two row tiles.
-// Both go over the same keys, so a block of keys in shared memory serves 256 queries, and while one tile's weights
-// are computed the tensor cores work for the other.  Items go sequence by sequence, the longest rows of a
-// sequence first (its keys are read from HBM once, and the last items are short); persistent CTAs, one an SM.
+// Both go over the same keys, so a block of keys in shared memory serves 256 queries.  Items go sequence by sequence, the longest rows
+// of a sequence first (its keys are read from HBM once, and the last items are short); persistent CTAs, one an SM.
+//
+// Blocks are 80 keys: so O, S and P of both tiles have tensor memory of their own (a tile's 256 columns: O [0, HD), S behind it, P
+// behind that), and the next scores are under way as soon as the threads have read these.  With blocks
+// of 128 keys for heads of 128 P has to lie over S, the chain scores - weights - product - next scores has no
+// slack, and 16384 rows took 1.63 ms.  Products of 80 keys are bound by shared memory (4 KB of Q and 2.5 KB of K a step, 51 cycles
+// where 128 keys take 65).
 //
 // Roles (384 threads):
-//   warp 0      TMA: Q tiles when the item before is done with them, key and value blocks into a ring;
-//   warp 1      owns the tensor memory; issues S = Q K^T and O += P V (P in tensor memory over the S it came from, V as the
-//               MN-major operand), a tile's next scores behind its product, so that one tile's softmax runs beside the other's products;
-//   warp 2      a sequence's last values land with it: those behind the last row become zeros (their weights are zeros, but a NaN
-//               would spoil the product), then the block counts as loaded;
-//   warp 3      finds the items: a scan over the sequences' lengths, 32 sequences a step, into a ring of descriptors;
-//               then the rows of no sequence;
-//   warps 4-11  one query row a thread: softmax, output (through shared memory, so that rows are stored in whole lines).
+//   warp 0       finds the items (a scan over the sequences' lengths, 32 sequences a step), hands their descriptors round and loads their tiles by
+//                TMA: Q when the item before is done with it, key and value blocks into a ring;
+//   warps 1, 2   issue S = Q K^T and O += P V (V as the MN-major operand), each of both tiles in turn: one warp for both products cannot
+//                keep up, at 250 to 500 cycles from one group of products to the next;
+//   warp 3       a sequence's last values land with it: those behind the last row become zeros (their weights are zeros, but a NaN
+//                would spoil the product), then the block counts as loaded; at the end the rows of no sequence;
+//   warps 4 - 11 one query row a thread: softmax, and the output through shared memory in whole sectors.  (Two threads a row: the
+//                exchange of their maxima costs what the shorter rows save.)
 // A row whose result is not finite is computed again from its own keys alone (attend_row): a NaN behind a row in its
 // block of keys does not count for it.
-// Tensor memory: S / P of the tiles [0, 128) [128, 256), O [256, 256 + HD) [384, 384 + HD).
 #include <algorithm>
+#include <type_traits>
 
 #include "gemm.h"
 #include "prompt_items.cuh"
@@ -32,22 +37,26 @@ namespace vla {
 
 namespace {
 
-constexpr int kThreads = 384;
-constexpr uint32_t kColS = 0, kColO = 256;
+constexpr int kThreads = 384, kSoftWarp0 = 4, kSoftWarps = 8;
 
 template <int HD>
 struct Smem {
-  static constexpr int kStages = HD == 128 ? 4 : 8;
-  static constexpr uint32_t kTileBytes = kTile * HD * 2;
-  static constexpr uint32_t kStaging = 8 * 4096;  // 32 rows x 128 bytes a softmax warp
-  static constexpr uint32_t kRing = 2 * kTileBytes, kStage = kRing + kStages * kTileBytes, kBars = kStage + kStaging;
+  static constexpr int kKeys = 80;  // keys of a block
+  static constexpr int kStages = HD == 128 ? 6 : 8;
+  static constexpr uint32_t kQBytes = kTile * HD * 2, kKvBytes = kKeys * HD * 2, kKvBlock = kKeys * 128;
+  static constexpr uint32_t kRing = 2 * kQBytes, kStage = kRing + kStages * kKvBytes, kBars = kStage + kSoftWarps * 2048;
   static constexpr uint32_t kTotal = 1024 + kBars + 1024;
-  static_assert(kTotal <= 232448, "shared memory per CTA");
+  static constexpr uint32_t kColS = HD, kColP = HD + kKeys;  // of a tile's 256 columns
+  static_assert(kTotal <= 232448 && kColP + kKeys / 2 <= 256 && kKvBlock % 1024 == 0, "shared and tensor memory");
 };
 
-// Barriers.
-enum : int { QFULL = 0, QFREE = 2, SFULL = 4, PFULL = 6, PVDONE = 8, DRAIN = 10, IFULL = 11, IFREE = 19, KVFULL = 27, KVFREE = 35, TAIL = 43, kBarCount = 51 };
-constexpr int kItemReaders = 1 + 1 + 1 + 8;  // producer, MMA, warp 2, softmax warps
+// Barriers.  Of each tile: Q loaded / free, S written / read, P written, its product done; end of the issuing warps' products; item
+// descriptors; ring slots, and loads into them that go through warp 3.
+enum : int {
+  QFULL = 0, QFREE = 2, SFULL = 4, SREAD = 6, PFULL = 8, PVDONE = 10, DRAIN = 12, IFULL = 16, IFREE = 24, KVFULL = 32, KVFREE = 40, TAIL = 48,
+  kBarCount = 56
+};
+constexpr int kItemReaders = 2 + 1 + kSoftWarps;
 
 struct Params {
   PromptArgs a;
@@ -56,19 +65,21 @@ struct Params {
   uint64_t wait_limit;
 };
 
-// An item is tiles 2 a and 2 a + 1 of key-value head b.  Blocks of keys of each (0: no such tile).
+// An item is tiles 2 a and 2 a + 1 of key-value head b.  Of each: the row tile, the query head, how many keys its rows see, and its blocks (0:
+// no such tile).
 struct Tiles {
-  int row_tile[2], head[2], nb[2];
+  int row_tile[2], head[2], keys[2], nb[2];
 };
+template <int HD>
 __device__ __forceinline__ Tiles tiles_of(const Item& it, int group) {
   Tiles t;
-  const int n = (it.len + kTile - 1) / kTile;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     const int x = 2 * it.a + k;
     t.row_tile[k] = x / group;
     t.head[k] = it.b * group + x % group;
-    t.nb[k] = t.row_tile[k] < n ? t.row_tile[k] + 1 : 0;
+    t.keys[k] = t.row_tile[k] * kTile < it.len ? min(it.len, (t.row_tile[k] + 1) * kTile) : 0;
+    t.nb[k] = (t.keys[k] + Smem<HD>::kKeys - 1) / Smem<HD>::kKeys;
   }
   return t;
 }
@@ -78,16 +89,16 @@ __global__ void __launch_bounds__(kThreads, 1)
     prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                        const __grid_constant__ CUtensorMap tm_v, const Params p) {
   using Sm = Smem<HD>;
-  constexpr int KB = HD / 64, NS = Sm::kStages;
+  constexpr int KB = HD / 64, NS = Sm::kStages, KN = Sm::kKeys;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + Sm::kBars);
   const uint32_t s0 = smem_u32(smem), b0 = smem_u32(bars);
   auto BAR = [&](int i) { return b0 + 8u * static_cast<uint32_t>(i); };
-  Item* items = reinterpret_cast<Item*>(bars + kBarCount + 1);
+  Item* items = reinterpret_cast<Item*>(bars + kBarCount);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(items + kItems);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert((kBarCount + 1) * 8 + kItems * 16 + 8 <= 1024 && (kBarCount + 1) % 2 == 0, "barrier area");
+  static_assert(kBarCount * 8 + kItems * 16 + 8 <= 1024 && kBarCount % 2 == 0, "barrier area");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint32_t* status = p.a.status;
   const uint64_t limit = p.wait_limit;
@@ -97,17 +108,18 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(BAR(QFULL + t), 1);
       mbar_init(BAR(QFREE + t), 1);
       mbar_init(BAR(SFULL + t), 1);
-      mbar_init(BAR(PFULL + t), 4);
+      mbar_init(BAR(SREAD + t), kSoftWarps / 2);
+      mbar_init(BAR(PFULL + t), kSoftWarps / 2);
       mbar_init(BAR(PVDONE + t), 1);
+      mbar_init(BAR(DRAIN + t), 1);
     }
-    mbar_init(BAR(DRAIN), 1);
     for (int i = 0; i < kItems; ++i) {
       mbar_init(BAR(IFULL + i), 1);
       mbar_init(BAR(IFREE + i), kItemReaders);
     }
     for (int s = 0; s < NS; ++s) {
       mbar_init(BAR(KVFULL + s), 1);
-      mbar_init(BAR(KVFREE + s), 2);
+      mbar_init(BAR(KVFREE + s), 1);
       mbar_init(BAR(TAIL + s), 1);
     }
     *abort_flag = 0;
@@ -118,174 +130,165 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  auto stage = [&](int f) { return s0 + Sm::kRing + (f % NS) * Sm::kTileBytes; };
-  auto wait1 = [&](int bar, uint32_t parity) { return quick_wait(BAR(bar), parity & 1u, abort_flag, status, limit); };
+  auto slot = [&](int s) { return s0 + Sm::kRing + static_cast<uint32_t>(s) * Sm::kKvBytes; };
+  auto waitw = [&](int bar, uint32_t phase) { return warp_waits(BAR(bar), phase & 1u, abort_flag, status, limit); };
+  // Next descriptor; false at the end or at a timeout.
+  auto take = [&](int k, Item& it) {
+    if (!waitw(IFULL + (k & 7), k >> 3)) return false;
+    it = items[k & 7];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(BAR(IFREE + (k & 7)));
+    return it.len >= 0;
+  };
 
   if (warp == 0) {
-    if (lane == 0) {
-      // ------------------------------------------------------------------ loads
-      int f = 0, used[2] = {0, 0};          // ring slots filled; Q tiles loaded
-      uint32_t on_tail = 0, tail_phase = 0;  // of each slot: its last load went to warp 2 first; how many did, modulo 2
-      bool ok = true;
-      for (int k = 0; ok; ++k) {
-        if (!(ok = wait1(IFULL + (k & 7), k >> 3))) break;
-        const Item it = items[k & 7];
-        mbar_arrive(BAR(IFREE + (k & 7)));
-        if (it.len < 0) break;
-        const Tiles t = tiles_of(it, p.group);
-        auto load_q = [&](int x) {
-          if (used[x] && !wait1(QFREE + x, used[x] - 1)) return false;
-          mbar_arrive_expect_tx(BAR(QFULL + x), Sm::kTileBytes);
-#pragma unroll
-          for (int kb = 0; kb < KB; ++kb)
-            tma_load_2d(s0 + x * Sm::kTileBytes + kb * kBlockBytes, &tm_q, BAR(QFULL + x), t.head[x] * HD + kb * 64,
-                        it.begin + t.row_tile[x] * kTile);
-          ++used[x];
-          return true;
-        };
-        auto load_kv = [&](const CUtensorMap* map, int j, bool tail) {
-          const int s = f % NS, bar = (tail ? TAIL : KVFULL) + s;
-          if (f >= NS && !wait1(KVFREE + s, f / NS - 1)) return false;
-          mbar_arrive_expect_tx(BAR(bar), Sm::kTileBytes);
-#pragma unroll
-          for (int kb = 0; kb < KB; ++kb) tma_load_2d(stage(f) + kb * kBlockBytes, map, BAR(bar), it.b * HD + kb * 64, it.begin + j * kTile);
-          on_tail = (on_tail & ~(1u << s)) | (static_cast<uint32_t>(tail) << s);
-          tail_phase ^= static_cast<uint32_t>(tail) << s;
-          ++f;
-          return true;
-        };
-        auto load_k = [&](int j) { return load_kv(&tm_k, j, false); };
-        auto load_v = [&](int j) { return load_kv(&tm_v, j, it.len - j * kTile < kTile); };
-        const int nb = max(t.nb[0], t.nb[1]);
-        ok = load_k(0) && (!t.nb[0] || load_q(0)) && (!t.nb[1] || load_q(1)) && load_v(0);
-        for (int j = 1; j < nb && ok; ++j) ok = load_k(j) && load_v(j);
-      }
-      // nothing may land after the CTA has gone
-      for (int i = max(0, f - NS); i < f; ++i) {
-        const int s = i % NS;
-        if ((on_tail >> s) & 1)
-          wait_drain(BAR(TAIL + s), ((tail_phase >> s) & 1) ^ 1, limit);
-        else
-          wait_drain(BAR(KVFULL + s), (i / NS) & 1, limit);
-      }
-      for (int x = 0; x < 2; ++x)
-        if (used[x]) wait_drain(BAR(QFULL + x), (used[x] - 1) & 1, limit);
-    }
-  } else if (warp == 1) {
-    // ------------------------------------------------------------------ MMAs
-    const uint32_t is = tile_idesc(128, FP16, false), io = tile_idesc(HD, FP16, true);
-    auto waits = [&](int bar, int phase) { return warp_waits(BAR(bar), static_cast<uint32_t>(phase) & 1u, abort_flag, status, limit); };
-    int base = 0, q[2] = {0, 0}, block[2] = {0, 0};  // blocks of the items before; Q tiles and blocks of each tile so far
-    auto free_kv = [&](int s, bool shared) {
-      tc_commit(BAR(KVFREE + s));
-      if (!shared) tc_commit(BAR(KVFREE + s));
-    };
-    // S of block j of tile x, over the weights of the block before (which its product has read)
-    auto scores = [&](const Tiles& t, int base, const int x, int j) {
-      const int f = 2 * (base + j), s = f % NS;
-      const bool first = j == 0, last = j == t.nb[x] - 1;
-      if (!waits(KVFULL + s, f / NS) || (first && !waits(QFULL + x, q[x])) || (block[x] > 0 && !waits(PVDONE + x, block[x] - 1))) return false;
-      tc_fence_after();
-      const uint32_t dq = tile_desc(s0 + x * Sm::kTileBytes), dk = tile_desc(stage(f)), tS = tmem + kColS + x * 128;
-      if (elected()) {
-#pragma unroll
-        for (int k = 0; k < HD / 16; ++k) tile_mma(tS, dq + k_major_step(k), dk + k_major_step(k), is, k > 0);
-        tc_commit(BAR(SFULL + x));
-        if (last) tc_commit(BAR(QFREE + x));
-        free_kv(s, j < t.nb[x ^ 1]);
-      }
-      __syncwarp();
-      q[x] += last;
-      return true;
-    };
-    auto product = [&](const Tiles& t, int len, const int x, int j) {
-      const int f = 2 * (base + j) + 1, s = f % NS, steps = (min(kTile, len - j * kTile) + 15) / 16;
-      if (!waits(KVFULL + s, f / NS) || !waits(PFULL + x, block[x])) return false;
-      tc_fence_after();
-      const uint32_t dv = tile_desc(stage(f)), tP = tmem + kColS + x * 128, tO = tmem + kColO + x * 128, more = j > 0;
-      if (elected()) {
-#pragma unroll
-        for (int k = 0; k < kTile / 16; ++k)
-          if (k < steps) tile_mma_ts(tO, tP + k * 8, dv + mn_major_step(k), io, k > 0 ? 1u : more);
-        tc_commit(BAR(PVDONE + x));
-        free_kv(s, j < t.nb[x ^ 1]);
-      }
-      __syncwarp();
-      ++block[x];
-      return true;
-    };
-    // An item's blocks: each tile's product, then its next scores; at the end the next item's first scores.
-    Item it;
-    auto take = [&](int k, Item& it, Tiles& t) {
-      if (!waits(IFULL + (k & 7), k >> 3)) return false;
-      const Item* src = items + (k & 7);
-      it = Item{0, uniform(src->len), uniform(src->a), uniform(src->b)};
-      if (lane == 0) mbar_arrive(BAR(IFREE + (k & 7)));
-      if (it.len >= 0) t = tiles_of(it, p.group);
-      return true;
-    };
-    Tiles t{};
-    bool ok = take(0, it, t);
-    if (ok && it.len >= 0) ok = scores(t, 0, 0, 0) && (!t.nb[1] || scores(t, 0, 1, 0));
-    for (int k = 1; ok && it.len >= 0; ++k) {
-      const int nb = max(t.nb[0], t.nb[1]);
-      for (int j = 0; j < nb && ok; ++j) {
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          if (j < t.nb[x]) ok = ok && product(t, it.len, x, j);
-          if (j + 1 < t.nb[x]) ok = ok && scores(t, base, x, j + 1);
-        }
-      }
-      base += nb;
-      ok = ok && take(k, it, t);
-      if (ok && it.len >= 0) ok = scores(t, base, 0, 0) && (!t.nb[1] || scores(t, base, 1, 0));
-    }
-    if (elected()) tc_commit(BAR(DRAIN));
-    wait_drain(BAR(DRAIN), 0, limit);
-  } else if (warp == 2) {
-    // ------------------------------------------------------------------ values behind the last row
-    int base = 0;
-    uint32_t phase = 0;
-    for (int k = 0;; ++k) {
-      if (!warp_waits(BAR(IFULL + (k & 7)), (k >> 3) & 1, abort_flag, status, limit)) break;
-      const Item it = items[k & 7];
-      __syncwarp();
-      if (lane == 0) mbar_arrive(BAR(IFREE + (k & 7)));
-      if (it.len < 0) break;
-      const Tiles t = tiles_of(it, p.group);
-      const int nb = max(t.nb[0], t.nb[1]), keys = it.len - (nb - 1) * kTile;
-      if (keys < kTile) {
-        const int f = 2 * (base + nb - 1) + 1, s = f % NS;
-        if (!warp_waits(BAR(TAIL + s), (phase >> s) & 1, abort_flag, status, limit)) break;
-        phase ^= 1u << s;
-        zero_tile_rows<HD>(smem + Sm::kRing + s * Sm::kTileBytes, keys, (keys + 15) & ~15);
-        fence_async_smem();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(BAR(KVFULL + s));
-      }
-      base += nb;
-    }
-  } else if (warp == 3) {
-    // ------------------------------------------------------------------ items
+    // ------------------------------------------------------------------ items and loads (a whole warp that waits, one thread that loads)
     const int n_seq = p.a.n_seq, group = p.group, Hk = p.a.n_kv_heads;
     if (blockIdx.x == 0) check_starts(p.a.seq_start, n_seq, p.a.rows, lane, 32, status);
     auto pairs_of = [&](int len) { return ((len + kTile - 1) / kTile * group + 1) / 2; };
     int k = 0;
     auto put = [&](const Item& it) {
-      if (k >= kItems && !warp_waits(BAR(IFREE + (k & 7)), ((k >> 3) - 1) & 1, abort_flag, status, limit)) return false;
+      if (k >= kItems && !waitw(IFREE + (k & 7), (k >> 3) - 1)) return false;
       if (lane == 0) {
         items[k & 7] = it;
         mbar_arrive(BAR(IFULL + (k & 7)));
       }
+      __syncwarp();
       ++k;
       return true;
+    };
+    int n = 0, used[2] = {0, 0};           // ring slots filled; Q tiles loaded
+    uint32_t on_tail = 0, tail_phase = 0;  // of each slot: its last load ends behind a sequence's last row; how many did, modulo 2
+    auto load = [&](const Item& it) {
+      const Tiles t = tiles_of<HD>(it, group);
+      auto load_q = [&](int x) {
+        if (used[x] && !waitw(QFREE + x, used[x] - 1)) return false;
+        if (lane == 0) {
+          mbar_arrive_expect_tx(BAR(QFULL + x), Sm::kQBytes);
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb)
+            tma_load_2d(s0 + x * Sm::kQBytes + kb * kBlockBytes, &tm_q, BAR(QFULL + x), t.head[x] * HD + kb * 64,
+                        it.begin + t.row_tile[x] * kTile);
+        }
+        __syncwarp();
+        ++used[x];
+        return true;
+      };
+      auto load_kv = [&](const CUtensorMap* map, int j, bool tail) {
+        const int s = n % NS, bar = (tail ? TAIL : KVFULL) + s;
+        if (n >= NS && !waitw(KVFREE + s, n / NS - 1)) return false;
+        if (lane == 0) {
+          mbar_arrive_expect_tx(BAR(bar), Sm::kKvBytes);
+#pragma unroll
+          for (int kb = 0; kb < KB; ++kb) tma_load_2d(slot(s) + kb * Sm::kKvBlock, map, BAR(bar), it.b * HD + kb * 64, it.begin + j * KN);
+        }
+        __syncwarp();
+        on_tail = (on_tail & ~(1u << s)) | (static_cast<uint32_t>(tail) << s);
+        tail_phase ^= static_cast<uint32_t>(tail) << s;
+        ++n;
+        return true;
+      };
+      auto load_k = [&](int j) { return load_kv(&tm_k, j, false); };
+      auto load_v = [&](int j) { return load_kv(&tm_v, j, it.len - j * KN < KN); };
+      const int nb = max(t.nb[0], t.nb[1]);
+      bool ok = load_k(0) && (!t.nb[0] || load_q(0)) && (!t.nb[1] || load_q(1)) && load_v(0);
+      for (int j = 1; j < nb && ok; ++j) ok = load_k(j) && load_v(j);
+      return ok;
     };
     if (find_items(
             p.a.seq_start, n_seq, p.a.rows, blockIdx.x, gridDim.x, p.items_bound,
             [&](int len) { return static_cast<int64_t>(pairs_of(len)) * Hk; },
-            [&](int begin, int len, int u) { return put(Item{begin, len, pairs_of(len) - 1 - u / Hk, u % Hk}); }))
+            [&](int begin, int len, int u) {
+              const Item it{begin, len, pairs_of(len) - 1 - u / Hk, u % Hk};
+              return put(it) && load(it);
+            }))
       put(Item{0, -1, 0, 0});
-    const Outside out(p.a.seq_start, n_seq, p.a.rows);
+    // nothing may land after the CTA has gone
+    for (int i = max(0, n - NS); i < n; ++i) {
+      const int s = i % NS;
+      if ((on_tail >> s) & 1)
+        wait_drain(BAR(TAIL + s), ((tail_phase >> s) & 1) ^ 1, limit);
+      else
+        wait_drain(BAR(KVFULL + s), (i / NS) & 1, limit);
+    }
+    for (int x = 0; x < 2; ++x)
+      if (used[x]) wait_drain(BAR(QFULL + x), (used[x] - 1) & 1, limit);
+  } else if (warp <= 2) {
+    // ------------------------------------------------------------------ products: S (warp 1), O (warp 2), of both tiles in turn
+    const bool is_o = warp == 2;
+    const uint32_t dq = tile_desc(s0), io = tile_idesc(HD, FP16, true);
+    int block[2] = {0, 0}, q[2] = {0, 0};  // blocks and Q tiles of each tile so far
+    int s = is_o ? 1 : 0, round = 0;       // ring slot of the next block, and how often the ring has gone round
+    Item it;
+    bool ok = true;
+    for (int k = 0; ok && take(k, it); ++k) {
+      it = Item{0, uniform(it.len), uniform(it.a), uniform(it.b)};
+      const Tiles t = tiles_of<HD>(it, p.group);
+      const int nb = max(t.nb[0], t.nb[1]);
+      for (int j = 0; j < nb && ok; ++j) {
+        const uint32_t kv = tile_desc(slot(s), Sm::kKvBlock);
+        if (!(ok = waitw(KVFULL + s, round))) break;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if (j >= t.nb[x]) continue;
+          const uint32_t tile = tmem + x * 256, tS = tile + Sm::kColS, tP = tile + Sm::kColP;
+          const int steps = (min(KN, t.keys[x] - j * KN) + 15) / 16;
+          const bool frees = x == 1 || j >= t.nb[1];  // the block's last reader (a commit covers what was issued before)
+          if (!is_o) {
+            const bool last = j == t.nb[x] - 1;
+            const uint32_t is = tile_idesc(16 * steps, FP16, false), dx = dq + x * (Sm::kQBytes >> 4);
+            if (!(ok = ok && (j > 0 || waitw(QFULL + x, q[x])) && (block[x] == 0 || waitw(SREAD + x, block[x] - 1)))) break;
+            tc_fence_after();
+            if (elected()) {
+#pragma unroll
+              for (int i = 0; i < HD / 16; ++i) tile_mma(tS, dx + k_major_step(i), kv + k_major_step(i, Sm::kKvBlock), is, i > 0);
+              tc_commit(BAR(SFULL + x));
+              if (last) tc_commit(BAR(QFREE + x));
+              if (frees) tc_commit(BAR(KVFREE + s));
+            }
+            q[x] += last;
+          } else {
+            const uint32_t more = j > 0;
+            if (!(ok = ok && waitw(PFULL + x, block[x]))) break;
+            tc_fence_after();
+            if (elected()) {
+#pragma unroll
+              for (int i = 0; i < KN / 16; ++i)
+                if (i < steps) tile_mma_ts(tile, tP + i * 8, kv + mn_major_step(i), io, i > 0 ? 1u : more);
+              tc_commit(BAR(PVDONE + x));
+              if (frees) tc_commit(BAR(KVFREE + s));
+            }
+          }
+          __syncwarp();
+          ++block[x];
+        }
+        s += 2;
+        if (s >= NS) {
+          s -= NS;
+          ++round;
+        }
+      }
+    }
+    if (elected()) tc_commit(BAR(DRAIN + warp - 1));
+    wait_drain(BAR(DRAIN + warp - 1), 0, limit);
+  } else if (warp == 3) {
+    // ------------------------------------------------------------------ values behind the last row, then rows of no sequence
+    int base = 0;
+    uint32_t phase = 0;
+    Item it;
+    for (int k = 0; take(k, it); ++k) {
+      const Tiles t = tiles_of<HD>(it, p.group);
+      base += max(t.nb[0], t.nb[1]);
+      const int rows = it.len - (max(t.nb[0], t.nb[1]) - 1) * KN, s = (2 * base - 1) % NS;
+      if (rows >= KN) continue;
+      if (!waitw(TAIL + s, phase >> s)) break;
+      phase ^= 1u << s;
+      zero_tile_rows<HD>(smem + Sm::kRing + s * Sm::kKvBytes, rows, (rows + 15) & ~15, Sm::kKvBlock);
+      fence_async_smem();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(BAR(KVFULL + s));
+    }
+    const Outside out(p.a.seq_start, p.a.n_seq, p.a.rows);
     for (int i = blockIdx.x; i < out.count(); i += gridDim.x) {
       const int row = out.row(i);
       zero_row(elem(p.a.out, row * p.a.ldo), p.a.n_q_heads * HD);
@@ -294,56 +297,62 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
   } else {
     // ------------------------------------------------------------------ softmax and output
-    const int x = (warp - 4) >> 2, q4 = warp & 3, r = q4 * 32 + lane;  // tile, lane quarter, row in the tile
-    const uint32_t tS = tmem + (static_cast<uint32_t>(q4 * 32) << 16) + kColS + x * 128;
-    const uint32_t tO = tmem + (static_cast<uint32_t>(q4 * 32) << 16) + kColO + x * 128;
-    uint8_t* staging = smem + Sm::kStage + (warp - 4) * 4096;
+    const int x = (warp - kSoftWarp0) >> 2, q4 = warp & 3, r = q4 * 32 + lane;  // tile, lane quarter, row in the tile
+    const uint32_t tO = tmem + (static_cast<uint32_t>(q4 * 32) << 16) + static_cast<uint32_t>(x) * 256;
+    const uint32_t tS = tO + Sm::kColS, tP = tO + Sm::kColP;
+    uint8_t* staging = smem + Sm::kStage + (warp - kSoftWarp0) * 2048;
     const float c = p.c;
+    const uint64_t c2 = pair_of(c, c);
     int block = 0;
     bool ok = true;
-    for (int k = 0; ok; ++k) {
-      if (!warp_waits(BAR(IFULL + (k & 7)), (k >> 3) & 1, abort_flag, status, limit)) break;
-      const Item it = items[k & 7];
-      __syncwarp();
-      if (lane == 0) mbar_arrive(BAR(IFREE + (k & 7)));
-      if (it.len < 0) break;
-      const Tiles t = tiles_of(it, p.group);
-      const int nb = t.nb[x];
+    Item it;
+    for (int k = 0; ok && take(k, it); ++k) {
+      const Tiles t = tiles_of<HD>(it, p.group);
+      const int nb = x ? t.nb[1] : t.nb[0], head = x ? t.head[1] : t.head[0], tile0 = (x ? t.row_tile[1] : t.row_tile[0]) * kTile;
       if (!nb) continue;
-      const int row0 = t.row_tile[x] * kTile + q4 * 32;  // the warp's first row in the sequence
-      const int live = min(32, it.len - row0);           // its rows, at most 0: none
+      const int live = min(32, it.len - tile0 - q4 * 32);  // the warp's rows of the sequence, at most 0: none
       float m = -INFINITY, l = 0.f;
       for (int j = 0; j < nb; ++j, ++block) {
-        if (!warp_waits(BAR(SFULL + x), block & 1, abort_flag, status, limit)) {
-          ok = false;
-          break;
-        }
+        if (!(ok = waitw(SFULL + x, block))) break;
         tc_fence_after();
+        uint32_t s[KN];
         if (live > 0) {
-          uint32_t s[128];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) tmem_ld32(tS + 32 * i, s + 32 * i);
+          for (int i = 0; i + 32 <= KN; i += 32) tmem_ld32(tS + i, s + i);
+          if constexpr (KN % 32) {
+            uint32_t v[16];
+            tmem_ld16(tS + KN - 16, v);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[KN - 16 + i] = v[i];
+          }
           tmem_wait_ld();
-          if (j == nb - 1) {
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(SREAD + x));
+        float alpha = 1.f;
+        if (live > 0) {
+          if ((j + 1) * KN > tile0) {  // keys behind the row
+            const int seen = tile0 + r - j * KN;
 #pragma unroll
-            for (int i = 0; i < 128; ++i) s[i] = i <= r ? s[i] : 0xff800000u;
+            for (int i = 0; i < KN; ++i) s[i] = i <= seen ? s[i] : 0xff800000u;
           }
           float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-          for (int i = 0; i < 128; ++i) top[i & 3] = fmaxf(top[i & 3], __uint_as_float(s[i]));
+          for (int i = 0; i < KN; i += 2)  // (three-input maxima)
+            top[(i >> 1) & 3] = fmaxf(top[(i >> 1) & 3], fmaxf(__uint_as_float(s[i]), __uint_as_float(s[i + 1])));
           const float mb = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-          float alpha = 1.f;
           if ((mb - m) * c > 8.f || j == 0) {
             alpha = j == 0 ? 0.f : ex2((m - mb) * c);
             m = mb == -INFINITY ? 0.f : mb;
             l *= alpha;
           }
+        }
+        // O and P are the last product's until it is done
+        if (block > 0 && !(ok = waitw(PVDONE + x, block - 1))) break;
+        tc_fence_after();
+        if (live > 0) {
           if (j > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
-            if (!warp_waits(BAR(PVDONE + x), (block - 1) & 1, abort_flag, status, limit)) {
-              ok = false;
-              break;
-            }
-            tc_fence_after();
 #pragma unroll 1
             for (int i = 0; i < HD; i += 16) {
               uint32_t v[16];
@@ -355,21 +364,26 @@ __global__ void __launch_bounds__(kThreads, 1)
             }
           }
           const float shift = fmaf(-m, c, p.offset);
-          const uint64_t c2 = pair_of(c, c), shift2 = pair_of(shift, shift);
-          uint64_t sum = 0;
+          const uint64_t shift2 = pair_of(shift, shift);
+          uint64_t sum[4] = {0, 0, 0, 0};
+          auto weights = [&](int i, auto count) {
+            uint32_t w[count() / 2];
 #pragma unroll
-          for (int i = 0; i < 128; i += 32) {
-            uint32_t w[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
+            for (int e = 0; e < count() / 2; ++e) {
               const float2 y = halves_of(fma2(pair_of(__uint_as_float(s[i + 2 * e]), __uint_as_float(s[i + 2 * e + 1])), c2, shift2));
               const float a = ex2(y.x), b = ex2(y.y);
-              sum = add2(sum, pair_of(a, b));
+              sum[e & 3] = add2(sum[e & 3], pair_of(a, b));
               w[e] = pack2<FP16>(a, b);
             }
-            tmem_st16(tS + i / 2, w);
-          }
-          const float2 both = halves_of(sum);
+            if constexpr (count() == 32)
+              tmem_st16(tP + i / 2, w);
+            else
+              tmem_st8(tP + i / 2, w);
+          };
+#pragma unroll
+          for (int i = 0; i + 32 <= KN; i += 32) weights(i, std::integral_constant<int, 32>());
+          if constexpr (KN % 32) weights(KN - 16, std::integral_constant<int, 16>());
+          const float2 both = halves_of(add2(add2(sum[0], sum[1]), add2(sum[2], sum[3])));
           l += both.x + both.y;
           tmem_wait_st();
         }
@@ -377,46 +391,17 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         if (lane == 0) mbar_arrive(BAR(PFULL + x));
       }
-      if (!ok || !warp_waits(BAR(PVDONE + x), (block - 1) & 1, abort_flag, status, limit)) break;
+      if (!ok || !(ok = waitw(PVDONE + x, block - 1))) break;
       tc_fence_after();
       if (live <= 0) continue;
-      // out = O / l: 64 channels at a time through shared memory, 4 rows of 128 bytes a store
-      const float inv = 1.f / l;
-      const int64_t row = it.begin + row0;
-      float bad = 0.f;
-#pragma unroll
-      for (int b = 0; b < KB; ++b) {
-        uint32_t v[64];
-        tmem_ld32(tO + 64 * b, v);
-        tmem_ld32(tO + 64 * b + 32, v + 32);
-        tmem_wait_ld();
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          uint32_t w[4];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float y0 = __uint_as_float(v[8 * e + 2 * i]) * inv, y1 = __uint_as_float(v[8 * e + 2 * i + 1]) * inv;
-            bad = fmaf(y0, 0.f, fmaf(y1, 0.f, bad));
-            w[i] = pack2<FP16>(y0, y1);
-          }
-          *reinterpret_cast<uint4*>(staging + lane * 128 + ((e ^ (lane & 7)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-        }
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const int rr = 4 * i + (lane >> 3), e = lane & 7;
-          if (rr < live)
-            *reinterpret_cast<uint4*>(elem(p.a.out, (row + rr) * p.a.ldo + t.head[x] * HD + b * 64 + e * 8)) =
-                *reinterpret_cast<const uint4*>(staging + rr * 128 + ((e ^ (rr & 7)) << 4));
-        }
-        __syncwarp();
-      }
-      if (p.a.lse && lane < live) p.a.lse[(row + lane) * p.a.n_q_heads + t.head[x]] = (log2f(l) - fmaf(-m, c, p.offset)) * kLn2;
-      uint32_t again = __ballot_sync(0xffffffffu, bad != 0.f && lane < live);
+      const int64_t row = it.begin + tile0 + q4 * 32;
+      const bool bad = store_tile<FP16, HD / 32>(tO, staging, 1.f / l, elem(p.a.out, row * p.a.ldo + head * HD), p.a.ldo, live);
+      if (p.a.lse && lane < live) p.a.lse[(row + lane) * p.a.n_q_heads + head] = (log2f(l) - fmaf(-m, c, p.offset)) * kLn2;
+      uint32_t again = __ballot_sync(0xffffffffu, bad && lane < live);
       while (again) {
         const int rr = __ffs(static_cast<int>(again)) - 1;
         again &= again - 1;
-        attend_row<HD, FP16>(p.a, static_cast<int>(row) + rr, t.head[x], it.begin);
+        attend_row<HD, FP16>(p.a, static_cast<int>(row) + rr, head, it.begin);
       }
     }
   }
@@ -443,8 +428,8 @@ int launch(const PromptArgs& a, cudaStream_t s) {
   p.items_bound = static_cast<int>(std::min<int64_t>((tiles + seqs + 1) / 2 * a.n_kv_heads, 0x7fffffff));
   CUtensorMap q, k, v;
   if (!make_tensor_map_2d(&q, a.q, a.rows, static_cast<int64_t>(a.n_q_heads) * HD, a.ldq, kTile, FP16) ||
-      !make_tensor_map_2d(&k, a.k, a.rows, static_cast<int64_t>(a.n_kv_heads) * HD, a.ldk, kTile, FP16) ||
-      !make_tensor_map_2d(&v, a.v, a.rows, static_cast<int64_t>(a.n_kv_heads) * HD, a.ldv, kTile, FP16))
+      !make_tensor_map_2d(&k, a.k, a.rows, static_cast<int64_t>(a.n_kv_heads) * HD, a.ldk, Smem<HD>::kKeys, FP16) ||
+      !make_tensor_map_2d(&v, a.v, a.rows, static_cast<int64_t>(a.n_kv_heads) * HD, a.ldv, Smem<HD>::kKeys, FP16))
     return cuda_fail(cudaErrorInvalidValue, "vla_prompt_attn: tensor maps");
   int sms = 0;
   if (const int rc = device_sms(&sms)) return rc;

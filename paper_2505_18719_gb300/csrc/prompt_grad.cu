@@ -133,36 +133,6 @@ __device__ __forceinline__ int ds_exponent(const Params& p, const Item& it) {
 }
 __device__ __forceinline__ float exp2_int(int e) { return __int_as_float((e + 127) << 23); }
 
-// `chunks` x 32 columns of this warp's 32 rows of tensor memory, times `scale`, to rows of `dst` (ld elements apart), of which `live` exist:
-// through 2 KB of shared memory, 8 rows of 64 bytes a store.
-template <bool FP16, int CHUNKS>
-__device__ __forceinline__ void store_tile(uint32_t tmem, uint8_t* staging, float scale, void* dst, int64_t ld, int live) {
-  const int lane = threadIdx.x & 31;
-#pragma unroll
-  for (int b = 0; b < CHUNKS; ++b) {
-    uint32_t v[32];
-    tmem_ld32(tmem + 32 * b, v);
-    tmem_wait_ld();
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      uint32_t w[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        w[i] = pack2<FP16>(__uint_as_float(v[8 * e + 2 * i]) * scale, __uint_as_float(v[8 * e + 2 * i + 1]) * scale);
-      *reinterpret_cast<uint4*>(staging + lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-    __syncwarp();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int rr = 8 * i + (lane >> 2), e = lane & 3;
-      if (rr < live)
-        *reinterpret_cast<uint4*>(elem(dst, rr * ld + b * 32 + e * 8)) =
-            *reinterpret_cast<const uint4*>(staging + rr * 64 + ((e ^ ((rr >> 1) & 3)) << 4));
-    }
-    __syncwarp();
-  }
-}
-
 template <int HD>
 struct Smem {
   static constexpr int kStages = HD == 128 ? 2 : 4;
@@ -287,9 +257,6 @@ struct RingLoads {
     }
   }
 };
-// Columns 16 k .. 16 k + 15 of a 16-bit operand whose halves lie over those of the 32-bit block that they came from.
-__device__ __forceinline__ uint32_t halves_step(int k) { return static_cast<uint32_t>((k >> 2) * 64 + (k & 3) * 8); }
-
 // ------------------------------------------------------------------------------------------- d_k, d_v
 // Item: key tile a, key-value head b.  Its blocks: query heads of the group, for each the query tiles from the last down to a (so that
 // CTAs of one head read the same tiles at about the same time).

@@ -57,4 +57,39 @@ __device__ __forceinline__ void zero_row(void* row, int n) {
   for (int e = threadIdx.x & 31; e < n / 8; e += 32) static_cast<uint4*>(row)[e] = make_uint4(0u, 0u, 0u, 0u);
 }
 
+// `chunks` x 32 columns of this warp's 32 rows of tensor memory, times `scale`, to rows of `dst` (ld elements apart), of which `live` exist:
+// through 2 KB of shared memory, 8 rows of 64 bytes a store.  Whether this thread's row has a NaN or an infinity.
+template <bool FP16, int CHUNKS>
+__device__ __forceinline__ bool store_tile(uint32_t tmem, uint8_t* staging, float scale, void* dst, int64_t ld, int live) {
+  const int lane = threadIdx.x & 31;
+  float bad = 0.f;
+#pragma unroll
+  for (int b = 0; b < CHUNKS; ++b) {
+    uint32_t v[32];
+    tmem_ld32(tmem + 32 * b, v);
+    tmem_wait_ld();
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      uint32_t w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float y0 = __uint_as_float(v[8 * e + 2 * i]) * scale, y1 = __uint_as_float(v[8 * e + 2 * i + 1]) * scale;
+        bad = fmaf(y0, 0.f, fmaf(y1, 0.f, bad));
+        w[i] = pack2<FP16>(y0, y1);
+      }
+      *reinterpret_cast<uint4*>(staging + lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int rr = 8 * i + (lane >> 2), e = lane & 3;
+      if (rr < live)
+        *reinterpret_cast<uint4*>(elem(dst, rr * ld + b * 32 + e * 8)) =
+            *reinterpret_cast<const uint4*>(staging + rr * 64 + ((e ^ ((rr >> 1) & 3)) << 4));
+    }
+    __syncwarp();
+  }
+  return bad != 0.f;
+}
+
 }  // namespace vla

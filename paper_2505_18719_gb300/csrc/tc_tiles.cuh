@@ -12,13 +12,20 @@ namespace vla {
 constexpr int kTile = 128;
 constexpr uint32_t kBlockBytes = kTile * 128;  // a column block of a tile
 
-// Low word of a tile's descriptor (the address, column blocks kBlockBytes apart); the high word is the same for all: groups of 8 rows
+// Low word of a tile's descriptor (the address, column blocks block_bytes apart); the high word is the same for all: groups of 8 rows
 // 1024 bytes apart, version 1, 128-byte swizzle.
 constexpr uint32_t kDescHigh = (1024u >> 4) | (1u << 14) | (2u << 29);
-__device__ __forceinline__ uint32_t tile_desc(uint32_t saddr) { return ((saddr & 0x3FFFFu) >> 4) | ((kBlockBytes >> 4) << 16); }
+__device__ __forceinline__ uint32_t tile_desc(uint32_t saddr, uint32_t block_bytes = kBlockBytes) {
+  return ((saddr & 0x3FFFFu) >> 4) | ((block_bytes >> 4) << 16);
+}
 // Offsets (in descriptor units of 16 bytes) of the k-th 16 elements along the sum: channels of a K-major operand, rows of an MN-major one.
-__device__ __forceinline__ constexpr uint32_t k_major_step(int k) { return (static_cast<uint32_t>(k >> 2) * kBlockBytes + (k & 3) * 32) >> 4; }
+__device__ __forceinline__ constexpr uint32_t k_major_step(int k, uint32_t block_bytes = kBlockBytes) {
+  return (static_cast<uint32_t>(k >> 2) * block_bytes + (k & 3) * 32) >> 4;
+}
 __device__ __forceinline__ constexpr uint32_t mn_major_step(int k) { return static_cast<uint32_t>(k) * (2048 >> 4); }
+
+// Columns 16 k .. 16 k + 15 of a 16-bit operand whose halves lie over those of the 32-bit block that they came from.
+__device__ __forceinline__ uint32_t halves_step(int k) { return static_cast<uint32_t>((k >> 2) * 64 + (k & 3) * 8); }
 
 // kind::f16, f32 sums, M = 128, N; A K-major (or in tensor memory), B K-major or MN-major.
 __device__ __forceinline__ uint32_t tile_idesc(int N, bool fp16, bool b_mn_major) {
@@ -83,6 +90,11 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
       "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
@@ -135,10 +147,10 @@ __device__ __forceinline__ bool warp_waits(uint32_t bar, uint32_t parity, volati
 
 // Rows `from` .. `to` - 1 of a tile in shared memory become zeros (one warp).
 template <int HD>
-__device__ __forceinline__ void zero_tile_rows(uint8_t* tile, int from, int to) {
+__device__ __forceinline__ void zero_tile_rows(uint8_t* tile, int from, int to, uint32_t block_bytes = kBlockBytes) {
   for (int i = threadIdx.x & 31; i < (to - from) * (HD / 8); i += 32) {
     const int row = from + i / (HD / 8), c = i % (HD / 8);
-    *reinterpret_cast<uint4*>(tile + (c >> 3) * kBlockBytes + row * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+    *reinterpret_cast<uint4*>(tile + (c >> 3) * block_bytes + row * 128 + (c & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
   }
 }
 
