@@ -19,10 +19,9 @@
 // Roles (384 threads):
 //   warp 0       finds the items (a scan over the sequences' lengths, 32 sequences a step), hands their descriptors round and loads their tiles by
 //                TMA: Q when the item before is done with it, key and value blocks into a ring;
-//   warps 1, 2   issue S = Q K^T and O += P V (V as the MN-major operand), each of both tiles in turn: one warp for both products cannot
-//                keep up, at 250 to 500 cycles from one group of products to the next;
-//   warp 3       a sequence's last values land with it: those behind the last row become zeros (their weights are zeros, but a NaN
-//                would spoil the product), then the block counts as loaded; at the end the rows of no sequence;
+//   warps 1, 2   issue S = Q K^T of a tile each;
+//   warp 3       issues O += P V of both (V as the MN-major operand).  One warp for all products cannot keep up, at 250 to 800 cycles from
+//                one group of products to the next beside the softmax;
 //   warps 4 - 11 one query row a thread: softmax, and the output through shared memory in whole sectors.  (Two threads a row: the
 //                exchange of their maxima costs what the shorter rows save.)
 // A row whose result is not finite is computed again from its own keys alone (attend_row): a NaN behind a row in its
@@ -51,12 +50,12 @@ struct Smem {
 };
 
 // Barriers.  Of each tile: Q loaded / free, S written / read, P written, its product done; end of the issuing warps' products; item
-// descriptors; ring slots, and loads into them that go through warp 3.
+// descriptors; ring slots, and loads into them that end behind a sequence's last row.
 enum : int {
   QFULL = 0, QFREE = 2, SFULL = 4, SREAD = 6, PFULL = 8, PVDONE = 10, DRAIN = 12, IFULL = 16, IFREE = 24, KVFULL = 32, KVFREE = 40, TAIL = 48,
   kBarCount = 56
 };
-constexpr int kItemReaders = 2 + 1 + kSoftWarps;
+constexpr int kItemReaders = 3 + kSoftWarps;
 
 struct Params {
   PromptArgs a;
@@ -111,15 +110,15 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(BAR(SREAD + t), kSoftWarps / 2);
       mbar_init(BAR(PFULL + t), kSoftWarps / 2);
       mbar_init(BAR(PVDONE + t), 1);
-      mbar_init(BAR(DRAIN + t), 1);
     }
+    for (int i = 0; i < 3; ++i) mbar_init(BAR(DRAIN + i), 1);
     for (int i = 0; i < kItems; ++i) {
       mbar_init(BAR(IFULL + i), 1);
       mbar_init(BAR(IFREE + i), kItemReaders);
     }
     for (int s = 0; s < NS; ++s) {
       mbar_init(BAR(KVFULL + s), 1);
-      mbar_init(BAR(KVFREE + s), 1);
+      mbar_init(BAR(KVFREE + s), (s & 1) ? 1 : 2);  // keys: read by a warp for each tile
       mbar_init(BAR(TAIL + s), 1);
     }
     *abort_flag = 0;
@@ -157,8 +156,9 @@ __global__ void __launch_bounds__(kThreads, 1)
       ++k;
       return true;
     };
-    int n = 0, used[2] = {0, 0};           // ring slots filled; Q tiles loaded
-    uint32_t on_tail = 0, tail_phase = 0;  // of each slot: its last load ends behind a sequence's last row; how many did, modulo 2
+    int n = 0, used[2] = {0, 0};  // ring slots filled; Q tiles loaded
+    // of each slot: its last load ends behind a sequence's last row; loads that did, and that did not, modulo 2
+    uint32_t on_tail = 0, tail_phase = 0, full_phase = 0;
     auto load = [&](const Item& it) {
       const Tiles t = tiles_of<HD>(it, group);
       auto load_q = [&](int x) {
@@ -185,6 +185,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncwarp();
         on_tail = (on_tail & ~(1u << s)) | (static_cast<uint32_t>(tail) << s);
         tail_phase ^= static_cast<uint32_t>(tail) << s;
+        full_phase ^= static_cast<uint32_t>(!tail) << s;
         ++n;
         return true;
       };
@@ -203,91 +204,6 @@ __global__ void __launch_bounds__(kThreads, 1)
               return put(it) && load(it);
             }))
       put(Item{0, -1, 0, 0});
-    // nothing may land after the CTA has gone
-    for (int i = max(0, n - NS); i < n; ++i) {
-      const int s = i % NS;
-      if ((on_tail >> s) & 1)
-        wait_drain(BAR(TAIL + s), ((tail_phase >> s) & 1) ^ 1, limit);
-      else
-        wait_drain(BAR(KVFULL + s), (i / NS) & 1, limit);
-    }
-    for (int x = 0; x < 2; ++x)
-      if (used[x]) wait_drain(BAR(QFULL + x), (used[x] - 1) & 1, limit);
-  } else if (warp <= 2) {
-    // ------------------------------------------------------------------ products: S (warp 1), O (warp 2), of both tiles in turn
-    const bool is_o = warp == 2;
-    const uint32_t dq = tile_desc(s0), io = tile_idesc(HD, FP16, true);
-    int block[2] = {0, 0}, q[2] = {0, 0};  // blocks and Q tiles of each tile so far
-    int s = is_o ? 1 : 0, round = 0;       // ring slot of the next block, and how often the ring has gone round
-    Item it;
-    bool ok = true;
-    for (int k = 0; ok && take(k, it); ++k) {
-      it = Item{0, uniform(it.len), uniform(it.a), uniform(it.b)};
-      const Tiles t = tiles_of<HD>(it, p.group);
-      const int nb = max(t.nb[0], t.nb[1]);
-      for (int j = 0; j < nb && ok; ++j) {
-        const uint32_t kv = tile_desc(slot(s), Sm::kKvBlock);
-        if (!(ok = waitw(KVFULL + s, round))) break;
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          if (j >= t.nb[x]) continue;
-          const uint32_t tile = tmem + x * 256, tS = tile + Sm::kColS, tP = tile + Sm::kColP;
-          const int steps = (min(KN, t.keys[x] - j * KN) + 15) / 16;
-          const bool frees = x == 1 || j >= t.nb[1];  // the block's last reader (a commit covers what was issued before)
-          if (!is_o) {
-            const bool last = j == t.nb[x] - 1;
-            const uint32_t is = tile_idesc(16 * steps, FP16, false), dx = dq + x * (Sm::kQBytes >> 4);
-            if (!(ok = ok && (j > 0 || waitw(QFULL + x, q[x])) && (block[x] == 0 || waitw(SREAD + x, block[x] - 1)))) break;
-            tc_fence_after();
-            if (elected()) {
-#pragma unroll
-              for (int i = 0; i < HD / 16; ++i) tile_mma(tS, dx + k_major_step(i), kv + k_major_step(i, Sm::kKvBlock), is, i > 0);
-              tc_commit(BAR(SFULL + x));
-              if (last) tc_commit(BAR(QFREE + x));
-              if (frees) tc_commit(BAR(KVFREE + s));
-            }
-            q[x] += last;
-          } else {
-            const uint32_t more = j > 0;
-            if (!(ok = ok && waitw(PFULL + x, block[x]))) break;
-            tc_fence_after();
-            if (elected()) {
-#pragma unroll
-              for (int i = 0; i < KN / 16; ++i)
-                if (i < steps) tile_mma_ts(tile, tP + i * 8, kv + mn_major_step(i), io, i > 0 ? 1u : more);
-              tc_commit(BAR(PVDONE + x));
-              if (frees) tc_commit(BAR(KVFREE + s));
-            }
-          }
-          __syncwarp();
-          ++block[x];
-        }
-        s += 2;
-        if (s >= NS) {
-          s -= NS;
-          ++round;
-        }
-      }
-    }
-    if (elected()) tc_commit(BAR(DRAIN + warp - 1));
-    wait_drain(BAR(DRAIN + warp - 1), 0, limit);
-  } else if (warp == 3) {
-    // ------------------------------------------------------------------ values behind the last row, then rows of no sequence
-    int base = 0;
-    uint32_t phase = 0;
-    Item it;
-    for (int k = 0; take(k, it); ++k) {
-      const Tiles t = tiles_of<HD>(it, p.group);
-      base += max(t.nb[0], t.nb[1]);
-      const int rows = it.len - (max(t.nb[0], t.nb[1]) - 1) * KN, s = (2 * base - 1) % NS;
-      if (rows >= KN) continue;
-      if (!waitw(TAIL + s, phase >> s)) break;
-      phase ^= 1u << s;
-      zero_tile_rows<HD>(smem + Sm::kRing + s * Sm::kKvBytes, rows, (rows + 15) & ~15, Sm::kKvBlock);
-      fence_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(BAR(KVFULL + s));
-    }
     const Outside out(p.a.seq_start, p.a.n_seq, p.a.rows);
     for (int i = blockIdx.x; i < out.count(); i += gridDim.x) {
       const int row = out.row(i);
@@ -295,6 +211,107 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (p.a.lse)
         for (int e = lane; e < p.a.n_q_heads; e += 32) p.a.lse[static_cast<int64_t>(row) * p.a.n_q_heads + e] = -INFINITY;
     }
+    // nothing may land after the CTA has gone
+    for (int i = max(0, n - NS); i < n; ++i) {
+      const int s = i % NS;
+      const bool tail = (on_tail >> s) & 1;
+      wait_drain(BAR((tail ? TAIL : KVFULL) + s), (((tail ? tail_phase : full_phase) >> s) & 1) ^ 1, limit);
+    }
+    for (int x = 0; x < 2; ++x)
+      if (used[x]) wait_drain(BAR(QFULL + x), (used[x] - 1) & 1, limit);
+  } else if (warp <= 2) {
+    // ------------------------------------------------------------------ S of tile x
+    const int x = warp - 1;
+    const uint32_t tS = tmem + static_cast<uint32_t>(x) * 256 + Sm::kColS, dq = tile_desc(s0 + x * Sm::kQBytes);
+    int block = 0, q = 0;  // blocks and Q tiles of this tile so far
+    int s = 0, round = 0;  // ring slot of the next block of keys, and how often the ring has gone round
+    auto next_slot = [&]() {
+      s += 2;
+      if (s >= NS) {
+        s = 0;
+        ++round;
+      }
+    };
+    Item it;
+    bool ok = true;
+    for (int k = 0; ok && take(k, it); ++k) {
+      it = Item{0, uniform(it.len), uniform(it.a), uniform(it.b)};
+      const Tiles t = tiles_of<HD>(it, p.group);
+      const int nb = x ? t.nb[1] : t.nb[0], other = x ? t.nb[0] : t.nb[1], keys = x ? t.keys[1] : t.keys[0];
+      for (int j = 0; j < nb; ++j, ++block) {
+        const uint32_t kv = tile_desc(slot(s), Sm::kKvBlock), is = tile_idesc((min(KN, keys - j * KN) + 15) & ~15, FP16, false);
+        const uint32_t freed = BAR(KVFREE + s);
+        const bool last = j == nb - 1, lone = j >= other;
+        // the scores go over those of the block before once the threads have read them
+        if (!(ok = waitw(KVFULL + s, round) && (j > 0 || waitw(QFULL + x, q)) && (block == 0 || waitw(SREAD + x, block - 1)))) break;
+        tc_fence_after();
+        if (elected()) {
+#pragma unroll
+          for (int i = 0; i < HD / 16; ++i) tile_mma(tS, dq + k_major_step(i), kv + k_major_step(i, Sm::kKvBlock), is, i > 0);
+          tc_commit(BAR(SFULL + x));
+          tc_commit(freed);
+          if (lone) tc_commit(freed);
+          if (last) tc_commit(BAR(QFREE + x));
+        }
+        __syncwarp();
+        next_slot();
+      }
+      q += nb > 0;
+      for (int j = nb; j < other; ++j) next_slot();
+    }
+    if (elected()) tc_commit(BAR(DRAIN + x));
+    wait_drain(BAR(DRAIN + x), 0, limit);
+  } else if (warp == 3) {
+    // ------------------------------------------------------------------ O += P V of both tiles in turn
+    const uint32_t io = tile_idesc(HD, FP16, true);
+    int block[2] = {0, 0};
+    int s = 1;
+    uint32_t tails = 0, fulls = 0;  // of each ring slot: its loads so far that end behind a sequence's last row, and the others, modulo 2
+    Item it;
+    bool ok = true;
+    for (int k = 0; ok && take(k, it); ++k) {
+      it = Item{0, uniform(it.len), uniform(it.a), uniform(it.b)};
+      const Tiles t = tiles_of<HD>(it, p.group);
+      const int nb = max(t.nb[0], t.nb[1]);
+      for (int j = 0; j < nb && ok; ++j) {
+        const uint32_t kv = tile_desc(slot(s), Sm::kKvBlock), freed = BAR(KVFREE + s);
+        const int rows = it.len - j * KN;
+        if (rows < KN) {
+          // values behind a sequence's last row become zeros: their weights are zeros, but a NaN would spoil the product
+          if (!(ok = waitw(TAIL + s, tails >> s))) break;
+          tails ^= 1u << s;
+          zero_tile_rows<HD>(smem + Sm::kRing + s * Sm::kKvBytes, rows, (rows + 15) & ~15, Sm::kKvBlock);
+          fence_async_smem();
+          __syncwarp();
+        } else if (!(ok = waitw(KVFULL + s, fulls >> s))) {
+          break;
+        } else {
+          fulls ^= 1u << s;
+        }
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          if (j >= t.nb[x]) continue;
+          const uint32_t tO = tmem + x * 256, tP = tO + Sm::kColP, more = j > 0;
+          const int steps = (min(KN, t.keys[x] - j * KN) + 15) / 16;
+          const bool frees = x == 1 || j >= t.nb[1];  // the block's last reader (a commit covers what was issued before)
+          if (!(ok = ok && waitw(PFULL + x, block[x]))) break;
+          tc_fence_after();
+          if (elected()) {
+#pragma unroll
+            for (int i = 0; i < KN / 16; ++i)
+              if (i < steps) tile_mma_ts(tO, tP + i * 8, kv + mn_major_step(i), io, i > 0 ? 1u : more);
+            tc_commit(BAR(PVDONE + x));
+            if (frees) tc_commit(freed);
+          }
+          __syncwarp();
+          ++block[x];
+        }
+        s += 2;
+        if (s >= NS) s = 1;
+      }
+    }
+    if (elected()) tc_commit(BAR(DRAIN + 2));
+    wait_drain(BAR(DRAIN + 2), 0, limit);
   } else {
     // ------------------------------------------------------------------ softmax and output
     const int x = (warp - kSoftWarp0) >> 2, q4 = warp & 3, r = q4 * 32 + lane;  // tile, lane quarter, row in the tile
@@ -330,6 +347,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         tc_fence_before();
         __syncwarp();
         if (lane == 0) mbar_arrive(BAR(SREAD + x));
+        // (asked for early: the answer takes 100 to 200 cycles)
+        const bool free_p = block == 0 || mbar_test_wait(BAR(PVDONE + x), (block - 1) & 1);
         float alpha = 1.f;
         if (live > 0) {
           if ((j + 1) * KN > tile0) {  // keys behind the row
@@ -337,11 +356,13 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
             for (int i = 0; i < KN; ++i) s[i] = i <= seen ? s[i] : 0xff800000u;
           }
-          float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+          float top[8];
 #pragma unroll
-          for (int i = 0; i < KN; i += 2)  // (three-input maxima)
-            top[(i >> 1) & 3] = fmaxf(top[(i >> 1) & 3], fmaxf(__uint_as_float(s[i]), __uint_as_float(s[i + 1])));
-          const float mb = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+          for (int i = 0; i < 8; ++i) top[i] = fmaxf(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
+#pragma unroll
+          for (int i = 16; i < KN; i += 2)  // (three-input maxima)
+            top[(i >> 1) & 7] = fmaxf(top[(i >> 1) & 7], fmaxf(__uint_as_float(s[i]), __uint_as_float(s[i + 1])));
+          const float mb = fmaxf(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), fmaxf(fmaxf(top[4], top[5]), fmaxf(top[6], top[7])));
           if ((mb - m) * c > 8.f || j == 0) {
             alpha = j == 0 ? 0.f : ex2((m - mb) * c);
             m = mb == -INFINITY ? 0.f : mb;
@@ -349,7 +370,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           }
         }
         // O and P are the last product's until it is done
-        if (block > 0 && !(ok = waitw(PVDONE + x, block - 1))) break;
+        if (!__all_sync(0xffffffffu, free_p) && !(ok = waitw(PVDONE + x, block - 1))) break;
         tc_fence_after();
         if (live > 0) {
           if (j > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
