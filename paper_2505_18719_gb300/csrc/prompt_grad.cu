@@ -29,7 +29,10 @@ namespace vla {
 
 namespace {
 
-constexpr int kThreads = 384;
+constexpr int kThreads = 512, kSumWarp0 = 8, kSumWarps = 8;
+// producer aside: scores, dP, sums (two of keys), rows behind the last, element-wise warps
+template <bool KEYS>
+constexpr int kItemReaders = 2 + (KEYS ? 2 : 1) + 1 + kSumWarps;
 constexpr int kRows = 4;         // blocks of rows' lse and D in flight
 constexpr int kNormRows = 32;    // rows of one entry of the largest norms
 constexpr float kPShift = 14.f;  // log2 of the fp16 weights' factor
@@ -133,644 +136,494 @@ __device__ __forceinline__ int ds_exponent(const Params& p, const Item& it) {
 }
 __device__ __forceinline__ float exp2_int(int e) { return __int_as_float((e + 127) << 23); }
 
-template <int HD>
-struct Smem {
-  static constexpr int kStages = HD == 128 ? 2 : 4;
-  static constexpr uint32_t kTileBytes = kTile * HD * 2;
-  // two tiles of the item, two rings, a warp's rows on their way out, rows' lse and D, barriers
-  static constexpr uint32_t kRingA = 2 * kTileBytes, kRingB = kRingA + kStages * kTileBytes, kStage = kRingB + kStages * kTileBytes;
+// The two kernels are one, with the parts of keys and queries exchanged: a CTA keeps a tile of 128 rows of two operands (KEYS: K and V; else Q
+// and dO) and streams blocks of kBlock rows of the other two (Q and dO; K and V) past it.
+template <int HD, bool KEYS>
+struct Shape {
+  static constexpr int kBlock = KEYS ? 80 : 128;
+  static constexpr int kStages = HD == 64 ? 4 : KEYS ? 3 : 2;
+  static constexpr int kHalf = kBlock / 2;  // columns of one of a row's two threads
+  // shared memory: the tile's two operands, two rings, a warp's rows on their way out, rows' lse and D, barriers
+  static constexpr uint32_t kTileBytes = kTile * HD * 2, kBlockBytes = kBlock * HD * 2, kColumns = kBlock * 128;
+  static constexpr uint32_t kRingA = 2 * kTileBytes, kRingB = kRingA + kStages * kBlockBytes, kStage = kRingB + kStages * kBlockBytes;
   static constexpr uint32_t kRowData = kStage + 8 * 2048, kBars = kRowData + kRows * 1024, kTotal = 1024 + kBars + 1024;
-  static_assert(kTotal <= 232448, "shared memory per CTA");
+  // tensor memory: scores, dP, P (KEYS), dS, sums (KEYS: d_v, d_k; else d_q)
+  static constexpr uint32_t kColS = 0, kColDp = kBlock, kColP = 2 * kBlock, kColDs = KEYS ? kColP + kBlock / 2 : kColP;
+  static constexpr uint32_t kColV = 256, kColSum = 384;
+  static_assert(kTotal <= 232448 && kColDs + kBlock / 2 <= (KEYS ? kColV : kColSum) && kColumns % 1024 == 0, "shared and tensor memory");
 };
 
-// Barriers: the item's two tiles, the rings A and B (up to 4 stages each), loads into them that go through warp 2, rows' data, the steps
-// of a block, the item's end, descriptors.
+// Barriers: the tile's two operands loaded / free; the rings A and B (up to 4 slots each), loads into them that end behind a sequence's
+// last row, rows' lse and D; of a block: scores written / read, dP written / read, P and dS written, the products with them done; the
+// issuing warps' ends; descriptors.
 enum : int {
   AFULL = 0, AFREE = 1, BFULL = 2, BFREE = 3, RAFULL = 4, RAFREE = 8, RBFULL = 12, RBFREE = 16, TAILA = 20, TAILB = 24, RFULL = 28, RFREE = 32,
-  SFULL = 36, SREAD = 37, PFULL = 38, DPFULL = 39, DSFULL = 41, DONE = 42, DRAIN = 43, IFULL = 44, IFREE = 52, kBarCount = 60
+  SFULL = 36, SREAD = 37, DPFULL = 38, DPREAD = 39, PFULL = 40, PDONE = 41, DSFULL = 42, DSDONE = 43, DRAIN = 44, IFULL = 48, IFREE = 56,
+  kBarCount = 64
 };
 
-struct Shared {
-  uint8_t* smem;
-  uint32_t s0, b0;
-  Item* items;
-  uint32_t* tmem_slot;
-  volatile int* abort_flag;
-  float* rows;
-  __device__ __forceinline__ uint32_t bar(int i) const { return b0 + 8u * static_cast<uint32_t>(i); }
-};
-template <int HD>
-__device__ __forceinline__ Shared shared_of(uint8_t* raw, int readers) {
-  using Sm = Smem<HD>;
-  Shared sh;
-  sh.smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(raw) + 1023) & ~static_cast<uintptr_t>(1023));
-  uint64_t* bars = reinterpret_cast<uint64_t*>(sh.smem + Sm::kBars);
-  sh.s0 = smem_u32(sh.smem);
-  sh.b0 = smem_u32(bars);
-  sh.items = reinterpret_cast<Item*>(bars + kBarCount);
-  sh.tmem_slot = reinterpret_cast<uint32_t*>(sh.items + kItems);
-  sh.abort_flag = reinterpret_cast<volatile int*>(sh.tmem_slot + 1);
-  sh.rows = reinterpret_cast<float*>(sh.smem + Sm::kRowData);
-  static_assert(kBarCount * 8 + kItems * 16 + 8 <= 1024 && kBarCount % 2 == 0, "barrier area");
-  if (threadIdx.x == 0) {
-    for (int i = 0; i < kBarCount; ++i) {
-      const bool eight = i == SREAD || i == PFULL || i == DSFULL || (i >= RFREE && i < RFREE + kRows);
-      mbar_init(sh.bar(i), i >= IFREE ? readers : eight ? 8 : 1);
-    }
-    *sh.abort_flag = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+// f(head, first row in the sequence, rows, whether it holds rows on both sides of the mask) of an item's blocks in order, until one says no.
+// KEYS: key tile a, key-value head b: the query heads that share it, for each the queries from the last block down to the keys' own (so that
+// CTAs of one head read the same rows at about the same time).  Else: query tile a, query head b: keys from the first on.
+template <int HD, bool KEYS, class F>
+__device__ __forceinline__ bool for_blocks(const Item& it, int group, const F& f) {
+  constexpr int N = Shape<HD, KEYS>::kBlock;
+  if constexpr (KEYS) {
+    const int row0 = it.a * kTile, n = (it.len - row0 + N - 1) / N;
+    for (int h = it.b * group; h < (it.b + 1) * group; ++h)
+      for (int i = n - 1; i >= 0; --i)
+        if (!f(h, row0 + i * N, min(N, it.len - row0 - i * N), i * N < kTile)) return false;
+  } else {
+    for (int i = 0; i <= it.a; ++i)
+      if (!f(it.b / group, i * N, min(N, it.len - i * N), i == it.a)) return false;
   }
-  if ((threadIdx.x >> 5) == 1) tmem_take(smem_u32(sh.tmem_slot));
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  return sh;
+  return true;
 }
-__device__ __forceinline__ void end_of_kernel(uint32_t tmem) {
-  __syncwarp();
-  tc_fence_before();
-  __syncthreads();
-  if ((threadIdx.x >> 5) == 1) {
-    tc_fence_after();
-    tmem_give(tmem);
-  }
-}
-// Next descriptor, for one thread or a whole warp of which lane 0 answers; false at a timeout.
-__device__ __forceinline__ bool next_item(const Shared& sh, int k, Item& it, uint32_t* status, uint64_t limit, bool whole_warp) {
-  if (whole_warp ? !warp_waits(sh.bar(IFULL + (k & 7)), (k >> 3) & 1, sh.abort_flag, status, limit)
-                 : !quick_wait(sh.bar(IFULL + (k & 7)), (k >> 3) & 1, sh.abort_flag, status, limit))
-    return false;
-  it = sh.items[k & 7];
-  if (whole_warp) __syncwarp();
-  if (!whole_warp || (threadIdx.x & 31) == 0) mbar_arrive(sh.bar(IFREE + (k & 7)));
-  return it.len >= 0;
-}
-// The warp that finds the items; count(len) and what(len, number) as a pair.
-template <class Count, class What>
-__device__ __forceinline__ void put_items(const Params& p, const Shared& sh, const Count& count, const What& what) {
-  const PromptArgs& f = p.g.f;
-  const int lane = threadIdx.x & 31;
-  int k = 0;
-  auto put = [&](const Item& it) {
-    if (k >= kItems && !warp_waits(sh.bar(IFREE + (k & 7)), ((k >> 3) - 1) & 1, sh.abort_flag, f.status, p.wait_limit)) return false;
-    if (lane == 0) {
-      sh.items[k & 7] = it;
-      mbar_arrive(sh.bar(IFULL + (k & 7)));
-    }
-    ++k;
-    return true;
-  };
-  if (find_items(f.seq_start, f.n_seq, f.rows, blockIdx.x, gridDim.x, p.items_bound, count, [&](int begin, int len, int u) {
-        const int2 w = what(len, u);
-        return put(Item{begin, len, w.x, w.y});
-      }))
-    put(Item{0, -1, 0, 0});
-}
-template <int HD>
-__device__ __forceinline__ void load_tile(const Shared& sh, uint32_t dst, const CUtensorMap* map, int bar, int head, int row) {
-  mbar_arrive_expect_tx(sh.bar(bar), Smem<HD>::kTileBytes);
-#pragma unroll
-  for (int kb = 0; kb < HD / 64; ++kb) tma_load_2d(dst + kb * kBlockBytes, map, sh.bar(bar), head * HD + kb * 64, row);
-}
-// Loads into a ring: of a sequence's last rows to the barrier of warp 2, which makes those behind the last zeros and hands the tile on.
-template <int HD>
-struct RingLoads {
-  static constexpr int NS = Smem<HD>::kStages;
-  const Shared& sh;
-  int full, tail, n = 0;
-  uint32_t base, on_tail = 0, tail_phase = 0;  // of each slot: its last load went to warp 2; how many did, modulo 2
-  __device__ __forceinline__ void load(const CUtensorMap* map, int head, int row, bool is_tail) {
-    const int s = n % NS;
-    load_tile<HD>(sh, base + s * Smem<HD>::kTileBytes, map, (is_tail ? tail : full) + s, head, row);
-    on_tail = (on_tail & ~(1u << s)) | (static_cast<uint32_t>(is_tail) << s);
-    tail_phase ^= static_cast<uint32_t>(is_tail) << s;
-    ++n;
-  }
-  // nothing may land after the CTA has gone
-  __device__ __forceinline__ void drain(uint64_t limit) const {
-    for (int i = max(0, n - NS); i < n; ++i) {
-      const int s = i % NS;
-      if ((on_tail >> s) & 1)
-        wait_drain(sh.bar(tail + s), ((tail_phase >> s) & 1) ^ 1, limit);
-      else
-        wait_drain(sh.bar(full + s), (i / NS) & 1, limit);
-    }
-  }
-};
-// ------------------------------------------------------------------------------------------- d_k, d_v
-// Item: key tile a, key-value head b.  Its blocks: query heads of the group, for each the query tiles from the last down to a (so that
-// CTAs of one head read the same tiles at about the same time).
-template <int HD, bool FP16>
+
+template <int HD, bool FP16, bool KEYS>
 __global__ void __launch_bounds__(kThreads, 1)
-    prompt_grad_keys_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-                            const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_g, const Params p) {
-  using Sm = Smem<HD>;
-  constexpr int NS = Sm::kStages;
+    prompt_grad_kernel(const __grid_constant__ CUtensorMap tm_tile_a, const __grid_constant__ CUtensorMap tm_tile_b,
+                       const __grid_constant__ CUtensorMap tm_ring_a, const __grid_constant__ CUtensorMap tm_ring_b, const Params p) {
+  using Sh = Shape<HD, KEYS>;
+  constexpr int NS = Sh::kStages, N = Sh::kBlock, NH = Sh::kHalf;
   extern __shared__ uint8_t smem_raw[];
-  const Shared sh = shared_of<HD>(smem_raw, 1 + 1 + 1 + 8);
-  const uint32_t tmem = *sh.tmem_slot;
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  uint64_t* bars = reinterpret_cast<uint64_t*>(smem + Sh::kBars);
+  const uint32_t s0 = smem_u32(smem), b0 = smem_u32(bars);
+  auto BAR = [&](int i) { return b0 + 8u * static_cast<uint32_t>(i); };
+  Item* items = reinterpret_cast<Item*>(bars + kBarCount);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(items + kItems);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  float* row_data = reinterpret_cast<float*>(smem + Sh::kRowData);
+  static_assert(kBarCount * 8 + kItems * 16 + 8 <= 1024 && kBarCount % 2 == 0, "barrier area");
   const PromptArgs& f = p.g.f;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint32_t* status = f.status;
   const uint64_t limit = p.wait_limit;
-  auto wait1 = [&](int bar, int phase) { return quick_wait(sh.bar(bar), static_cast<uint32_t>(phase) & 1u, sh.abort_flag, status, limit); };
-  auto waitw = [&](int bar, int phase) { return warp_waits(sh.bar(bar), static_cast<uint32_t>(phase) & 1u, sh.abort_flag, status, limit); };
-  auto tiles = [](const Item& it) { return (it.len + kTile - 1) / kTile; };
-  auto rows_of = [](const Item& it, int t) { return min(kTile, it.len - t * kTile); };
-  auto slot_a = [&](int w) { return sh.s0 + Sm::kRingA + (w % NS) * Sm::kTileBytes; };  // Q
-  auto slot_b = [&](int w) { return sh.s0 + Sm::kRingB + (w % NS) * Sm::kTileBytes; };  // dO
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kBarCount; ++i) {
+      const bool all = i == SREAD || i == DPREAD || i == PFULL || i == DSFULL || (i >= RFREE && i < RFREE + kRows);
+      // (a dO tile is done when dP and d_v have been taken from it)
+      mbar_init(BAR(i), i >= IFREE ? kItemReaders<KEYS> : all ? kSumWarps : KEYS && i >= RBFREE && i < RBFREE + 4 ? 2 : 1);
+    }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) tmem_take(smem_u32(tmem_slot));
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  auto waitw = [&](int bar, uint32_t phase) { return warp_waits(BAR(bar), phase & 1u, abort_flag, status, limit); };
+  auto take = [&](int k, Item& it) {  // next descriptor; false at the end or at a timeout
+    if (!waitw(IFULL + (k & 7), k >> 3)) return false;
+    it = items[k & 7];
+    __syncwarp();
+    if (lane == 0) mbar_arrive(BAR(IFREE + (k & 7)));
+    return it.len >= 0;
+  };
+  auto take_uniform = [&](int k, Item& it) {
+    if (!take(k, it)) return false;
+    it = Item{0, uniform(it.len), uniform(it.a), uniform(it.b)};
+    return true;
+  };
+  // Slot of the next block of a ring, and how often the ring has gone round.
+  struct Ring {
+    int s = 0, round = 0;
+    __device__ __forceinline__ void next() {
+      if (++s == NS) {
+        s = 0;
+        ++round;
+      }
+    }
+  };
+  auto slot_a = [&](int s) { return s0 + Sh::kRingA + static_cast<uint32_t>(s) * Sh::kBlockBytes; };
+  auto slot_b = [&](int s) { return s0 + Sh::kRingB + static_cast<uint32_t>(s) * Sh::kBlockBytes; };
 
   if (warp == 0) {
-    if (lane == 0) {
-      RingLoads<HD> q{sh, RAFULL, TAILA, 0, sh.s0 + Sm::kRingA}, g{sh, RBFULL, TAILB, 0, sh.s0 + Sm::kRingB};
-      int w = 0, k = 0, n_k = 0, n_v = 0;  // blocks, items, K and V tiles loaded
-      Item it;
-      bool ok = true;
-      for (; ok && next_item(sh, k, it, status, limit, false); ++k) {
-        const int nt = tiles(it), row = it.begin + it.a * kTile;
-        bool first = true;
-        for (int h = it.b * p.group; h < (it.b + 1) * p.group && ok; ++h) {
-          for (int t = nt - 1; t >= it.a && ok; --t, ++w, first = false) {
-            const bool tail = rows_of(it, t) < kTile;
-            if (first) {
-              if (!(ok = k == 0 || wait1(AFREE, k - 1))) break;
-              load_tile<HD>(sh, sh.s0, &tm_k, AFULL, it.b, row);
-              ++n_k;
-            }
-            if (!(ok = w < NS || wait1(RAFREE + w % NS, w / NS - 1))) break;
-            q.load(&tm_q, h, it.begin + t * kTile, tail);
-            if (first) {
-              if (!(ok = k == 0 || wait1(BFREE, k - 1))) break;
-              load_tile<HD>(sh, sh.s0 + Sm::kTileBytes, &tm_v, BFULL, it.b, row);
-              ++n_v;
-            }
-            if (!(ok = w < NS || wait1(RBFREE + w % NS, w / NS - 1))) break;
-            g.load(&tm_g, h, it.begin + t * kTile, tail);
-          }
-        }
+    // ------------------------------------------------------------------ items and loads
+    const int heads = KEYS ? f.n_kv_heads : f.n_q_heads;
+    int k = 0, loaded = 0;  // items; blocks
+    // Of each slot of ring A, of ring B: its last load ends behind a sequence's last row; loads that did, and all, modulo 2.
+    uint32_t tails = 0, phase_tail = 0, phase = 0, b_tails = 0, b_phase_tail = 0, b_phase = 0;
+    int b_loaded = 0;
+    Ring ring;
+    auto put = [&](const Item& it) {
+      if (k >= kItems && !waitw(IFREE + (k & 7), (k >> 3) - 1)) return false;
+      if (lane == 0) {
+        items[k & 7] = it;
+        mbar_arrive(BAR(IFULL + (k & 7)));
       }
-      q.drain(limit);
-      g.drain(limit);
-      if (n_k) wait_drain(sh.bar(AFULL), (n_k - 1) & 1, limit);
-      if (n_v) wait_drain(sh.bar(BFULL), (n_v - 1) & 1, limit);
-    }
-  } else if (warp == 1) {
-    const uint32_t tS = tmem, tP = tmem + 128, tV = tmem + 256, tK = tmem + 384;
-    const uint32_t dk = tile_desc(sh.s0), dv = tile_desc(sh.s0 + Sm::kTileBytes), io = tile_idesc(HD, FP16, true);
-    int w = 0, k = 0;
-    Item it;
-    bool ok = true;
-    for (; ok && next_item(sh, k, it, status, limit, true); ++k) {
-      it = Item{0, uniform(it.len), uniform(it.a), uniform(it.b)};
-      const int nt = tiles(it), per_head = nt - it.a, units = per_head * p.group;
-      int ahead = 0;  // the next scores' block within its head
-      auto steps_at = [&](int at) { return (rows_of(it, nt - 1 - at) + 15) / 16; };
-      // S of block u; dP
-      auto scores = [&](int u) {
-        const int s = (w + u) % NS;
-        if (!waitw(RAFULL + s, (w + u) / NS)) return false;
-        tc_fence_after();
-        const uint32_t dq = tile_desc(slot_a(w + u)), id = tile_idesc(16 * steps_at(ahead), FP16, false);
-        if (elected()) {
-#pragma unroll
-          for (int i = 0; i < HD / 16; ++i) tile_mma(tS, dk + k_major_step(i), dq + k_major_step(i), id, i > 0);
-          tc_commit(sh.bar(SFULL));
-          if (u == units - 1) tc_commit(sh.bar(AFREE));
-        }
-        __syncwarp();
-        return true;
-      };
-      auto products = [&](int u) {
-        const int s = (w + u) % NS;
-        if (!waitw(RBFULL + s, (w + u) / NS)) return false;
-        tc_fence_after();
-        const uint32_t dg = tile_desc(slot_b(w + u)), id = tile_idesc(16 * steps_at(ahead), FP16, false);
-        if (elected()) {
-#pragma unroll
-          for (int i = 0; i < HD / 16; ++i) tile_mma(tP, dv + k_major_step(i), dg + k_major_step(i), id, i > 0);
-          tc_commit(sh.bar(DPFULL));
-          if (u == units - 1) tc_commit(sh.bar(BFREE));
-        }
-        __syncwarp();
-        return true;
-      };
-      if (!(ok = waitw(AFULL, k) && (w == 0 || waitw(RBFREE + (w - 1) % NS, (w - 1) / NS)) && scores(0) && waitw(BFULL, k) &&
-                 (w == 0 || waitw(RAFREE + (w - 1) % NS, (w - 1) / NS)) && products(0)))
-        break;
-      for (int u = 0; u < units && ok; ++u) {
-        const int s = (w + u) % NS, steps = steps_at(ahead);
-        ahead = ahead + 1 == per_head ? 0 : ahead + 1;
-        if (!(ok = waitw(PFULL, w + u))) break;
-        tc_fence_after();
-        const uint32_t dg = tile_desc(slot_b(w + u)), dq = tile_desc(slot_a(w + u)), more = u > 0;
-        if (elected()) {
-#pragma unroll
-          for (int i = 0; i < kTile / 16; ++i)
-            if (i < steps) tile_mma_ts(tV, tS + halves_step(i), dg + mn_major_step(i), io, i > 0 ? 1u : more);
-          tc_commit(sh.bar(RBFREE + s));
-        }
-        __syncwarp();
-        // the next scores go over P once d_v has read it, the next dP over dS once d_k has; the first two in the order in which they get ready
-        bool next_s = u + 1 < units, this_k = true;
-        uint64_t since = 0;
-        uint32_t spins = 0;
-        while (ok && (next_s || this_k)) {
-          if (this_k && warp_ready(sh.bar(DSFULL), (w + u) & 1)) {
-            tc_fence_after();
-            if (elected()) {
-#pragma unroll
-              for (int i = 0; i < kTile / 16; ++i)
-                if (i < steps) tile_mma_ts(tK, tP + halves_step(i), dq + mn_major_step(i), io, i > 0 ? 1u : more);
-              tc_commit(sh.bar(RAFREE + s));
-            }
-            __syncwarp();
-            this_k = false;
-          } else if (next_s && warp_ready(sh.bar(RBFREE + s), ((w + u) / NS) & 1)) {
-            if (!(ok = scores(u + 1))) break;
-            next_s = false;
-          } else if ((++spins & 1023u) == 0) {  // (the clock is slow to read)
-            if (spins == 1024) since = globaltimer();
-            if (__any_sync(0xffffffffu, *sh.abort_flag != 0)) {
-              ok = false;
-            } else if (__any_sync(0xffffffffu, globaltimer() - since > limit)) {
-              if (lane == 0) {
-                *sh.abort_flag = 1;
-                if (status) atomicOr(status, VLA_STATUS_TIMEOUT);
-              }
-              ok = false;
-            }
-          }
-        }
-        if (ok && u + 1 < units) ok = waitw(RAFREE + s, (w + u) / NS) && products(u + 1);
-      }
-      if (elected()) tc_commit(sh.bar(DONE));
       __syncwarp();
-      w += units;
+      return true;
+    };
+    auto load = [&](uint32_t dst, const CUtensorMap* map, int bar, uint32_t bytes, uint32_t columns, int head, int row) {
+      if (lane == 0) {
+        mbar_arrive_expect_tx(BAR(bar), bytes);
+#pragma unroll
+        for (int kb = 0; kb < HD / 64; ++kb) tma_load_2d(dst + kb * columns, map, BAR(bar), head * HD + kb * 64, row);
+      }
+      __syncwarp();
+    };
+    int in_a = 0, in_b = 0;  // tile operands loaded
+    auto load_item = [&](const Item& it) {
+      bool first = true;
+      return for_blocks<HD, KEYS>(it, p.group, [&](int head, int row, int rows, bool) {
+        const int s = ring.s;
+        const bool tail = rows < N;
+        if (first) {
+          if (k && !waitw(AFREE, k - 1)) return false;
+          load(s0, &tm_tile_a, AFULL, Sh::kTileBytes, kBlockBytes, it.b, it.begin + it.a * kTile);
+          ++in_a;
+        }
+        if (ring.round && !waitw(RAFREE + s, ring.round - 1)) return false;
+        load(slot_a(s), &tm_ring_a, (tail ? TAILA : RAFULL) + s, Sh::kBlockBytes, Sh::kColumns, head, it.begin + row);
+        tails = (tails & ~(1u << s)) | (static_cast<uint32_t>(tail) << s);
+        phase_tail ^= static_cast<uint32_t>(tail) << s;
+        phase ^= 1u << s;
+        ++loaded;
+        if (first) {
+          if (k && !waitw(BFREE, k - 1)) return false;
+          load(s0 + Sh::kTileBytes, &tm_tile_b, BFULL, Sh::kTileBytes, kBlockBytes, it.b, it.begin + it.a * kTile);
+          ++in_b;
+          first = false;
+        }
+        if (ring.round && !waitw(RBFREE + s, ring.round - 1)) return false;
+        load(slot_b(s), &tm_ring_b, (tail ? TAILB : RBFULL) + s, Sh::kBlockBytes, Sh::kColumns, head, it.begin + row);
+        b_tails = (b_tails & ~(1u << s)) | (static_cast<uint32_t>(tail) << s);
+        b_phase_tail ^= static_cast<uint32_t>(tail) << s;
+        b_phase ^= 1u << s;
+        ++b_loaded;
+        ring.next();
+        return true;
+      });
+    };
+    if (find_items(
+            f.seq_start, f.n_seq, f.rows, blockIdx.x, gridDim.x, p.items_bound,
+            [&](int len) { return static_cast<int64_t>((len + kTile - 1) / kTile) * heads; },
+            [&](int begin, int len, int u) {
+              // the most work first: the first keys, the last queries
+              const int t = u / heads;
+              const Item it{begin, len, KEYS ? t : (len + kTile - 1) / kTile - 1 - t, u % heads};
+              const bool ok = put(it) && load_item(it);
+              ++k;
+              return ok;
+            }))
+      put(Item{0, -1, 0, 0});
+    const Outside out(f.seq_start, f.n_seq, f.rows);
+    for (int i = blockIdx.x; i < out.count(); i += gridDim.x) {
+      if constexpr (KEYS) {
+        zero_row(elem(p.g.d_k, out.row(i) * p.g.lddk), heads * HD);
+        zero_row(elem(p.g.d_v, out.row(i) * p.g.lddv), heads * HD);
+      } else {
+        zero_row(elem(p.g.d_q, out.row(i) * p.g.lddq), heads * HD);
+      }
     }
-    if (elected()) tc_commit(sh.bar(DRAIN));
-    wait_drain(sh.bar(DRAIN), 0, limit);
-  } else if (warp == 2) {
-    int w = 0, k = 0, phase = 0;  // phase: of each slot, its tiles so far that came here first, modulo 2
+    // nothing may land after the CTA has gone
+    for (int s = 0; s < NS; ++s) {
+      const bool ta = (tails >> s) & 1, tb = (b_tails >> s) & 1;
+      if (s < loaded) wait_drain(BAR((ta ? TAILA : RAFULL) + s), (((ta ? phase_tail : phase) >> s) & 1) ^ 1, limit);
+      if (s < b_loaded) wait_drain(BAR((tb ? TAILB : RBFULL) + s), (((tb ? b_phase_tail : b_phase) >> s) & 1) ^ 1, limit);
+    }
+    if (in_a) wait_drain(BAR(AFULL), (in_a - 1) & 1, limit);
+    if (in_b) wait_drain(BAR(BFULL), (in_b - 1) & 1, limit);
+  } else if (warp <= 2) {
+    // ------------------------------------------------------------------ scores (warp 1), dP (warp 2)
+    const bool dp = warp == 2;
+    const uint32_t tile = tile_desc(s0 + (dp ? Sh::kTileBytes : 0)), d = tmem + (dp ? Sh::kColDp : Sh::kColS);
+    const int bar_tile = dp ? BFULL : AFULL, bar_ring = dp ? RBFULL : RAFULL, bar_read = dp ? DPREAD : SREAD;
+    const uint32_t full = BAR(dp ? DPFULL : SFULL), ring_free = BAR(RBFREE), tile_free = BAR(dp ? BFREE : AFREE);
+    Ring ring;
+    int w = 0;
     Item it;
     bool ok = true;
-    for (; ok && next_item(sh, k, it, status, limit, true); ++k) {
-      const int nt = tiles(it);
-      for (int h = it.b * p.group; h < (it.b + 1) * p.group && ok; ++h) {
-        for (int t = nt - 1; t >= it.a; --t, ++w) {
-          const int live = rows_of(it, t), s = w % NS;
-          float l[4], d[4];
+    for (int k = 0; ok && take_uniform(k, it); ++k) {
+      if (!(ok = waitw(bar_tile, k))) break;
+      ok = for_blocks<HD, KEYS>(it, p.group, [&](int, int, int rows, bool) {
+        const uint32_t block = tile_desc(dp ? slot_b(ring.s) : slot_a(ring.s), Sh::kColumns);
+        const uint32_t id = tile_idesc((rows + 15) & ~15, FP16, false), freed = ring_free + 8u * static_cast<uint32_t>(ring.s);
+        // over what the threads have read
+        if (!waitw(bar_ring + ring.s, ring.round) || (w > 0 && !waitw(bar_read, w - 1))) return false;
+        tc_fence_after();
+        if (elected()) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < HD / 16; ++i) tile_mma(d, tile + k_major_step(i), block + k_major_step(i, Sh::kColumns), id, i > 0);
+          tc_commit(full);
+          if (dp) tc_commit(freed);
+        }
+        __syncwarp();
+        ring.next();
+        ++w;
+        return true;
+      });
+      if (elected()) tc_commit(tile_free);
+      __syncwarp();
+    }
+    if (elected()) tc_commit(BAR(DRAIN + warp - 1));
+    wait_drain(BAR(DRAIN + warp - 1), 0, limit);
+  } else if (warp == 4 || (KEYS && warp == 3)) {
+    // ------------------------------------------------------------------ d_v += P^T dO (warp 3); d_k += dS^T Q or d_q += dS K (warp 4)
+    const bool dv = warp == 3;
+    const uint32_t a = tmem + (dv ? Sh::kColP : Sh::kColDs), d = tmem + (dv ? Sh::kColV : Sh::kColSum), io = tile_idesc(HD, FP16, true);
+    const int bar_ring = dv ? RBFULL : RAFULL, bar_a = dv ? PFULL : DSFULL;
+    const uint32_t done = BAR(dv ? PDONE : DSDONE), ring_free = BAR(dv ? RBFREE : RAFREE);
+    Ring ring;
+    int w = 0;
+    Item it;
+    bool ok = true;
+    for (int k = 0; ok && take_uniform(k, it); ++k) {
+      uint32_t more = 0;
+      ok = for_blocks<HD, KEYS>(it, p.group, [&](int, int, int rows, bool) {
+        const uint32_t block = tile_desc(dv ? slot_b(ring.s) : slot_a(ring.s), Sh::kColumns), freed = ring_free + 8u * static_cast<uint32_t>(ring.s);
+        const int steps = (rows + 15) / 16;
+        if (!waitw(bar_ring + ring.s, ring.round) || !waitw(bar_a, w)) return false;
+        tc_fence_after();
+        if (elected()) {
+#pragma unroll
+          for (int i = 0; i < N / 16; ++i)
+            if (i < steps) tile_mma_ts(d, a + i * 8, block + mn_major_step(i), io, i > 0 ? 1u : more);
+          tc_commit(done);
+          tc_commit(freed);
+        }
+        __syncwarp();
+        ring.next();
+        more = 1;
+        ++w;
+        return true;
+      });
+    }
+    if (elected()) tc_commit(BAR(DRAIN + warp - 1));
+    wait_drain(BAR(DRAIN + warp - 1), 0, limit);
+  } else if (warp == 5) {
+    // ------------------------------------------------------------------ rows behind the last; of KEYS, queries' lse and D
+    Ring ring;
+    uint32_t phase = 0;  // of each slot: blocks so far that end behind a sequence's last row, modulo 2
+    int w = 0;
+    Item it;
+    bool ok = true;
+    for (int k = 0; ok && take(k, it); ++k) {
+      ok = for_blocks<HD, KEYS>(it, p.group, [&](int head, int row, int rows, bool) {
+        const int s = ring.s;
+        if constexpr (KEYS) {
+          constexpr int R = (N + 31) / 32;
+          float l[R], d[R];
+#pragma unroll
+          for (int i = 0; i < R; ++i) {
             const int r = i * 32 + lane;
-            const int64_t at = static_cast<int64_t>(it.begin + t * kTile + min(r, live - 1)) * f.n_q_heads + h;
-            l[i] = r < live ? fmaf(f.lse[at], -kLog2e, FP16 ? kPShift : 0.f) : -INFINITY;  // weights of 0 behind the last row
-            d[i] = r < live ? p.delta[at] : 0.f;
+            const int64_t at = static_cast<int64_t>(it.begin + row + min(r, rows - 1)) * f.n_q_heads + head;
+            l[i] = r < rows ? fmaf(f.lse[at], -kLog2e, FP16 ? kPShift : 0.f) : -INFINITY;  // weights of 0 behind the last row
+            d[i] = r < rows ? -p.delta[at] : 0.f;
           }
-          if (!(ok = w < kRows || waitw(RFREE + w % kRows, w / kRows - 1))) break;
-          float* dst = sh.rows + (w % kRows) * 256;
+          if (w >= kRows && !waitw(RFREE + w % kRows, w / kRows - 1)) return false;
+          float* dst = row_data + (w % kRows) * 256;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
+          for (int i = 0; i < R; ++i) {
             dst[i * 32 + lane] = l[i];
             dst[128 + i * 32 + lane] = d[i];
           }
           __syncwarp();
-          if (lane == 0) mbar_arrive(sh.bar(RFULL + w % kRows));
-          if (live < kTile) {
-            if (!(ok = waitw(TAILA + s, phase >> s))) break;
-            zero_tile_rows<HD>(sh.smem + (slot_a(w) - sh.s0), live, (live + 15) & ~15);
+          if (lane == 0) mbar_arrive(BAR(RFULL + w % kRows));
+        }
+        if (rows < N) {
+#pragma unroll
+          for (int b = 0; b < 2; ++b) {
+            if (!waitw((b ? TAILB : TAILA) + s, phase >> s)) return false;
+            zero_tile_rows<HD>(smem + ((b ? slot_b(s) : slot_a(s)) - s0), rows, (rows + 15) & ~15, Sh::kColumns);
             fence_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(sh.bar(RAFULL + s));
-            if (!(ok = waitw(TAILB + s, phase >> s))) break;
-            zero_tile_rows<HD>(sh.smem + (slot_b(w) - sh.s0), live, (live + 15) & ~15);
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(sh.bar(RBFULL + s));
-            phase ^= 1 << s;
+            if (lane == 0) mbar_arrive(BAR((b ? RBFULL : RAFULL) + s));
           }
+          phase ^= 1u << s;
         }
-      }
-    }
-  } else if (warp == 3) {
-    const int Hk = f.n_kv_heads;
-    put_items(
-        p, sh, [&](int len) { return static_cast<int64_t>((len + kTile - 1) / kTile) * Hk; }, [&](int, int u) { return make_int2(u / Hk, u % Hk); });
-    const Outside out(f.seq_start, f.n_seq, f.rows);
-    for (int i = blockIdx.x; i < out.count(); i += gridDim.x) {
-      zero_row(elem(p.g.d_k, out.row(i) * p.g.lddk), Hk * HD);
-      zero_row(elem(p.g.d_v, out.row(i) * p.g.lddv), Hk * HD);
-    }
-  } else {
-    const int half = (warp - 4) >> 2, q4 = warp & 3, r = q4 * 32 + lane;  // columns 64 half .. 64 half + 63 of row (key) r
-    const uint32_t quarter = static_cast<uint32_t>(q4 * 32) << 16;
-    const uint32_t tS = tmem + quarter + 64 * half, tP = tS + 128;
-    uint8_t* staging = sh.smem + Sm::kStage + (warp - 4) * 2048;
-    int w = 0, k = 0;
-    Item it;
-    bool ok = true;
-    for (; ok && next_item(sh, k, it, status, limit, true); ++k) {
-      const int nt = tiles(it), e = FP16 ? ds_exponent(p, it) : 0;
-      const float up = FP16 ? exp2_int(e - static_cast<int>(kPShift)) : 1.f;
-      for (int h = 0; h < p.group && ok; ++h) {
-        for (int t = nt - 1; t >= it.a; --t, ++w) {
-          const bool work = 64 * half < rows_of(it, t);  // else no product reads these columns
-          const float4* rl = reinterpret_cast<const float4*>(sh.rows + (w % kRows) * 256 + 64 * half);
-          uint32_t s[64], x[64];
-          if (!(ok = waitw(RFULL + w % kRows, w / kRows) && waitw(SFULL, w))) break;
-          tc_fence_after();
-          if (work) {
-            tmem_ld32(tS, s);
-            tmem_ld32(tS + 32, s + 32);
-            tmem_wait_ld();
-            const uint64_t c2 = pair_of(p.c, p.c);
-#pragma unroll
-            for (int i = 0; i < 64; i += 32) {
-              uint32_t y[16];
-#pragma unroll
-              for (int j = 0; j < 32; j += 4) {
-                const float4 l = rl[(i + j) / 4];
-                const float2 a = halves_of(fma2(pair_of(__uint_as_float(s[i + j]), __uint_as_float(s[i + j + 1])), c2, pair_of(l.x, l.y)));
-                const float2 b = halves_of(fma2(pair_of(__uint_as_float(s[i + j + 2]), __uint_as_float(s[i + j + 3])), c2, pair_of(l.z, l.w)));
-                float v[4] = {ex2(a.x), ex2(a.y), ex2(b.x), ex2(b.y)};
-                if (t == it.a) {  // queries before the key do not see it
-#pragma unroll
-                  for (int q = 0; q < 4; ++q) v[q] = 64 * half + i + j + q >= r ? v[q] : 0.f;
-                }
-#pragma unroll
-                for (int q = 0; q < 4; ++q) s[i + j + q] = __float_as_uint(v[q]);
-                y[j / 2] = pack2<FP16>(v[0], v[1]);
-                y[j / 2 + 1] = pack2<FP16>(v[2], v[3]);
-              }
-              tmem_st16(tS + i / 2, y);
-            }
-            tmem_wait_st();
-          }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) mbar_arrive(sh.bar(PFULL));
-          if (!(ok = waitw(DPFULL, w))) break;
-          tc_fence_after();
-          if (work) {
-            tmem_ld32(tP, x);
-            tmem_ld32(tP + 32, x + 32);
-            tmem_wait_ld();
-            const uint64_t up2 = pair_of(up, up), minus = pair_of(-1.f, -1.f);
-#pragma unroll
-            for (int i = 0; i < 64; i += 32) {
-              uint32_t y[16];
-#pragma unroll
-              for (int j = 0; j < 32; j += 4) {
-                const float4 d = rl[32 + (i + j) / 4];
-                uint64_t a = fma2(pair_of(d.x, d.y), minus, pair_of(__uint_as_float(x[i + j]), __uint_as_float(x[i + j + 1])));
-                uint64_t b = fma2(pair_of(d.z, d.w), minus, pair_of(__uint_as_float(x[i + j + 2]), __uint_as_float(x[i + j + 3])));
-                if (FP16) {
-                  a = mul2(a, up2);
-                  b = mul2(b, up2);
-                }
-                const float2 ya = halves_of(mul2(a, pair_of(__uint_as_float(s[i + j]), __uint_as_float(s[i + j + 1]))));
-                const float2 yb = halves_of(mul2(b, pair_of(__uint_as_float(s[i + j + 2]), __uint_as_float(s[i + j + 3]))));
-                y[j / 2] = pack2<FP16>(ya.x, ya.y);
-                y[j / 2 + 1] = pack2<FP16>(yb.x, yb.y);
-              }
-              tmem_st16(tP + i / 2, y);
-            }
-            tmem_wait_st();
-          }
-          tc_fence_before();
-          __syncwarp();
-          if (lane == 0) {
-            mbar_arrive(sh.bar(DSFULL));
-            mbar_arrive(sh.bar(RFREE + w % kRows));
-          }
-        }
-      }
-      if (!ok || !(ok = waitw(DONE, k))) break;
-      tc_fence_after();
-      const int row0 = it.a * kTile + q4 * 32;
-      if (half == 0)
-        store_tile<FP16, HD / 32>(tmem + quarter + 256, staging, FP16 ? exp2_int(-static_cast<int>(kPShift)) : 1.f,
-                                  elem(p.g.d_v, (it.begin + row0) * p.g.lddv + it.b * HD), p.g.lddv, it.len - row0);
-      else
-        store_tile<FP16, HD / 32>(tmem + quarter + 384, staging, FP16 ? f.scale * exp2_int(-e) : f.scale,
-                                  elem(p.g.d_k, (it.begin + row0) * p.g.lddk + it.b * HD), p.g.lddk, it.len - row0);
-      tc_fence_before();
-    }
-  }
-  end_of_kernel(tmem);
-}
-
-// ------------------------------------------------------------------------------------------- d_q
-// Item: query tile a, query head b; key tiles 0 .. a.
-template <int HD, bool FP16>
-__global__ void __launch_bounds__(kThreads, 1)
-    prompt_grad_queries_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
-                               const __grid_constant__ CUtensorMap tm_v, const __grid_constant__ CUtensorMap tm_g, const Params p) {
-  using Sm = Smem<HD>;
-  constexpr int NS = Sm::kStages;
-  extern __shared__ uint8_t smem_raw[];
-  const Shared sh = shared_of<HD>(smem_raw, 1 + 1 + 1 + 8);
-  const uint32_t tmem = *sh.tmem_slot;
-  const PromptArgs& f = p.g.f;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  uint32_t* status = f.status;
-  const uint64_t limit = p.wait_limit;
-  auto wait1 = [&](int bar, int phase) { return quick_wait(sh.bar(bar), static_cast<uint32_t>(phase) & 1u, sh.abort_flag, status, limit); };
-  auto waitw = [&](int bar, int phase) { return warp_waits(sh.bar(bar), static_cast<uint32_t>(phase) & 1u, sh.abort_flag, status, limit); };
-  auto slot_a = [&](int w) { return sh.s0 + Sm::kRingA + (w % NS) * Sm::kTileBytes; };  // K
-  auto slot_b = [&](int w) { return sh.s0 + Sm::kRingB + (w % NS) * Sm::kTileBytes; };  // V
-
-  if (warp == 0) {
-    if (lane == 0) {
-      RingLoads<HD> kr{sh, RAFULL, TAILA, 0, sh.s0 + Sm::kRingA}, vr{sh, RBFULL, TAILB, 0, sh.s0 + Sm::kRingB};
-      int w = 0, k = 0, n_q = 0, n_g = 0;  // blocks, items, Q and dO tiles loaded
-      Item it;
-      bool ok = true;
-      for (; ok && next_item(sh, k, it, status, limit, false); ++k) {
-        const int g = it.b / p.group, row = it.begin + it.a * kTile;
-        for (int j = 0; j <= it.a && ok; ++j, ++w) {
-          if (j == 0) {
-            if (!(ok = k == 0 || wait1(AFREE, k - 1))) break;
-            load_tile<HD>(sh, sh.s0, &tm_q, AFULL, it.b, row);
-            ++n_q;
-          }
-          if (!(ok = w < NS || wait1(RAFREE + w % NS, w / NS - 1))) break;
-          kr.load(&tm_k, g, it.begin + j * kTile, it.len - j * kTile < kTile);
-          if (j == 0) {
-            if (!(ok = k == 0 || wait1(BFREE, k - 1))) break;
-            load_tile<HD>(sh, sh.s0 + Sm::kTileBytes, &tm_g, BFULL, it.b, row);
-            ++n_g;
-          }
-          if (!(ok = w < NS || wait1(RBFREE + w % NS, w / NS - 1))) break;
-          vr.load(&tm_v, g, it.begin + j * kTile, false);
-        }
-      }
-      kr.drain(limit);
-      vr.drain(limit);
-      if (n_q) wait_drain(sh.bar(AFULL), (n_q - 1) & 1, limit);
-      if (n_g) wait_drain(sh.bar(BFULL), (n_g - 1) & 1, limit);
-    }
-  } else if (warp == 1) {
-    const uint32_t tS = tmem, tQ = tmem + 384;
-    const uint32_t dq = tile_desc(sh.s0), dg = tile_desc(sh.s0 + Sm::kTileBytes), io = tile_idesc(HD, FP16, true);
-    int w = 0, k = 0;
-    Item it;
-    bool ok = true;
-    for (; ok && next_item(sh, k, it, status, limit, true); ++k) {
-      it = Item{0, uniform(it.len), uniform(it.a), uniform(it.b)};
-      auto steps_of = [&](int j) { return (min(kTile, it.len - j * kTile) + 15) / 16; };
-      auto scores = [&](int j) {
-        const int s = (w + j) % NS;
-        if (!waitw(RAFULL + s, (w + j) / NS)) return false;
-        tc_fence_after();
-        const uint32_t dk = tile_desc(slot_a(w + j)), id = tile_idesc(16 * steps_of(j), FP16, false);
-        if (elected()) {
-#pragma unroll
-          for (int i = 0; i < HD / 16; ++i) tile_mma(tS, dq + k_major_step(i), dk + k_major_step(i), id, i > 0);
-          tc_commit(sh.bar(SFULL));
-          if (j == it.a) tc_commit(sh.bar(AFREE));
-        }
-        __syncwarp();
+        ring.next();
+        ++w;
         return true;
-      };
-      auto products = [&](int j) {
-        const int s = (w + j) % NS;
-        if (!waitw(RBFULL + s, (w + j) / NS)) return false;
-        tc_fence_after();
-        const uint32_t dv = tile_desc(slot_b(w + j)), id = tile_idesc(16 * steps_of(j), FP16, false), tP = tmem + 128 + ((w + j) & 1) * 128;
-        if (elected()) {
-#pragma unroll
-          for (int i = 0; i < HD / 16; ++i) tile_mma(tP, dg + k_major_step(i), dv + k_major_step(i), id, i > 0);
-          tc_commit(sh.bar(DPFULL + ((w + j) & 1)));
-          tc_commit(sh.bar(RBFREE + s));
-          if (j == it.a) tc_commit(sh.bar(BFREE));
-        }
-        __syncwarp();
-        return true;
-      };
-      // (an item's first dP: the item before has ended, or the threads would not have read its last scores)
-      if (!(ok = waitw(AFULL, k) && (w == 0 || waitw(SREAD, w - 1)) && scores(0) && waitw(BFULL, k) &&
-                 (w < 2 || waitw(RAFREE + (w - 2) % NS, (w - 2) / NS)) && products(0)))
-        break;
-      for (int j = 0; j <= it.a && ok; ++j) {
-        // the next scores once the threads have read these, the next dP over the dS of the block before once d_q has read it
-        if (j < it.a && !(ok = waitw(SREAD, w + j) && scores(j + 1) && (w + j == 0 || waitw(RAFREE + (w + j - 1) % NS, (w + j - 1) / NS)) &&
-                               products(j + 1)))
-          break;
-        if (!(ok = waitw(DSFULL, w + j))) break;
-        tc_fence_after();
-        const uint32_t dk = tile_desc(slot_a(w + j)), tD = tmem + 128 + ((w + j) & 1) * 128, more = j > 0;
-        const int steps = steps_of(j);
-        if (elected()) {
-#pragma unroll
-          for (int i = 0; i < kTile / 16; ++i)
-            if (i < steps) tile_mma_ts(tQ, tD + halves_step(i), dk + mn_major_step(i), io, i > 0 ? 1u : more);
-          tc_commit(sh.bar(RAFREE + (w + j) % NS));
-        }
-        __syncwarp();
-      }
-      if (elected()) tc_commit(sh.bar(DONE));
-      __syncwarp();
-      w += it.a + 1;
+      });
     }
-    if (elected()) tc_commit(sh.bar(DRAIN));
-    wait_drain(sh.bar(DRAIN), 0, limit);
-  } else if (warp == 2) {
-    int w = 0, k = 0, phase = 0;
-    Item it;
-    for (; next_item(sh, k, it, status, limit, true); ++k) {
-      w += it.a + 1;
-      const int live = it.len - it.a * kTile, s = (w - 1) % NS;
-      if (live >= kTile) continue;
-      if (!waitw(TAILA + s, phase >> s)) break;
-      phase ^= 1 << s;
-      zero_tile_rows<HD>(sh.smem + (slot_a(w - 1) - sh.s0), live, (live + 15) & ~15);
-      fence_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(sh.bar(RAFULL + s));
-    }
-  } else if (warp == 3) {
-    const int H = f.n_q_heads;
-    put_items(
-        p, sh, [&](int len) { return static_cast<int64_t>((len + kTile - 1) / kTile) * H; },
-        [&](int len, int u) { return make_int2((len + kTile - 1) / kTile - 1 - u / H, u % H); });
-    const Outside out(f.seq_start, f.n_seq, f.rows);
-    for (int i = blockIdx.x; i < out.count(); i += gridDim.x) zero_row(elem(p.g.d_q, out.row(i) * p.g.lddq), H * HD);
-  } else {
-    const int half = (warp - 4) >> 2, q4 = warp & 3, r = q4 * 32 + lane;
-    const uint32_t quarter = static_cast<uint32_t>(q4 * 32) << 16;
-    const uint32_t tS = tmem + quarter + 64 * half;
-    uint8_t* staging = sh.smem + Sm::kStage + (warp - 4) * 2048;
-    int w = 0, k = 0;
+  } else if (warp >= kSumWarp0) {
+    // ------------------------------------------------------------------ P and dS, and the output
+    // Row r of the tile, NH columns of its blocks from NH half on.
+    const int half = (warp - kSumWarp0) >> 2, q4 = warp & 3, r = q4 * 32 + lane;
+    const uint32_t quarter = tmem + (static_cast<uint32_t>(q4 * 32) << 16);
+    const uint32_t tS = quarter + Sh::kColS + NH * half, tDp = quarter + Sh::kColDp + NH * half;
+    const uint32_t tP = quarter + Sh::kColP + NH / 2 * half, tDs = quarter + Sh::kColDs + NH / 2 * half;
+    uint8_t* staging = smem + Sh::kStage + (warp - kSumWarp0) * 2048;
+    const uint64_t c2 = pair_of(p.c, p.c);
+    int w = 0;
     Item it;
     bool ok = true;
-    for (; ok && next_item(sh, k, it, status, limit, true); ++k) {
+    for (int k = 0; ok && take(k, it); ++k) {
       const int e = FP16 ? ds_exponent(p, it) : 0;
-      const int row = it.a * kTile + r;
-      const int64_t at = static_cast<int64_t>(it.begin + min(row, it.len - 1)) * f.n_q_heads + it.b;
-      // 2^e goes into the weights
-      const float l = fmaf(f.lse[at], -kLog2e, static_cast<float>(e)), d = -p.delta[at];
-      const uint64_t c2 = pair_of(p.c, p.c), l2 = pair_of(l, l), d2 = pair_of(d, d);
-      for (int j = 0; j <= it.a; ++j, ++w) {
-        const uint32_t tP = tS + 128 + (w & 1) * 128;
-        const bool work = 64 * half < it.len - j * kTile;
-        uint32_t s[64], x[64];
-        if (!(ok = waitw(SFULL, w))) break;
+      const int row0 = it.a * kTile + q4 * 32;
+      // the factor of dS beside the weights' own; of a query row its lse (with the factor) and -D
+      const float up = FP16 ? exp2_int(e - static_cast<int>(kPShift)) : 1.f;
+      uint64_t l2 = 0, d2 = 0;
+      if constexpr (!KEYS) {
+        const int64_t at = static_cast<int64_t>(it.begin + min(it.a * kTile + r, it.len - 1)) * f.n_q_heads + it.b;
+        const float l = fmaf(f.lse[at], -kLog2e, static_cast<float>(e)), d = -p.delta[at];
+        l2 = pair_of(l, l);
+        d2 = pair_of(d, d);
+      }
+      ok = for_blocks<HD, KEYS>(it, p.group, [&](int, int row, int rows, bool edge) {
+        const bool work = NH * half < ((rows + 15) & ~15);  // else no product reads these columns
+        // columns of keys up to the query, or of queries from the key on
+        const int bound = it.a * kTile + r - row - NH * half;
+        const float4* rl = reinterpret_cast<const float4*>(row_data + (w % kRows) * 256 + NH * half);
+        uint32_t s[NH];
+        if ((KEYS && !waitw(RFULL + w % kRows, w / kRows)) || !waitw(SFULL, w)) return false;
         tc_fence_after();
         if (work) {
-          tmem_ld32(tS, s);
-          tmem_ld32(tS + 32, s + 32);
+          tmem_load<NH>(tS, s);
           tmem_wait_ld();
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(sh.bar(SREAD));
+        if (lane == 0) mbar_arrive(BAR(SREAD));
+        const bool free_p = !KEYS || w == 0 || mbar_test_wait(BAR(PDONE), (w - 1) & 1);
         if (work) {
 #pragma unroll
-          for (int i = 0; i < 64; i += 2) {
-            const float2 a = halves_of(fma2(pair_of(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), c2, l2));
+          for (int i = 0; i < NH; i += 4) {
+            uint64_t la = l2, lb = l2;
+            if constexpr (KEYS) {
+              const float4 l = rl[i / 4];
+              la = pair_of(l.x, l.y);
+              lb = pair_of(l.z, l.w);
+            }
+            const float2 a = halves_of(fma2(pair_of(__uint_as_float(s[i]), __uint_as_float(s[i + 1])), c2, la));
+            const float2 b = halves_of(fma2(pair_of(__uint_as_float(s[i + 2]), __uint_as_float(s[i + 3])), c2, lb));
             s[i] = __float_as_uint(ex2(a.x));
             s[i + 1] = __float_as_uint(ex2(a.y));
+            s[i + 2] = __float_as_uint(ex2(b.x));
+            s[i + 3] = __float_as_uint(ex2(b.y));
+          }
+          if (edge) {
+#pragma unroll
+            for (int i = 0; i < NH; ++i) s[i] = (KEYS ? i >= bound : i <= bound) ? s[i] : 0u;
           }
         }
-        if (!(ok = waitw(DPFULL + (w & 1), w >> 1))) break;
+        if constexpr (KEYS) {
+          // P is the last product's until that is done
+          if (!__all_sync(0xffffffffu, free_p) && !waitw(PDONE, w - 1)) return false;
+          tc_fence_after();
+          if (work) {
+            uint32_t y[NH / 2];
+#pragma unroll
+            for (int i = 0; i < NH / 2; ++i) y[i] = pack2<FP16>(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
+            tmem_store<NH / 2>(tP, y);
+            tmem_wait_st();
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(BAR(PFULL));
+        }
+        if (!waitw(DPFULL, w)) return false;
+        const bool free_ds = w == 0 || mbar_test_wait(BAR(DSDONE), (w - 1) & 1);
+        tc_fence_after();
+        uint32_t y[NH / 2];
+        if (work) {
+          constexpr int C = NH % 32 ? NH : 32;  // columns at a time
+#pragma unroll
+          for (int j = 0; j < NH; j += C) {
+            uint32_t x[C];
+            tmem_load<C>(tDp + j, x);
+            tmem_wait_ld();
+#pragma unroll
+            for (int i = 0; i < C; i += 4) {
+              uint64_t da = d2, db = d2;
+              if constexpr (KEYS) {
+                const float4 d = rl[32 + (i + j) / 4];
+                da = pair_of(d.x, d.y);
+                db = pair_of(d.z, d.w);
+              }
+              uint64_t a = add2(pair_of(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), da);
+              uint64_t b = add2(pair_of(__uint_as_float(x[i + 2]), __uint_as_float(x[i + 3])), db);
+              if (FP16 && KEYS) {
+                a = mul2(a, pair_of(up, up));
+                b = mul2(b, pair_of(up, up));
+              }
+              float2 ya = halves_of(mul2(a, pair_of(__uint_as_float(s[i + j]), __uint_as_float(s[i + j + 1]))));
+              float2 yb = halves_of(mul2(b, pair_of(__uint_as_float(s[i + j + 2]), __uint_as_float(s[i + j + 3]))));
+              if (edge) {  // (what the mask hides may be NaN)
+                const int q = i + j;
+                ya.x = (KEYS ? q >= bound : q <= bound) ? ya.x : 0.f;
+                ya.y = (KEYS ? q + 1 >= bound : q + 1 <= bound) ? ya.y : 0.f;
+                yb.x = (KEYS ? q + 2 >= bound : q + 2 <= bound) ? yb.x : 0.f;
+                yb.y = (KEYS ? q + 3 >= bound : q + 3 <= bound) ? yb.y : 0.f;
+              }
+              y[(i + j) / 2] = pack2<FP16>(ya.x, ya.y);
+              y[(i + j) / 2 + 1] = pack2<FP16>(yb.x, yb.y);
+            }
+          }
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          mbar_arrive(BAR(DPREAD));
+          if (KEYS) mbar_arrive(BAR(RFREE + w % kRows));
+        }
+        if (!__all_sync(0xffffffffu, free_ds) && !waitw(DSDONE, w - 1)) return false;
         tc_fence_after();
         if (work) {
-          tmem_ld32(tP, x);
-          tmem_ld32(tP + 32, x + 32);
-          tmem_wait_ld();
-#pragma unroll
-          for (int i = 0; i < 64; i += 32) {
-            uint32_t y[16];
-#pragma unroll
-            for (int q = 0; q < 32; q += 2) {
-              float2 a = halves_of(mul2(add2(pair_of(__uint_as_float(x[i + q]), __uint_as_float(x[i + q + 1])), d2),
-                                        pair_of(__uint_as_float(s[i + q]), __uint_as_float(s[i + q + 1]))));
-              if (j == it.a) {  // keys behind the query
-                a.x = 64 * half + i + q <= r ? a.x : 0.f;
-                a.y = 64 * half + i + q + 1 <= r ? a.y : 0.f;
-              }
-              y[q / 2] = pack2<FP16>(a.x, a.y);
-            }
-            tmem_st16(tP + i / 2, y);
-          }
+          tmem_store<NH / 2>(tDs, y);
           tmem_wait_st();
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(sh.bar(DSFULL));
-      }
-      if (!ok || !(ok = waitw(DONE, k))) break;
+        if (lane == 0) mbar_arrive(BAR(DSFULL));
+        ++w;
+        return true;
+      });
+      if (!ok || !(ok = (!KEYS || waitw(PDONE, w - 1)) && waitw(DSDONE, w - 1))) break;
       tc_fence_after();
-      const int row0 = it.a * kTile + q4 * 32;
-      store_tile<FP16, HD / 64>(tmem + quarter + 384 + half * (HD / 2), staging, FP16 ? f.scale * exp2_int(-e) : f.scale,
-                                elem(p.g.d_q, (it.begin + row0) * p.g.lddq + it.b * HD + half * (HD / 2)), p.g.lddq, it.len - row0);
+      const int64_t at = it.begin + row0;
+      if constexpr (KEYS) {
+        if (half == 0)
+          store_tile<FP16, HD / 32>(quarter + Sh::kColV, staging, FP16 ? exp2_int(-static_cast<int>(kPShift)) : 1.f,
+                                    elem(p.g.d_v, at * p.g.lddv + it.b * HD), p.g.lddv, it.len - row0);
+        else
+          store_tile<FP16, HD / 32>(quarter + Sh::kColSum, staging, FP16 ? f.scale * exp2_int(-e) : f.scale,
+                                    elem(p.g.d_k, at * p.g.lddk + it.b * HD), p.g.lddk, it.len - row0);
+      } else {
+        store_tile<FP16, HD / 64>(quarter + Sh::kColSum + half * (HD / 2), staging, FP16 ? f.scale * exp2_int(-e) : f.scale,
+                                  elem(p.g.d_q, at * p.g.lddq + it.b * HD + half * (HD / 2)), p.g.lddq, it.len - row0);
+      }
       tc_fence_before();
     }
   }
-  end_of_kernel(tmem);
+
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_give(tmem);
+  }
 }
 
 int norm_blocks_of(int rows) { return (rows + kNormRows - 1) / kNormRows; }
+
+template <int HD, bool FP16, bool KEYS>
+int launch_part(Params p, int sms, cudaStream_t s) {
+  using Sh = Shape<HD, KEYS>;
+  const PromptArgs& f = p.g.f;
+  const int q_tile = KEYS ? Sh::kBlock : kTile, kv_tile = KEYS ? kTile : Sh::kBlock;
+  CUtensorMap q, k, v, g;
+  if (!make_tensor_map_2d(&q, f.q, f.rows, static_cast<int64_t>(f.n_q_heads) * HD, f.ldq, q_tile, FP16) ||
+      !make_tensor_map_2d(&k, f.k, f.rows, static_cast<int64_t>(f.n_kv_heads) * HD, f.ldk, kv_tile, FP16) ||
+      !make_tensor_map_2d(&v, f.v, f.rows, static_cast<int64_t>(f.n_kv_heads) * HD, f.ldv, kv_tile, FP16) ||
+      !make_tensor_map_2d(&g, p.g.d_out, f.rows, static_cast<int64_t>(f.n_q_heads) * HD, p.g.lddo, q_tile, FP16))
+    return cuda_fail(cudaErrorInvalidValue, "vla_prompt_attn_grad: tensor maps");
+  const int64_t tiles = f.rows / kTile + std::min(f.n_seq, f.rows);  // as many as well-formed sequences can have
+  p.items_bound = static_cast<int>(std::min<int64_t>(tiles * (KEYS ? f.n_kv_heads : f.n_q_heads), 0x7fffffff));
+  const auto kern = prompt_grad_kernel<HD, FP16, KEYS>;
+  static std::atomic<uint64_t> done{0};
+  VLA_CUDA_TRY(set_smem_limit(kern, Sh::kTotal, done));
+  VLA_CUDA_TRY(launch_at(Start::kInOrder, kern, dim3(static_cast<unsigned>(std::min(p.items_bound, sms))), dim3(kThreads), Sh::kTotal, s,
+                         KEYS ? k : q, KEYS ? v : g, KEYS ? q : k, KEYS ? g : v, p));
+  note_launch();
+  return VLA_OK;
+}
 
 template <int HD, bool FP16>
 int launch(const PromptGradArgs& a, cudaStream_t s) {
@@ -785,30 +638,13 @@ int launch(const PromptGradArgs& a, cudaStream_t s) {
   p.norms = norms;
   p.norm_blocks = norm_blocks_of(f.rows);
   p.wait_limit = g_wait_limit_ns.load(std::memory_order_relaxed);
-  CUtensorMap q, k, v, g;
-  if (!make_tensor_map_2d(&q, f.q, f.rows, static_cast<int64_t>(f.n_q_heads) * HD, f.ldq, kTile, FP16) ||
-      !make_tensor_map_2d(&k, f.k, f.rows, static_cast<int64_t>(f.n_kv_heads) * HD, f.ldk, kTile, FP16) ||
-      !make_tensor_map_2d(&v, f.v, f.rows, static_cast<int64_t>(f.n_kv_heads) * HD, f.ldv, kTile, FP16) ||
-      !make_tensor_map_2d(&g, a.d_out, f.rows, static_cast<int64_t>(f.n_q_heads) * HD, a.lddo, kTile, FP16))
-    return cuda_fail(cudaErrorInvalidValue, "vla_prompt_attn_grad: tensor maps");
   int sms = 0;
   if (const int rc = device_sms(&sms)) return rc;
   VLA_CUDA_TRY(launch_at(Start::kInOrder, prompt_delta_kernel<HD, FP16>, dim3(static_cast<unsigned>(p.norm_blocks)), dim3(256), 0, s, a, delta,
                          norms, p.norm_blocks));
   note_launch();
-  const int64_t most = f.rows / kTile + std::min(f.n_seq, f.rows);  // tiles that well-formed sequences can have
-  static std::atomic<uint64_t> done_k{0}, done_q{0};
-  VLA_CUDA_TRY(set_smem_limit(prompt_grad_keys_kernel<HD, FP16>, Smem<HD>::kTotal, done_k));
-  VLA_CUDA_TRY(set_smem_limit(prompt_grad_queries_kernel<HD, FP16>, Smem<HD>::kTotal, done_q));
-  p.items_bound = static_cast<int>(std::min<int64_t>(most * f.n_kv_heads, 0x7fffffff));
-  VLA_CUDA_TRY(launch_at(Start::kInOrder, prompt_grad_keys_kernel<HD, FP16>, dim3(static_cast<unsigned>(std::min(p.items_bound, sms))), dim3(kThreads),
-                         Smem<HD>::kTotal, s, q, k, v, g, p));
-  note_launch();
-  p.items_bound = static_cast<int>(std::min<int64_t>(most * f.n_q_heads, 0x7fffffff));
-  VLA_CUDA_TRY(launch_at(Start::kInOrder, prompt_grad_queries_kernel<HD, FP16>, dim3(static_cast<unsigned>(std::min(p.items_bound, sms))), dim3(kThreads),
-                         Smem<HD>::kTotal, s, q, k, v, g, p));
-  note_launch();
-  return VLA_OK;
+  if (const int rc = launch_part<HD, FP16, true>(p, sms, s)) return rc;
+  return launch_part<HD, FP16, false>(p, sms, s);
 }
 
 }  // namespace

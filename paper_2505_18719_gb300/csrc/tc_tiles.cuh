@@ -24,9 +24,6 @@ __device__ __forceinline__ constexpr uint32_t k_major_step(int k, uint32_t block
 }
 __device__ __forceinline__ constexpr uint32_t mn_major_step(int k) { return static_cast<uint32_t>(k) * (2048 >> 4); }
 
-// Columns 16 k .. 16 k + 15 of a 16-bit operand whose halves lie over those of the 32-bit block that they came from.
-__device__ __forceinline__ uint32_t halves_step(int k) { return static_cast<uint32_t>((k >> 2) * 64 + (k & 3) * 8); }
-
 // kind::f16, f32 sums, M = 128, N; A K-major (or in tensor memory), B K-major or MN-major.
 __device__ __forceinline__ uint32_t tile_idesc(int N, bool fp16, bool b_mn_major) {
   return (1u << 4) | (fp16 ? 0u : (1u << 7) | (1u << 10)) | (b_mn_major ? 1u << 16 : 0u) | (static_cast<uint32_t>(N >> 3) << 17) |
@@ -90,10 +87,34 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t* r) {
       "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
       : "memory");
 }
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t* r) {
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7])
+               : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3])
+               : "memory");
+}
 __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
                "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
                : "memory");
+}
+// N columns (a multiple of 8) from tensor memory; N / 2 to it.
+template <int N>
+__device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t* r) {
+#pragma unroll
+  for (int i = 0; i + 32 <= N; i += 32) tmem_ld32(taddr + i, r + i);
+#pragma unroll
+  for (int i = N / 32 * 32; i < N; i += 8) tmem_ld8(taddr + i, r + i);
+}
+template <int N>
+__device__ __forceinline__ void tmem_store(uint32_t taddr, const uint32_t* r) {
+#pragma unroll
+  for (int i = 0; i + 16 <= N; i += 16) tmem_st16(taddr + i, r + i);
+#pragma unroll
+  for (int i = N / 16 * 16; i < N; i += 4) tmem_st4(taddr + i, r + i);
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
