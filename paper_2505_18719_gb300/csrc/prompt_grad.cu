@@ -30,10 +30,9 @@ namespace vla {
 namespace {
 
 constexpr int kThreads = 512, kSumWarp0 = 8, kSumWarps = 8;
-// producer aside: scores, dP, sums (two of keys), rows behind the last, element-wise warps
+// producer aside: scores, dP, sums (two of keys), of keys two for the rows' lse and D, rows behind the last, element-wise warps
 template <bool KEYS>
-constexpr int kItemReaders = 2 + (KEYS ? 2 : 1) + 1 + kSumWarps;
-constexpr int kRows = 4;         // blocks of rows' lse and D in flight
+constexpr int kItemReaders = 2 + (KEYS ? 2 + 2 : 1) + 1 + kSumWarps;
 constexpr int kNormRows = 32;    // rows of one entry of the largest norms
 constexpr float kPShift = 14.f;  // log2 of the fp16 weights' factor
 
@@ -140,29 +139,45 @@ __device__ __forceinline__ float exp2_int(int e) { return __int_as_float((e + 12
 // and dO) and streams blocks of kBlock rows of the other two (Q and dO; K and V) past it.
 template <int HD, bool KEYS>
 struct Shape {
-  static constexpr int kBlock = KEYS ? 80 : 128;
-  static constexpr int kStages = HD == 64 ? 4 : KEYS ? 3 : 2;
+  static constexpr int kBlock = KEYS ? 80 : 96;
+  static constexpr int kStages = HD == 64 ? 4 : 3;
   static constexpr int kHalf = kBlock / 2;  // columns of one of a row's two threads
+  static constexpr int kRows = 2;           // blocks of queries' lse and D in flight (KEYS)
+  static constexpr uint32_t kRowBytes = KEYS ? kRows * kBlock * 128 : 0;
   // shared memory: the tile's two operands, two rings, a warp's rows on their way out, rows' lse and D, barriers
   static constexpr uint32_t kTileBytes = kTile * HD * 2, kBlockBytes = kBlock * HD * 2, kColumns = kBlock * 128;
   static constexpr uint32_t kRingA = 2 * kTileBytes, kRingB = kRingA + kStages * kBlockBytes, kStage = kRingB + kStages * kBlockBytes;
-  static constexpr uint32_t kRowData = kStage + 8 * 2048, kBars = kRowData + kRows * 1024, kTotal = 1024 + kBars + 1024;
-  // tensor memory: scores, dP, P (KEYS), dS, sums (KEYS: d_v, d_k; else d_q)
-  static constexpr uint32_t kColS = 0, kColDp = kBlock, kColP = 2 * kBlock, kColDs = KEYS ? kColP + kBlock / 2 : kColP;
-  static constexpr uint32_t kColV = 256, kColSum = 384;
-  static_assert(kTotal <= 232448 && kColDs + kBlock / 2 <= (KEYS ? kColV : kColSum) && kColumns % 1024 == 0, "shared and tensor memory");
+  static constexpr uint32_t kRowData = kStage + 8 * 2048, kBars = kRowData + kRowBytes, kTotal = 1024 + kBars + 1024;
+  // Tensor memory: scores, dP, P and dS (KEYS; else two blocks of dP, and dS over each of them), 8 columns of ones, sums (KEYS: d_v, d_k; else d_q).
+  static constexpr uint32_t kColS = 0, kColDp = kBlock, kColP = 2 * kBlock, kColDs = KEYS ? kColP + kBlock / 2 : kColDp;
+  static constexpr uint32_t kColOnes = kColDs + kBlock / 2, kColV = 256, kColSum = 384;
+  static_assert(kTotal <= 232448 && (KEYS ? kColOnes + 8 <= kColV : kColDp + 2 * kBlock <= kColSum) && kColumns % 1024 == 0,
+                "shared and tensor memory");
 };
+// Of KEYS in bf16, queries' lse and D enter S and dP as 16 more channels (ones on the side of the keys): see prompt_grad_kernel.
+template <bool FP16, bool KEYS>
+constexpr bool kExtra = KEYS && !FP16;
 
 // Barriers: the tile's two operands loaded / free; the rings A and B (up to 4 slots each), loads into them that end behind a sequence's
-// last row, rows' lse and D; of a block: scores written / read, dP written / read, P and dS written, the products with them done; the
+// last row, rows' lse and D; of a block: scores written / read, dP written / read, P written, its product
+// done, dS written, its product done (of dP and dS, where not KEYS, two: even and odd blocks, of which no warp is then two ahead of another); the
 // issuing warps' ends; descriptors.
 enum : int {
-  AFULL = 0, AFREE = 1, BFULL = 2, BFREE = 3, RAFULL = 4, RAFREE = 8, RBFULL = 12, RBFREE = 16, TAILA = 20, TAILB = 24, RFULL = 28, RFREE = 32,
-  SFULL = 36, SREAD = 37, DPFULL = 38, DPREAD = 39, PFULL = 40, PDONE = 41, DSFULL = 42, DSDONE = 43, DRAIN = 44, IFULL = 48, IFREE = 56,
+  AFULL = 0, AFREE = 1, BFULL = 2, BFREE = 3, RAFULL = 4, RAFREE = 8, RBFULL = 12, RBFREE = 16, TAILA = 20, TAILB = 24, RFULL = 28, RFREE = 30,
+  SFULL = 32, SREAD = 33, DPFULL = 34, DPREAD = 36, PFULL = 37, PDONE = 38, DSFULL = 39, DSDONE = 41, DRAIN = 43, IFULL = 47, IFREE = 55,
   kBarCount = 64
 };
 
-// f(head, first row in the sequence, rows, whether it holds rows on both sides of the mask) of an item's blocks in order, until one says no.
+// A number as the sum of three bf16 (24 bits of it), in the first three of four.
+__device__ __forceinline__ uint2 three_terms(float x) {
+  bf16 a, b;
+  split_bf16(x, a, b);
+  const float rest = x - bf2f(a) - bf2f(b);
+  return make_uint2(static_cast<uint32_t>(__bfloat16_as_ushort(a)) | static_cast<uint32_t>(__bfloat16_as_ushort(b)) << 16,
+                    __bfloat16_as_ushort(f2bf(rest)));
+}
+
+// f(head, first row in the sequence, rows that count, whether the mask hides any of it) of an item's blocks in order, until one says no.
 // KEYS: key tile a, key-value head b: the query heads that share it, for each the queries from the last block down to the keys' own (so that
 // CTAs of one head read the same rows at about the same time).  Else: query tile a, query head b: keys from the first on.
 template <int HD, bool KEYS, class F>
@@ -174,12 +189,17 @@ __device__ __forceinline__ bool for_blocks(const Item& it, int group, const F& f
       for (int i = n - 1; i >= 0; --i)
         if (!f(h, row0 + i * N, min(N, it.len - row0 - i * N), i * N < kTile)) return false;
   } else {
-    for (int i = 0; i <= it.a; ++i)
-      if (!f(it.b / group, i * N, min(N, it.len - i * N), i == it.a)) return false;
+    const int end = min(it.len, (it.a + 1) * kTile);
+    for (int i = 0; i < end; i += N)
+      if (!f(it.b / group, i, min(N, end - i), i + N > it.a * kTile)) return false;
   }
   return true;
 }
 
+// S^T and dP^T have queries as columns, so a query's lse and D are of every thread, for each of its columns.  In bf16 the products bring them:
+// 16 more channels, ones on the side of the keys (in tensor memory), -lse / scale and -D as three bf16 numbers each on that of the queries, so
+// that S^T - lse / scale and dP^T - D come out.  From shared memory, which the products keep busy (128 bytes a cycle), the threads'
+// reads of them took 9 us of every 20.  fp16 does not hold the range of lse / scale and D, and reads them there.
 template <int HD, bool FP16, bool KEYS>
 __global__ void __launch_bounds__(kThreads, 1)
     prompt_grad_kernel(const __grid_constant__ CUtensorMap tm_tile_a, const __grid_constant__ CUtensorMap tm_tile_b,
@@ -197,24 +217,39 @@ __global__ void __launch_bounds__(kThreads, 1)
   float* row_data = reinterpret_cast<float*>(smem + Sh::kRowData);
   static_assert(kBarCount * 8 + kItems * 16 + 8 <= 1024 && kBarCount % 2 == 0, "barrier area");
   const PromptArgs& f = p.g.f;
+  constexpr int kRows = Sh::kRows;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint32_t* status = f.status;
   const uint64_t limit = p.wait_limit;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < kBarCount; ++i) {
-      const bool all = i == SREAD || i == DPREAD || i == PFULL || i == DSFULL || (i >= RFREE && i < RFREE + kRows);
+      const bool rows = i >= RFREE && i < RFREE + Sh::kRows;  // (read by S and dP, or by the element-wise warps)
+      const bool all = i == SREAD || i == DPREAD || i == PFULL || i == DSFULL || i == DSFULL + 1 || (rows && !kExtra<FP16, KEYS>);
       // (a dO tile is done when dP and d_v have been taken from it)
-      mbar_init(BAR(i), i >= IFREE ? kItemReaders<KEYS> : all ? kSumWarps : KEYS && i >= RBFREE && i < RBFREE + 4 ? 2 : 1);
+      mbar_init(BAR(i), i >= IFREE ? kItemReaders<KEYS> : all ? kSumWarps : (rows || (KEYS && i >= RBFREE && i < RBFREE + 4)) ? 2 : 1);
     }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) tmem_take(smem_u32(tmem_slot));
+  if constexpr (kExtra<FP16, KEYS>)
+    for (uint32_t i = threadIdx.x; i < Sh::kRowBytes / 16; i += kThreads) reinterpret_cast<uint4*>(row_data)[i] = make_uint4(0u, 0u, 0u, 0u);
+  fence_async_smem();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
+  if constexpr (kExtra<FP16, KEYS>) {
+    if (warp >= kSumWarp0 && warp < kSumWarp0 + 4) {  // three ones, thirteen zeros in every row
+      const uint32_t ones[8] = {0x3f803f80u, 0x00003f80u, 0u, 0u, 0u, 0u, 0u, 0u};
+      tmem_st8(tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + Sh::kColOnes, ones);
+      tmem_wait_st();
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+  }
   auto waitw = [&](int bar, uint32_t phase) { return warp_waits(BAR(bar), phase & 1u, abort_flag, status, limit); };
   auto take = [&](int k, Item& it) {  // next descriptor; false at the end or at a timeout
     if (!waitw(IFULL + (k & 7), k >> 3)) return false;
@@ -245,7 +280,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     // ------------------------------------------------------------------ items and loads
     const int heads = KEYS ? f.n_kv_heads : f.n_q_heads;
     int k = 0, loaded = 0;  // items; blocks
-    // Of each slot of ring A, of ring B: its last load ends behind a sequence's last row; loads that did, and all, modulo 2.
+    // Of each slot of ring A, of ring B: its last load has rows that have to become zeros; loads that did, and all, modulo 2.
     uint32_t tails = 0, phase_tail = 0, phase = 0, b_tails = 0, b_phase_tail = 0, b_phase = 0;
     int b_loaded = 0;
     Ring ring;
@@ -271,7 +306,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       bool first = true;
       return for_blocks<HD, KEYS>(it, p.group, [&](int head, int row, int rows, bool) {
         const int s = ring.s;
-        const bool tail = rows < N;
+        const bool tail = rows & 15;
         if (first) {
           if (k && !waitw(AFREE, k - 1)) return false;
           load(s0, &tm_tile_a, AFULL, Sh::kTileBytes, kBlockBytes, it.b, it.begin + it.a * kTile);
@@ -333,7 +368,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     const bool dp = warp == 2;
     const uint32_t tile = tile_desc(s0 + (dp ? Sh::kTileBytes : 0)), d = tmem + (dp ? Sh::kColDp : Sh::kColS);
     const int bar_tile = dp ? BFULL : AFULL, bar_ring = dp ? RBFULL : RAFULL, bar_read = dp ? DPREAD : SREAD;
-    const uint32_t full = BAR(dp ? DPFULL : SFULL), ring_free = BAR(RBFREE), tile_free = BAR(dp ? BFREE : AFREE);
+    const uint32_t ring_free = BAR(RBFREE), tile_free = BAR(dp ? BFREE : AFREE);
+    const uint32_t extra = tile_desc(smem_u32(row_data)) + (dp ? 2 : 0);
     Ring ring;
     int w = 0;
     Item it;
@@ -343,12 +379,19 @@ __global__ void __launch_bounds__(kThreads, 1)
       ok = for_blocks<HD, KEYS>(it, p.group, [&](int, int, int rows, bool) {
         const uint32_t block = tile_desc(dp ? slot_b(ring.s) : slot_a(ring.s), Sh::kColumns);
         const uint32_t id = tile_idesc((rows + 15) & ~15, FP16, false), freed = ring_free + 8u * static_cast<uint32_t>(ring.s);
-        // over what the threads have read
-        if (!waitw(bar_ring + ring.s, ring.round) || (w > 0 && !waitw(bar_read, w - 1))) return false;
+        const int buffer = !KEYS && dp ? w & 1 : 0, slot = w % kRows;
+        const uint32_t dst = d + static_cast<uint32_t>(buffer) * N, full = BAR((dp ? DPFULL : SFULL) + buffer);
+        // over what the threads have read (the dS that lies over dP: what d_q has been taken from)
+        const bool free_now = !KEYS && dp ? w < 2 || waitw(DSDONE + buffer, (w >> 1) - 1) : w < 1 || waitw(bar_read, w - 1);
+        if (!free_now || !waitw(bar_ring + ring.s, ring.round) || (kExtra<FP16, KEYS> && !waitw(RFULL + slot, w / kRows))) return false;
         tc_fence_after();
         if (elected()) {
 #pragma unroll
-          for (int i = 0; i < HD / 16; ++i) tile_mma(d, tile + k_major_step(i), block + k_major_step(i, Sh::kColumns), id, i > 0);
+          for (int i = 0; i < HD / 16; ++i) tile_mma(dst, tile + k_major_step(i), block + k_major_step(i, Sh::kColumns), id, i > 0);
+          if constexpr (kExtra<FP16, KEYS>) {
+            tile_mma_ts(dst, tmem + Sh::kColOnes, extra + static_cast<uint32_t>(slot) * (Sh::kColumns >> 4), id, 1u);
+            tc_commit(BAR(RFREE + slot));
+          }
           tc_commit(full);
           if (dp) tc_commit(freed);
         }
@@ -367,7 +410,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const bool dv = warp == 3;
     const uint32_t a = tmem + (dv ? Sh::kColP : Sh::kColDs), d = tmem + (dv ? Sh::kColV : Sh::kColSum), io = tile_idesc(HD, FP16, true);
     const int bar_ring = dv ? RBFULL : RAFULL, bar_a = dv ? PFULL : DSFULL;
-    const uint32_t done = BAR(dv ? PDONE : DSDONE), ring_free = BAR(dv ? RBFREE : RAFREE);
+    const uint32_t done0 = BAR(dv ? PDONE : DSDONE), ring_free = BAR(dv ? RBFREE : RAFREE);
     Ring ring;
     int w = 0;
     Item it;
@@ -376,13 +419,15 @@ __global__ void __launch_bounds__(kThreads, 1)
       uint32_t more = 0;
       ok = for_blocks<HD, KEYS>(it, p.group, [&](int, int, int rows, bool) {
         const uint32_t block = tile_desc(dv ? slot_b(ring.s) : slot_a(ring.s), Sh::kColumns), freed = ring_free + 8u * static_cast<uint32_t>(ring.s);
+        const uint32_t operand = a + (KEYS ? 0u : static_cast<uint32_t>(w & 1) * N);
+        const uint32_t done = done0 + (KEYS ? 0u : 8u * (w & 1));
         const int steps = (rows + 15) / 16;
-        if (!waitw(bar_ring + ring.s, ring.round) || !waitw(bar_a, w)) return false;
+        if (!waitw(bar_ring + ring.s, ring.round) || !waitw(bar_a + (KEYS ? 0 : w & 1), KEYS ? w : w >> 1)) return false;
         tc_fence_after();
         if (elected()) {
 #pragma unroll
           for (int i = 0; i < N / 16; ++i)
-            if (i < steps) tile_mma_ts(d, a + i * 8, block + mn_major_step(i), io, i > 0 ? 1u : more);
+            if (i < steps) tile_mma_ts(d, operand + (KEYS ? i * 8 : i / (N / 32) * NH + i % (N / 32) * 8), block + mn_major_step(i), io, i > 0 ? 1u : more);
           tc_commit(done);
           tc_commit(freed);
         }
@@ -395,37 +440,61 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     if (elected()) tc_commit(BAR(DRAIN + warp - 1));
     wait_drain(BAR(DRAIN + warp - 1), 0, limit);
-  } else if (warp == 5) {
-    // ------------------------------------------------------------------ rows behind the last; of KEYS, queries' lse and D
-    Ring ring;
-    uint32_t phase = 0;  // of each slot: blocks so far that end behind a sequence's last row, modulo 2
+  } else if (KEYS && (warp == 5 || warp == 6)) {
+    // ------------------------------------------------------------------ queries' lse and D: of even and odd blocks
+    constexpr int R = (N + 31) / 32;
+    const float unit = kExtra<FP16, KEYS> ? -1.f / f.scale : -kLog2e, shift = FP16 ? kPShift : 0.f;
     int w = 0;
     Item it;
     bool ok = true;
     for (int k = 0; ok && take(k, it); ++k) {
       ok = for_blocks<HD, KEYS>(it, p.group, [&](int head, int row, int rows, bool) {
-        const int s = ring.s;
-        if constexpr (KEYS) {
-          constexpr int R = (N + 31) / 32;
-          float l[R], d[R];
-#pragma unroll
-          for (int i = 0; i < R; ++i) {
-            const int r = i * 32 + lane;
-            const int64_t at = static_cast<int64_t>(it.begin + row + min(r, rows - 1)) * f.n_q_heads + head;
-            l[i] = r < rows ? fmaf(f.lse[at], -kLog2e, FP16 ? kPShift : 0.f) : -INFINITY;  // weights of 0 behind the last row
-            d[i] = r < rows ? -p.delta[at] : 0.f;
-          }
-          if (w >= kRows && !waitw(RFREE + w % kRows, w / kRows - 1)) return false;
-          float* dst = row_data + (w % kRows) * 256;
-#pragma unroll
-          for (int i = 0; i < R; ++i) {
-            dst[i * 32 + lane] = l[i];
-            dst[128 + i * 32 + lane] = d[i];
-          }
-          __syncwarp();
-          if (lane == 0) mbar_arrive(BAR(RFULL + w % kRows));
+        if ((w & 1) != warp - 5) {
+          ++w;
+          return true;
         }
-        if (rows < N) {
+        float l[R], d[R];
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          const int r = i * 32 + lane;
+          const int64_t at = static_cast<int64_t>(it.begin + row + min(r, rows - 1)) * f.n_q_heads + head;
+          // (rows behind the last are zeros everywhere)
+          l[i] = r < rows ? fmaf(f.lse[at], unit, shift) : 0.f;
+          d[i] = r < rows ? -p.delta[at] : 0.f;
+        }
+        const int slot = w % kRows;
+        if (w >= kRows && !waitw(RFREE + slot, w / kRows - 1)) return false;
+#pragma unroll
+        for (int i = 0; i < R; ++i) {
+          const int r = i * 32 + lane;
+          if constexpr (kExtra<FP16, KEYS>) {
+            if (r < N) {
+              uint8_t* dst = reinterpret_cast<uint8_t*>(row_data) + slot * Sh::kColumns + r * 128;
+              *reinterpret_cast<uint2*>(dst + ((0 ^ (r & 7)) << 4)) = three_terms(l[i]);
+              *reinterpret_cast<uint2*>(dst + ((2 ^ (r & 7)) << 4)) = three_terms(d[i]);
+            }
+          } else {
+            row_data[slot * 256 + r] = l[i];
+            row_data[slot * 256 + 128 + r] = d[i];
+          }
+        }
+        if constexpr (kExtra<FP16, KEYS>) fence_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(BAR(RFULL + slot));
+        ++w;
+        return true;
+      });
+    }
+  } else if (warp == 7) {
+    // ------------------------------------------------------------------ rows behind the last
+    Ring ring;
+    uint32_t phase = 0;  // of each slot: blocks so far with rows that have to become zeros, modulo 2
+    Item it;
+    bool ok = true;
+    for (int k = 0; ok && take(k, it); ++k) {
+      ok = for_blocks<HD, KEYS>(it, p.group, [&](int, int, int rows, bool) {
+        const int s = ring.s;
+        if (rows & 15) {
 #pragma unroll
           for (int b = 0; b < 2; ++b) {
             if (!waitw((b ? TAILB : TAILA) + s, phase >> s)) return false;
@@ -437,7 +506,6 @@ __global__ void __launch_bounds__(kThreads, 1)
           phase ^= 1u << s;
         }
         ring.next();
-        ++w;
         return true;
       });
     }
@@ -447,7 +515,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     const int half = (warp - kSumWarp0) >> 2, q4 = warp & 3, r = q4 * 32 + lane;
     const uint32_t quarter = tmem + (static_cast<uint32_t>(q4 * 32) << 16);
     const uint32_t tS = quarter + Sh::kColS + NH * half, tDp = quarter + Sh::kColDp + NH * half;
-    const uint32_t tP = quarter + Sh::kColP + NH / 2 * half, tDs = quarter + Sh::kColDs + NH / 2 * half;
+    const uint32_t tP = quarter + Sh::kColP + NH / 2 * half, tDs = quarter + Sh::kColDs + (KEYS ? NH / 2 : NH) * half;
     uint8_t* staging = smem + Sh::kStage + (warp - kSumWarp0) * 2048;
     const uint64_t c2 = pair_of(p.c, p.c);
     int w = 0;
@@ -471,7 +539,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int bound = it.a * kTile + r - row - NH * half;
         const float4* rl = reinterpret_cast<const float4*>(row_data + (w % kRows) * 256 + NH * half);
         uint32_t s[NH];
-        if ((KEYS && !waitw(RFULL + w % kRows, w / kRows)) || !waitw(SFULL, w)) return false;
+        if ((KEYS && FP16 && !waitw(RFULL + w % kRows, w / kRows)) || !waitw(SFULL, w)) return false;
         tc_fence_after();
         if (work) {
           tmem_load<NH>(tS, s);
@@ -485,7 +553,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
           for (int i = 0; i < NH; i += 4) {
             uint64_t la = l2, lb = l2;
-            if constexpr (KEYS) {
+            if constexpr (KEYS && FP16) {
               const float4 l = rl[i / 4];
               la = pair_of(l.x, l.y);
               lb = pair_of(l.z, l.w);
@@ -517,64 +585,86 @@ __global__ void __launch_bounds__(kThreads, 1)
           __syncwarp();
           if (lane == 0) mbar_arrive(BAR(PFULL));
         }
-        if (!waitw(DPFULL, w)) return false;
-        const bool free_ds = w == 0 || mbar_test_wait(BAR(DSDONE), (w - 1) & 1);
+        const int buffer = KEYS ? 0 : w & 1;
+        if (!waitw(DPFULL + buffer, KEYS ? w : w >> 1)) return false;
+        const bool free_ds = !KEYS || w == 0 || mbar_test_wait(BAR(DSDONE), (w - 1) & 1);
         tc_fence_after();
-        uint32_t y[NH / 2];
-        if (work) {
-          constexpr int C = NH % 32 ? NH : 32;  // columns at a time
+        // dS over s, columns j .. j + C - 1, from dP
+        constexpr int C = KEYS ? NH : 16;
+        uint32_t x[C];
+        auto gradients = [&](int j) {
 #pragma unroll
-          for (int j = 0; j < NH; j += C) {
-            uint32_t x[C];
-            tmem_load<C>(tDp + j, x);
-            tmem_wait_ld();
-#pragma unroll
-            for (int i = 0; i < C; i += 4) {
+          for (int i = 0; i < C; i += 4) {
+            uint64_t a = pair_of(__uint_as_float(x[i]), __uint_as_float(x[i + 1]));
+            uint64_t b = pair_of(__uint_as_float(x[i + 2]), __uint_as_float(x[i + 3]));
+            if constexpr (!kExtra<FP16, KEYS>) {
               uint64_t da = d2, db = d2;
               if constexpr (KEYS) {
                 const float4 d = rl[32 + (i + j) / 4];
                 da = pair_of(d.x, d.y);
                 db = pair_of(d.z, d.w);
               }
-              uint64_t a = add2(pair_of(__uint_as_float(x[i]), __uint_as_float(x[i + 1])), da);
-              uint64_t b = add2(pair_of(__uint_as_float(x[i + 2]), __uint_as_float(x[i + 3])), db);
-              if (FP16 && KEYS) {
+              a = add2(a, da);
+              b = add2(b, db);
+              if constexpr (KEYS) {
                 a = mul2(a, pair_of(up, up));
                 b = mul2(b, pair_of(up, up));
               }
-              float2 ya = halves_of(mul2(a, pair_of(__uint_as_float(s[i + j]), __uint_as_float(s[i + j + 1]))));
-              float2 yb = halves_of(mul2(b, pair_of(__uint_as_float(s[i + j + 2]), __uint_as_float(s[i + j + 3]))));
-              if (edge) {  // (what the mask hides may be NaN)
-                const int q = i + j;
-                ya.x = (KEYS ? q >= bound : q <= bound) ? ya.x : 0.f;
-                ya.y = (KEYS ? q + 1 >= bound : q + 1 <= bound) ? ya.y : 0.f;
-                yb.x = (KEYS ? q + 2 >= bound : q + 2 <= bound) ? yb.x : 0.f;
-                yb.y = (KEYS ? q + 3 >= bound : q + 3 <= bound) ? yb.y : 0.f;
-              }
-              y[(i + j) / 2] = pack2<FP16>(ya.x, ya.y);
-              y[(i + j) / 2 + 1] = pack2<FP16>(yb.x, yb.y);
             }
+            const float2 ya = halves_of(mul2(a, pair_of(__uint_as_float(s[i + j]), __uint_as_float(s[i + j + 1]))));
+            const float2 yb = halves_of(mul2(b, pair_of(__uint_as_float(s[i + j + 2]), __uint_as_float(s[i + j + 3]))));
+            s[i + j] = __float_as_uint(ya.x);
+            s[i + j + 1] = __float_as_uint(ya.y);
+            s[i + j + 2] = __float_as_uint(yb.x);
+            s[i + j + 3] = __float_as_uint(yb.y);
+          }
+          if (edge) {  // (what the mask hides may be NaN)
+#pragma unroll
+            for (int i = j; i < j + C; ++i) s[i] = (KEYS ? i >= bound : i <= bound) ? s[i] : 0u;
+          }
+        };
+        if constexpr (KEYS) {
+          if (work) {
+            tmem_load<NH>(tDp, x);
+            tmem_wait_ld();
+          }
+          tc_fence_before();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(BAR(DPREAD));
+          if (work) gradients(0);
+          if (FP16) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(BAR(RFREE + w % kRows));
+          }
+          if (!__all_sync(0xffffffffu, free_ds) && !waitw(DSDONE, w - 1)) return false;
+          tc_fence_after();
+          if (work) {
+            uint32_t y[NH / 2];
+#pragma unroll
+            for (int i = 0; i < NH / 2; ++i) y[i] = pack2<FP16>(__uint_as_float(s[2 * i]), __uint_as_float(s[2 * i + 1]));
+            tmem_store<NH / 2>(tDs, y);
+          }
+        } else if (work) {
+          const uint32_t from = tDp + static_cast<uint32_t>(buffer) * N, to = tDs + static_cast<uint32_t>(buffer) * N;
+#pragma unroll
+          for (int j = 0; j < NH; j += C) {
+            tmem_ld16(from + j, x);
+            tmem_wait_ld();
+            gradients(j);
+            uint32_t y[C / 2];  // (over columns that this thread has read)
+#pragma unroll
+            for (int i = 0; i < C / 2; ++i) y[i] = pack2<FP16>(__uint_as_float(s[j + 2 * i]), __uint_as_float(s[j + 2 * i + 1]));
+            tmem_st8(to + j / 2, y);
           }
         }
+        tmem_wait_st();
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) {
-          mbar_arrive(BAR(DPREAD));
-          if (KEYS) mbar_arrive(BAR(RFREE + w % kRows));
-        }
-        if (!__all_sync(0xffffffffu, free_ds) && !waitw(DSDONE, w - 1)) return false;
-        tc_fence_after();
-        if (work) {
-          tmem_store<NH / 2>(tDs, y);
-          tmem_wait_st();
-        }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(BAR(DSFULL));
+        if (lane == 0) mbar_arrive(BAR(DSFULL + buffer));
         ++w;
         return true;
       });
-      if (!ok || !(ok = (!KEYS || waitw(PDONE, w - 1)) && waitw(DSDONE, w - 1))) break;
+      if (!ok || !(ok = KEYS ? waitw(PDONE, w - 1) && waitw(DSDONE, w - 1) : waitw(DSDONE + ((w - 1) & 1), (w - 1) >> 1))) break;
       tc_fence_after();
       const int64_t at = it.begin + row0;
       if constexpr (KEYS) {
