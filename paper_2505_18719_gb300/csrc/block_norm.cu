@@ -12,12 +12,15 @@
 #include <type_traits>
 
 #include "learn.h"
+#include "ptx.cuh"
 
 namespace vla {
 
 namespace {
 
-constexpr int kParts = 304;  // CTAs of the gradient: two an SM
+// CTAs of the gradient, each a share of the rows: 152 SMs with as many as hide a row's latency.
+int parts_of(int rows, int dim) { return std::min(rows, 152 * (dim <= 1024 ? 6 : dim <= 2048 ? 4 : 2)); }
+constexpr uint32_t kStagedBytes = 100 * 1024;  // of two rows: two CTAs an SM
 
 template <class T>
 __device__ __forceinline__ float to_f(T x) {
@@ -66,6 +69,28 @@ __device__ __forceinline__ void store_row(T* row, int dim, const float (&y)[E]) 
     } else {
       row[i] = from_f<T>(y[c]);
     }
+  }
+}
+
+template <int V, class T>
+__device__ __forceinline__ void load_some(const T* p, float (&y)[V]) {
+  if constexpr (V == 8) {
+    const Eight<T> w = *reinterpret_cast<const Eight<T>*>(p);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[e] = to_f(w.x[e]);
+  } else {
+    y[0] = to_f(*p);
+  }
+}
+template <int V, class T>
+__device__ __forceinline__ void store_some(T* p, const float (&y)[V]) {
+  if constexpr (V == 8) {
+    Eight<T> w;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) w.x[e] = from_f<T>(y[e]);
+    *reinterpret_cast<Eight<T>*>(p) = w;
+  } else {
+    *p = from_f<T>(y[0]);
   }
 }
 
@@ -129,109 +154,168 @@ __global__ void __launch_bounds__(E == 8 ? 256 : 512) block_norm_kernel(const Bl
   }
 }
 
-template <class T, class H, int V, int E>
+// Rows on their way through shared memory: two, each its h_out, d_x, d_h_out, y and gate behind one another.  A row that does not begin or end on
+// a 16-byte boundary comes with the bytes around it up to the next.
+struct Stage {
+  uint32_t at[5], bytes;  // offsets of the five, of the next row
+};
+__host__ __device__ inline Stage stage_of(int dim, int act, int stream, bool d_h_out, bool y, bool gate) {
+  Stage s{};
+  const int size[5] = {stream, act, d_h_out ? stream : 0, y ? act : 0, gate ? act : 0};
+  for (int k = 0; k < 5; ++k) {
+    s.at[k] = s.bytes;
+    s.bytes += size[k] ? (static_cast<uint32_t>(dim * size[k]) + 31u) & ~15u : 0u;
+  }
+  return s;
+}
+
+template <class T, class H, int V, int E, bool STAGED>
 __global__ void __launch_bounds__(E == 8 ? 256 : 512) block_norm_grad_kernel(const BlockNormGradArgs a) {
   __shared__ float red[2][3 * 32];
+  __shared__ uint64_t full[2];
+  extern __shared__ uint8_t rows_raw[];
   pdl_launch_dependents();
   const int dim = a.f.dim;
   const bool post = a.f.post_gain, gated = a.f.gate, own_gate = a.f.ldg != 0;
+  const Stage st = stage_of(dim, sizeof(T), sizeof(H), a.d_h_out, a.f.y, gated && own_gate);
+  uint8_t* stages = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(rows_raw) + 15) & ~static_cast<uintptr_t>(15));
+  const void* const base[5] = {a.f.h, a.d_x, a.d_h_out, a.f.y, own_gate ? a.f.gate : nullptr};
+  const int64_t ld[5] = {a.f.ldh * static_cast<int64_t>(sizeof(H)), a.lddx * static_cast<int64_t>(sizeof(T)),
+                         a.lddho * static_cast<int64_t>(sizeof(H)), a.f.ldy * static_cast<int64_t>(sizeof(T)),
+                         a.f.ldg * static_cast<int64_t>(sizeof(T))};
+  auto request = [&](int64_t r, int s) {  // one thread
+    uint32_t total = 0, bytes[5];
+    uintptr_t from[5];
+#pragma unroll
+    for (int k = 0; k < 5; ++k) {
+      const uintptr_t p = reinterpret_cast<uintptr_t>(base[k]) + static_cast<uintptr_t>(r * ld[k]);
+      const uintptr_t end = (p + static_cast<uint32_t>(dim) * (k == 0 || k == 2 ? sizeof(H) : sizeof(T)) + 15) & ~static_cast<uintptr_t>(15);
+      from[k] = p & ~static_cast<uintptr_t>(15);
+      bytes[k] = base[k] ? static_cast<uint32_t>(end - from[k]) : 0u;
+      total += bytes[k];
+    }
+    mbar_arrive_expect_tx(smem_u32(full + s), total);
+#pragma unroll
+    for (int k = 0; k < 5; ++k)
+      if (bytes[k]) bulk_load(smem_u32(stages + s * st.bytes + st.at[k]), reinterpret_cast<const void*>(from[k]), bytes[k], smem_u32(full + s));
+  };
+  if constexpr (STAGED) {
+    if (threadIdx.x == 0) {
+      mbar_init(smem_u32(full), 1);
+      mbar_init(smem_u32(full + 1), 1);
+      asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+      if (static_cast<int>(blockIdx.x) < a.f.rows) request(blockIdx.x, 0);
+    }
+    __syncthreads();
+  }
   float d_pre[E] = {}, d_post[E] = {}, d_gate[E] = {};
-  int buf = 0;
-  for (int64_t r = blockIdx.x; r < a.f.rows; r += gridDim.x, buf ^= 1) {
+  int n_rows = 0;
+  for (int64_t r = blockIdx.x; r < a.f.rows; r += gridDim.x, ++n_rows) {
+    const int buf = n_rows & 1;
     const float r_y = post ? a.f.rstd[2 * r] : 1.f, r_h = a.f.rstd[2 * r + 1];
-    float n[E], g[E], d[E], m[E], t[E];
-    load_row<V, E>(static_cast<const H*>(a.f.h) + r * a.f.ldh, dim, n);
-    load_row<V, E>(static_cast<const T*>(a.d_x) + r * a.lddx, dim, g);
-    if (a.d_h_out) {
-      load_row<V, E>(static_cast<const H*>(a.d_h_out) + r * a.lddho, dim, d);
-    } else {
+    const void* row[5];
 #pragma unroll
-      for (int e = 0; e < E; ++e) d[e] = 0.f;
+    for (int k = 0; k < 5; ++k) {
+      const uintptr_t p = reinterpret_cast<uintptr_t>(base[k]) + static_cast<uintptr_t>(r * ld[k]);
+      row[k] = STAGED ? stages + buf * st.bytes + st.at[k] + (p & 15) : reinterpret_cast<const uint8_t*>(p);
     }
-    if (a.f.y) load_row<V, E>(static_cast<const T*>(a.f.y) + r * a.f.ldy, dim, m);
+    if (!own_gate) row[4] = a.f.gate;
+    if constexpr (STAGED)
+      if (!wait_drain_reported(smem_u32(full + buf), (n_rows >> 1) & 1, a.status, a.wait_limit)) break;
     float sum[3] = {0.f, 0.f, 0.f};
-    load_row<V, E>(a.f.pre_gain, dim, t);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      n[e] *= r_h;
-      d_pre[e] = fmaf(g[e], n[e], d_pre[e]);
-      g[e] *= t[e];
-      sum[0] = fmaf(g[e], n[e], sum[0]);
-      d[e] = fmaf(r_h, g[e], d[e]);
-    }
-    float q[E];  // residual_scale gate post_gain
-    if (post) {
-      load_row<V, E>(a.f.post_gain, dim, t);
+    for (int c = 0; c < E / V; ++c) {
+      const int i = (c * blockDim.x + threadIdx.x) * V;
+      if (i >= dim) break;
+      float n[V], g[V], w[V];
+      load_some<V>(static_cast<const H*>(row[0]) + i, n);
+      load_some<V>(static_cast<const T*>(row[1]) + i, g);
+      load_some<V>(a.f.pre_gain + i, w);
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        q[e] = a.f.residual_scale * t[e];
-        m[e] *= r_y;
+      for (int e = 0; e < V; ++e) {
+        n[e] *= r_h;
+        d_pre[c * V + e] = fmaf(g[e], n[e], d_pre[c * V + e]);
+        g[e] *= w[e];
+        sum[0] = fmaf(g[e], n[e], sum[0]);
       }
+      if (!post) continue;
+      float m[V], q[V];
+      load_some<V>(static_cast<const T*>(row[3]) + i, m);
+      load_some<V>(a.f.post_gain + i, q);
+#pragma unroll
+      for (int e = 0; e < V; ++e) q[e] *= a.f.residual_scale * r_y * m[e];
       if (gated) {
-        load_row<V, E>(static_cast<const T*>(a.f.gate) + r * a.f.ldg, dim, t);
+        load_some<V>(static_cast<const T*>(row[4]) + i, w);
 #pragma unroll
-        for (int e = 0; e < E; ++e) q[e] *= t[e];
+        for (int e = 0; e < V; ++e) q[e] *= w[e];
+      }
+      if (a.d_h_out) {
+        load_some<V>(static_cast<const H*>(row[2]) + i, w);
+#pragma unroll
+        for (int e = 0; e < V; ++e) g[e] = fmaf(r_h, g[e], w[e]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < V; ++e) g[e] *= r_h;
       }
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        sum[1] = fmaf(q[e] * m[e], d[e], sum[1]);
-        sum[2] = fmaf(q[e] * m[e], r_h * n[e], sum[2]);
+      for (int e = 0; e < V; ++e) {
+        sum[1] = fmaf(q[e], g[e], sum[1]);
+        sum[2] = fmaf(q[e], r_h * n[e], sum[2]);
       }
-      cta_sums(sum, red[buf]);
-    } else {
-      if (a.f.y) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) q[e] = a.f.residual_scale;
-        if (gated) {
-          load_row<V, E>(static_cast<const T*>(a.f.gate) + r * a.f.ldg, dim, t);
-#pragma unroll
-          for (int e = 0; e < E; ++e) q[e] *= t[e];
-        }
-      }
-      float one[1] = {sum[0]};
-      cta_sums(one, red[buf]);
-      sum[0] = one[0];
+    }
+    cta_sums(sum, red[buf]);
+    if constexpr (STAGED) {
+      __syncwarp();
+      // (the row before, in the other stage, is done with: all threads have come to these sums)
+      if (threadIdx.x == 0 && r + gridDim.x < a.f.rows) request(r + gridDim.x, buf ^ 1);
     }
     const float inv = 1.f / static_cast<float>(dim), c1 = sum[0] * inv, c2 = (sum[1] - c1 * sum[2]) * inv;
 #pragma unroll
-    for (int e = 0; e < E; ++e) d[e] = fmaf(-r_h * c1, n[e], d[e]);
-    store_row<V, E>(static_cast<H*>(a.d_h) + r * a.lddh, dim, d);
-    if (!a.f.y) continue;
-    if (gated) {  // d_gate = residual_scale u d_h
+    for (int c = 0; c < E / V; ++c) {
+      const int i = (c * blockDim.x + threadIdx.x) * V;
+      if (i >= dim) break;
+      float d[V], n[V], w[V];
+      load_some<V>(static_cast<const T*>(row[1]) + i, d);
+      load_some<V>(a.f.pre_gain + i, w);
+      load_some<V>(static_cast<const H*>(row[0]) + i, n);
+#pragma unroll
+      for (int e = 0; e < V; ++e) d[e] = r_h * fmaf(-r_h * n[e], c1, d[e] * w[e]);
+      if (a.d_h_out) {
+        load_some<V>(static_cast<const H*>(row[2]) + i, w);
+#pragma unroll
+        for (int e = 0; e < V; ++e) d[e] += w[e];
+      }
+      store_some<V>(static_cast<H*>(a.d_h) + r * a.lddh + i, d);
+      if (!a.f.y) continue;
+      float m[V];
+      load_some<V>(static_cast<const T*>(row[3]) + i, m);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        d[e] *= a.f.residual_scale;
+        m[e] *= r_y;  // (1 without post_gain)
+        w[e] = 1.f;
+      }
+      if (post) load_some<V>(a.f.post_gain + i, w);
+      if (gated) {  // d_gate = residual_scale d_h u
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          n[e] = d[e] * m[e] * w[e];
+          d_gate[c * V + e] += n[e];
+        }
+        if (own_gate) store_some<V>(static_cast<T*>(a.d_gate) + r * a.lddg + i, n);
+        load_some<V>(static_cast<const T*>(row[4]) + i, n);
+#pragma unroll
+        for (int e = 0; e < V; ++e) d[e] *= n[e];
+      }
       if (post) {
-        load_row<V, E>(a.f.post_gain, dim, t);
 #pragma unroll
-        for (int e = 0; e < E; ++e) t[e] *= m[e];
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) t[e] = m[e];
+        for (int e = 0; e < V; ++e) {
+          d_post[c * V + e] = fmaf(d[e], m[e], d_post[c * V + e]);
+          d[e] = r_y * fmaf(w[e], d[e], -m[e] * c2);
+        }
       }
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        t[e] *= a.f.residual_scale * d[e];
-        d_gate[e] += t[e];
-      }
-      if (own_gate) store_row<V, E>(static_cast<T*>(a.d_gate) + r * a.lddg, dim, t);
+      store_some<V>(static_cast<T*>(a.d_y) + r * a.lddy + i, d);
     }
-    if (post) {
-      if (gated) {
-        load_row<V, E>(static_cast<const T*>(a.f.gate) + r * a.f.ldg, dim, t);
-#pragma unroll
-        for (int e = 0; e < E; ++e) t[e] *= a.f.residual_scale;
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) t[e] = a.f.residual_scale;
-      }
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        d_post[e] = fmaf(t[e] * d[e], m[e], d_post[e]);
-        d[e] = r_y * fmaf(q[e], d[e], -m[e] * c2);
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) d[e] *= q[e];
-    }
-    store_row<V, E>(static_cast<T*>(a.d_y) + r * a.lddy, dim, d);
   }
   float* part = a.workspace + static_cast<int64_t>(blockIdx.x) * 3 * dim;
   auto keep = [&](int k, const float(&v)[E]) {
@@ -253,23 +337,23 @@ struct ColumnSums {
   int n, dim;
   float* out[3];       // or null
 };
-__global__ void __launch_bounds__(256) column_sums_kernel(const ColumnSums a) {
-  __shared__ float red[8][33];
+// 32 columns a CTA, every 32nd part a warp, 10 to 30 loads in flight a thread.
+__global__ void __launch_bounds__(1024) column_sums_kernel(const ColumnSums a) {
+  __shared__ float red[32][33];
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
   const int i = blockIdx.x * 32 + lane, k = blockIdx.y;
-  pdl_wait();
   if (!a.out[k]) return;
+  pdl_wait();
   float s = 0.f;
   if (i < a.dim) {
-#pragma unroll 8
-    for (int p = w; p < a.n; p += 8) s += __ldcg(a.parts + (static_cast<int64_t>(p) * 3 + k) * a.dim + i);
+#pragma unroll 10
+    for (int p = w; p < a.n; p += 32) s += __ldcg(a.parts + (static_cast<int64_t>(p) * 3 + k) * a.dim + i);
   }
   red[w][lane] = s;
   __syncthreads();
-  if (w || i >= a.dim) return;
-#pragma unroll
-  for (int j = 1; j < 8; ++j) s += red[j][lane];
-  a.out[k][i] = s;
+  s = warp_sum(red[lane][w]);
+  const int j = blockIdx.x * 32 + w;
+  if (lane == 0 && j < a.dim) a.out[k][j] = s;
 }
 
 // 16-byte accesses to every row?
@@ -312,25 +396,33 @@ int block_norm_launch(const BlockNormArgs& a, cudaStream_t s) {
   });
 }
 
-size_t block_norm_grad_workspace(int rows, int dim) { return static_cast<size_t>(std::max(1, std::min(rows, kParts))) * 3 * dim * sizeof(float); }
+size_t block_norm_grad_workspace(int rows, int dim) { return static_cast<size_t>(std::max(1, parts_of(rows, dim))) * 3 * dim * sizeof(float); }
 
 int block_norm_grad_launch(const BlockNormGradArgs& a, cudaStream_t s) {
   const BlockNormArgs& f = a.f;
-  const int parts = std::min(f.rows, kParts);
+  const int parts = parts_of(f.rows, f.dim);
   if (parts > 0) {
     const bool vec = f.dim % 8 == 0 && wide(f.y, f.ldy) && wide(f.h, f.ldh) && wide(f.gate, f.ldg) &&
                      wide(f.post_gain, 0) && wide(f.pre_gain, 0) && wide(a.d_x, a.lddx) && wide(a.d_h_out, a.lddho) &&
                      wide(a.d_h, a.lddh) && wide(a.d_y, a.lddy) && (!f.ldg || wide(a.d_gate, a.lddg));
     const int rc = dispatch(f.dtype, f.h_dtype, vec, f.dim, [&](auto t, auto h, auto v, auto e) -> int {
-      VLA_CUDA_TRY(launch_at(Start::kInOrder, block_norm_grad_kernel<decltype(t), decltype(h), v(), e()>, dim3(static_cast<unsigned>(parts)),
-                             dim3(threads_for(f.dim)), 0, s, a));
+      const uint32_t staged = 2 * stage_of(f.dim, sizeof(t), sizeof(h), a.d_h_out, f.y, f.gate && f.ldg).bytes + 16;
+      if (staged <= kStagedBytes) {
+        const auto kern = block_norm_grad_kernel<decltype(t), decltype(h), v(), e(), true>;
+        static std::atomic<uint64_t> done{0};
+        VLA_CUDA_TRY(set_smem_limit(kern, kStagedBytes, done));
+        VLA_CUDA_TRY(launch_at(Start::kInOrder, kern, dim3(static_cast<unsigned>(parts)), dim3(threads_for(f.dim)), staged, s, a));
+      } else {
+        VLA_CUDA_TRY(launch_at(Start::kInOrder, block_norm_grad_kernel<decltype(t), decltype(h), v(), e(), false>, dim3(static_cast<unsigned>(parts)),
+                               dim3(threads_for(f.dim)), 0, s, a));
+      }
       note_launch();
       return VLA_OK;
     });
     if (rc) return rc;
   }
   const ColumnSums c{a.workspace, parts, f.dim, {a.d_pre_gain, a.d_post_gain, f.gate && !f.ldg ? static_cast<float*>(a.d_gate) : nullptr}};
-  VLA_CUDA_TRY(launch_pdl(column_sums_kernel, dim3(static_cast<unsigned>((f.dim + 31) / 32), 3), dim3(256), 0, s, c));
+  VLA_CUDA_TRY(launch_pdl(column_sums_kernel, dim3(static_cast<unsigned>((f.dim + 31) / 32), 3), dim3(1024), 0, s, c));
   note_launch();
   return VLA_OK;
 }

@@ -80,6 +80,8 @@ struct BlockNormGradArgs {
   float* d_post_gain;
   float* d_pre_gain;
   float* workspace;
+  uint32_t* status;
+  uint64_t wait_limit;
 };
 int block_norm_grad_launch(const BlockNormGradArgs& a, cudaStream_t s);
 size_t block_norm_grad_workspace(int rows, int dim);

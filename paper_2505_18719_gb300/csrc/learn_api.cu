@@ -138,7 +138,7 @@ int vla_block_norm_grad(const void* y, int64_t ldy, int dtype, const void* h_out
   BlockNormGradArgs a{{y, ldy, dtype, h_out, ldho, h_dtype, rows, dim, static_cast<const bf16*>(post_gain), gate, ldg, residual_scale,
                        static_cast<const bf16*>(pre_gain), 0.f, nullptr, 0, nullptr, 0, const_cast<float*>(rstd)},
                       d_x, lddx, d_h_out, lddho, d_h, lddh, d_y, lddy, d_gate, lddg, d_post_gain, d_pre_gain,
-                      static_cast<float*>(workspace)};
+                      static_cast<float*>(workspace), nullptr, g_wait_limit_ns.load(std::memory_order_relaxed)};
   if (const int rc = check_norm(a.f, kNames)) return rc;
   if (!d_pre_gain || misaligned(d_pre_gain, 4) || (post_gain && (!d_post_gain || misaligned(d_post_gain, 4))))
     return record_error(VLA_ERR_ARG, "vla_block_norm_grad: a gain without its gradient, or that off 4 bytes");
@@ -150,6 +150,7 @@ int vla_block_norm_grad(const void* y, int64_t ldy, int dtype, const void* h_out
       return record_error(VLA_ERR_ARG, "vla_block_norm_grad: rstd NULL, or d_x, d_h_out, d_h, d_y NULL, off their type or of a stride below dim");
     if (!workspace || misaligned(workspace, 16) || workspace_bytes < block_norm_grad_workspace(rows, dim))
       return record_error(VLA_ERR_ARG, "vla_block_norm_grad: workspace NULL, off 16 bytes or too small");
+    if (const int rs = op_status_word(&a.status)) return rs;
   }
   return block_norm_grad_launch(a, static_cast<cudaStream_t>(cuda_stream));
 }
