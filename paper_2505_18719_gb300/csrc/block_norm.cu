@@ -19,8 +19,8 @@ namespace vla {
 namespace {
 
 // CTAs of the gradient, each a share of the rows: 152 SMs with as many as hide a row's latency.
-int parts_of(int rows, int dim) { return std::min(rows, 152 * (dim <= 1024 ? 6 : dim <= 2048 ? 4 : 2)); }
-constexpr uint32_t kStagedBytes = 100 * 1024;  // of two rows: two CTAs an SM
+int parts_of(int rows, int dim) { return std::min(rows, 152 * (dim <= 512 ? 6 : dim <= 1024 ? 4 : dim <= 2048 ? 3 : dim <= 4096 ? 2 : 1)); }
+uint32_t staged_limit(int dim) { return dim <= 4096 ? 100 * 1024 : 200 * 1024; }  // of two rows of each of those CTAs
 
 template <class T>
 __device__ __forceinline__ float to_f(T x) {
@@ -82,6 +82,19 @@ __device__ __forceinline__ void load_some(const T* p, float (&y)[V]) {
     y[0] = to_f(*p);
   }
 }
+// An element from shared memory.
+template <class T>
+__device__ __forceinline__ float load_shared(uint32_t at) {
+  if constexpr (sizeof(T) == 2) {
+    uint16_t w;
+    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(at));
+    return std::is_same_v<T, f16> ? __half2float(__ushort_as_half(w)) : __bfloat162float(__ushort_as_bfloat16(w));
+  } else {
+    float y;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(y) : "r"(at));
+    return y;
+  }
+}
 template <int V, class T>
 __device__ __forceinline__ void store_some(T* p, const float (&y)[V]) {
   if constexpr (V == 8) {
@@ -113,6 +126,8 @@ __device__ __forceinline__ void cta_sums(float (&v)[N], float* red) {
 template <class T, class H, int V, int E>
 __global__ void __launch_bounds__(E == 8 ? 256 : 512) block_norm_kernel(const BlockNormArgs a) {
   __shared__ float red[2][32];
+  pdl_launch_dependents();
+  pdl_wait();
   const int64_t r = blockIdx.x;
   const int dim = a.dim;
   float h[E], u[E], w[E];
@@ -170,11 +185,12 @@ __host__ __device__ inline Stage stage_of(int dim, int act, int stream, bool d_h
 }
 
 template <class T, class H, int V, int E, bool STAGED>
-__global__ void __launch_bounds__(E == 8 ? 256 : 512) block_norm_grad_kernel(const BlockNormGradArgs a) {
+__global__ void __launch_bounds__(E == 8 ? 256 : 512, E == 8 ? 2 : 1) block_norm_grad_kernel(const BlockNormGradArgs a) {
   __shared__ float red[2][3 * 32];
   __shared__ uint64_t full[2];
   extern __shared__ uint8_t rows_raw[];
   pdl_launch_dependents();
+  pdl_wait();
   const int dim = a.f.dim;
   const bool post = a.f.post_gain, gated = a.f.gate, own_gate = a.f.ldg != 0;
   const Stage st = stage_of(dim, sizeof(T), sizeof(H), a.d_h_out, a.f.y, gated && own_gate);
@@ -209,48 +225,155 @@ __global__ void __launch_bounds__(E == 8 ? 256 : 512) block_norm_grad_kernel(con
     __syncthreads();
   }
   float d_pre[E] = {}, d_post[E] = {}, d_gate[E] = {};
+  float w_pre[E == 8 ? E : 1], w_post[E == 8 ? E : 1];
+  if constexpr (E == 8) {
+#pragma unroll
+    for (int c = 0; c < E / V; ++c) {
+      const int i = min(static_cast<int>((c * blockDim.x + threadIdx.x) * V), dim - V);
+      float x[V];
+      load_some<V>(a.f.pre_gain + i, x);
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        w_pre[c * V + e] = x[e];
+        x[e] = 1.f;
+      }
+      if (post) load_some<V>(a.f.post_gain + i, x);
+#pragma unroll
+      for (int e = 0; e < V; ++e) w_post[c * V + e] = x[e];
+    }
+  }
   int n_rows = 0;
   for (int64_t r = blockIdx.x; r < a.f.rows; r += gridDim.x, ++n_rows) {
     const int buf = n_rows & 1;
     const float r_y = post ? a.f.rstd[2 * r] : 1.f, r_h = a.f.rstd[2 * r + 1];
-    const void* row[5];
+    const uint8_t* row[5];
 #pragma unroll
     for (int k = 0; k < 5; ++k) {
-      const uintptr_t p = reinterpret_cast<uintptr_t>(base[k]) + static_cast<uintptr_t>(r * ld[k]);
-      row[k] = STAGED ? stages + buf * st.bytes + st.at[k] + (p & 15) : reinterpret_cast<const uint8_t*>(p);
+      row[k] = reinterpret_cast<const uint8_t*>(base[k]) + r * ld[k];
+      if (STAGED) row[k] = stages + buf * st.bytes + st.at[k] + (reinterpret_cast<uintptr_t>(row[k]) & 15);
     }
-    if (!own_gate) row[4] = a.f.gate;
+    // element i of the row's h_out, d_x, d_h_out, y or gate of its own
+    auto load = [&](auto type, int k, int i, float(&y)[V]) {
+      using X = decltype(type);
+      if constexpr (STAGED && V == 1)
+        y[0] = load_shared<X>(smem_u32(row[k]) + static_cast<uint32_t>(i * sizeof(X)));
+      else
+        load_some<V>(reinterpret_cast<const X*>(row[k]) + i, y);
+    };
+    auto load_gate = [&](int i, float(&y)[V]) {
+      if (own_gate)
+        load(T(), 4, i, y);
+      else
+        load_some<V>(static_cast<const T*>(a.f.gate) + i, y);
+    };
     if constexpr (STAGED)
-      if (!wait_drain_reported(smem_u32(full + buf), (n_rows >> 1) & 1, a.status, a.wait_limit)) break;
+      if (!mbar_try_wait(smem_u32(full + buf), (n_rows >> 1) & 1) &&
+          !wait_drain_reported(smem_u32(full + buf), (n_rows >> 1) & 1, a.status, a.wait_limit))
+        break;
+    if constexpr (E == 8) {  // values and gains of a short row stay in registers
+      float n[E], g[E], d[E], m[E], q[E], sum[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+      for (int c = 0; c < E / V; ++c) {
+        const int own = (c * blockDim.x + threadIdx.x) * V, i = min(own, dim - V);
+        const bool on = own < dim;
+        float x[V];
+        load(H(), 0, i, x);
+#pragma unroll
+        for (int e = 0; e < V; ++e) n[c * V + e] = on ? x[e] * r_h : 0.f;
+        load(T(), 1, i, x);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          d_pre[c * V + e] = fmaf(x[e], n[c * V + e], d_pre[c * V + e]);
+          g[c * V + e] = on ? x[e] * w_pre[c * V + e] : 0.f;
+          x[e] = 0.f;
+        }
+        if (a.d_h_out) load(H(), 2, i, x);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          sum[0] = fmaf(g[c * V + e], n[c * V + e], sum[0]);
+          d[c * V + e] = on ? fmaf(r_h, g[c * V + e], x[e]) : 0.f;
+          x[e] = 0.f;
+        }
+        if (a.f.y) load(T(), 3, i, x);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          m[c * V + e] = on ? x[e] * r_y : 0.f;
+          x[e] = 1.f;
+        }
+        if (gated) load_gate(i, x);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          g[c * V + e] = x[e];
+          q[c * V + e] = a.f.residual_scale * x[e] * w_post[c * V + e];
+        }
+        if (post) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const float z = on ? q[c * V + e] * m[c * V + e] : 0.f;
+            sum[1] = fmaf(z, d[c * V + e], sum[1]);
+            sum[2] = fmaf(z, r_h * n[c * V + e], sum[2]);
+          }
+        }
+      }
+      cta_sums(sum, red[buf]);
+      if constexpr (STAGED) {
+        __syncwarp();
+        if (threadIdx.x == 0 && r + gridDim.x < a.f.rows) request(r + gridDim.x, buf ^ 1);
+      }
+      const float inv = 1.f / static_cast<float>(dim), c1 = sum[0] * inv, c2 = (sum[1] - c1 * sum[2]) * inv;
+#pragma unroll
+      for (int c = 0; c < E / V; ++c) {
+        const int i = (c * blockDim.x + threadIdx.x) * V;
+        if (i >= dim) continue;
+        float x[V], z[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) x[e] = fmaf(-r_h * c1, n[c * V + e], d[c * V + e]);
+        store_some<V>(static_cast<H*>(a.d_h) + r * a.lddh + i, x);
+        if (!a.f.y) continue;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float y = a.f.residual_scale * x[e] * m[c * V + e];  // times post_gain: d_gate
+          z[e] = y * w_post[c * V + e];
+          d_gate[c * V + e] += z[e];
+          d_post[c * V + e] = fmaf(y, g[c * V + e], d_post[c * V + e]);
+          x[e] = post ? r_y * fmaf(q[c * V + e], x[e], -m[c * V + e] * c2) : q[c * V + e] * x[e];
+        }
+        if (gated && own_gate) store_some<V>(static_cast<T*>(a.d_gate) + r * a.lddg + i, z);
+        store_some<V>(static_cast<T*>(a.d_y) + r * a.lddy + i, x);
+      }
+      continue;
+    }
     float sum[3] = {0.f, 0.f, 0.f};
 #pragma unroll
     for (int c = 0; c < E / V; ++c) {
-      const int i = (c * blockDim.x + threadIdx.x) * V;
-      if (i >= dim) break;
+      // (past the row: its last channels again, without effect)
+      const int own = (c * blockDim.x + threadIdx.x) * V, i = min(own, dim - V);
+      const bool on = own < dim;
       float n[V], g[V], w[V];
-      load_some<V>(static_cast<const H*>(row[0]) + i, n);
-      load_some<V>(static_cast<const T*>(row[1]) + i, g);
+      load(H(), 0, i, n);
+      load(T(), 1, i, g);
       load_some<V>(a.f.pre_gain + i, w);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         n[e] *= r_h;
+        g[e] = on ? g[e] : 0.f;
         d_pre[c * V + e] = fmaf(g[e], n[e], d_pre[c * V + e]);
         g[e] *= w[e];
         sum[0] = fmaf(g[e], n[e], sum[0]);
       }
       if (!post) continue;
       float m[V], q[V];
-      load_some<V>(static_cast<const T*>(row[3]) + i, m);
+      load(T(), 3, i, m);
       load_some<V>(a.f.post_gain + i, q);
 #pragma unroll
-      for (int e = 0; e < V; ++e) q[e] *= a.f.residual_scale * r_y * m[e];
+      for (int e = 0; e < V; ++e) q[e] = on ? q[e] * (a.f.residual_scale * r_y * m[e]) : 0.f;
       if (gated) {
-        load_some<V>(static_cast<const T*>(row[4]) + i, w);
+        load_gate(i, w);
 #pragma unroll
         for (int e = 0; e < V; ++e) q[e] *= w[e];
       }
       if (a.d_h_out) {
-        load_some<V>(static_cast<const H*>(row[2]) + i, w);
+        load(H(), 2, i, w);
 #pragma unroll
         for (int e = 0; e < V; ++e) g[e] = fmaf(r_h, g[e], w[e]);
       } else {
@@ -272,23 +395,24 @@ __global__ void __launch_bounds__(E == 8 ? 256 : 512) block_norm_grad_kernel(con
     const float inv = 1.f / static_cast<float>(dim), c1 = sum[0] * inv, c2 = (sum[1] - c1 * sum[2]) * inv;
 #pragma unroll
     for (int c = 0; c < E / V; ++c) {
-      const int i = (c * blockDim.x + threadIdx.x) * V;
-      if (i >= dim) break;
+      // (past the row: its last channels again, without effect)
+      const int own = (c * blockDim.x + threadIdx.x) * V, i = min(own, dim - V);
+      const bool on = own < dim;
       float d[V], n[V], w[V];
-      load_some<V>(static_cast<const T*>(row[1]) + i, d);
+      load(T(), 1, i, d);
       load_some<V>(a.f.pre_gain + i, w);
-      load_some<V>(static_cast<const H*>(row[0]) + i, n);
+      load(H(), 0, i, n);
 #pragma unroll
       for (int e = 0; e < V; ++e) d[e] = r_h * fmaf(-r_h * n[e], c1, d[e] * w[e]);
       if (a.d_h_out) {
-        load_some<V>(static_cast<const H*>(row[2]) + i, w);
+        load(H(), 2, i, w);
 #pragma unroll
         for (int e = 0; e < V; ++e) d[e] += w[e];
       }
-      store_some<V>(static_cast<H*>(a.d_h) + r * a.lddh + i, d);
+      if (on) store_some<V>(static_cast<H*>(a.d_h) + r * a.lddh + i, d);
       if (!a.f.y) continue;
       float m[V];
-      load_some<V>(static_cast<const T*>(row[3]) + i, m);
+      load(T(), 3, i, m);
 #pragma unroll
       for (int e = 0; e < V; ++e) {
         d[e] *= a.f.residual_scale;
@@ -302,8 +426,8 @@ __global__ void __launch_bounds__(E == 8 ? 256 : 512) block_norm_grad_kernel(con
           n[e] = d[e] * m[e] * w[e];
           d_gate[c * V + e] += n[e];
         }
-        if (own_gate) store_some<V>(static_cast<T*>(a.d_gate) + r * a.lddg + i, n);
-        load_some<V>(static_cast<const T*>(row[4]) + i, n);
+        if (own_gate && on) store_some<V>(static_cast<T*>(a.d_gate) + r * a.lddg + i, n);
+        load_gate(i, n);
 #pragma unroll
         for (int e = 0; e < V; ++e) d[e] *= n[e];
       }
@@ -314,7 +438,7 @@ __global__ void __launch_bounds__(E == 8 ? 256 : 512) block_norm_grad_kernel(con
           d[e] = r_y * fmaf(w[e], d[e], -m[e] * c2);
         }
       }
-      store_some<V>(static_cast<T*>(a.d_y) + r * a.lddy + i, d);
+      if (on) store_some<V>(static_cast<T*>(a.d_y) + r * a.lddy + i, d);
     }
   }
   float* part = a.workspace + static_cast<int64_t>(blockIdx.x) * 3 * dim;
@@ -389,7 +513,7 @@ int block_norm_launch(const BlockNormArgs& a, cudaStream_t s) {
   const bool vec = a.dim % 8 == 0 && wide(a.y, a.ldy) && wide(a.h, a.ldh) && wide(a.gate, a.ldg) && wide(a.post_gain, 0) &&
                    wide(a.pre_gain, 0) && wide(a.h_out, a.ldho) && wide(a.x, a.ldx);
   return dispatch(a.dtype, a.h_dtype, vec, a.dim, [&](auto t, auto h, auto v, auto e) -> int {
-    VLA_CUDA_TRY(launch_at(Start::kInOrder, block_norm_kernel<decltype(t), decltype(h), v(), e()>, dim3(static_cast<unsigned>(a.rows)),
+    VLA_CUDA_TRY(launch_pdl(block_norm_kernel<decltype(t), decltype(h), v(), e()>, dim3(static_cast<unsigned>(a.rows)),
                            dim3(threads_for(a.dim)), 0, s, a));
     note_launch();
     return VLA_OK;
@@ -407,13 +531,13 @@ int block_norm_grad_launch(const BlockNormGradArgs& a, cudaStream_t s) {
                      wide(a.d_h, a.lddh) && wide(a.d_y, a.lddy) && (!f.ldg || wide(a.d_gate, a.lddg));
     const int rc = dispatch(f.dtype, f.h_dtype, vec, f.dim, [&](auto t, auto h, auto v, auto e) -> int {
       const uint32_t staged = 2 * stage_of(f.dim, sizeof(t), sizeof(h), a.d_h_out, f.y, f.gate && f.ldg).bytes + 16;
-      if (staged <= kStagedBytes) {
+      if (staged <= staged_limit(f.dim)) {
         const auto kern = block_norm_grad_kernel<decltype(t), decltype(h), v(), e(), true>;
         static std::atomic<uint64_t> done{0};
-        VLA_CUDA_TRY(set_smem_limit(kern, kStagedBytes, done));
-        VLA_CUDA_TRY(launch_at(Start::kInOrder, kern, dim3(static_cast<unsigned>(parts)), dim3(threads_for(f.dim)), staged, s, a));
+        VLA_CUDA_TRY(set_smem_limit(kern, 200 * 1024, done));
+        VLA_CUDA_TRY(launch_pdl(kern, dim3(static_cast<unsigned>(parts)), dim3(threads_for(f.dim)), staged, s, a));
       } else {
-        VLA_CUDA_TRY(launch_at(Start::kInOrder, block_norm_grad_kernel<decltype(t), decltype(h), v(), e(), false>, dim3(static_cast<unsigned>(parts)),
+        VLA_CUDA_TRY(launch_pdl(block_norm_grad_kernel<decltype(t), decltype(h), v(), e(), false>, dim3(static_cast<unsigned>(parts)),
                                dim3(threads_for(f.dim)), 0, s, a));
       }
       note_launch();
