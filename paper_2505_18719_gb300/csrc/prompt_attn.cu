@@ -36,26 +36,28 @@ namespace vla {
 
 namespace {
 
-constexpr int kThreads = 384, kSoftWarp0 = 4, kSoftWarps = 8;
+constexpr int kSoftWarps = 8;
 
-template <int HD>
+template <int HD, bool PAIRED>
 struct Smem {
-  static constexpr int kKeys = 80;  // keys of a block
-  static constexpr int kStages = HD == 128 ? 6 : 8;
+  static constexpr int kSoftWarp0 = PAIRED ? 4 : 8, kThreads = 32 * (kSoftWarp0 + kSoftWarps);
+  static constexpr int kKeys = PAIRED ? 80 : 64;                    // keys of a block
+  static constexpr int kStages = !PAIRED ? 4 : HD == 128 ? 6 : 8;  // of a ring
+  static constexpr int kRings = PAIRED ? 1 : 2;                     // for both tiles, or one each
+  static constexpr int kItemReaders = PAIRED ? 3 + kSoftWarps : 2 + kSoftWarps / 2;
   static constexpr uint32_t kQBytes = kTile * HD * 2, kKvBytes = kKeys * HD * 2, kKvBlock = kKeys * 128;
-  static constexpr uint32_t kRing = 2 * kQBytes, kStage = kRing + kStages * kKvBytes, kBars = kStage + kSoftWarps * 2048;
+  static constexpr uint32_t kRing = 2 * kQBytes, kStage = kRing + kRings * kStages * kKvBytes, kBars = kStage + kSoftWarps * 2048;
   static constexpr uint32_t kTotal = 1024 + kBars + 1024;
   static constexpr uint32_t kColS = HD, kColP = HD + kKeys;  // of a tile's 256 columns
   static_assert(kTotal <= 232448 && kColP + kKeys / 2 <= 256 && kKvBlock % 1024 == 0, "shared and tensor memory");
 };
 
 // Barriers.  Of each tile: Q loaded / free, S written / read, P written, its product done; end of the issuing warps' products; item
-// descriptors; ring slots, and loads into them that end behind a sequence's last row.
+// descriptors (of each tile, where not PAIRED); ring slots (likewise), and loads into them that end behind a sequence's last row.
 enum : int {
-  QFULL = 0, QFREE = 2, SFULL = 4, SREAD = 6, PFULL = 8, PVDONE = 10, DRAIN = 12, IFULL = 16, IFREE = 24, KVFULL = 32, KVFREE = 40, TAIL = 48,
-  kBarCount = 56
+  QFULL = 0, QFREE = 2, SFULL = 4, SREAD = 6, PFULL = 8, PVDONE = 10, DRAIN = 12, IFULL = 16, IFREE = 32, KVFULL = 48, KVFREE = 56, TAIL = 64,
+  kBarCount = 72
 };
-constexpr int kItemReaders = 3 + kSoftWarps;
 
 struct Params {
   PromptArgs a;
@@ -64,30 +66,26 @@ struct Params {
   uint64_t wait_limit;
 };
 
-// An item is tiles 2 a and 2 a + 1 of key-value head b.  Of each: the row tile, the query head, how many keys its rows see, and its blocks (0:
-// no such tile).
-struct Tiles {
-  int row_tile[2], head[2], keys[2], nb[2];
+// An item of PAIRED is tiles 2 a and 2 a + 1 of key-value head b, else tile a.  Of a tile: the row tile, the query head, how many keys its
+// rows see, and its blocks (0: no such tile).
+struct Tile {
+  int row_tile, head, keys, nb;
 };
-template <int HD>
-__device__ __forceinline__ Tiles tiles_of(const Item& it, int group) {
-  Tiles t;
-#pragma unroll
-  for (int k = 0; k < 2; ++k) {
-    const int x = 2 * it.a + k;
-    t.row_tile[k] = x / group;
-    t.head[k] = it.b * group + x % group;
-    t.keys[k] = t.row_tile[k] * kTile < it.len ? min(it.len, (t.row_tile[k] + 1) * kTile) : 0;
-    t.nb[k] = (t.keys[k] + Smem<HD>::kKeys - 1) / Smem<HD>::kKeys;
-  }
+template <int KN>
+__device__ __forceinline__ Tile tile_of(const Item& it, int number, int group) {
+  Tile t;
+  t.row_tile = number / group;
+  t.head = it.b * group + number % group;
+  t.keys = t.row_tile * kTile < it.len ? min(it.len, (t.row_tile + 1) * kTile) : 0;
+  t.nb = (t.keys + KN - 1) / KN;
   return t;
 }
 
-template <int HD, bool FP16>
-__global__ void __launch_bounds__(kThreads, 1)
+template <int HD, bool FP16, bool PAIRED>
+__global__ void __launch_bounds__((Smem<HD, PAIRED>::kThreads), 1)
     prompt_attn_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                        const __grid_constant__ CUtensorMap tm_v, const Params p) {
-  using Sm = Smem<HD>;
+  using Sm = Smem<HD, PAIRED>;
   constexpr int KB = HD / 64, NS = Sm::kStages, KN = Sm::kKeys;
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
@@ -95,9 +93,9 @@ __global__ void __launch_bounds__(kThreads, 1)
   const uint32_t s0 = smem_u32(smem), b0 = smem_u32(bars);
   auto BAR = [&](int i) { return b0 + 8u * static_cast<uint32_t>(i); };
   Item* items = reinterpret_cast<Item*>(bars + kBarCount);
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(items + kItems);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(items + 2 * kItems);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert(kBarCount * 8 + kItems * 16 + 8 <= 1024 && kBarCount % 2 == 0, "barrier area");
+  static_assert(kBarCount * 8 + 2 * kItems * 16 + 8 <= 1024 && kBarCount % 2 == 0, "barrier area");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint32_t* status = p.a.status;
   const uint64_t limit = p.wait_limit;
@@ -111,14 +109,14 @@ __global__ void __launch_bounds__(kThreads, 1)
       mbar_init(BAR(PFULL + t), kSoftWarps / 2);
       mbar_init(BAR(PVDONE + t), 1);
     }
-    for (int i = 0; i < 3; ++i) mbar_init(BAR(DRAIN + i), 1);
-    for (int i = 0; i < kItems; ++i) {
+    for (int i = 0; i < 4; ++i) mbar_init(BAR(DRAIN + i), 1);
+    for (int i = 0; i < 2 * kItems; ++i) {
       mbar_init(BAR(IFULL + i), 1);
-      mbar_init(BAR(IFREE + i), kItemReaders);
+      mbar_init(BAR(IFREE + i), Sm::kItemReaders);
     }
-    for (int s = 0; s < NS; ++s) {
+    for (int s = 0; s < 8; ++s) {
       mbar_init(BAR(KVFULL + s), 1);
-      mbar_init(BAR(KVFREE + s), (s & 1) ? 1 : 2);  // keys: read by a warp for each tile
+      mbar_init(BAR(KVFREE + s), PAIRED && !(s & 1) ? 2 : 1);  // (keys of both tiles: read by a warp for each)
       mbar_init(BAR(TAIL + s), 1);
     }
     *abort_flag = 0;
@@ -129,28 +127,37 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  auto slot = [&](int s) { return s0 + Sm::kRing + static_cast<uint32_t>(s) * Sm::kKvBytes; };
+  // The tile that this warp works for (its S, its softmax; where not PAIRED also its loads and its product with the values), and its ring.
+  const int x = warp >= Sm::kSoftWarp0 ? (warp - Sm::kSoftWarp0) >> 2 : PAIRED ? warp - 1 : warp & 1;
+  const int lane0 = PAIRED ? 0 : x, ring0 = lane0 * NS;
+  auto slot = [&](int s) { return s0 + Sm::kRing + static_cast<uint32_t>(ring0 + s) * Sm::kKvBytes; };
   auto waitw = [&](int bar, uint32_t phase) { return warp_waits(BAR(bar), phase & 1u, abort_flag, status, limit); };
   // Next descriptor; false at the end or at a timeout.
   auto take = [&](int k, Item& it) {
-    if (!waitw(IFULL + (k & 7), k >> 3)) return false;
-    it = items[k & 7];
+    const int i = 8 * lane0 + (k & 7);
+    if (!waitw(IFULL + i, k >> 3)) return false;
+    it = items[i];
     __syncwarp();
-    if (lane == 0) mbar_arrive(BAR(IFREE + (k & 7)));
+    if (lane == 0) mbar_arrive(BAR(IFREE + i));
     return it.len >= 0;
   };
+  auto number = [&](const Item& it, int tile) { return PAIRED ? 2 * it.a + tile : it.a; };
 
-  if (warp == 0) {
+  if (PAIRED ? warp == 0 : warp <= 1) {
     // ------------------------------------------------------------------ items and loads (a whole warp that waits, one thread that loads)
     const int n_seq = p.a.n_seq, group = p.group, Hk = p.a.n_kv_heads;
-    if (blockIdx.x == 0) check_starts(p.a.seq_start, n_seq, p.a.rows, lane, 32, status);
-    auto pairs_of = [&](int len) { return ((len + kTile - 1) / kTile * group + 1) / 2; };
+    if (blockIdx.x == 0 && warp == 0) check_starts(p.a.seq_start, n_seq, p.a.rows, lane, 32, status);
+    auto items_of = [&](int len) {  // of a key-value head
+      const int tiles = (len + kTile - 1) / kTile * group;
+      return PAIRED ? (tiles + 1) / 2 : tiles;
+    };
     int k = 0;
     auto put = [&](const Item& it) {
-      if (k >= kItems && !waitw(IFREE + (k & 7), (k >> 3) - 1)) return false;
+      const int i = 8 * lane0 + (k & 7);
+      if (k >= kItems && !waitw(IFREE + i, (k >> 3) - 1)) return false;
       if (lane == 0) {
-        items[k & 7] = it;
-        mbar_arrive(BAR(IFULL + (k & 7)));
+        items[i] = it;
+        mbar_arrive(BAR(IFULL + i));
       }
       __syncwarp();
       ++k;
@@ -160,23 +167,24 @@ __global__ void __launch_bounds__(kThreads, 1)
     // of each slot: its last load ends behind a sequence's last row; loads that did, and that did not, modulo 2
     uint32_t on_tail = 0, tail_phase = 0, full_phase = 0;
     auto load = [&](const Item& it) {
-      const Tiles t = tiles_of<HD>(it, group);
-      auto load_q = [&](int x) {
-        if (used[x] && !waitw(QFREE + x, used[x] - 1)) return false;
+      const Tile t0 = tile_of<KN>(it, number(it, 0), group), t1 = tile_of<KN>(it, number(it, 1), group);
+      auto load_q = [&](const Tile& t, int x) {
+        if (!t.nb) return true;
+        int& loaded = used[PAIRED ? x : 0];
+        if (loaded && !waitw(QFREE + x, loaded - 1)) return false;
         if (lane == 0) {
           mbar_arrive_expect_tx(BAR(QFULL + x), Sm::kQBytes);
 #pragma unroll
           for (int kb = 0; kb < KB; ++kb)
-            tma_load_2d(s0 + x * Sm::kQBytes + kb * kBlockBytes, &tm_q, BAR(QFULL + x), t.head[x] * HD + kb * 64,
-                        it.begin + t.row_tile[x] * kTile);
+            tma_load_2d(s0 + x * Sm::kQBytes + kb * kBlockBytes, &tm_q, BAR(QFULL + x), t.head * HD + kb * 64, it.begin + t.row_tile * kTile);
         }
         __syncwarp();
-        ++used[x];
+        ++loaded;
         return true;
       };
       auto load_kv = [&](const CUtensorMap* map, int j, bool tail) {
-        const int s = n % NS, bar = (tail ? TAIL : KVFULL) + s;
-        if (n >= NS && !waitw(KVFREE + s, n / NS - 1)) return false;
+        const int s = n % NS, bar = (tail ? TAIL : KVFULL) + ring0 + s;
+        if (n >= NS && !waitw(KVFREE + ring0 + s, n / NS - 1)) return false;
         if (lane == 0) {
           mbar_arrive_expect_tx(BAR(bar), Sm::kKvBytes);
 #pragma unroll
@@ -191,21 +199,21 @@ __global__ void __launch_bounds__(kThreads, 1)
       };
       auto load_k = [&](int j) { return load_kv(&tm_k, j, false); };
       auto load_v = [&](int j) { return load_kv(&tm_v, j, it.len - j * KN < KN); };
-      const int nb = max(t.nb[0], t.nb[1]);
-      bool ok = load_k(0) && (!t.nb[0] || load_q(0)) && (!t.nb[1] || load_q(1)) && load_v(0);
+      const int nb = max(t0.nb, t1.nb);
+      bool ok = load_k(0) && (PAIRED ? load_q(t0, 0) && load_q(t1, 1) : load_q(t0, lane0)) && load_v(0);
       for (int j = 1; j < nb && ok; ++j) ok = load_k(j) && load_v(j);
       return ok;
     };
     if (find_items(
-            p.a.seq_start, n_seq, p.a.rows, blockIdx.x, gridDim.x, p.items_bound,
-            [&](int len) { return static_cast<int64_t>(pairs_of(len)) * Hk; },
+            p.a.seq_start, n_seq, p.a.rows, blockIdx.x + lane0 * gridDim.x, Sm::kRings * gridDim.x, p.items_bound,
+            [&](int len) { return static_cast<int64_t>(items_of(len)) * Hk; },
             [&](int begin, int len, int u) {
-              const Item it{begin, len, pairs_of(len) - 1 - u / Hk, u % Hk};
+              const Item it{begin, len, items_of(len) - 1 - u / Hk, u % Hk};
               return put(it) && load(it);
             }))
       put(Item{0, -1, 0, 0});
     const Outside out(p.a.seq_start, p.a.n_seq, p.a.rows);
-    for (int i = blockIdx.x; i < out.count(); i += gridDim.x) {
+    for (int i = blockIdx.x + lane0 * gridDim.x; i < out.count(); i += Sm::kRings * gridDim.x) {
       const int row = out.row(i);
       zero_row(elem(p.a.out, row * p.a.ldo), p.a.n_q_heads * HD);
       if (p.a.lse)
@@ -215,13 +223,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     for (int i = max(0, n - NS); i < n; ++i) {
       const int s = i % NS;
       const bool tail = (on_tail >> s) & 1;
-      wait_drain(BAR((tail ? TAIL : KVFULL) + s), (((tail ? tail_phase : full_phase) >> s) & 1) ^ 1, limit);
+      wait_drain(BAR((tail ? TAIL : KVFULL) + ring0 + s), (((tail ? tail_phase : full_phase) >> s) & 1) ^ 1, limit);
     }
-    for (int x = 0; x < 2; ++x)
-      if (used[x]) wait_drain(BAR(QFULL + x), (used[x] - 1) & 1, limit);
-  } else if (warp <= 2) {
+    for (int i = 0; i < (PAIRED ? 2 : 1); ++i)
+      if (used[i]) wait_drain(BAR(QFULL + (PAIRED ? i : lane0)), (used[i] - 1) & 1, limit);
+  } else if (PAIRED ? warp <= 2 : warp <= 3) {
     // ------------------------------------------------------------------ S of tile x
-    const int x = warp - 1;
     const uint32_t tS = tmem + static_cast<uint32_t>(x) * 256 + Sm::kColS, dq = tile_desc(s0 + x * Sm::kQBytes);
     int block = 0, q = 0;  // blocks and Q tiles of this tile so far
     int s = 0, round = 0;  // ring slot of the next block of keys, and how often the ring has gone round
@@ -236,14 +243,14 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true;
     for (int k = 0; ok && take(k, it); ++k) {
       it = Item{0, uniform(it.len), uniform(it.a), uniform(it.b)};
-      const Tiles t = tiles_of<HD>(it, p.group);
-      const int nb = x ? t.nb[1] : t.nb[0], other = x ? t.nb[0] : t.nb[1], keys = x ? t.keys[1] : t.keys[0];
+      const Tile t = tile_of<KN>(it, number(it, x), p.group);
+      const int nb = t.nb, other = PAIRED ? tile_of<KN>(it, number(it, x ^ 1), p.group).nb : 0, keys = t.keys;
       for (int j = 0; j < nb; ++j, ++block) {
         const uint32_t kv = tile_desc(slot(s), Sm::kKvBlock), is = tile_idesc((min(KN, keys - j * KN) + 15) & ~15, FP16, false);
-        const uint32_t freed = BAR(KVFREE + s);
-        const bool last = j == nb - 1, lone = j >= other;
+        const uint32_t freed = BAR(KVFREE + ring0 + s);
+        const bool last = j == nb - 1, lone = PAIRED && j >= other;
         // the scores go over those of the block before once the threads have read them
-        if (!(ok = waitw(KVFULL + s, round) && (j > 0 || waitw(QFULL + x, q)) && (block == 0 || waitw(SREAD + x, block - 1)))) break;
+        if (!(ok = waitw(KVFULL + ring0 + s, round) && (j > 0 || waitw(QFULL + x, q)) && (block == 0 || waitw(SREAD + x, block - 1)))) break;
         tc_fence_after();
         if (elected()) {
 #pragma unroll
@@ -261,8 +268,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     if (elected()) tc_commit(BAR(DRAIN + x));
     wait_drain(BAR(DRAIN + x), 0, limit);
-  } else if (warp == 3) {
-    // ------------------------------------------------------------------ O += P V of both tiles in turn
+  } else if (PAIRED ? warp == 3 : warp <= 5) {
+    // ------------------------------------------------------------------ O += P V, of both tiles in turn (not PAIRED: of tile x)
     const uint32_t io = tile_idesc(HD, FP16, true);
     int block[2] = {0, 0};
     int s = 1;
@@ -271,61 +278,62 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true;
     for (int k = 0; ok && take(k, it); ++k) {
       it = Item{0, uniform(it.len), uniform(it.a), uniform(it.b)};
-      const Tiles t = tiles_of<HD>(it, p.group);
-      const int nb = max(t.nb[0], t.nb[1]);
+      const Tile t[2] = {tile_of<KN>(it, number(it, 0), p.group), tile_of<KN>(it, number(it, 1), p.group)};
+      const int nb = max(t[0].nb, t[1].nb);
       for (int j = 0; j < nb && ok; ++j) {
-        const uint32_t kv = tile_desc(slot(s), Sm::kKvBlock), freed = BAR(KVFREE + s);
+        const uint32_t kv = tile_desc(slot(s), Sm::kKvBlock), freed = BAR(KVFREE + ring0 + s);
         const int rows = it.len - j * KN;
         if (rows < KN) {
           // values behind a sequence's last row become zeros: their weights are zeros, but a NaN would spoil the product
-          if (!(ok = waitw(TAIL + s, tails >> s))) break;
+          if (!(ok = waitw(TAIL + ring0 + s, tails >> s))) break;
           tails ^= 1u << s;
-          zero_tile_rows<HD>(smem + Sm::kRing + s * Sm::kKvBytes, rows, (rows + 15) & ~15, Sm::kKvBlock);
+          zero_tile_rows<HD>(smem + Sm::kRing + (ring0 + s) * Sm::kKvBytes, rows, (rows + 15) & ~15, Sm::kKvBlock);
           fence_async_smem();
           __syncwarp();
-        } else if (!(ok = waitw(KVFULL + s, fulls >> s))) {
+        } else if (!(ok = waitw(KVFULL + ring0 + s, fulls >> s))) {
           break;
         } else {
           fulls ^= 1u << s;
         }
 #pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          if (j >= t.nb[x]) continue;
-          const uint32_t tO = tmem + x * 256, tP = tO + Sm::kColP, more = j > 0;
-          const int steps = (min(KN, t.keys[x] - j * KN) + 15) / 16;
-          const bool frees = x == 1 || j >= t.nb[1];  // the block's last reader (a commit covers what was issued before)
-          if (!(ok = ok && waitw(PFULL + x, block[x]))) break;
+        for (int i2 = 0; i2 < (PAIRED ? 2 : 1); ++i2) {
+          if (j >= t[i2].nb) continue;
+          const int y = PAIRED ? i2 : x;
+          const uint32_t tO = tmem + static_cast<uint32_t>(y) * 256, tP = tO + Sm::kColP, more = j > 0;
+          const int steps = (min(KN, t[i2].keys - j * KN) + 15) / 16;
+          const bool frees = !PAIRED || i2 == 1 || j >= t[1].nb;  // the block's last reader (a commit covers what was issued before)
+          if (!(ok = ok && waitw(PFULL + y, block[i2]))) break;
           tc_fence_after();
           if (elected()) {
 #pragma unroll
             for (int i = 0; i < KN / 16; ++i)
               if (i < steps) tile_mma_ts(tO, tP + i * 8, kv + mn_major_step(i), io, i > 0 ? 1u : more);
-            tc_commit(BAR(PVDONE + x));
+            tc_commit(BAR(PVDONE + y));
             if (frees) tc_commit(freed);
           }
           __syncwarp();
-          ++block[x];
+          ++block[i2];
         }
         s += 2;
         if (s >= NS) s = 1;
       }
     }
-    if (elected()) tc_commit(BAR(DRAIN + 2));
-    wait_drain(BAR(DRAIN + 2), 0, limit);
-  } else {
+    if (elected()) tc_commit(BAR(DRAIN + 2 + lane0));
+    wait_drain(BAR(DRAIN + 2 + lane0), 0, limit);
+  } else if (warp >= Sm::kSoftWarp0) {
     // ------------------------------------------------------------------ softmax and output
-    const int x = (warp - kSoftWarp0) >> 2, q4 = warp & 3, r = q4 * 32 + lane;  // tile, lane quarter, row in the tile
+    const int q4 = warp & 3, r = q4 * 32 + lane;  // lane quarter, row in the tile
     const uint32_t tO = tmem + (static_cast<uint32_t>(q4 * 32) << 16) + static_cast<uint32_t>(x) * 256;
     const uint32_t tS = tO + Sm::kColS, tP = tO + Sm::kColP;
-    uint8_t* staging = smem + Sm::kStage + (warp - kSoftWarp0) * 2048;
+    uint8_t* staging = smem + Sm::kStage + (warp - Sm::kSoftWarp0) * 2048;
     const float c = p.c;
     const uint64_t c2 = pair_of(c, c);
     int block = 0;
     bool ok = true;
     Item it;
     for (int k = 0; ok && take(k, it); ++k) {
-      const Tiles t = tiles_of<HD>(it, p.group);
-      const int nb = x ? t.nb[1] : t.nb[0], head = x ? t.head[1] : t.head[0], tile0 = (x ? t.row_tile[1] : t.row_tile[0]) * kTile;
+      const Tile t = tile_of<KN>(it, number(it, x), p.group);
+      const int nb = t.nb, head = t.head, tile0 = t.row_tile * kTile;
       if (!nb) continue;
       const int live = min(32, it.len - tile0 - q4 * 32);  // the warp's rows of the sequence, at most 0: none
       float m = -INFINITY, l = 0.f;
@@ -436,37 +444,46 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
 }
 
-template <int HD, bool FP16>
+// Sequences of fewer rows than this on average: a tile each for the two halves of a CTA.
+constexpr int kShort = 768;
+
+template <int HD, bool FP16, bool PAIRED>
 int launch(const PromptArgs& a, cudaStream_t s) {
+  using Sm = Smem<HD, PAIRED>;
   Params p{};
   p.a = a;
   p.group = a.n_q_heads / a.n_kv_heads;
   p.c = a.scale * kLog2e;
   p.offset = FP16 ? 7.f : 0.f;
   p.wait_limit = g_wait_limit_ns.load(std::memory_order_relaxed);
-  // as many items as well-formed sequences can have: a last row tile and a lone last tile each
+  // as many items as well-formed sequences can have: a last row tile each (and a lone last tile)
   const int64_t seqs = std::min(a.n_seq, a.rows), tiles = (a.rows / kTile + seqs) * p.group;
-  p.items_bound = static_cast<int>(std::min<int64_t>((tiles + seqs + 1) / 2 * a.n_kv_heads, 0x7fffffff));
+  p.items_bound = static_cast<int>(std::min<int64_t>((PAIRED ? (tiles + seqs + 1) / 2 : tiles) * a.n_kv_heads, 0x7fffffff));
   CUtensorMap q, k, v;
   if (!make_tensor_map_2d(&q, a.q, a.rows, static_cast<int64_t>(a.n_q_heads) * HD, a.ldq, kTile, FP16) ||
-      !make_tensor_map_2d(&k, a.k, a.rows, static_cast<int64_t>(a.n_kv_heads) * HD, a.ldk, Smem<HD>::kKeys, FP16) ||
-      !make_tensor_map_2d(&v, a.v, a.rows, static_cast<int64_t>(a.n_kv_heads) * HD, a.ldv, Smem<HD>::kKeys, FP16))
+      !make_tensor_map_2d(&k, a.k, a.rows, static_cast<int64_t>(a.n_kv_heads) * HD, a.ldk, Sm::kKeys, FP16) ||
+      !make_tensor_map_2d(&v, a.v, a.rows, static_cast<int64_t>(a.n_kv_heads) * HD, a.ldv, Sm::kKeys, FP16))
     return cuda_fail(cudaErrorInvalidValue, "vla_prompt_attn: tensor maps");
   int sms = 0;
   if (const int rc = device_sms(&sms)) return rc;
+  const auto kern = prompt_attn_kernel<HD, FP16, PAIRED>;
   static std::atomic<uint64_t> done{0};
-  VLA_CUDA_TRY(set_smem_limit(prompt_attn_kernel<HD, FP16>, Smem<HD>::kTotal, done));
-  VLA_CUDA_TRY(launch_at(Start::kInOrder, prompt_attn_kernel<HD, FP16>, dim3(static_cast<unsigned>(std::min(p.items_bound, sms))), dim3(kThreads),
-                         Smem<HD>::kTotal, s, q, k, v, p));
+  VLA_CUDA_TRY(set_smem_limit(kern, Sm::kTotal, done));
+  VLA_CUDA_TRY(launch_at(Start::kInOrder, kern, dim3(static_cast<unsigned>(std::min(p.items_bound, sms))), dim3(Sm::kThreads), Sm::kTotal, s, q, k, v,
+                         p));
   note_launch();
   return VLA_OK;
+}
+template <int HD, bool FP16>
+int launch_for(const PromptArgs& a, cudaStream_t s) {
+  return a.rows / std::min(a.n_seq, a.rows) < kShort ? launch<HD, FP16, false>(a, s) : launch<HD, FP16, true>(a, s);
 }
 
 }  // namespace
 
 int prompt_attn_launch(const PromptArgs& a, cudaStream_t s) {
-  if (a.head_dim == 128) return a.fp16 ? launch<128, true>(a, s) : launch<128, false>(a, s);
-  return a.fp16 ? launch<64, true>(a, s) : launch<64, false>(a, s);
+  if (a.head_dim == 128) return a.fp16 ? launch_for<128, true>(a, s) : launch_for<128, false>(a, s);
+  return a.fp16 ? launch_for<64, true>(a, s) : launch_for<64, false>(a, s);
 }
 
 }  // namespace vla
