@@ -22,7 +22,7 @@
 //   warps 1, 2   issue S = Q K^T of a tile each;
 //   warp 3       issues O += P V of both (V as the MN-major operand).  One warp for all products cannot keep up, at 250 to 800 cycles from
 //                one group of products to the next beside the softmax;
-//   warps 4 - 11 one query row a thread: softmax, and the output through shared memory in whole sectors.  (Two threads a row: the
+//   warps 4 - 11 one query row a thread: softmax, and the output.  (Two threads a row: the
 //                exchange of their maxima costs what the shorter rows save.)
 // A row whose result is not finite is computed again from its own keys alone (attend_row): a NaN behind a row in its
 // block of keys does not count for it.
@@ -42,11 +42,11 @@ template <int HD, bool PAIRED>
 struct Smem {
   static constexpr int kSoftWarp0 = PAIRED ? 4 : 8, kThreads = 32 * (kSoftWarp0 + kSoftWarps);
   static constexpr int kKeys = PAIRED ? 80 : 64;                    // keys of a block
-  static constexpr int kStages = !PAIRED ? 4 : HD == 128 ? 6 : 8;  // of a ring
+  static constexpr int kStages = PAIRED ? 8 : 4;  // of a ring
   static constexpr int kRings = PAIRED ? 1 : 2;                     // for both tiles, or one each
   static constexpr int kItemReaders = PAIRED ? 3 + kSoftWarps : 2 + kSoftWarps / 2;
   static constexpr uint32_t kQBytes = kTile * HD * 2, kKvBytes = kKeys * HD * 2, kKvBlock = kKeys * 128;
-  static constexpr uint32_t kRing = 2 * kQBytes, kStage = kRing + kRings * kStages * kKvBytes, kBars = kStage + kSoftWarps * 2048;
+  static constexpr uint32_t kRing = 2 * kQBytes, kBars = kRing + kRings * kStages * kKvBytes;
   static constexpr uint32_t kTotal = 1024 + kBars + 1024;
   static constexpr uint32_t kColS = HD, kColP = HD + kKeys;  // of a tile's 256 columns
   static_assert(kTotal <= 232448 && kColP + kKeys / 2 <= 256 && kKvBlock % 1024 == 0, "shared and tensor memory");
@@ -325,7 +325,6 @@ __global__ void __launch_bounds__((Smem<HD, PAIRED>::kThreads), 1)
     const int q4 = warp & 3, r = q4 * 32 + lane;  // lane quarter, row in the tile
     const uint32_t tO = tmem + (static_cast<uint32_t>(q4 * 32) << 16) + static_cast<uint32_t>(x) * 256;
     const uint32_t tS = tO + Sm::kColS, tP = tO + Sm::kColP;
-    uint8_t* staging = smem + Sm::kStage + (warp - Sm::kSoftWarp0) * 2048;
     const float c = p.c;
     const uint64_t c2 = pair_of(c, c);
     int block = 0;
@@ -424,7 +423,7 @@ __global__ void __launch_bounds__((Smem<HD, PAIRED>::kThreads), 1)
       tc_fence_after();
       if (live <= 0) continue;
       const int64_t row = it.begin + tile0 + q4 * 32;
-      const bool bad = store_tile<FP16, HD / 32>(tO, staging, 1.f / l, elem(p.a.out, row * p.a.ldo + head * HD), p.a.ldo, live);
+      const bool bad = store_tile<FP16, HD / 32>(tO, 1.f / l, elem(p.a.out, row * p.a.ldo + head * HD), p.a.ldo, live);
       if (p.a.lse && lane < live) p.a.lse[(row + lane) * p.a.n_q_heads + head] = (log2f(l) - fmaf(-m, c, p.offset)) * kLn2;
       uint32_t again = __ballot_sync(0xffffffffu, bad && lane < live);
       while (again) {

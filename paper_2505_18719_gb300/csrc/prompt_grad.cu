@@ -144,10 +144,10 @@ struct Shape {
   static constexpr int kHalf = kBlock / 2;  // columns of one of a row's two threads
   static constexpr int kRows = 2;           // blocks of queries' lse and D in flight (KEYS)
   static constexpr uint32_t kRowBytes = KEYS ? kRows * kBlock * 128 : 0;
-  // shared memory: the tile's two operands, two rings, a warp's rows on their way out, rows' lse and D, barriers
+  // shared memory: the tile's two operands, two rings, rows' lse and D, barriers
   static constexpr uint32_t kTileBytes = kTile * HD * 2, kBlockBytes = kBlock * HD * 2, kColumns = kBlock * 128;
-  static constexpr uint32_t kRingA = 2 * kTileBytes, kRingB = kRingA + kStages * kBlockBytes, kStage = kRingB + kStages * kBlockBytes;
-  static constexpr uint32_t kRowData = kStage + 8 * 2048, kBars = kRowData + kRowBytes, kTotal = 1024 + kBars + 1024;
+  static constexpr uint32_t kRingA = 2 * kTileBytes, kRingB = kRingA + kStages * kBlockBytes, kRowData = kRingB + kStages * kBlockBytes;
+  static constexpr uint32_t kBars = kRowData + kRowBytes, kTotal = 1024 + kBars + 1024;
   // Tensor memory: scores, dP, P and dS (KEYS; else two blocks of dP, and dS over each of them), 8 columns of ones, sums (KEYS: d_v, d_k; else d_q).
   static constexpr uint32_t kColS = 0, kColDp = kBlock, kColP = 2 * kBlock, kColDs = KEYS ? kColP + kBlock / 2 : kColDp;
   static constexpr uint32_t kColOnes = kColDs + kBlock / 2, kColV = 256, kColSum = 384;
@@ -519,7 +519,6 @@ __global__ void __launch_bounds__(kThreads, 1)
     const uint32_t quarter = tmem + (static_cast<uint32_t>(q4 * 32) << 16);
     const uint32_t tS = quarter + Sh::kColS + NH * half, tDp = quarter + Sh::kColDp + NH * half;
     const uint32_t tP = quarter + Sh::kColP + NH / 2 * half, tDs = quarter + Sh::kColDs + (KEYS ? NH / 2 : NH) * half;
-    uint8_t* staging = smem + Sh::kStage + (warp - kSumWarp0) * 2048;
     const uint64_t c2 = pair_of(p.c, p.c);
     int w = 0;
     Item it;
@@ -672,13 +671,13 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int64_t at = it.begin + row0;
       if constexpr (KEYS) {
         if (half == 0)
-          store_tile<FP16, HD / 32>(quarter + Sh::kColV, staging, FP16 ? exp2_int(-static_cast<int>(kPShift)) : 1.f,
+          store_tile<FP16, HD / 32>(quarter + Sh::kColV, FP16 ? exp2_int(-static_cast<int>(kPShift)) : 1.f,
                                     elem(p.g.d_v, at * p.g.lddv + it.b * HD), p.g.lddv, it.len - row0);
         else
-          store_tile<FP16, HD / 32>(quarter + Sh::kColSum, staging, FP16 ? f.scale * exp2_int(-e) : f.scale,
+          store_tile<FP16, HD / 32>(quarter + Sh::kColSum, FP16 ? f.scale * exp2_int(-e) : f.scale,
                                     elem(p.g.d_k, at * p.g.lddk + it.b * HD), p.g.lddk, it.len - row0);
       } else {
-        store_tile<FP16, HD / 64>(quarter + Sh::kColSum + half * (HD / 2), staging, FP16 ? f.scale * exp2_int(-e) : f.scale,
+        store_tile<FP16, HD / 64>(quarter + Sh::kColSum + half * (HD / 2), FP16 ? f.scale * exp2_int(-e) : f.scale,
                                   elem(p.g.d_q, at * p.g.lddq + it.b * HD + half * (HD / 2)), p.g.lddq, it.len - row0);
       }
       tc_fence_before();

@@ -57,37 +57,38 @@ __device__ __forceinline__ void zero_row(void* row, int n) {
   for (int e = threadIdx.x & 31; e < n / 8; e += 32) static_cast<uint4*>(row)[e] = make_uint4(0u, 0u, 0u, 0u);
 }
 
-// `chunks` x 32 columns of this warp's 32 rows of tensor memory, times `scale`, to rows of `dst` (ld elements apart), of which `live` exist:
-// through 2 KB of shared memory, 8 rows of 64 bytes a store.  Whether this thread's row has a NaN or an infinity.
+// CHUNKS x 32 columns of this warp's 32 rows of tensor memory, times `scale`, to rows of `dst` (ld elements apart), of which `live` exist; each
+// thread its own row, 32 bytes a store where rows lie for it (`wide`).  (Through shared memory, with lanes side by side in a row, the
+// products' operands were in the way: 4000 cycles a tile.)  Whether this thread's row has a NaN or an infinity.
+__device__ __forceinline__ bool wide_rows(const void* dst, int64_t ld) { return !((reinterpret_cast<uintptr_t>(dst) & 31) | (ld & 15)); }
 template <bool FP16, int CHUNKS>
-__device__ __forceinline__ bool store_tile(uint32_t tmem, uint8_t* staging, float scale, void* dst, int64_t ld, int live) {
+__device__ __forceinline__ bool store_tile(uint32_t tmem, float scale, void* dst, int64_t ld, int live) {
   const int lane = threadIdx.x & 31;
+  const bool wide = wide_rows(dst, ld);
+  uint4* row = static_cast<uint4*>(elem(dst, lane * ld));
   float bad = 0.f;
 #pragma unroll
   for (int b = 0; b < CHUNKS; ++b) {
-    uint32_t v[32];
+    uint32_t v[32], w[16];
     tmem_ld32(tmem + 32 * b, v);
     tmem_wait_ld();
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      uint32_t w[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float y0 = __uint_as_float(v[8 * e + 2 * i]) * scale, y1 = __uint_as_float(v[8 * e + 2 * i + 1]) * scale;
-        bad = fmaf(y0, 0.f, fmaf(y1, 0.f, bad));
-        w[i] = pack2<FP16>(y0, y1);
-      }
-      *reinterpret_cast<uint4*>(staging + lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4)) = make_uint4(w[0], w[1], w[2], w[3]);
+    for (int i = 0; i < 16; ++i) {
+      const float y0 = __uint_as_float(v[2 * i]) * scale, y1 = __uint_as_float(v[2 * i + 1]) * scale;
+      bad = fmaf(y0, 0.f, fmaf(y1, 0.f, bad));
+      w[i] = pack2<FP16>(y0, y1);
     }
-    __syncwarp();
+    if (lane >= live) continue;
+    if (wide) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int rr = 8 * i + (lane >> 2), e = lane & 3;
-      if (rr < live)
-        *reinterpret_cast<uint4*>(elem(dst, rr * ld + b * 32 + e * 8)) =
-            *reinterpret_cast<const uint4*>(staging + rr * 64 + ((e ^ ((rr >> 1) & 3)) << 4));
+      for (int h = 0; h < 2; ++h)
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(row + 4 * b + 2 * h), "r"(w[8 * h]), "r"(w[8 * h + 1]),
+                     "r"(w[8 * h + 2]), "r"(w[8 * h + 3]), "r"(w[8 * h + 4]), "r"(w[8 * h + 5]), "r"(w[8 * h + 6]), "r"(w[8 * h + 7])
+                     : "memory");
+    } else {
+#pragma unroll
+      for (int h = 0; h < 4; ++h) row[4 * b + h] = make_uint4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]);
     }
-    __syncwarp();
   }
   return bad != 0.f;
 }
