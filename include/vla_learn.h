@@ -29,11 +29,11 @@ extern "C" {
  *   q, out     [rows][n_q_heads][head_dim], row strides ldq, ldo;  k, v  [rows][n_kv_heads][head_dim], row strides ldk, ldv:
  *              of type `dtype` (VLA_F16 or VLA_BF16), 16-byte aligned, strides multiples of 8 elements (parts of one q|k|v
  *              buffer fit); head_dim 64 or 128;
- *   scale      > 0;
+ *   scale      1e-30 or more;
  *   lse        f32 [rows][n_q_heads] or NULL: log sum_j exp(scale q . k[j]); -infinity in rows of no sequence.
  * Scores, their maxima and sums are 32-bit; the weights of the values are rounded to `dtype`, relative to their maximum.  A row depends
  * on nothing behind it and on no other sequence: NaN and infinities there stay there.  Equal calls give
- * equal bits.  rows 0 or more; rows * n_q_heads at most 2^30. */
+ * equal bits.  out overlaps nothing that the call reads.  rows 0 or more; rows * n_q_heads at most 2^30. */
 int vla_prompt_attn(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int dtype, int rows,
                     int n_q_heads, int n_kv_heads, int head_dim, const int32_t* seq_start, int n_seq, float scale, void* out,
                     int64_t ldo, float* lse, void* cuda_stream);
@@ -43,7 +43,7 @@ int vla_prompt_attn(const void* q, int64_t ldq, const void* k, int64_t ldk, cons
  * that share them, in 32 bits.  With P the softmax weights, D[i] = d_out[i] . out[i]:
  *   d_v[j] = sum_i P[i][j] d_out[i],   dS[i][j] = P[i][j] (d_out[i] . v[j] - D[i]),
  *   d_q[i] = scale sum_j dS[i][j] k[j],   d_k[j] = scale sum_i dS[i][j] q[i].
- * P and dS are rounded to `dtype` in these sums.  The gradients may overwrite nothing that the call reads.  Equal
+ * P and dS are rounded to `dtype` in these sums.  NaN and infinities stay in their sequence.  The gradients may overwrite nothing that the call reads.  Equal
  * calls give equal bits (no atomics).  `workspace` of vla_prompt_attn_grad_workspace_bytes, 16-byte aligned, any
  * content; not shared by calls that may overlap. */
 int vla_prompt_attn_grad(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int dtype, int rows,

@@ -8,6 +8,7 @@ namespace vla {
 namespace {
 
 constexpr int kMostHeads = 65535;
+constexpr float kLeastScale = 1e-30f;  // the gradient takes lse / scale
 
 bool misaligned(const void* p, uintptr_t bytes) { return reinterpret_cast<uintptr_t>(p) & (bytes - 1); }
 int elem_bytes(int d) { return d == VLA_F32 ? 4 : 2; }
@@ -32,7 +33,7 @@ int check_prompt(const PromptArgs& a, int dtype, const PromptNames& n) {
       bad_rows(a.out, a.ldo, a.n_q_heads * hd))
     return record_error(VLA_ERR_ARG, n.tensors);
   if (misaligned(a.lse, 4)) return record_error(VLA_ERR_ARG, n.tensors);
-  if (!a.seq_start || misaligned(a.seq_start, 4) || a.n_seq < 1 || !(a.scale > 0.f) || !isfinite(a.scale)) return record_error(VLA_ERR_ARG, n.sequences);
+  if (!a.seq_start || misaligned(a.seq_start, 4) || a.n_seq < 1 || !(a.scale >= kLeastScale) || !isfinite(a.scale)) return record_error(VLA_ERR_ARG, n.sequences);
   return VLA_OK;
 }
 
@@ -65,7 +66,7 @@ int vla_prompt_attn(const void* q, int64_t ldq, const void* k, int64_t ldk, cons
   static constexpr PromptNames kNames{"vla_prompt_attn: fp16 or bf16", "vla_prompt_attn: rows < 0, or query heads no multiple of the key-value heads",
                                       "vla_prompt_attn: heads of 64 or 128", "vla_prompt_attn: more than 65535 heads or 2^30 rows x query heads",
                                       "vla_prompt_attn: q, k, v, out: 16-byte aligned, row strides multiples of 8 that hold a row",
-                                      "vla_prompt_attn: no sequences, or a scale that is not above 0"};
+                                      "vla_prompt_attn: no sequences, or a scale below 1e-30 or infinite"};
   PromptArgs a{q, k, v, ldq, ldk, ldv, dtype == VLA_F16, rows, n_q_heads, n_kv_heads, head_dim, seq_start, n_seq, scale, out, ldo, lse, nullptr};
   if (const int rc = check_prompt(a, dtype, kNames)) return rc;
   if (rows == 0) return VLA_OK;
@@ -89,7 +90,7 @@ int vla_prompt_attn_grad(const void* q, int64_t ldq, const void* k, int64_t ldk,
       "vla_prompt_attn_grad: fp16 or bf16", "vla_prompt_attn_grad: rows < 0, or query heads no multiple of the key-value heads",
       "vla_prompt_attn_grad: heads of 64 or 128", "vla_prompt_attn_grad: more than 65535 heads or 2^30 rows x query heads",
       "vla_prompt_attn_grad: q, k, v, out: 16-byte aligned, row strides multiples of 8 that hold a row",
-      "vla_prompt_attn_grad: no sequences, or a scale that is not above 0"};
+      "vla_prompt_attn_grad: no sequences, or a scale below 1e-30 or infinite"};
   PromptGradArgs a{{q, k, v, ldq, ldk, ldv, dtype == VLA_F16, rows, n_q_heads, n_kv_heads, head_dim, seq_start, n_seq, scale,
                     const_cast<void*>(out), ldo, const_cast<float*>(lse), nullptr},
                    d_out, lddo, d_q, d_k, d_v, lddq, lddk, lddv, workspace};

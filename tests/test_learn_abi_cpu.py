@@ -46,7 +46,7 @@ def attend_grad(**kw):
 
 BOTH = [dict(q_ptr=0), dict(k_ptr=0), dict(v_ptr=0), dict(out_ptr=0), dict(seq_start_ptr=0), dict(seq_start_ptr=18), dict(q_ptr=8), dict(k_ptr=24),
         dict(v_ptr=18), dict(out_ptr=20), dict(ldq=248), dict(ldk=120), dict(ldv=130), dict(ldo=250), dict(ldo=260), dict(rows=-1), dict(n_q_heads=0),
-        dict(n_kv_heads=0), dict(n_kv_heads=3), dict(n_kv_heads=8), dict(n_seq=0), dict(n_seq=-1), dict(scale=0.0), dict(scale=-1.0),
+        dict(n_kv_heads=0), dict(n_kv_heads=3), dict(n_kv_heads=8), dict(n_seq=0), dict(n_seq=-1), dict(scale=0.0), dict(scale=1e-31), dict(scale=-1.0),
         dict(scale=float("nan")), dict(scale=float("inf")), dict(lse_ptr=18)]
 
 
