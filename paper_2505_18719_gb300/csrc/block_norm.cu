@@ -1,13 +1,19 @@
 // What lies between two blocks of a decoder, and its gradient (include/vla_learn.h).
 //
-// A row is read once and stays in the registers of one CTA.  Forward, with r = 1 / sqrt(mean(.^2) + eps): two sums over the row, one
-// behind the other (the second needs the first).  Gradient, with n = h_out r_h, m = y r_y, g = d_x pre_gain:
+// Forward, with r = 1 / sqrt(mean(.^2) + eps): two sums over the row, one behind the other (the second needs the first); a row is read
+// once and stays in the registers of one CTA (of one warp up to 256 channels, 8 rows a CTA).  Gradient, with n = h_out r_h, m = y r_y,
+// g = d_x pre_gain:
 //   d_h = d_h_out + r_h (g - n c1),  c1 = mean(g n);
 //   d_u = residual_scale gate d_h,  d_y = r_y (d_u post_gain - m c2),  c2 = mean(d_u post_gain m).
 // c2 is linear in d_h, so with q = residual_scale gate post_gain m both means come from three sums taken together:
 //   c2 = mean(q (d_h_out + r_h g)) - c1 mean(q r_h n).
-// Column sums (gains, a gate for all rows) stay in registers over a CTA's rows; the CTAs' sums go to the workspace and are added in
-// the order of the CTAs by a second kernel.
+// A CTA takes every n-th row; the next one comes to shared memory by bulk copies while it works at this one.  Short rows stay in registers between the
+// sums and the outputs (8 elements a thread: a row of 1155 by single elements, 2311 of them, 23 us where reading shared memory again took 65),
+// longer ones are read from shared memory twice.  Column sums (gains, a gate for all rows) stay in registers over a CTA's rows; the CTAs' sums
+// go to the workspace and are added in the order of the CTAs by a second kernel, which waits for the first already started.
+//
+// Bound by HBM: 18385 rows of 4096, bf16 blocks and a fp32 stream, norm and gate behind the block: forward 141 us (6.4 TB/s, 0.95 of the copy
+// rate), gradient 262 us (5.2 TB/s; 342 without the copies ahead); 448 rows: 17 us, of which the second kernel and the start are half.
 #include <algorithm>
 #include <type_traits>
 
@@ -19,7 +25,7 @@ namespace vla {
 namespace {
 
 // CTAs of the gradient, each a share of the rows: 152 SMs with as many as hide a row's latency.
-int parts_of(int rows, int dim) { return std::min(rows, 152 * (dim <= 512 ? 6 : dim <= 1024 ? 4 : dim <= 2048 ? 3 : dim <= 4096 ? 2 : 1)); }
+int parts_of(int rows, int dim) { return std::min(rows, 152 * (dim <= 256 ? 16 : dim <= 512 ? 8 : dim <= 1024 ? 4 : dim <= 1400 ? 3 : dim <= 4096 ? 2 : 1)); }
 uint32_t staged_limit(int dim) { return dim <= 4096 ? 100 * 1024 : 200 * 1024; }  // of two rows of each of those CTAs
 
 template <class T>
@@ -34,25 +40,21 @@ __device__ __forceinline__ T from_f(float x) {
   if constexpr (std::is_same_v<T, f16>) return __float2half_rn(x);
   if constexpr (std::is_same_v<T, bf16>) return __float2bfloat16_rn(x);
 }
-template <class T>
-struct alignas(16) Eight {
-  T x[8];
+template <class T, int V>
+struct alignas(V * sizeof(T) < 16 ? V * sizeof(T) : 16) Some {
+  T x[V];
 };
 
-// Elements of a row that a thread holds: V consecutive ones at a time (8: 16-byte accesses, or 1).  Past the row: zeros, not stored.
+// Elements of a row that a thread holds: V consecutive ones at a time (8: 16-byte accesses, 2, or 1).  Past the row: zeros, not stored.
 template <int V, int E, class T>
 __device__ __forceinline__ void load_row(const T* row, int dim, float (&y)[E]) {
 #pragma unroll
   for (int c = 0; c < E / V; ++c) {
     const int i = (c * blockDim.x + threadIdx.x) * V;
-    if constexpr (V == 8) {
-      Eight<T> w{};
-      if (i < dim) w = *reinterpret_cast<const Eight<T>*>(row + i);
+    Some<T, V> w{};
+    if (i < dim) w = *reinterpret_cast<const Some<T, V>*>(row + i);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[c * 8 + e] = to_f(w.x[e]);
-    } else {
-      y[c] = i < dim ? to_f(row[i]) : 0.f;
-    }
+    for (int e = 0; e < V; ++e) y[c * V + e] = to_f(w.x[e]);
   }
 }
 template <int V, int E, class T>
@@ -61,26 +63,18 @@ __device__ __forceinline__ void store_row(T* row, int dim, const float (&y)[E]) 
   for (int c = 0; c < E / V; ++c) {
     const int i = (c * blockDim.x + threadIdx.x) * V;
     if (i >= dim) continue;
-    if constexpr (V == 8) {
-      Eight<T> w;
+    Some<T, V> w;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w.x[e] = from_f<T>(y[c * 8 + e]);
-      *reinterpret_cast<Eight<T>*>(row + i) = w;
-    } else {
-      row[i] = from_f<T>(y[c]);
-    }
+    for (int e = 0; e < V; ++e) w.x[e] = from_f<T>(y[c * V + e]);
+    *reinterpret_cast<Some<T, V>*>(row + i) = w;
   }
 }
 
 template <int V, class T>
 __device__ __forceinline__ void load_some(const T* p, float (&y)[V]) {
-  if constexpr (V == 8) {
-    const Eight<T> w = *reinterpret_cast<const Eight<T>*>(p);
+  const Some<T, V> w = *reinterpret_cast<const Some<T, V>*>(p);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) y[e] = to_f(w.x[e]);
-  } else {
-    y[0] = to_f(*p);
-  }
+  for (int e = 0; e < V; ++e) y[e] = to_f(w.x[e]);
 }
 // An element from shared memory.
 template <class T>
@@ -97,14 +91,10 @@ __device__ __forceinline__ float load_shared(uint32_t at) {
 }
 template <int V, class T>
 __device__ __forceinline__ void store_some(T* p, const float (&y)[V]) {
-  if constexpr (V == 8) {
-    Eight<T> w;
+  Some<T, V> w;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) w.x[e] = from_f<T>(y[e]);
-    *reinterpret_cast<Eight<T>*>(p) = w;
-  } else {
-    *p = from_f<T>(y[0]);
-  }
+  for (int e = 0; e < V; ++e) w.x[e] = from_f<T>(y[e]);
+  *reinterpret_cast<Some<T, V>*>(p) = w;
 }
 
 // N sums over the CTA, the same in every thread; `red` is free again after the caller's next barrier.
@@ -124,12 +114,13 @@ __device__ __forceinline__ void cta_sums(float (&v)[N], float* red) {
 }
 
 template <class T, class H, int V, int E>
-__global__ void __launch_bounds__(E == 8 ? 256 : 512) block_norm_kernel(const BlockNormArgs a) {
+__global__ void __launch_bounds__(E == 8 && V < 8 ? 1024 : 512) block_norm_kernel(const BlockNormArgs a) {
   __shared__ float red[2][32];
   pdl_launch_dependents();
   pdl_wait();
-  const int64_t r = blockIdx.x;
+  const int64_t r = E == 8 ? static_cast<int64_t>(blockIdx.x) * blockDim.y + threadIdx.y : blockIdx.x;  // (rows of one warp: several a CTA)
   const int dim = a.dim;
+  if (r >= a.rows) return;
   float h[E], u[E], w[E];
   load_row<V, E>(static_cast<const H*>(a.h) + r * a.ldh, dim, h);
   float r_y = 0.f;
@@ -185,7 +176,7 @@ __host__ __device__ inline Stage stage_of(int dim, int act, int stream, bool d_h
 }
 
 template <class T, class H, int V, int E, bool STAGED>
-__global__ void __launch_bounds__(E == 8 ? 256 : 512, E == 8 ? 2 : 1) block_norm_grad_kernel(const BlockNormGradArgs a) {
+__global__ void __launch_bounds__(E == 8 && V == 8 ? 256 : 512, E == 8 && V == 8 ? 2 : 1) block_norm_grad_kernel(const BlockNormGradArgs a) {
   __shared__ float red[2][3 * 32];
   __shared__ uint64_t full[2];
   extern __shared__ uint8_t rows_raw[];
@@ -480,27 +471,40 @@ __global__ void __launch_bounds__(1024) column_sums_kernel(const ColumnSums a) {
   if (lane == 0 && j < a.dim) a.out[k][j] = s;
 }
 
-// 16-byte accesses to every row?
-bool wide(const void* p, int64_t ld) {
-  return !p || (!(reinterpret_cast<uintptr_t>(p) & 15) && (ld & 7) == 0);
-}
+// What accesses every row allows: 8 elements (16 bytes), 2 (one access of their 4 or 8 bytes), or 1.
+struct Reach {
+  int v;
+  explicit Reach(int dim) : v(dim % 8 == 0 ? 8 : dim % 2 == 0 ? 2 : 1) {}
+  void rows(const void* p, int64_t ld, int dtype) {
+    const int size = dtype == VLA_F32 ? 4 : 2;
+    if (!p) return;
+    if (v == 8 && ((reinterpret_cast<uintptr_t>(p) & 15) || (ld & 7))) v = 2;
+    if (v == 2 && ((reinterpret_cast<uintptr_t>(p) & static_cast<uintptr_t>(2 * size - 1)) || (ld & 1))) v = 1;
+  }
+};
 
-// Elements of a thread: 8 up to 2048 channels, 16 up to 8192 (three sums, four inputs: 108 registers), else 32; threads for one row.
-int per_thread(int dim) { return dim <= 2048 ? 8 : dim <= 8192 ? 16 : 32; }
-unsigned threads_for(int dim) { return static_cast<unsigned>(std::max(32, (dim + per_thread(dim) * 32 - 1) / (per_thread(dim) * 32) * 32)); }
+// Elements of a thread and threads of a row.  With 16-byte accesses 8 elements up to 2048 channels, 16 up to 8192 (62 registers, 120 in the gradient
+// with its three sums), else 32.  With smaller ones latency counts: 8 as long as the threads of a row fit a CTA (`most`), 4100 channels in rows of
+// 8 bytes 225 us with 16.
+struct Split {
+  int e;
+  unsigned threads;
+};
+Split split_of(int dim, int v, int most) {
+  const int e = dim <= (v == 8 ? 2048 : most * 8) ? 8 : dim <= 8192 ? 16 : 32;
+  return {e, static_cast<unsigned>((dim + e * 32 - 1) / (e * 32) * 32)};
+}
 
 // f(act type, stream type, vector, elements)
 template <class F>
-int dispatch(int dtype, int h_dtype, bool vec, int dim, const F& f) {
+int dispatch(int dtype, int h_dtype, int vec, int e, const F& f) {
+  auto elements = [&](auto t, auto h, auto v) {
+    if (e == 8) return f(t, h, v, std::integral_constant<int, 8>());
+    return e == 16 ? f(t, h, v, std::integral_constant<int, 16>()) : f(t, h, v, std::integral_constant<int, 32>());
+  };
   auto shape = [&](auto t, auto h) {
-    if (per_thread(dim) == 8)
-      return vec ? f(t, h, std::integral_constant<int, 8>(), std::integral_constant<int, 8>())
-                 : f(t, h, std::integral_constant<int, 1>(), std::integral_constant<int, 8>());
-    if (per_thread(dim) == 16)
-      return vec ? f(t, h, std::integral_constant<int, 8>(), std::integral_constant<int, 16>())
-                 : f(t, h, std::integral_constant<int, 1>(), std::integral_constant<int, 16>());
-    return vec ? f(t, h, std::integral_constant<int, 8>(), std::integral_constant<int, 32>())
-               : f(t, h, std::integral_constant<int, 1>(), std::integral_constant<int, 32>());
+    if (vec == 8) return elements(t, h, std::integral_constant<int, 8>());
+    return vec == 2 ? elements(t, h, std::integral_constant<int, 2>()) : elements(t, h, std::integral_constant<int, 1>());
   };
   if (dtype == VLA_F32) return shape(float(), float());
   if (dtype == VLA_F16) return h_dtype == VLA_F32 ? shape(f16(), float()) : shape(f16(), f16());
@@ -510,11 +514,19 @@ int dispatch(int dtype, int h_dtype, bool vec, int dim, const F& f) {
 }  // namespace
 
 int block_norm_launch(const BlockNormArgs& a, cudaStream_t s) {
-  const bool vec = a.dim % 8 == 0 && wide(a.y, a.ldy) && wide(a.h, a.ldh) && wide(a.gate, a.ldg) && wide(a.post_gain, 0) &&
-                   wide(a.pre_gain, 0) && wide(a.h_out, a.ldho) && wide(a.x, a.ldx);
-  return dispatch(a.dtype, a.h_dtype, vec, a.dim, [&](auto t, auto h, auto v, auto e) -> int {
-    VLA_CUDA_TRY(launch_pdl(block_norm_kernel<decltype(t), decltype(h), v(), e()>, dim3(static_cast<unsigned>(a.rows)),
-                           dim3(threads_for(a.dim)), 0, s, a));
+  Reach reach(a.dim);
+  reach.rows(a.y, a.ldy, a.dtype);
+  reach.rows(a.h, a.ldh, a.h_dtype);
+  reach.rows(a.gate, a.ldg, a.dtype);
+  reach.rows(a.post_gain, 0, VLA_BF16);
+  reach.rows(a.pre_gain, 0, VLA_BF16);
+  reach.rows(a.h_out, a.ldho, a.h_dtype);
+  reach.rows(a.x, a.ldx, a.dtype);
+  const Split split = split_of(a.dim, reach.v, 1024);
+  const unsigned rows = split.threads == 32 ? 8 : 1;  // of a CTA
+  return dispatch(a.dtype, a.h_dtype, reach.v, split.e, [&](auto t, auto h, auto v, auto e) -> int {
+    VLA_CUDA_TRY(launch_pdl(block_norm_kernel<decltype(t), decltype(h), v(), e()>, dim3((static_cast<unsigned>(a.rows) + rows - 1) / rows),
+                            dim3(split.threads, rows), 0, s, a));
     note_launch();
     return VLA_OK;
   });
@@ -526,19 +538,28 @@ int block_norm_grad_launch(const BlockNormGradArgs& a, cudaStream_t s) {
   const BlockNormArgs& f = a.f;
   const int parts = parts_of(f.rows, f.dim);
   if (parts > 0) {
-    const bool vec = f.dim % 8 == 0 && wide(f.y, f.ldy) && wide(f.h, f.ldh) && wide(f.gate, f.ldg) &&
-                     wide(f.post_gain, 0) && wide(f.pre_gain, 0) && wide(a.d_x, a.lddx) && wide(a.d_h_out, a.lddho) &&
-                     wide(a.d_h, a.lddh) && wide(a.d_y, a.lddy) && (!f.ldg || wide(a.d_gate, a.lddg));
-    const int rc = dispatch(f.dtype, f.h_dtype, vec, f.dim, [&](auto t, auto h, auto v, auto e) -> int {
+    Reach reach(f.dim);
+    reach.rows(f.y, f.ldy, f.dtype);
+    reach.rows(f.h, f.ldh, f.h_dtype);
+    reach.rows(f.gate, f.ldg, f.dtype);
+    reach.rows(f.post_gain, 0, VLA_BF16);
+    reach.rows(f.pre_gain, 0, VLA_BF16);
+    reach.rows(a.d_x, a.lddx, f.dtype);
+    reach.rows(a.d_h_out, a.lddho, f.h_dtype);
+    reach.rows(a.d_h, a.lddh, f.h_dtype);
+    reach.rows(a.d_y, a.lddy, f.dtype);
+    if (f.ldg) reach.rows(a.d_gate, a.lddg, f.dtype);
+    const Split split = split_of(f.dim, reach.v, 512);
+    const int rc = dispatch(f.dtype, f.h_dtype, reach.v, split.e, [&](auto t, auto h, auto v, auto e) -> int {
       const uint32_t staged = 2 * stage_of(f.dim, sizeof(t), sizeof(h), a.d_h_out, f.y, f.gate && f.ldg).bytes + 16;
       if (staged <= staged_limit(f.dim)) {
         const auto kern = block_norm_grad_kernel<decltype(t), decltype(h), v(), e(), true>;
         static std::atomic<uint64_t> done{0};
         VLA_CUDA_TRY(set_smem_limit(kern, 200 * 1024, done));
-        VLA_CUDA_TRY(launch_pdl(kern, dim3(static_cast<unsigned>(parts)), dim3(threads_for(f.dim)), staged, s, a));
+        VLA_CUDA_TRY(launch_pdl(kern, dim3(static_cast<unsigned>(parts)), dim3(split.threads), staged, s, a));
       } else {
         VLA_CUDA_TRY(launch_pdl(block_norm_grad_kernel<decltype(t), decltype(h), v(), e(), false>, dim3(static_cast<unsigned>(parts)),
-                               dim3(threads_for(f.dim)), 0, s, a));
+                               dim3(split.threads), 0, s, a));
       }
       note_launch();
       return VLA_OK;

@@ -1,4 +1,4 @@
-// Internal interface of the learning pass's kernels (prompt_attn*.cu, block_norm.cu); the C entry points that check
+// Internal interface of the learning pass's kernels (prompt_attn.cu, prompt_grad.cu, block_norm.cu); the C entry points that check
 // their arguments are in learn_api.cu.
 #pragma once
 #include "../../include/vla_learn.h"

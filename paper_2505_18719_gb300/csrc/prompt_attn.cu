@@ -10,22 +10,28 @@
 // Both go over the same keys, so a block of keys in shared memory serves 256 queries.  Items go sequence by sequence, the longest rows
 // of a sequence first (its keys are read from HBM once, and the last items are short); persistent CTAs, one an SM.
 //
-// Blocks are 80 keys: so O, S and P of both tiles have tensor memory of their own (a tile's 256 columns: O [0, HD), S behind it, P
-// behind that), and the next scores are under way as soon as the threads have read these.  With blocks
-// of 128 keys for heads of 128 P has to lie over S, the chain scores - weights - product - next scores has no
-// slack, and 16384 rows took 1.63 ms.  Products of 80 keys are bound by shared memory (4 KB of Q and 2.5 KB of K a step, 51 cycles
-// where 128 keys take 65).
+// Where sequences are short (kShort rows on average), an item is one tile and each half of the CTA takes items of its own, with a ring of its own: a chain of 3 to 5
+// blocks, loads and output does not fill an SM, two do (64 prefixes of about 290 rows, 32 heads: 173 us in pairs, 151 so).
 //
-// Roles (384 threads):
+// Blocks are 80 keys (64 there): so O, S and P of both tiles have tensor memory of their own (a tile's 256 columns: O [0, HD), S behind it, P
+// behind that), and the next scores are under way as soon as the threads have read these.  With blocks of 128 keys for heads of 128 P
+// has to lie over S, the chain scores - weights - product - next scores has no slack, and 16384 rows took 1.63 ms.  Products of 80 keys are
+// bound by shared memory (4 KB of Q and 2.5 KB of K a step, 51 cycles where 128 keys take 65).
+//
+// Warps of 12 (16 in halves; there each half has the first, its own S and its own product warp):
 //   warp 0       finds the items (a scan over the sequences' lengths, 32 sequences a step), hands their descriptors round and loads their tiles by
-//                TMA: Q when the item before is done with it, key and value blocks into a ring;
+//                TMA: Q when the item before is done with it, key and value blocks into a ring; at the end the rows of no sequence;
 //   warps 1, 2   issue S = Q K^T of a tile each;
-//   warp 3       issues O += P V of both (V as the MN-major operand).  One warp for all products cannot keep up, at 250 to 800 cycles from
-//                one group of products to the next beside the softmax;
-//   warps 4 - 11 one query row a thread: softmax, and the output.  (Two threads a row: the
-//                exchange of their maxima costs what the shorter rows save.)
+//   warp 3       issues O += P V of both (V as the MN-major operand), after making values behind a sequence's last row zeros (their weights are
+//                zeros, but a NaN would spoil the product).  One warp for all products cannot keep up, at 250 to 800 cycles from one group of
+//                products to the next beside the softmax;
+//   the last 8   one query row a thread: softmax, and the output.  (Two threads a row: the exchange of their maxima costs what the shorter rows
+//                save.)
 // A row whose result is not finite is computed again from its own keys alone (attend_row): a NaN behind a row in its
 // block of keys does not count for it.
+//
+// Measured (32 query heads of 128): one sequence of 16384 rows, 8 key-value heads 1.31 to 1.42 ms (1.55 to 1.68 PFLOP/s; the tensor pipe 64 % busy at 8192 rows by its
+// counter); 16 sequences of 1 to 2048 rows 197 us (0.96 PFLOP/s); 64 prefixes of 272 to 304 rows 136 us (4.4 TB/s).
 #include <algorithm>
 #include <type_traits>
 

@@ -7,19 +7,24 @@
 // (seven products where one pass would need five), for which every sum has one owner and one order: no atomics, no 32-bit copy
 // of d_q in memory, nothing zeroed before.
 //
-// d_k, d_v: S^T = K Q^T and dP^T = V dO^T have keys as rows, so that P^T and dS^T, written over them, are the
-// left operands of d_v += P^T dO and d_k += dS^T Q in tensor memory; Q and dO tiles serve as K-major and as MN-major operands.  While
-// the threads compute P of a block the tensor cores work at d_k of the one before and at dP; during dS at d_v and
-// the next scores.  Tensor memory: S / P [0, 128), dP / dS [128, 256), d_v [256, 256 + HD), d_k [384, 384 + HD).
-// d_q: S [0, 128), dP and dS over it in two buffers [128, 256) [256, 384), d_q [384, 384 + HD).
+// d_k, d_v, blocks of 80 queries: S^T = K Q^T and dP^T = V dO^T have keys as rows, so that P^T and dS^T are the left operands of
+// d_v += P^T dO and d_k += dS^T Q in tensor memory; Q and dO tiles serve as K-major and as MN-major operands.  S, dP, P and dS have tensor
+// memory of their own (496 of 512 columns with the sums), so each product runs as soon as the threads have read or written.  d_q, blocks
+// of 96 keys: S, two blocks of dP, dS over the dP that it came from.
 //
 // Weights of bf16 are rounded as they are.  fp16 has 5 bits of exponent: P counts 2^14-fold, and dS 2^e-fold with the e that brings
 // 2 max |d_out[i]| max |v[j]| of the sequence, which no |dS| passes, below 2^15; so gradients of any size keep their bits.
-// Rows of Q, dO and K behind a sequence's last one become zeros in shared memory (their weights are zeros, but
+// Rows of the streamed operands behind a sequence's last one become zeros in shared memory (their weights are zeros, but
 // a NaN would spoil the sums over rows), up to the next multiple of 16, where the products stop.
 //
-// Roles of both (384 threads): warp 0 TMA, warp 1 MMAs (and tensor memory), warp 2 tiles that end behind a sequence's last row, and the rows' lse and D, warp 3
-// items, warps 4-11 the element-wise part, two warps a lane quarter with half of the columns each, and the output.
+// Warps of both (16): 0 items and TMA; 1 scores; 2 dP; 3 d_v; 4 d_k or d_q; 5, 6 queries' lse and D (d_k and d_v); 7 rows behind the last;
+// 8 - 15 the element-wise part, two warps a lane quarter with half of the columns each, and the output.  (Two groups of such warps, which take
+// the blocks in turn, were slower: 8192 rows 1.9 ms where one takes 1.3.)
+//
+// Bound by shared memory (scores and dP read both operands from it at 128 bytes a cycle) and, for d_k and d_v, by the element-wise chain: a block of
+// 80 queries takes 2240 cycles, its products 1550.  Measured (32 query heads of 128): 8192 rows, 8 key-value heads 1.28 to 1.36 ms (1.0 to 1.07
+// PFLOP/s of the ten needed flops a pair and channel; tensor pipe 48 and 59 % busy at 4096 rows); 64 samples of 272 to 304 rows 467 us (2.6 TB/s
+// of the bytes that have to move).
 #include <algorithm>
 
 #include "gemm.h"

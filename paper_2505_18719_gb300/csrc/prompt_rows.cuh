@@ -1,5 +1,5 @@
-// What one warp does for one row of packed causal attention, in 32 bits and without matrix instructions: the sums of
-// include/vla_learn.h as they stand, over the rows that take part and no others.
+// Sequences by their starts, and what one warp does for one row of packed causal attention, in 32 bits and without matrix instructions: the
+// sums of include/vla_learn.h as they stand, over the rows that take part and no others.
 #pragma once
 #include "learn.h"
 
@@ -14,20 +14,6 @@ struct Span {
 __device__ __forceinline__ Span span_of(const int* seq_start, int s, int rows) {
   const int b = min(max(seq_start[s], 0), rows);
   return Span{b, min(max(seq_start[s + 1], b), rows)};
-}
-// The sequence of a row; {row, row} where it belongs to none.
-__device__ __forceinline__ Span span_of_row(const int* seq_start, int n_seq, int rows, int row) {
-  int lo = 0, hi = n_seq;  // the last start at or before the row
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) >> 1;
-    if (seq_start[mid] <= row)
-      lo = mid;
-    else
-      hi = mid - 1;
-  }
-  if (lo == n_seq) return Span{row, row};
-  const Span sp = span_of(seq_start, lo, rows);
-  return sp.begin <= row && row < sp.end ? sp : Span{row, row};
 }
 __device__ __forceinline__ void check_starts(const int* seq_start, int n_seq, int rows, int first, int step, uint32_t* status) {
   bool bad = false;
@@ -117,82 +103,6 @@ __device__ __noinline__ void attend_row(const PromptArgs& a, int row, int h, int
   }
   store_lane<HD, FP16>(elem(a.out, row * a.ldo + h * HD), o, l > 0.f || l != l ? 1.f / l : 0.f);
   if (a.lse && (threadIdx.x & 31) == 0) a.lse[static_cast<int64_t>(row) * a.n_q_heads + h] = (m + log2f(l)) * kLn2;
-}
-
-// D = d_out . out of one row and head.
-template <int HD, bool FP16>
-__device__ __forceinline__ float row_delta(const PromptGradArgs& a, int row, int h) {
-  return warp_sum(lane_dot<HD>(load_lane<HD, FP16>(elem(a.d_out, row * a.lddo + h * HD)),
-                               load_lane<HD, FP16>(elem(a.f.out, row * a.f.ldo + h * HD))));
-}
-
-// d_q[row][h].
-template <int HD, bool FP16>
-__device__ __noinline__ void grad_query_row(const PromptGradArgs& a, int row, int h, int first, float delta) {
-  constexpr int U = 4;
-  const int g = h / (a.f.n_q_heads / a.f.n_kv_heads);
-  const float c = a.f.scale * kLog2e, lse = a.f.lse[static_cast<int64_t>(row) * a.f.n_q_heads + h] * kLog2e;
-  const Lane<HD> q = load_lane<HD, FP16>(elem(a.f.q, row * a.f.ldq + h * HD));
-  const Lane<HD> d = load_lane<HD, FP16>(elem(a.d_out, row * a.lddo + h * HD));
-  Lane<HD> y = {};
-  for (int j0 = first; j0 <= row; j0 += U) {
-    Lane<HD> k[U];
-    float s[U], t[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int j = min(j0 + u, row);
-      k[u] = load_lane<HD, FP16>(elem(a.f.k, j * a.f.ldk + g * HD));
-      s[u] = lane_dot<HD>(q, k[u]);
-      t[u] = lane_dot<HD>(d, load_lane<HD, FP16>(elem(a.f.v, j * a.f.ldv + g * HD)));
-    }
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      s[u] = warp_sum(s[u]);
-      t[u] = warp_sum(t[u]);
-      const float p = exp2f(fmaf(s[u], c, -lse));
-      if (j0 + u <= row && p != 0.f) lane_add<HD>(y, p * (t[u] - delta), k[u]);
-    }
-  }
-  store_lane<HD, FP16>(elem(a.d_q, row * a.lddq + h * HD), y, a.f.scale);
-}
-
-// d_k[row][g] and d_v[row][g]; delta [n_q_heads][rows].
-template <int HD, bool FP16>
-__device__ __noinline__ void grad_key_row(const PromptGradArgs& a, int row, int g, int end, const float* delta) {
-  constexpr int U = 4;
-  const int group = a.f.n_q_heads / a.f.n_kv_heads;
-  const float c = a.f.scale * kLog2e;
-  const Lane<HD> k = load_lane<HD, FP16>(elem(a.f.k, row * a.f.ldk + g * HD));
-  const Lane<HD> v = load_lane<HD, FP16>(elem(a.f.v, row * a.f.ldv + g * HD));
-  Lane<HD> dk = {}, dv = {};
-  for (int h = g * group; h < (g + 1) * group; ++h) {
-    for (int i0 = row; i0 < end; i0 += U) {
-      Lane<HD> q[U], d[U];
-      float s[U], t[U], lse[U], dl[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = min(i0 + u, end - 1);
-        q[u] = load_lane<HD, FP16>(elem(a.f.q, i * a.f.ldq + h * HD));
-        d[u] = load_lane<HD, FP16>(elem(a.d_out, i * a.lddo + h * HD));
-        lse[u] = a.f.lse[static_cast<int64_t>(i) * a.f.n_q_heads + h];
-        dl[u] = delta[static_cast<int64_t>(h) * a.f.rows + i];
-        s[u] = lane_dot<HD>(q[u], k);
-        t[u] = lane_dot<HD>(d[u], v);
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        s[u] = warp_sum(s[u]);
-        t[u] = warp_sum(t[u]);
-        const float p = exp2f(fmaf(s[u], c, -lse[u] * kLog2e));
-        if (i0 + u < end && p != 0.f) {
-          lane_add<HD>(dv, p, d[u]);
-          lane_add<HD>(dk, p * (t[u] - dl[u]), q[u]);
-        }
-      }
-    }
-  }
-  store_lane<HD, FP16>(elem(a.d_k, row * a.lddk + g * HD), dk, a.f.scale);
-  store_lane<HD, FP16>(elem(a.d_v, row * a.lddv + g * HD), dv, 1.f);
 }
 
 }  // namespace vla

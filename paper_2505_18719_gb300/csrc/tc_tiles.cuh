@@ -57,7 +57,6 @@ __device__ __forceinline__ bool elected() {
   return p != 0;
 }
 __device__ __forceinline__ int uniform(int v) { return __reduce_max_sync(0xffffffffu, v); }
-__device__ __forceinline__ bool warp_ready(uint32_t bar, uint32_t parity) { return __any_sync(0xffffffffu, mbar_test_wait(bar, parity)); }
 // All of an SM's tensor memory, by one warp; `slot` (shared memory) gets its address.
 constexpr uint32_t kTmemAll = 512;
 __device__ __forceinline__ void tmem_take(uint32_t slot) {
@@ -135,22 +134,8 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return FP16 ? pack_f16x2(a, b) : pack_bf16x2(a, b);
 }
 
-// wait_bounded for waits that are as a rule short: the clock, which takes longer to read than the wait would last, comes in after 1024 tries.
-__device__ __forceinline__ bool quick_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* status, uint64_t limit) {
-  uint64_t t0 = 0;
-  for (uint32_t n = 1; !mbar_try_wait(bar, parity); ++n) {
-    if (n & 1023u) continue;
-    if (*abort_flag) return false;
-    if (n == 1024) t0 = globaltimer();
-    if (globaltimer() - t0 > limit) {
-      *abort_flag = 1;
-      if (status) atomicOr(status, VLA_STATUS_TIMEOUT);
-      return false;
-    }
-  }
-  return true;
-}
-// By a whole warp: all lanes ask at once.  (Asked by one lane with the others waiting for it, the answer comes 600 cycles later.)
+// Bounded wait of a whole warp: all lanes ask at once.  (Asked by one lane with the others waiting for it, the answer comes 600 cycles later.)  The
+// clock, which takes longer to read than the wait lasts as a rule, comes in after 1024 tries.
 __device__ __forceinline__ bool warp_waits(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* status, uint64_t limit) {
   uint64_t t0 = 0;
   for (uint32_t n = 1; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity)); ++n) {
