@@ -58,6 +58,7 @@ __global__ void __launch_bounds__(256) prompt_delta_kernel(const PromptGradArgs 
   __shared__ float red[2][8];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   float most[2] = {0.f, 0.f};
+  pdl_wait();  // (no kernel starts beside this one: it lets none start before its end)
   if (blockIdx.x == 0) check_starts(a.f.seq_start, a.f.n_seq, a.f.rows, threadIdx.x, 256, a.f.status);
   auto eight = [](uint4 w, float (&y)[8]) {
     const uint32_t u[4] = {w.x, w.y, w.z, w.w};
@@ -245,9 +246,12 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  // The kernel of d_q may start beside that of d_k and d_v, which started behind that of D, and takes the SMs that it leaves; it waits for
-  // it at its end, so that its end is that of both.
-  if (KEYS) pdl_launch_dependents();
+  // The kernel of d_q may start beside that of d_k and d_v, once this one knows that of D at its end, and takes the SMs that it leaves; it
+  // waits for it at its end, so that its end is that of both.
+  if (KEYS) {
+    pdl_wait();
+    pdl_launch_dependents();
+  }
   if constexpr (kExtra<FP16, KEYS>) {
     if (warp >= kSumWarp0 && warp < kSumWarp0 + 4) {  // three ones, thirteen zeros in every row
       const uint32_t ones[8] = {0x3f803f80u, 0x00003f80u, 0u, 0u, 0u, 0u, 0u, 0u};
@@ -717,8 +721,8 @@ int launch_part(Params p, int sms, cudaStream_t s) {
   const auto kern = prompt_grad_kernel<HD, FP16, KEYS>;
   static std::atomic<uint64_t> done{0};
   VLA_CUDA_TRY(set_smem_limit(kern, Sh::kTotal, done));
-  // (d_k and d_v early, beside the kernel of D, made 64 samples 130 us slower)
-  VLA_CUDA_TRY(launch_at(KEYS ? Start::kInOrder : Start::kEarly, kern, dim3(static_cast<unsigned>(std::min(p.items_bound, sms))), dim3(kThreads), Sh::kTotal, s,
+  // (d_k and d_v beside the kernel of D, which would have to let them start, made 64 samples 130 us slower)
+  VLA_CUDA_TRY(launch_at(Start::kEarly, kern, dim3(static_cast<unsigned>(std::min(p.items_bound, sms))), dim3(kThreads), Sh::kTotal, s,
                          KEYS ? k : q, KEYS ? v : g, KEYS ? q : k, KEYS ? g : v, p));
   note_launch();
   return VLA_OK;
@@ -739,7 +743,7 @@ int launch(const PromptGradArgs& a, cudaStream_t s) {
   p.wait_limit = g_wait_limit_ns.load(std::memory_order_relaxed);
   int sms = 0;
   if (const int rc = device_sms(&sms)) return rc;
-  VLA_CUDA_TRY(launch_at(Start::kInOrder, prompt_delta_kernel<HD, FP16>, dim3(static_cast<unsigned>(p.norm_blocks)), dim3(256), 0, s, a, delta,
+  VLA_CUDA_TRY(launch_at(Start::kEarly, prompt_delta_kernel<HD, FP16>, dim3(static_cast<unsigned>(p.norm_blocks)), dim3(256), 0, s, a, delta,
                          norms, p.norm_blocks));
   note_launch();
   if (const int rc = launch_part<HD, FP16, true>(p, sms, s)) return rc;
