@@ -31,6 +31,7 @@ extern "C" {
  *              buffer fit); head_dim 64 or 128;
  *   scale      1e-30 or more;
  *   lse        f32 [rows][n_q_heads] or NULL: log sum_j exp(scale q . k[j]); -infinity in rows of no sequence.
+ * A key whose score is -infinity has no weight; a row with no other keys gives zeros and -infinity.
  * Scores, their maxima and sums are 32-bit; the weights of the values are rounded to `dtype`, relative to their maximum.  A row depends
  * on nothing behind it and on no other sequence: NaN and infinities there stay there.  Equal calls give
  * equal bits.  out overlaps nothing that the call reads.  rows 0 or more; rows * n_q_heads at most 2^30. */

@@ -2,7 +2,7 @@
 //
 // With c = scale log2(e), for a query i over blocks of keys: s = q K^T, m = max s, weights 2^(c (s - m)), l their sum,
 // O = 2^(c (m' - m)) O + P V; out = O / l, lse = ln 2 (c m + log2 l).  The reference m moves only when a maximum passes it by more than
-// 2^8, so O is scaled again in few blocks.  Weights go to the values' type; fp16 ones are 2^7 times as large, so that one of
+// 2^8, so O is scaled again in few blocks; it is -infinity until a row has met a score above that.  Weights go to the values' type; fp16 ones are 2^7 times as large, so that one of
 // 2^-21 of the row's largest still keeps all its bits (at most 2^15 with the reference 2^8 behind).
 //
 // A tile is 128 rows of one sequence and query head.  The tiles of a sequence and key-value head are numbered row tile after row tile, query
@@ -376,9 +376,10 @@ __global__ void __launch_bounds__((Smem<HD, PAIRED>::kThreads), 1)
           for (int i = 16; i < KN; i += 2)  // (three-input maxima)
             top[(i >> 1) & 7] = fmaxf(top[(i >> 1) & 7], fmaxf(__uint_as_float(s[i]), __uint_as_float(s[i + 1])));
           const float mb = fmaxf(fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), fmaxf(fmaxf(top[4], top[5]), fmaxf(top[6], top[7])));
+          // (a row whose keys so far all score -infinity has no reference yet: the first finite score sets it; -inf + inf is no move)
           if ((mb - m) * c > 8.f || j == 0) {
             alpha = j == 0 ? 0.f : ex2((m - mb) * c);
-            m = mb == -INFINITY ? 0.f : mb;
+            m = mb;
             l *= alpha;
           }
         }
@@ -397,7 +398,7 @@ __global__ void __launch_bounds__((Smem<HD, PAIRED>::kThreads), 1)
               tmem_st16(tO + i, v);
             }
           }
-          const float shift = fmaf(-m, c, p.offset);
+          const float shift = m == -INFINITY ? p.offset : fmaf(-m, c, p.offset);
           const uint64_t shift2 = pair_of(shift, shift);
           uint64_t sum[4] = {0, 0, 0, 0};
           auto weights = [&](int i, auto count) {
