@@ -44,7 +44,8 @@ int vla_prompt_attn(const void* q, int64_t ldq, const void* k, int64_t ldk, cons
  * that share them, in 32 bits.  With P the softmax weights, D[i] = d_out[i] . out[i]:
  *   d_v[j] = sum_i P[i][j] d_out[i],   dS[i][j] = P[i][j] (d_out[i] . v[j] - D[i]),
  *   d_q[i] = scale sum_j dS[i][j] k[j],   d_k[j] = scale sum_i dS[i][j] q[i].
- * P and dS are rounded to `dtype` in these sums.  NaN and infinities stay in their sequence.  The gradients may overwrite nothing that the call reads.  Equal
+ * P and dS are rounded to `dtype` in these sums, in fp16 dS relative to the largest that it can be in the row of d_q or d_k (what lies 2^38
+ * below that may count as 0): rows, heads and sequences of very different sizes keep their own bits.  NaN and infinities stay in their sequence.  The gradients may overwrite nothing that the call reads.  Equal
  * calls give equal bits (no atomics).  `workspace` of vla_prompt_attn_grad_workspace_bytes, 16-byte aligned, any
  * content; not shared by calls that may overlap. */
 int vla_prompt_attn_grad(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int dtype, int rows,

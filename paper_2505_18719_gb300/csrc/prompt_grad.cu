@@ -12,8 +12,12 @@
 // memory of their own (496 of 512 columns with the sums), so each product runs as soon as the threads have read or written.  d_q, blocks
 // of 96 keys: S, two blocks of dP, dS over the dP that it came from.
 //
-// Weights of bf16 are rounded as they are.  fp16 has 5 bits of exponent: P counts 2^14-fold, and dS 2^e-fold with the e that brings
-// 2 max |d_out[i]| max |v[j]| of the sequence, which no |dS| passes, below 2^15; so gradients of any size keep their bits.
+// Weights of bf16 are rounded as they are.  fp16 has 5 bits of exponent: P counts 2^14-fold, and dS 2^e-fold with an e of its own for each row
+// of d_q and d_k, which brings what no |dS| of the row passes to 2^13 .. 2^14: |d_out[i]| max |v[j]| + |D[i]| over the keys that query i sees,
+// |v[j]| max |d_out[i]| + max |D[i]| over the queries (and heads) that see key j.  So a row's bits depend on its own sequence alone, and
+// neither on larger gradients beside it; what lies 2^38 below that largest is rounded away.  The kernel of D writes the norms of rows and their maxima
+// over 32 rows for it; a row's thread scales its sums back, so the factors cost nothing but their maxima (8192 rows of fp16
+// take 1.55 ms, with one factor for all of a sequence 1.54; 64 samples of 272 to 304 rows 602 and 594 us).
 // Rows of the streamed operands behind a sequence's last one become zeros in shared memory (their weights are zeros, but
 // a NaN would spoil the sums over rows), up to the next multiple of 16, where the products stop.
 //
@@ -38,26 +42,42 @@ constexpr int kThreads = 512, kSumWarp0 = 8, kSumWarps = 8;
 // producer aside: scores, dP, sums (two of keys), of keys two for the rows' lse and D, rows behind the last, element-wise warps
 template <bool KEYS>
 constexpr int kItemReaders = 2 + (KEYS ? 2 + 2 : 1) + 1 + kSumWarps;
-constexpr int kNormRows = 32;    // rows of one entry of the largest norms
+constexpr int kNormRows = 32;    // rows of one entry of the largest norms (lanes of a warp)
 constexpr float kPShift = 14.f;  // log2 of the fp16 weights' factor
+
+// What the factors of dS come from (fp16): |d_out| of each row and query head; of each key-value head and row the largest |d_out| and |D| of
+// the query heads that share it, and |v| (rows side by side: a warp reads those of 32); the largest of these of each block of kNormRows rows
+// that all belong to sequences.
+struct Norms {
+  float* d_out;       // [rows][n_q_heads]
+  float* of_rows;     // [3][n_kv_heads][rows]: d_out, D, v
+  float* of_blocks;   // [3][n_kv_heads][blocks]
+  int blocks;
+};
 
 struct Params {
   PromptGradArgs g;
   int group, items_bound;
-  float c;               // scale log2(e)
-  const float* delta;    // [rows][n_q_heads]
-  const float* norms;    // [2][blocks of kNormRows rows]: largest |d_out| and |v| (fp16)
-  int norm_blocks;
+  float c;       // scale log2(e)
+  float* delta;  // [rows][n_q_heads]
+  Norms norms;
   uint64_t wait_limit;
 };
 
 // ------------------------------------------------------------------------------------------- D
+__device__ __forceinline__ float2 larger(float2 a, float2 b) { return make_float2(fmaxf(a.x, b.x), fmaxf(a.y, b.y)); }
+// Norms of head g and kind k: of all rows, of all blocks.
+__device__ __forceinline__ float* row_norms(const Params& p, int k, int g) {
+  return p.norms.of_rows + (static_cast<int64_t>(k) * p.g.f.n_kv_heads + g) * p.g.f.rows;
+}
+__device__ __forceinline__ float* block_norms(const Params& p, int k, int g) {
+  return p.norms.of_blocks + (static_cast<int64_t>(k) * p.g.f.n_kv_heads + g) * p.norms.blocks;
+}
 template <int HD, bool FP16>
-__global__ void __launch_bounds__(256) prompt_delta_kernel(const PromptGradArgs a, float* delta, float* norms, int norm_blocks) {
+__global__ void __launch_bounds__(256) prompt_delta_kernel(const Params p) {
   constexpr int L = HD / 8, HEADS = 32 / L;  // lanes of a head, heads of a step
-  __shared__ float red[2][8];
+  const PromptGradArgs& a = p.g;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  float most[2] = {0.f, 0.f};
   pdl_wait();  // (no kernel starts beside this one: it lets none start before its end)
   if (blockIdx.x == 0) check_starts(a.f.seq_start, a.f.n_seq, a.f.rows, threadIdx.x, 256, a.f.status);
   auto eight = [](uint4 w, float (&y)[8]) {
@@ -74,8 +94,6 @@ __global__ void __launch_bounds__(256) prompt_delta_kernel(const PromptGradArgs 
     for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
   };
-  // a sequence of finite numbers keeps its factor, whatever lies around it
-  auto finite = [](float v) { return v <= 3e38f ? v : 0.f; };
   const Outside out(a.f.seq_start, a.f.n_seq, a.f.rows);
   for (int i = warp; i < kNormRows; i += 8) {
     const int row = blockIdx.x * kNormRows + i;
@@ -83,60 +101,134 @@ __global__ void __launch_bounds__(256) prompt_delta_kernel(const PromptGradArgs 
     if (row < out.first) continue;
     const uint4* o = static_cast<const uint4*>(elem(a.f.out, row * a.f.ldo));
     const uint4* d = static_cast<const uint4*>(elem(a.d_out, row * a.lddo));
-#pragma unroll 4
-    for (int h = 0; h < a.f.n_q_heads; h += HEADS) {
-      const bool on = h + lane / L < a.f.n_q_heads;
-      float x[8], y[8], s = 0.f, n = 0.f;
-      eight(on ? o[h * L + lane] : make_uint4(0u, 0u, 0u, 0u), x);
-      eight(on ? d[h * L + lane] : make_uint4(0u, 0u, 0u, 0u), y);
+    // four steps' loads before the first store (which they may not pass)
+    for (int h0 = lane / L; h0 - lane / L < a.f.n_q_heads; h0 += 4 * HEADS) {
+      uint4 ow[4], dw[4];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) s = fmaf(x[e], y[e], s);
-      s = over_head(s);
-      if (on && lane % L == 0) delta[static_cast<int64_t>(row) * a.f.n_q_heads + h + lane / L] = s;
-      if (FP16) {
+      for (int u = 0; u < 4; ++u) {
+        const bool on = h0 + u * HEADS < a.f.n_q_heads;
+        ow[u] = on ? o[(h0 + u * HEADS) * L + lane % L] : make_uint4(0u, 0u, 0u, 0u);
+        dw[u] = on ? d[(h0 + u * HEADS) * L + lane % L] : make_uint4(0u, 0u, 0u, 0u);
+      }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) n = fmaf(y[e], y[e], n);
-        most[0] = fmaxf(most[0], finite(over_head(n)));
+      for (int u = 0; u < 4; ++u) {
+        const int h = h0 + u * HEADS;
+        const bool stores = h < a.f.n_q_heads && lane % L == 0;
+        const int64_t at = static_cast<int64_t>(row) * a.f.n_q_heads + h;
+        float x[8], y[8], s = 0.f, n = 0.f;
+        eight(ow[u], x);
+        eight(dw[u], y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s = fmaf(x[e], y[e], s);
+        s = over_head(s);
+        if (stores) p.delta[at] = s;
+        if (FP16) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) n = fmaf(y[e], y[e], n);
+          n = over_head(n);
+          if (stores) p.norms.d_out[at] = sqrtf(n);
+        }
       }
     }
     if (FP16) {
       const uint4* v = static_cast<const uint4*>(elem(a.f.v, row * a.f.ldv));
-      for (int h = 0; h < a.f.n_kv_heads; h += HEADS) {
-        float y[8], n = 0.f;
-        eight(h + lane / L < a.f.n_kv_heads ? v[h * L + lane] : make_uint4(0u, 0u, 0u, 0u), y);
+      for (int h0 = lane / L; h0 - lane / L < a.f.n_kv_heads; h0 += 4 * HEADS) {
+        uint4 vw[4];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) n = fmaf(y[e], y[e], n);
-        most[1] = fmaxf(most[1], finite(over_head(n)));
+        for (int u = 0; u < 4; ++u) vw[u] = h0 + u * HEADS < a.f.n_kv_heads ? v[(h0 + u * HEADS) * L + lane % L] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+          const int h = h0 + u * HEADS;
+          float y[8], n = 0.f;
+          eight(vw[u], y);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) n = fmaf(y[e], y[e], n);
+          n = over_head(n);
+          if (h < a.f.n_kv_heads && lane % L == 0) row_norms(p, 2, h)[row] = sqrtf(n);
+        }
       }
     }
   }
   if constexpr (FP16) {
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      most[k] = warp_max(most[k]);
-      if (lane == 0) red[k][warp] = most[k];
-    }
     __syncthreads();
-    if (threadIdx.x >= 2) return;
-    float m = 0.f;
-    for (int w = 0; w < 8; ++w) m = fmaxf(m, red[threadIdx.x][w]);
-    norms[threadIdx.x * norm_blocks + blockIdx.x] = sqrtf(m);
+    const int row = static_cast<int>(blockIdx.x) * kNormRows + lane;
+    const bool on = row >= out.first && row < out.last;
+    const int64_t at = static_cast<int64_t>(row) * a.f.n_q_heads;
+    // (four heads a warp at once, for the loads' latency)
+    for (int g0 = warp; g0 < a.f.n_kv_heads; g0 += 32) {
+      float m[3][4] = {};
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int g = g0 + 8 * u;
+        if (!on || g >= a.f.n_kv_heads) continue;
+        m[2][u] = __ldcg(row_norms(p, 2, g) + row);
+        for (int h = g * p.group; h < (g + 1) * p.group; ++h) {
+          m[0][u] = fmaxf(m[0][u], __ldcg(p.norms.d_out + at + h));
+          m[1][u] = fmaxf(m[1][u], fabsf(__ldcg(p.delta + at + h)));
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int g = g0 + 8 * u;
+        if (g >= a.f.n_kv_heads) break;
+#pragma unroll
+        for (int k = 0; k < 3; ++k) {
+          if (on && k < 2) row_norms(p, k, g)[row] = m[k][u];
+          const float most = warp_max(m[k][u]);
+          if (lane == 0) block_norms(p, k, g)[blockIdx.x] = most;
+        }
+      }
+    }
   }
 }
 
 // ------------------------------------------------------------------------------------- both kernels
-// The exponent e of a sequence's factor 2^e of dS (fp16): 2 |d_out| |v| 2^e <= 2^15 (whole warp).
-__device__ __forceinline__ int ds_exponent(const Params& p, const Item& it) {
-  float n[2] = {0.f, 0.f};
-  const int b0 = it.begin / kNormRows, b1 = (it.begin + it.len - 1) / kNormRows;
-  for (int b = b0 + (threadIdx.x & 31); b <= b1; b += 32) {
-    n[0] = fmaxf(n[0], __ldcg(p.norms + b));
-    n[1] = fmaxf(n[1], __ldcg(p.norms + p.norm_blocks + b));
+// This lane's share of the largest norms over rows lo .. hi - 1: of single rows up to the first block, of whole blocks, of rows behind them.
+__device__ __forceinline__ float share_of_largest(const float* of_rows, const float* of_blocks, int lo, int hi) {
+  const int lane = threadIdx.x & 31, b0 = (lo + kNormRows - 1) / kNormRows, b1 = hi / kNormRows;
+  float m = 0.f;
+  if (lo + lane < min(hi, b0 * kNormRows)) m = __ldcg(of_rows + lo + lane);
+  if (b1 >= b0 && b1 * kNormRows + lane < hi) m = fmaxf(m, __ldcg(of_rows + b1 * kNormRows + lane));
+#pragma unroll 4
+  for (int b = b0 + lane; b < b1; b += 32) m = fmaxf(m, __ldcg(of_blocks + b));
+  return m;
+}
+// The exponent e of the factor 2^e of dS in row r of an item's tile (fp16; whole warp, 32 rows from a multiple of 32 on).  All loads first.
+template <bool KEYS>
+__device__ __forceinline__ int ds_exponent(const Params& p, const Item& it, int r) {
+  const PromptArgs& f = p.g.f;
+  const int lane = threadIdx.x & 31, first = it.a * kTile + (r & ~31), row = it.begin + min(it.a * kTile + r, it.len - 1);
+  float most;
+  if constexpr (KEYS) {
+    const int lo = it.begin + min(first + 32, it.len), hi = it.begin + it.len;
+    const float v = __ldcg(row_norms(p, 2, it.b) + row);
+    float2 m = make_float2(__ldcg(row_norms(p, 0, it.b) + row), __ldcg(row_norms(p, 1, it.b) + row));
+    float2 behind = make_float2(share_of_largest(row_norms(p, 0, it.b), block_norms(p, 0, it.b), lo, hi),
+                                share_of_largest(row_norms(p, 1, it.b), block_norms(p, 1, it.b), lo, hi));
+    behind = make_float2(warp_max(behind.x), warp_max(behind.y));
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const float2 y = make_float2(__shfl_down_sync(0xffffffffu, m.x, o), __shfl_down_sync(0xffffffffu, m.y, o));
+      if (lane + o < 32) m = larger(m, y);
+    }
+    m = larger(m, behind);
+    most = fmaf(v, m.x, m.y);
+  } else {
+    const int g = it.b / p.group;
+    const int64_t at = static_cast<int64_t>(row) * f.n_q_heads + it.b;
+    const float d_out = __ldcg(p.norms.d_out + at), delta = __ldcg(p.delta + at);
+    float v = __ldcg(row_norms(p, 2, g) + row);
+    const float before = warp_max(share_of_largest(row_norms(p, 2, g), block_norms(p, 2, g), it.begin, it.begin + min(first, it.len)));
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const float y = __shfl_up_sync(0xffffffffu, v, o);
+      if (lane >= o) v = fmaxf(v, y);
+    }
+    most = fmaf(d_out, fmaxf(v, before), fabsf(delta));
   }
-  const float most = warp_max(n[0]) * warp_max(n[1]);
   if (!(most > 0.f) || most > 1e37f) return 0;
   int e;
-  frexpf(most, &e);  // most <= 2^e
+  frexpf(most, &e);  // most < 2^e
   return min(max(14 - e, -100), 100);
 }
 __device__ __forceinline__ float exp2_int(int e) { return __int_as_float((e + 127) << 23); }
@@ -533,10 +625,12 @@ __global__ void __launch_bounds__(kThreads, 1)
     Item it;
     bool ok = true;
     for (int k = 0; ok && take(k, it); ++k) {
-      const int e = FP16 ? ds_exponent(p, it) : 0;
       const int row0 = it.a * kTile + q4 * 32;
-      // the factor of dS beside the weights' own; of a query row its lse (with the factor) and -D
-      const float up = FP16 ? exp2_int(e - static_cast<int>(kPShift)) : 1.f;
+      // (fp16) the exponent of this row's factor of dS; of a query row its lse (with the factor) and -D
+      const int e = FP16 ? ds_exponent<KEYS>(p, it, r) : 0;
+      // d_k's factor beside the weights' own waits in shared memory for its use: as registers it costs spills, 8192 rows 1.71 ms for 1.55
+      volatile float* const factor = row_data + 2 * 256 + (threadIdx.x - 32 * kSumWarp0);
+      if constexpr (KEYS && FP16) *factor = exp2_int(e - static_cast<int>(kPShift));
       uint64_t l2 = 0, d2 = 0;
       if constexpr (!KEYS) {
         const int64_t at = static_cast<int64_t>(it.begin + min(it.a * kTile + r, it.len - 1)) * f.n_q_heads + it.b;
@@ -604,6 +698,7 @@ __global__ void __launch_bounds__(kThreads, 1)
         constexpr int C = KEYS ? NH : 16;
         uint32_t x[C];
         auto gradients = [&](int j) {
+          const float up = KEYS && FP16 ? *factor : 1.f;
 #pragma unroll
           for (int i = 0; i < C; i += 4) {
             uint64_t a = pair_of(__uint_as_float(x[i]), __uint_as_float(x[i + 1]));
@@ -683,7 +778,7 @@ __global__ void __launch_bounds__(kThreads, 1)
           store_tile<FP16, HD / 32>(quarter + Sh::kColV, FP16 ? exp2_int(-static_cast<int>(kPShift)) : 1.f,
                                     elem(p.g.d_v, at * p.g.lddv + it.b * HD), p.g.lddv, it.len - row0);
         else
-          store_tile<FP16, HD / 32>(quarter + Sh::kColSum, FP16 ? f.scale * exp2_int(-e) : f.scale,
+          store_tile<FP16, HD / 32>(quarter + Sh::kColSum, FP16 ? f.scale * exp2_int(-static_cast<int>(kPShift)) / *factor : f.scale,
                                     elem(p.g.d_k, at * p.g.lddk + it.b * HD), p.g.lddk, it.len - row0);
       } else {
         store_tile<FP16, HD / 64>(quarter + Sh::kColSum + half * (HD / 2), FP16 ? f.scale * exp2_int(-e) : f.scale,
@@ -735,16 +830,14 @@ int launch(const PromptGradArgs& a, cudaStream_t s) {
   p.g = a;
   p.group = f.n_q_heads / f.n_kv_heads;
   p.c = f.scale * kLog2e;
-  float* delta = static_cast<float*>(a.workspace);
-  float* norms = delta + static_cast<int64_t>(f.rows) * f.n_q_heads;
-  p.delta = delta;
-  p.norms = norms;
-  p.norm_blocks = norm_blocks_of(f.rows);
+  const int blocks = norm_blocks_of(f.rows);
+  const int64_t q_rows = static_cast<int64_t>(f.rows) * f.n_q_heads, kv_rows = static_cast<int64_t>(f.rows) * f.n_kv_heads;
+  p.delta = static_cast<float*>(a.workspace);
+  p.norms = Norms{p.delta + q_rows, p.delta + 2 * q_rows, p.delta + 2 * q_rows + 3 * kv_rows, blocks};
   p.wait_limit = g_wait_limit_ns.load(std::memory_order_relaxed);
   int sms = 0;
   if (const int rc = device_sms(&sms)) return rc;
-  VLA_CUDA_TRY(launch_at(Start::kEarly, prompt_delta_kernel<HD, FP16>, dim3(static_cast<unsigned>(p.norm_blocks)), dim3(256), 0, s, a, delta,
-                         norms, p.norm_blocks));
+  VLA_CUDA_TRY(launch_at(Start::kEarly, prompt_delta_kernel<HD, FP16>, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, p));
   note_launch();
   if (const int rc = launch_part<HD, FP16, true>(p, sms, s)) return rc;
   return launch_part<HD, FP16, false>(p, sms, s);
@@ -752,8 +845,9 @@ int launch(const PromptGradArgs& a, cudaStream_t s) {
 
 }  // namespace
 
-size_t prompt_attn_grad_workspace(int rows, int n_q_heads, int, int) {
-  return (static_cast<size_t>(rows) * n_q_heads + 2 * static_cast<size_t>(norm_blocks_of(rows))) * sizeof(float);
+size_t prompt_attn_grad_workspace(int rows, int n_q_heads, int n_kv_heads, int) {
+  const size_t n = rows, blocks = norm_blocks_of(rows);
+  return (2 * n * n_q_heads + 3 * (n + blocks) * n_kv_heads) * sizeof(float);
 }
 
 int prompt_attn_grad_launch(const PromptGradArgs& a, cudaStream_t s) {
