@@ -77,7 +77,7 @@ def _dense(t: Optional[torch.Tensor], n: int, dim: int, what: str) -> int:
         return dim
     if t.shape != (n, dim) or (dim > 1 and t.stride(1) != 1):
         raise ValueError(f"{what}: [rows, channels] with dense rows expected, got {tuple(t.shape)} with strides {t.stride()}")
-    return t.stride(0) if n > 1 else dim  # (a stride below the channels, rows that overlap, is refused by the call)
+    return t.stride(0) if n > 1 else dim  # (rows that overlap, a stride below the channels, are refused by the call)
 
 
 class _BlockNorm(torch.autograd.Function):
@@ -95,6 +95,8 @@ class _BlockNorm(torch.autograd.Function):
         if gate is not None and gate.dim() == 1 and (gate.shape[0] != dim or not gate.is_contiguous()):
             raise ValueError("gate: [channels] or [rows, channels]")
         _on_gpu(y, h, pre_gain, post_gain, gate)
+        if gate is not None and gate.dim() == 2 and gate.shape == (n, dim) and gate.stride(0) < dim and (dim == 1 or gate.stride(1) == 1):
+            gate = gate.contiguous()  # (one row for all, as a view: its gradient is one of each row, and stride 0 means [channels] to the call)
         ldy, ldh = _dense(y, n, dim, "y"), _dense(h, n, dim, "h")
         ldg = 0 if gate is None or gate.dim() == 1 else _dense(gate, n, dim, "gate")
         act = dtype if y is None else y.dtype
@@ -135,7 +137,8 @@ class _BlockNorm(torch.autograd.Function):
 
 def block_norm(y, h, pre_gain, post_gain=None, gate=None, residual_scale: float = 1.0, eps: float = 1e-6):
     """Between two blocks: ``h_out = h + residual_scale * gate * norm(y)`` and ``x = norm(h_out)``, the norms with their gains (bf16
-    [channels]; without `post_gain` y is added as it is).  `gate`: [channels], [rows, channels] or None, of y's type.
+    [channels]; without `post_gain` y is added as it is).  `gate`: [channels], [rows, channels] (an expanded row among them) or None, of
+    y's type.
     Returns (x, h_out), both differentiable."""
     if y is None:
         raise ValueError("y: the block's output (first_norm takes the stream alone)")
