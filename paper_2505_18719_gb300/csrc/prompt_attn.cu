@@ -432,6 +432,7 @@ __global__ void __launch_bounds__((Smem<HD, PAIRED>::kThreads), 1)
       const int64_t row = it.begin + tile0 + q4 * 32;
       const bool bad = store_tile<FP16, HD / 32>(tO, 1.f / l, elem(p.a.out, row * p.a.ldo + head * HD), p.a.ldo, live);
       if (p.a.lse && lane < live) p.a.lse[(row + lane) * p.a.n_q_heads + head] = (log2f(l) - fmaf(-m, c, p.offset)) * kLn2;
+      __syncwarp();  // (attend_row's lanes write what other lanes have written here)
       uint32_t again = __ballot_sync(0xffffffffu, bad && lane < live);
       while (again) {
         const int rr = __ffs(static_cast<int>(again)) - 1;

@@ -1,0 +1,20 @@
+"""What the learning pass's kernels owe to the order of their instructions and no run shows for certain, checked on their source."""
+import os
+import re
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2505_18719_gb300", "csrc")
+
+
+def source(path):
+    return re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, path)).read())
+
+
+def between(text, first, second):
+    """The text from `first` up to the next `second`; both have to be there."""
+    at = text.index(first)
+    return text[at:text.index(second, at)]
+
+
+def test_a_row_stored_by_its_lane_is_complete_before_other_lanes_write_it():
+    part = between(source("prompt_attn.cu"), "store_tile<", "attend_row<")
+    assert part.index("p.a.lse[") < part.index("__syncwarp()")  # (a ballot orders no memory)
