@@ -70,6 +70,7 @@ __device__ __forceinline__ bool store_tile(uint32_t tmem, float scale, void* dst
 #pragma unroll
   for (int b = 0; b < CHUNKS; ++b) {
     uint32_t v[32], w[16];
+    __syncwarp();  // (lanes without a row stored nothing; the load is the whole warp's)
     tmem_ld32(tmem + 32 * b, v);
     tmem_wait_ld();
 #pragma unroll
@@ -78,14 +79,13 @@ __device__ __forceinline__ bool store_tile(uint32_t tmem, float scale, void* dst
       bad = fmaf(y0, 0.f, fmaf(y1, 0.f, bad));
       w[i] = pack2<FP16>(y0, y1);
     }
-    if (lane >= live) continue;
-    if (wide) {
+    if (lane < live && wide) {
 #pragma unroll
       for (int h = 0; h < 2; ++h)
         asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(row + 4 * b + 2 * h), "r"(w[8 * h]), "r"(w[8 * h + 1]),
                      "r"(w[8 * h + 2]), "r"(w[8 * h + 3]), "r"(w[8 * h + 4]), "r"(w[8 * h + 5]), "r"(w[8 * h + 6]), "r"(w[8 * h + 7])
                      : "memory");
-    } else {
+    } else if (lane < live) {
 #pragma unroll
       for (int h = 0; h < 4; ++h) row[4 * b + h] = make_uint4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]);
     }

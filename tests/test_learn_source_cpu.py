@@ -18,3 +18,10 @@ def between(text, first, second):
 def test_a_row_stored_by_its_lane_is_complete_before_other_lanes_write_it():
     part = between(source("prompt_attn.cu"), "store_tile<", "attend_row<")
     assert part.index("p.a.lse[") < part.index("__syncwarp()")  # (a ballot orders no memory)
+
+
+def test_lanes_meet_before_each_load_from_tensor_memory():
+    loop = between(source("prompt_items.cuh"), "store_tile(uint32_t", "return bad")
+    loop = loop[loop.index("for (int b = 0"):]
+    assert 0 <= loop.index("__syncwarp()") < loop.index("tmem_ld32(")
+    assert "continue" not in loop
