@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(E == 8 && V == 8 ? 256 : 512, E == 8 && V == 8
   __shared__ uint64_t full[2];
   extern __shared__ uint8_t rows_raw[];
   pdl_launch_dependents();
-  pdl_wait();
+  if constexpr (STAGED) pdl_wait_async(); else pdl_wait();
   const int dim = a.f.dim;
   const bool post = a.f.post_gain, gated = a.f.gate, own_gate = a.f.ldg != 0;
   const Stage st = stage_of(dim, sizeof(T), sizeof(H), a.d_h_out, a.f.y, gated && own_gate);

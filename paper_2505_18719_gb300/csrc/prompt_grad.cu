@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   // The kernel of d_q may start beside that of d_k and d_v, once this one knows that of D at its end, and takes the SMs that it leaves; it
   // waits for it at its end, so that its end is that of both.
   if (KEYS) {
-    pdl_wait();
+    pdl_wait_async();
     pdl_launch_dependents();
   }
   if constexpr (kExtra<FP16, KEYS>) {
@@ -381,6 +381,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   auto slot_b = [&](int s) { return s0 + Sh::kRingB + static_cast<uint32_t>(s) * Sh::kBlockBytes; };
 
   if (warp == 0) {
+    if (!KEYS) fence_async_global();
     // ------------------------------------------------------------------ items and loads
     const int heads = KEYS ? f.n_kv_heads : f.n_q_heads;
     int k = 0, loaded = 0;  // items; blocks

@@ -116,6 +116,8 @@ __device__ __forceinline__ void tmem_store(uint32_t taddr, const uint32_t* r) {
   for (int i = N / 16 * 16; i < N; i += 4) tmem_st4(taddr + i, r + i);
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+// Earlier kernels' ordinary stores before this thread's TMA and bulk loads of them (a kernel that starts beside another has no launch between).
+__device__ __forceinline__ void fence_async_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
 __device__ __forceinline__ void fence_async_smem() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 
 // 2^x (2^-inf = 0; results below the smallest normal number are 0)

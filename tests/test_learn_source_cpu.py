@@ -25,3 +25,16 @@ def test_lanes_meet_before_each_load_from_tensor_memory():
     loop = loop[loop.index("for (int b = 0"):]
     assert 0 <= loop.index("__syncwarp()") < loop.index("tmem_ld32(")
     assert "continue" not in loop
+
+
+def test_kernels_that_start_early_order_earlier_stores_before_their_bulk_reads():
+    norm = between(source("block_norm.cu"), "block_norm_grad_kernel(const", "request(blockIdx.x, 0)")
+    assert "pdl_wait_async();" in norm and not re.search(r"pdl_wait\(\);", norm.replace("else pdl_wait();", ""))
+    grad = source("prompt_grad.cu")
+    start = between(grad, "    prompt_grad_kernel(const", "if (warp == 0)")
+    assert start.index("pdl_wait_async();") < start.index("pdl_launch_dependents();") and "pdl_wait();" not in start
+    # the kernel of d_q begins without a wait of its own
+    assert re.match(r"if \(warp == 0\) \{\s*if \(!KEYS\) fence_async_global\(\);", between(grad, "if (warp == 0) {", "tma_load_2d("))
+    assert "fence.proxy.async.global" in between(source("tc_tiles.cuh"), "fence_async_global()", "}")
+    # the forward kernel is no programmatic dependent
+    assert re.search(r"launch_at\(Start::kInOrder, kern\b", source("prompt_attn.cu")) and "kEarly" not in source("prompt_attn.cu")
