@@ -19,6 +19,7 @@
 
 #include "learn.h"
 #include "ptx.cuh"
+#include "row_copy.h"
 
 namespace vla {
 
@@ -161,7 +162,7 @@ __global__ void __launch_bounds__(E == 8 && V < 8 ? 1024 : 512) block_norm_kerne
 }
 
 // Rows on their way through shared memory: two, each its h_out, d_x, d_h_out, y and gate behind one another.  A row that does not begin or end on
-// a 16-byte boundary comes with the bytes around it up to the next.
+// a 16-byte boundary comes with the bytes around it up to the next, as far as its tensor has them (row_copy).
 struct Stage {
   uint32_t at[5], bytes;  // offsets of the five, of the next row
 };
@@ -190,21 +191,58 @@ __global__ void __launch_bounds__(E == 8 && V == 8 ? 256 : 512, E == 8 && V == 8
   const int64_t ld[5] = {a.f.ldh * static_cast<int64_t>(sizeof(H)), a.lddx * static_cast<int64_t>(sizeof(T)),
                          a.lddho * static_cast<int64_t>(sizeof(H)), a.f.ldy * static_cast<int64_t>(sizeof(T)),
                          a.f.ldg * static_cast<int64_t>(sizeof(T))};
+  // A tensor's first and last rows, of which bytes around them may lie outside it (rows for 16-byte accesses have none around them).
+  const int ends = V < 8 ? (8 + dim - 1) / dim : 0;
+  auto is_end = [&](int64_t r) { return V < 8 && (r < ends || r >= a.f.rows - ends); };
+  auto copy_of = [&](int64_t r, int k) {
+    const uint32_t n = static_cast<uint32_t>(dim) * (k == 0 || k == 2 ? sizeof(H) : sizeof(T));
+    const uintptr_t lo = reinterpret_cast<uintptr_t>(base[k]);
+    return row_copy(lo + static_cast<uintptr_t>(r * ld[k]), n, lo, lo + static_cast<uintptr_t>((a.f.rows - 1) * ld[k]) + n);
+  };
   auto request = [&](int64_t r, int s) {  // one thread
-    uint32_t total = 0, bytes[5];
+    uint32_t total = 0, bytes[5], skip[5];
     uintptr_t from[5];
 #pragma unroll
     for (int k = 0; k < 5; ++k) {
       const uintptr_t p = reinterpret_cast<uintptr_t>(base[k]) + static_cast<uintptr_t>(r * ld[k]);
       const uintptr_t end = (p + static_cast<uint32_t>(dim) * (k == 0 || k == 2 ? sizeof(H) : sizeof(T)) + 15) & ~static_cast<uintptr_t>(15);
       from[k] = p & ~static_cast<uintptr_t>(15);
+      skip[k] = 0;
       bytes[k] = base[k] ? static_cast<uint32_t>(end - from[k]) : 0u;
+      if (is_end(r) && base[k]) {
+        const RowCopy c = copy_of(r, k);
+        skip[k] = static_cast<uint32_t>(c.from - from[k]);
+        bytes[k] = c.bytes;
+      }
       total += bytes[k];
     }
     mbar_arrive_expect_tx(smem_u32(full + s), total);
 #pragma unroll
     for (int k = 0; k < 5; ++k)
-      if (bytes[k]) bulk_load(smem_u32(stages + s * st.bytes + st.at[k]), reinterpret_cast<const void*>(from[k]), bytes[k], smem_u32(full + s));
+      if (bytes[k])
+        bulk_load(smem_u32(stages + s * st.bytes + st.at[k]) + skip[k], reinterpret_cast<const void*>(from[k] + skip[k]), bytes[k], smem_u32(full + s));
+  };
+  // What a request leaves out of such a row, 2 bytes a thread (8 threads its begin, 8 its end), by the whole CTA.
+  auto add_ends = [&](int64_t r, int s) {
+    uint16_t w[5] = {};
+    uint32_t at[5];
+    const uint32_t i = 2 * (threadIdx.x & 7);
+#pragma unroll
+    for (int k = 0; k < 5; ++k) {
+      at[k] = ~0u;
+      if (!base[k] || threadIdx.x >= 16) continue;
+      const RowCopy c = copy_of(r, k);
+      if (i >= (threadIdx.x < 8 ? c.head : c.tail)) continue;
+      at[k] = threadIdx.x < 8 ? i : static_cast<uint32_t>(dim) * (k == 0 || k == 2 ? sizeof(H) : sizeof(T)) - c.tail + i;
+      w[k] = *reinterpret_cast<const uint16_t*>(static_cast<const uint8_t*>(base[k]) + r * ld[k] + at[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < 5; ++k) {
+      const uint32_t row = static_cast<uint32_t>(reinterpret_cast<uintptr_t>(base[k]) + static_cast<uintptr_t>(r * ld[k])) & 15;
+      if (at[k] != ~0u)
+        asm volatile("st.shared.u16 [%0], %1;" ::"r"(smem_u32(stages + s * st.bytes + st.at[k]) + row + at[k]), "h"(w[k]) : "memory");
+    }
+    __syncthreads();
   };
   if constexpr (STAGED) {
     if (threadIdx.x == 0) {
@@ -257,10 +295,12 @@ __global__ void __launch_bounds__(E == 8 && V == 8 ? 256 : 512, E == 8 && V == 8
       else
         load_some<V>(static_cast<const T*>(a.f.gate) + i, y);
     };
-    if constexpr (STAGED)
+    if constexpr (STAGED) {
       if (!mbar_try_wait(smem_u32(full + buf), (n_rows >> 1) & 1) &&
           !wait_drain_reported(smem_u32(full + buf), (n_rows >> 1) & 1, a.status, a.wait_limit))
         break;
+      if (is_end(r)) add_ends(r, buf);
+    }
     if constexpr (E == 8) {  // values and gains of a short row stay in registers
       float n[E], g[E], d[E], m[E], q[E], sum[3] = {0.f, 0.f, 0.f};
 #pragma unroll
