@@ -101,7 +101,7 @@ __global__ void __launch_bounds__((Smem<HD, PAIRED>::kThreads), 1)
   Item* items = reinterpret_cast<Item*>(bars + kBarCount);
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(items + 2 * kItems);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  static_assert(kBarCount * 8 + 2 * kItems * 16 + 8 <= 1024 && kBarCount % 2 == 0, "barrier area");
+  static_assert(kBarCount * 8 + 2 * kItems * 16 + 12 <= 1024 && kBarCount % 2 == 0, "barrier area");
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint32_t* status = p.a.status;
   const uint64_t limit = p.wait_limit;
@@ -125,7 +125,7 @@ __global__ void __launch_bounds__((Smem<HD, PAIRED>::kThreads), 1)
       mbar_init(BAR(KVFREE + s), PAIRED && !(s & 1) ? 2 : 1);  // (keys of both tiles: read by a warp for each)
       mbar_init(BAR(TAIL + s), 1);
     }
-    *abort_flag = 0;
+    abort_flag[0] = abort_flag[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) tmem_take(smem_u32(tmem_slot));
@@ -437,7 +437,7 @@ __global__ void __launch_bounds__((Smem<HD, PAIRED>::kThreads), 1)
       while (again) {
         const int rr = __ffs(static_cast<int>(again)) - 1;
         again &= again - 1;
-        attend_row<HD, FP16>(p.a, static_cast<int>(row) + rr, head, it.begin);
+        attend_row<HD, FP16>(p.a, static_cast<int>(row) + rr, head, it.begin, const_cast<int*>(abort_flag) + 1);
       }
     }
   }

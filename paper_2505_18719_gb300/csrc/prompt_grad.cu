@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(items + kItems);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   float* row_data = reinterpret_cast<float*>(smem + Sh::kRowData);
-  static_assert(kBarCount * 8 + kItems * 16 + 8 <= 1024 && kBarCount % 2 == 0, "barrier area");
+  static_assert(kBarCount * 8 + kItems * 16 + 12 <= 1024 && kBarCount % 2 == 0, "barrier area");
   const PromptArgs& f = p.g.f;
   constexpr int kRows = Sh::kRows;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -327,7 +327,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       // (a dO tile is done when dP and d_v have been taken from it)
       mbar_init(BAR(i), i >= IFREE ? kItemReaders<KEYS> : all ? kSumWarps : (rows || (KEYS && i >= RBFREE && i < RBFREE + 4)) ? 2 : 1);
     }
-    *abort_flag = 0;
+    abort_flag[0] = abort_flag[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) tmem_take(smem_u32(tmem_slot));

@@ -64,9 +64,9 @@ __device__ __forceinline__ void lane_add(Lane<HD>& y, float p, const Lane<HD>& v
 __device__ __forceinline__ const void* elem(const void* p, int64_t i) { return static_cast<const uint16_t*>(p) + i; }
 __device__ __forceinline__ void* elem(void* p, int64_t i) { return static_cast<uint16_t*>(p) + i; }
 
-// out[row][h] and its lse.
+// out[row][h] and its lse.  `work` (shared memory) grows every 64 keys.
 template <int HD, bool FP16>
-__device__ __noinline__ void attend_row(const PromptArgs& a, int row, int h, int first) {
+__device__ __noinline__ void attend_row(const PromptArgs& a, int row, int h, int first, int* work) {
   constexpr int U = 4;
   const int g = h / (a.n_q_heads / a.n_kv_heads);
   const float c = a.scale * kLog2e;
@@ -74,6 +74,7 @@ __device__ __noinline__ void attend_row(const PromptArgs& a, int row, int h, int
   Lane<HD> o = {};
   float m = -INFINITY, l = 0.f;
   for (int j0 = first; j0 <= row; j0 += U) {
+    if (((j0 - first) & 63) == 0 && (threadIdx.x & 31) == 0) atomicAdd(work, 1);
     Lane<HD> v[U];
     float s[U];
 #pragma unroll

@@ -137,12 +137,18 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 }
 
 // Bounded wait of a whole warp: all lanes ask at once.  (Asked by one lane with the others waiting for it, the answer comes 600 cycles later.)  The
-// clock, which takes longer to read than the wait lasts as a rule, comes in after 1024 tries.
+// clock, which takes longer to read than the wait lasts as a rule, comes in after 1024 tries.  abort_flag[0]: a wait of the CTA has given up;
+// abort_flag[1]: grows while a warp is at something that may take longer than the limit (attend_row, whose loop ends by itself), which
+// begins anew each time.
 __device__ __forceinline__ bool warp_waits(uint32_t bar, uint32_t parity, volatile int* abort_flag, uint32_t* status, uint64_t limit) {
   uint64_t t0 = 0;
+  int work = 0;
   for (uint32_t n = 1; !__all_sync(0xffffffffu, mbar_try_wait(bar, parity)); ++n) {
     if (n & 1023u) continue;
-    if (n == 1024) t0 = globaltimer();
+    if (const int now = uniform(abort_flag[1]); n == 1024 || now != work) {
+      t0 = globaltimer();
+      work = now;
+    }
     const bool late = globaltimer() - t0 > limit, given_up = *abort_flag != 0;
     if (__any_sync(0xffffffffu, late) && (threadIdx.x & 31) == 0) {
       *abort_flag = 1;

@@ -4,6 +4,7 @@ import math
 import pytest
 import torch
 
+from paper_2505_18719_gb300 import vla as V
 from tests import learn_reference as R
 from tests.test_gpu_learn import Prompt
 from tests.test_gpu_lm_ops import status, within
@@ -49,3 +50,55 @@ def test_prompt_attention_first_block_far_below_the_next():
     within(p.heads(out)[64:], want, t_out, "out")
     within(lse[64:], w_lse, t_lse, "lse")
     assert status() == 0
+
+
+def rows_reference(p, a, rows):
+    """(out, lse, tolerances) of the given rows of the sequence from a on that 32-bit dot products compute, keys one by one, in 64 bits.
+    A channel in which a row sees a value that is no number has none itself."""
+    q, k, v = [p.heads(t).to(R.F64) for t in (p.q, p.k, p.v)]
+    out, t_out = [torch.zeros(len(rows), p.H, p.hd, dtype=R.F64, device="cuda") for _ in range(2)]
+    lse, t_lse = [torch.zeros(len(rows), p.H, dtype=R.F64, device="cuda") for _ in range(2)]
+    at = torch.tensor(rows, device="cuda")
+    n = max(rows) + 1 - a
+    for h in range(p.H):
+        K, W = k[a:a + n, h // (p.H // p.Hk)], v[a:a + n, h // (p.H // p.Hk)]
+        seen = torch.arange(a, a + n, device="cuda")[None] <= at[:, None]
+        s = torch.where(seen, p.scale * q[at, h] @ K.T, -math.inf)
+        w = torch.softmax(s, -1)
+        number = torch.isfinite(W)
+        out[:, h] = torch.where(seen.to(R.F64) @ (~number).to(R.F64) > 0, math.nan, w @ torch.where(number, W, 0.0))
+        lse[:, h] = torch.logsumexp(s, -1)
+        # a score: a rounding for each of its products and sums; sums over the keys, whose roundings fall either way; the result's own
+        e_s = torch.where(seen, p.scale * q[at, h].abs() @ K.abs().T, 0.0).amax(-1, keepdim=True) * (p.hd + 4) * R.E
+        size = w @ torch.where(number, W, 0.0).abs()
+        t_out[:, h] = R.U[p.act] * out[:, h].abs() + (2 * e_s + 2 * (8 + n ** 0.5) * R.E) * size + R.TINY[p.act]
+        t_lse[:, h] = e_s.squeeze(-1) + (8 + n ** 0.5) * R.E + 4 * R.E * lse[:, h].abs()
+    return out, lse, t_out, t_lse
+
+
+@pytest.fixture
+def short_waits():
+    # 2 ms a wait, of 1 s: shorter than what is computed again below takes
+    assert V.vla_test_set_wait_limit_ns(2_000_000) == 0
+    yield
+    V.vla_test_set_wait_limit_ns(0)
+
+
+@pytest.mark.parametrize("act", ["f16", "bf16"])
+def test_rows_computed_again_keep_no_other_sequence_waiting(act, short_waits):
+    # a NaN in the last value of a long sequence: the rows before it in its tile are computed again, over all their keys, while the
+    # other warps of that CTA wait with the rows of the next sequence
+    p = Prompt(52, [16384, 8192], 4, 2, 64, act)
+    want, w_lse = p.forward()
+    assert status() == 0
+    bad = 16383
+    p.heads(p.v)[bad] = math.nan
+    out, lse = p.forward()
+    assert status() == 0
+    rest = [i for i in (*range(bad // 128 * 128), *range(bad + 1, p.rows))]
+    assert torch.equal(out[rest], want[rest]) and torch.equal(lse[rest], w_lse[rest])
+    tile = list(range(bad // 128 * 128, bad))
+    exact, e_lse, t_out, t_lse = rows_reference(p, 0, tile)
+    within(p.heads(out)[tile], exact, t_out, "out")
+    within(lse[tile], e_lse, t_lse, "lse")
+    assert bool(torch.isnan(p.heads(out)[bad]).all())

@@ -38,3 +38,11 @@ def test_kernels_that_start_early_order_earlier_stores_before_their_bulk_reads()
     assert "fence.proxy.async.global" in between(source("tc_tiles.cuh"), "fence_async_global()", "}")
     # the forward kernel is no programmatic dependent
     assert re.search(r"launch_at\(Start::kInOrder, kern\b", source("prompt_attn.cu")) and "kEarly" not in source("prompt_attn.cu")
+
+
+def test_a_wait_is_as_long_as_the_work_it_waits_for():
+    waits = between(source("tc_tiles.cuh"), "bool warp_waits(", "return true;")
+    assert "now != work" in waits and waits.index("t0 = globaltimer();") < waits.index("> limit")
+    assert "atomicAdd(work, 1)" in between(source("prompt_rows.cuh"), "attend_row(", "store_lane<")
+    for path in ("prompt_attn.cu", "prompt_grad.cu"):  # (the count begins as the flag does)
+        assert "abort_flag[0] = abort_flag[1] = 0;" in source(path)
