@@ -33,8 +33,9 @@ extern "C" {
  *   lse        f32 [rows][n_q_heads] or NULL: log sum_j exp(scale q . k[j]); -infinity in rows of no sequence.
  * A key whose score is -infinity has no weight; a row with no other keys gives zeros and -infinity.
  * Scores, their maxima and sums are 32-bit; the weights of the values are rounded to `dtype`, relative to their maximum.  A row depends
- * on nothing behind it and on no other sequence: NaN and infinities there stay there.  Equal calls give
- * equal bits.  out overlaps nothing that the call reads.  rows 0 or more; rows * n_q_heads at most 2^30. */
+ * on nothing behind it and on no other sequence: NaN and infinities there stay there.  In the rows that see one it shows, or not where its
+ * weight is 0 in 32 bits.  (Up to 127 rows before such a value are computed again, one by one over all their keys: 0.15 s
+ * where it is the last of 16384.)  Equal calls give equal bits.  out overlaps nothing that the call reads.  rows 0 or more; rows * n_q_heads at most 2^30. */
 int vla_prompt_attn(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int dtype, int rows,
                     int n_q_heads, int n_kv_heads, int head_dim, const int32_t* seq_start, int n_seq, float scale, void* out,
                     int64_t ldo, float* lse, void* cuda_stream);

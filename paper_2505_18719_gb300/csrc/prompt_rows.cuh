@@ -106,4 +106,48 @@ __device__ __noinline__ void attend_row(const PromptArgs& a, int row, int h, int
   if (a.lse && (threadIdx.x & 31) == 0) a.lse[static_cast<int64_t>(row) * a.n_q_heads + h] = (m + log2f(l)) * kLn2;
 }
 
+// Which of `rows` (bits, of the 32 rows from `row` on) that have a channel without a number have it from values behind them, which do not
+// count for them: no value that the row sees is without a number in that channel.  The others show what they see, and computing them again would
+// take longer for every row the longer the sequence is.  Looks from the sequence's begin on, until all such channels have been seen.
+template <int HD, bool FP16>
+__device__ __noinline__ uint32_t spoilt_rows(const PromptArgs& a, int row, int h, int first, uint32_t rows, int* work) {
+  constexpr int N = Lane<HD>::N, U = 8;
+  const int g = h / (a.n_q_heads / a.n_kv_heads), last = row + 31 - __clz(static_cast<int>(rows));
+  auto no_number = [](const Lane<HD>& y) {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) m |= static_cast<uint32_t>(!(fabsf(y.x[i]) < INFINITY)) << i;
+    return m;
+  };
+  auto of_row = [&](int r) { return no_number(load_lane<HD, FP16>(elem(a.out, (row + r) * a.ldo + h * HD))); };
+  uint32_t open = 0;  // channels of this lane that none of the values so far explains
+  for (uint32_t rest = rows; rest; rest &= rest - 1) open |= of_row(__ffs(static_cast<int>(rest)) - 1);
+  int seen[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) seen[i] = 0x7fffffff;
+  for (int j0 = first; j0 <= last && __any_sync(0xffffffffu, open != 0); j0 += U) {
+    if (((j0 - first) & 63) == 0 && (threadIdx.x & 31) == 0) atomicAdd(work, 1);
+    Lane<HD> v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) v[u] = load_lane<HD, FP16>(elem(a.v, min(j0 + u, last) * a.ldv + g * HD));
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const uint32_t found = no_number(v[u]) & open;
+#pragma unroll
+      for (int i = 0; i < N; ++i) seen[i] = (found >> i) & 1 ? min(j0 + u, last) : seen[i];
+      open &= ~found;
+    }
+  }
+  uint32_t spoilt = 0;
+  for (uint32_t rest = rows; rest; rest &= rest - 1) {
+    const int r = __ffs(static_cast<int>(rest)) - 1;
+    const uint32_t m = of_row(r);
+    bool behind = false;
+#pragma unroll
+    for (int i = 0; i < N; ++i) behind |= (m >> i) & 1 && seen[i] > row + r;
+    if (__any_sync(0xffffffffu, behind)) spoilt |= 1u << r;
+  }
+  return spoilt;
+}
+
 }  // namespace vla

@@ -102,3 +102,81 @@ def test_rows_computed_again_keep_no_other_sequence_waiting(act, short_waits):
     within(p.heads(out)[tile], exact, t_out, "out")
     within(lse[tile], e_lse, t_lse, "lse")
     assert bool(torch.isnan(p.heads(out)[bad]).all())
+
+
+@pytest.mark.parametrize("act,hd", [("f16", 64), ("bf16", 128)])
+@pytest.mark.parametrize("n", [700, 1700])
+@pytest.mark.parametrize("where", ["first channel", "first row", "here and there", "tile ends", "scattered"])
+def test_a_value_without_a_number_shows_in_its_channel_from_its_row_on(n, where, act, hd):
+    p = Prompt(53, [40, n, 90], 4, 2, hd, act)
+    v = p.heads(p.v)
+    clean = p.forward()
+    if where == "first channel":
+        v[40, :, 0] = math.nan
+    elif where == "first row":
+        v[40] = math.nan
+    elif where == "here and there":  # (the second key-value head has one row only)
+        v[40, 0, 0], v[40 + 130, 0, 1], v[40 + 300, 0], v[40 + n - 2, 1, 5] = [math.nan] * 4
+    elif where == "tile ends":  # rows that see one in another channel, spoilt by the last of each tile
+        v[40, :, 7] = math.nan
+        for i in range(127, n, 128):
+            v[40 + i, :, i // 128] = math.nan
+    else:
+        at = torch.randint(0, n, (20,), generator=torch.Generator().manual_seed(3))
+        for i, r in enumerate(at.tolist()):
+            v[40 + r, i % 2, (7 * i) % hd] = math.nan
+    out, lse = p.forward()
+    assert status() == 0
+    rows = list(range(40, 40 + n))
+    want, _, _, _ = rows_reference(p, 40, rows)
+    numbers = torch.where(torch.isfinite(v), v, 0)
+    _, _, tol, _ = R.prompt(p.heads(p.q), p.heads(p.k), numbers, p.start, p.scale, act)
+    within(p.heads(out)[40:40 + n], want, tol[40:40 + n], "out")
+    assert torch.equal(lse, clean[1]) or bool(((lse - clean[1]).abs() <= 1e-5 * (1 + clean[1].abs())).all())
+    for part in (slice(0, 40), slice(40 + n, p.rows)):
+        assert torch.equal(out[part], clean[0][part])
+
+
+def test_values_near_the_largest_bf16():
+    # sums of weights up to 2^8 with a reference that lags behind pass the largest number; the row itself does not
+    p = Prompt(54, [900], 2, 1, 64, "bf16")
+    q, k, v = p.heads(p.q), p.heads(p.k), p.heads(p.v)
+    q[:] = 0
+    q[:, :, 0] = 1
+    k[:] = 0
+    k[:, :, 0] = (torch.linspace(0, 5.0, 900, device="cuda")[:, None] / p.scale).bfloat16()
+    v[:] = 1e34
+    out, lse = p.forward()
+    assert status() == 0
+    want, w_lse, t_out, t_lse = R.prompt(q, k, v, p.start, p.scale, "bf16")
+    within(p.heads(out), want, t_out, "out")
+    within(lse, w_lse, t_lse, "lse")
+
+
+def test_a_long_sequence_without_numbers_takes_no_longer(short_waits):
+    p = Prompt(55, [16384, 300], 8, 2, 128, "bf16")
+
+    def time():
+        best = math.inf
+        for _ in range(3):
+            a, b = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+            a.record()
+            got = p.forward()
+            b.record()
+            torch.cuda.synchronize()
+            best = min(best, a.elapsed_time(b))
+        assert status() == 0
+        return (*got, best)
+
+    out, lse, ms = time()
+    for name in ("v", "k", "q"):
+        t = p.heads(getattr(p, name))
+        keep = t[0].clone()
+        for channels in (slice(None), slice(3, 4)):
+            t[0, :, channels] = math.nan
+            o2, l2, ms2 = time()
+            assert torch.equal(o2[16384:], out[16384:]) and torch.equal(l2[16384:], lse[16384:])
+            if name != "q":
+                assert bool(torch.isnan(p.heads(o2)[:16384, :, channels]).all())
+            assert ms2 < 10 * ms  # (each row computed again: 100 times)
+            t[0] = keep
