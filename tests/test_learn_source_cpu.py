@@ -46,3 +46,33 @@ def test_a_wait_is_as_long_as_the_work_it_waits_for():
     assert "atomicAdd(work, 1)" in between(source("prompt_rows.cuh"), "attend_row(", "store_lane<")
     for path in ("prompt_attn.cu", "prompt_grad.cu"):  # (the count begins as the flag does)
         assert "abort_flag[0] = abort_flag[1] = 0;" in source(path)
+
+
+def test_every_wait_gives_up():
+    kernels = {p: source(p) for p in ("prompt_attn.cu", "prompt_grad.cu", "block_norm.cu")}
+    for path, text in kernels.items():
+        # all waits of the kernels are these helpers' (a try stands before one of them, as its first question), and there are some
+        waits = re.findall(r"\b(warp_waits|wait_drain|wait_drain_reported)\(", text)
+        assert len(waits) >= 1, path
+        for m in re.finditer(r"mbar_try_wait\(", text):
+            assert "wait_drain_reported(" in text[m.start():m.start() + 200], path
+        for m in re.finditer(r"\bwhile\s*\(", text):  # no loop of its own around a barrier
+            assert "mbar" not in text[m.start():text.index("\n", m.start())], path
+    assert "warp_waits(" in kernels["prompt_attn.cu"] and "warp_waits(" in kernels["prompt_grad.cu"]
+    helpers = {"tc_tiles.cuh": ["warp_waits"], "ptx.cuh": ["wait_bounded", "wait_drain", "wait_drain_reported", "wait_cluster_data"]}
+    for path, names in helpers.items():
+        text = source(path)
+        for name in names:
+            body = between(text, f" {name}(", "\n}\n")
+            assert len(re.findall(r"try_wait", body)) >= 1 and re.search(r"globaltimer\(\) - t0 > limit", body), name
+        # and no other function of the file tries in a loop
+        loops = len(re.findall(r"(?:while|for) \([^{;]*(?:;[^{]*)?mbar_try_wait", text))
+        assert loops == {"tc_tiles.cuh": 1, "ptx.cuh": 2}[path], (path, loops)
+
+
+def test_dependents_start_where_they_may():
+    grad, attn = source("prompt_grad.cu"), source("prompt_attn.cu")
+    assert grad.count("pdl_launch_dependents()") == 1 and attn.count("pdl_launch_dependents()") == 0
+    # the only one stands behind the allocation of tensor memory and the wait for the kernel of D
+    order = [grad.index(x, grad.index("    prompt_grad_kernel(const")) for x in ("tmem_take(", "tc_fence_after();", "pdl_wait_async();", "pdl_launch_dependents();")]
+    assert order == sorted(order)
