@@ -25,8 +25,11 @@ namespace vla {
 
 namespace {
 
-// CTAs of the gradient, each a share of the rows: 152 SMs with as many as hide a row's latency.
-int parts_of(int rows, int dim) { return std::min(rows, 152 * (dim <= 256 ? 16 : dim <= 512 ? 8 : dim <= 1024 ? 4 : dim <= 1400 ? 3 : dim <= 4096 ? 2 : 1)); }
+// CTAs of the gradient, each a share of the rows: as many as the registers of 152 SMs hold at once (512 threads of 128 registers an SM, and 8 elements a
+// thread up to 2048 channels, 16 up to 4096); a share more than that waits for a second round.  18385 rows of 1152, 1280 and 1400 channels: with 2 a
+// SM 122, 126, 133 us, with 3 95, 99, 165 (192 threads do not fit three times), with 4 131, 135, 138.  The number is a GB300's whatever
+// the device, for the workspace's size goes by it.
+int parts_of(int rows, int dim) { return std::min(rows, 152 * (dim <= 256 ? 16 : dim <= 512 ? 8 : dim <= 1024 ? 4 : dim <= 1280 ? 3 : dim <= 4096 ? 2 : 1)); }
 uint32_t staged_limit(int dim) { return dim <= 4096 ? 100 * 1024 : 200 * 1024; }  // of two rows of each of those CTAs
 
 template <class T>
