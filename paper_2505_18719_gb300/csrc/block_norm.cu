@@ -203,27 +203,35 @@ __global__ void __launch_bounds__(E == 8 && V == 8 ? 256 : 512, E == 8 && V == 8
     return row_copy(lo + static_cast<uintptr_t>(r * ld[k]), n, lo, lo + static_cast<uintptr_t>((a.f.rows - 1) * ld[k]) + n);
   };
   auto request = [&](int64_t r, int s) {  // one thread
-    uint32_t total = 0, bytes[5], skip[5];
+    const uint32_t bar = smem_u32(full + s), to = smem_u32(stages + s * st.bytes);
+    if (is_end(r)) {
+      uint32_t total = 0;
+#pragma unroll
+      for (int k = 0; k < 5; ++k) total += base[k] ? copy_of(r, k).bytes : 0u;
+      mbar_arrive_expect_tx(bar, total);
+#pragma unroll
+      for (int k = 0; k < 5; ++k) {
+        if (!base[k]) continue;
+        const RowCopy c = copy_of(r, k);
+        const uintptr_t p = reinterpret_cast<uintptr_t>(base[k]) + static_cast<uintptr_t>(r * ld[k]);
+        if (c.bytes) bulk_load(to + st.at[k] + static_cast<uint32_t>(c.from - (p & ~static_cast<uintptr_t>(15))), reinterpret_cast<const void*>(c.from), c.bytes, bar);
+      }
+      return;
+    }
+    uint32_t total = 0, bytes[5];
     uintptr_t from[5];
 #pragma unroll
     for (int k = 0; k < 5; ++k) {
       const uintptr_t p = reinterpret_cast<uintptr_t>(base[k]) + static_cast<uintptr_t>(r * ld[k]);
       const uintptr_t end = (p + static_cast<uint32_t>(dim) * (k == 0 || k == 2 ? sizeof(H) : sizeof(T)) + 15) & ~static_cast<uintptr_t>(15);
       from[k] = p & ~static_cast<uintptr_t>(15);
-      skip[k] = 0;
       bytes[k] = base[k] ? static_cast<uint32_t>(end - from[k]) : 0u;
-      if (is_end(r) && base[k]) {
-        const RowCopy c = copy_of(r, k);
-        skip[k] = static_cast<uint32_t>(c.from - from[k]);
-        bytes[k] = c.bytes;
-      }
       total += bytes[k];
     }
-    mbar_arrive_expect_tx(smem_u32(full + s), total);
+    mbar_arrive_expect_tx(bar, total);
 #pragma unroll
     for (int k = 0; k < 5; ++k)
-      if (bytes[k])
-        bulk_load(smem_u32(stages + s * st.bytes + st.at[k]) + skip[k], reinterpret_cast<const void*>(from[k] + skip[k]), bytes[k], smem_u32(full + s));
+      if (bytes[k]) bulk_load(to + st.at[k], reinterpret_cast<const void*>(from[k]), bytes[k], bar);
   };
   // What a request leaves out of such a row, 2 bytes a thread (8 threads its begin, 8 its end), by the whole CTA.
   auto add_ends = [&](int64_t r, int s) {

@@ -55,7 +55,10 @@ def test_rows_of_every_alignment(tmp_path):
 
 def test_the_norm_gradient_reads_by_it_at_the_ends():
     text = open(os.path.join(CSRC, "block_norm.cu")).read()
-    assert text.count("bulk_load(") == 1 and "if (is_end(r) && base[k])" in text and "if (is_end(r)) add_ends(r, buf);" in text
+    request = text[text.index("auto request = "):text.index("auto add_ends = ")]
+    at_ends = request[request.index("if (is_end(r)) {"):request.index("return;")]
+    assert text.count("bulk_load(") == request.count("bulk_load(") == 2 and at_ends.count("bulk_load(") == 1
+    assert "c.from), c.bytes" in at_ends and "copy_of(r, k)" in at_ends and "if (is_end(r)) add_ends(r, buf);" in text
     assert "row_copy(lo + static_cast<uintptr_t>(r * ld[k]), n, lo, lo + static_cast<uintptr_t>((a.f.rows - 1) * ld[k]) + n)" in text
     # rows that are not among `ends` have 16 bytes of their tensor before and behind them, of the narrowest type and without gaps
     assert "const int ends = V < 8 ? (8 + dim - 1) / dim : 0;" in text
