@@ -3,6 +3,8 @@
 The kernels round dS to fp16 times a power of two that brings the largest it can be in a row (of d_q: a query's, over the keys it sees; of
 d_k: a key's, over the queries that see it) to 2^13 at least and 2^15 at most.  Half the spacing of the smallest fp16 numbers is 2^-25, so
 beside the relative half-step a dS is off by at most 2^-38 of that largest.  The rest is as in learn_reference.py."""
+import math
+
 import pytest
 import torch
 
@@ -134,3 +136,31 @@ def test_the_workspace_holds_what_the_rows_need():
     ws = torch.full((n + 4096,), 0x7F, dtype=torch.uint8, device="cuda")
     p.backward(out, lse, workspace=ws)
     assert bool((ws[n:] == 0x7F).all())
+
+
+def test_rows_of_no_sequence_and_other_lengths_by_one_graph():
+    # what lies around the sequences is no number; the same captured calls go over other starts
+    p = Prompt(66, [70, 201, 0, 33], 6, 2, 64, "f16", before=45, behind=100)
+    inside = torch.zeros(p.rows, dtype=torch.bool, device="cuda")
+    inside[p.start[0]:p.start[-1]] = True
+    want = p.backward(*p.forward())
+    for t in (p.q, p.k, p.v, p.d_out):
+        t[~inside] = math.nan
+    out, lse = p.forward()
+    for a, b in zip(p.backward(out, lse), want):
+        assert torch.equal(a, b) and bool((a[~inside] == 0).all())
+    for t in (p.q, p.k, p.v, p.d_out):
+        t[~inside] = 0.5
+    ws = torch.empty(V.vla_prompt_attn_grad_workspace_bytes(p.rows, p.H, p.Hk, p.hd), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        o, l = p.forward()  # noqa: E741
+        d = p.backward(o, l, workspace=ws)
+    for start in ([0, 449, 449, 449, 449], [3, 40, 300, 301, 420], p.start):
+        p.start = start
+        p.starts.copy_(torch.tensor(start, dtype=torch.int32))
+        graph.replay()
+        for a, b in zip(d, p.backward(*p.forward())):
+            assert torch.equal(a, b)
+    assert status() == 0
