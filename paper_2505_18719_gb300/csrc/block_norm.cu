@@ -8,7 +8,7 @@
 // c2 is linear in d_h, so with q = residual_scale gate post_gain m both means come from three sums taken together:
 //   c2 = mean(q (d_h_out + r_h g)) - c1 mean(q r_h n).
 // A CTA takes every n-th row; the next one comes to shared memory by bulk copies while it works at this one.  Short rows stay in registers between the
-// sums and the outputs (8 elements a thread: a row of 1155 by single elements, 2311 of them, 23 us where reading shared memory again took 65),
+// sums and the outputs (8 elements a thread: a row of 1155 by single elements, 2311 of them, 24 us where reading shared memory again took 65),
 // longer ones are read from shared memory twice.  Column sums (gains, a gate for all rows) stay in registers over a CTA's rows; the CTAs' sums
 // go to the workspace and are added in the order of the CTAs by a second kernel, which waits for the first already started.
 //

@@ -3,7 +3,8 @@
 // With c = scale log2(e), for a query i over blocks of keys: s = q K^T, m = max s, weights 2^(c (s - m)), l their sum,
 // O = 2^(c (m' - m)) O + P V; out = O / l, lse = ln 2 (c m + log2 l).  The reference m moves only when a maximum passes it by more than
 // 2^8, so O is scaled again in few blocks; it is -infinity until a row has met a score above that.  Weights go to the values' type; fp16 ones are 2^7 times as large, so that one of
-// 2^-21 of the row's largest still keeps all its bits (at most 2^15 with the reference 2^8 behind).
+// 2^-21 of the row's largest still keeps all its bits (at most 2^15 with the reference 2^8 behind).  One 16-bit term a weight: outputs of bf16 are
+// 0.0020 of their size off the 64-bit ones, where 32-bit weights and one rounding at the end give 0.0016; a second term would be a second product.
 //
 // A tile is 128 rows of one sequence and query head.  The tiles of a sequence and key-value head are numbered row tile after row tile, query
 // head after query head, and an item is two neighbours: two query heads over the same rows where heads are shared, else two row tiles.
@@ -31,8 +32,9 @@
 // (attend_row).  Rows that see such a value stay as they are (spoilt_rows): 16384 rows of 32 heads that all see a NaN take 1.5 ms, and
 // took 880 when each of them was computed again; the 127 rows before a NaN in the last one take 150.
 //
-// Measured (32 query heads of 128): one sequence of 16384 rows, 8 key-value heads 1.31 to 1.42 ms (1.55 to 1.68 PFLOP/s; the tensor pipe 64 % busy at 8192 rows by its
-// counter); 16 sequences of 1 to 2048 rows 197 us (0.96 PFLOP/s); 64 prefixes of 272 to 304 rows 136 us (4.4 TB/s).
+// Measured (32 query heads of 128): one sequence of 16384 rows, 8 key-value heads 1.41 to 1.45 ms warm (1.52 to 1.56 PFLOP/s; the tensor pipe 63 % busy at 8192 rows by
+// its counter); 16 sequences of 1 to 2048 rows 198 us (0.95 PFLOP/s); 64 prefixes of 272 to 304 rows 140 us (4.3 TB/s); heads of 64: 8192 rows of 32 and
+// 8 heads 342 us (0.80 PFLOP/s), the 64 prefixes 105 us.
 #include <algorithm>
 #include <type_traits>
 
@@ -455,7 +457,10 @@ __global__ void __launch_bounds__((Smem<HD, PAIRED>::kThreads), 1)
   }
 }
 
-// Sequences of fewer rows than this on average: a tile each for the two halves of a CTA.
+// Sequences of fewer rows than this on average: a tile each for the two halves of a CTA.  32768 rows of bf16 in sequences of 128, 256, 384, 512, 640,
+// 767, 1024 and 2048, pairs / halves in us: 32 and 8 heads of 128: 155/160, 179/176, 192/196, 213/217, 228/257, 240/249, 282/298, 441/489;
+// 32 and 32 of 128: 263/173, 221/200, 219/213, 242/229, 259/268, 263/268, 301/328, 458/527; 16 and 4 of 64: 74/70, 86/83, 92/98, 102/100,
+// 107/111, 113/113, 132/134, 209/227.  What the halves gain is with heads of their own; where they lose below the border it is by 2 to 13 %.
 constexpr int kShort = 768;
 
 template <int HD, bool FP16, bool PAIRED>

@@ -17,7 +17,8 @@
 // |v[j]| max |d_out[i]| + max |D[i]| over the queries (and heads) that see key j.  So a row's bits depend on its own sequence alone, and
 // neither on larger gradients beside it; what lies 2^38 below that largest is rounded away.  The kernel of D writes the norms of rows and their maxima
 // over 32 rows for it; a row's thread scales its sums back, so the factors cost nothing but their maxima (8192 rows of fp16
-// take 1.55 ms, with one factor for all of a sequence 1.54; 64 samples of 272 to 304 rows 602 and 594 us).
+// take 1.64 ms, with one factor for all of a sequence 1.59; 64 samples of 272 to 304 rows 625 and 590 us).  Gradients are 0.0025 of their size
+// off the 64-bit ones, where 32-bit P and dS and one rounding at the end give 0.0019; second terms would double three of the products.
 // Rows of the streamed operands behind a sequence's last one become zeros in shared memory (their weights are zeros, but
 // a NaN would spoil the sums over rows), up to the next multiple of 16, where the products stop.
 //
@@ -26,9 +27,10 @@
 // the blocks in turn, were slower: 8192 rows 1.9 ms where one takes 1.3.)
 //
 // Bound by shared memory (scores and dP read both operands from it at 128 bytes a cycle) and, for d_k and d_v, by the element-wise chain: a block of
-// 80 queries takes 2240 cycles, its products 1550.  Measured (32 query heads of 128): 8192 rows, 8 key-value heads 1.28 to 1.36 ms (1.0 to 1.07
-// PFLOP/s of the ten needed flops a pair and channel; tensor pipe 48 and 59 % busy at 4096 rows); 64 samples of 272 to 304 rows 467 us (2.6 TB/s
-// of the bytes that have to move).
+// 80 queries takes 2240 cycles, its products 1550.  Measured (32 query heads of 128): 8192 rows, 8 key-value heads 1.32 to 1.38 ms (1.0 to 1.04
+// PFLOP/s of the ten needed flops a pair and channel; tensor pipe 46 and 58 % busy at 4096 rows); 64 samples of 272 to 304 rows 447 us (2.7 TB/s
+// of the bytes that have to move); heads of 64: 8192 rows 1.19 ms, the samples 350 us.  The kernel of D: 20 us at 4096 rows (3.3 TB/s: 128 CTAs), its
+// loads four steps ahead of its stores.  Few items leave SMs without work: 2048 rows of 8 heads on one key-value head 190 us.
 #include <algorithm>
 
 #include "gemm.h"
@@ -629,7 +631,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int row0 = it.a * kTile + q4 * 32;
       // (fp16) the exponent of this row's factor of dS; of a query row its lse (with the factor) and -D
       const int e = FP16 ? ds_exponent<KEYS>(p, it, r) : 0;
-      // d_k's factor beside the weights' own waits in shared memory for its use: as registers it costs spills, 8192 rows 1.71 ms for 1.55
+      // d_k's factor beside the weights' own waits in shared memory for its use: as registers it costs spills, 8192 rows 1.71 ms for 1.66
       volatile float* const factor = row_data + 2 * 256 + (threadIdx.x - 32 * kSumWarp0);
       if constexpr (KEYS && FP16) *factor = exp2_int(e - static_cast<int>(kPShift));
       uint64_t l2 = 0, d2 = 0;
