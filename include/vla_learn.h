@@ -32,10 +32,11 @@ extern "C" {
  *   scale      1e-30 or more;
  *   lse        f32 [rows][n_q_heads] or NULL: log sum_j exp(scale q . k[j]); -infinity in rows of no sequence.
  * A key whose score is -infinity has no weight; a row with no other keys gives zeros and -infinity.
- * Scores, their maxima and sums are 32-bit; the weights of the values are rounded to `dtype`, relative to their maximum.  A row depends
- * on nothing behind it and on no other sequence: NaN and infinities there stay there.  In the rows that see one it shows, or not where its
- * weight is 0 in 32 bits.  (Up to 127 rows before such a value are computed again, one by one over all their keys: 0.15 s
- * where it is the last of 16384.)  Equal calls give equal bits.  out overlaps nothing that the call reads.  rows 0 or more; rows * n_q_heads at most 2^30. */
+ * Scores, their maxima and sums are 32-bit; the weights of the values are rounded to `dtype`, relative to their maximum (so means of values
+ * within 1 part in 512 of the type's largest number may come out infinite).  A row depends on nothing behind it and on no other sequence: NaN
+ * and infinities there stay there.  In the rows that see one it shows, or not where its weight is 0 in 32 bits.  (Up to 127 rows before such a
+ * value are computed again, one by one over all their keys: 0.15 s where it is the last of 16384.)  Equal calls give equal bits.  out
+ * overlaps nothing that the call reads.  rows 0 or more; rows * n_q_heads at most 2^30. */
 int vla_prompt_attn(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int dtype, int rows,
                     int n_q_heads, int n_kv_heads, int head_dim, const int32_t* seq_start, int n_seq, float scale, void* out,
                     int64_t ldo, float* lse, void* cuda_stream);
@@ -46,9 +47,9 @@ int vla_prompt_attn(const void* q, int64_t ldq, const void* k, int64_t ldk, cons
  *   d_v[j] = sum_i P[i][j] d_out[i],   dS[i][j] = P[i][j] (d_out[i] . v[j] - D[i]),
  *   d_q[i] = scale sum_j dS[i][j] k[j],   d_k[j] = scale sum_i dS[i][j] q[i].
  * P and dS are rounded to `dtype` in these sums, in fp16 dS relative to the largest that it can be in the row of d_q or d_k (what lies 2^38
- * below that may count as 0): rows, heads and sequences of very different sizes keep their own bits.  NaN and infinities stay in their sequence.  The gradients may overwrite nothing that the call reads.  Equal
- * calls give equal bits (no atomics).  `workspace` of vla_prompt_attn_grad_workspace_bytes, 16-byte aligned, any
- * content; not shared by calls that may overlap. */
+ * below that may count as 0): rows, heads and sequences of very different sizes keep their own bits.  NaN and infinities stay in their sequence.
+ * The gradients may overwrite nothing that the call reads.  Equal calls give equal bits (no atomics).  `workspace` of
+ * vla_prompt_attn_grad_workspace_bytes, 16-byte aligned, any content; not shared by calls that may overlap. */
 int vla_prompt_attn_grad(const void* q, int64_t ldq, const void* k, int64_t ldk, const void* v, int64_t ldv, int dtype, int rows,
                          int n_q_heads, int n_kv_heads, int head_dim, const int32_t* seq_start, int n_seq, float scale,
                          const void* out, int64_t ldo, const float* lse, const void* d_out, int64_t lddo, void* d_q, int64_t lddq,
